@@ -124,13 +124,16 @@ int l2kv_workspace_bytes(const l2kv_layout* lay, int32_t max_len, size_t* bytes)
  * *status becomes
  *   L2KV_OK                   nothing happened;
  *   L2KV_ERR_DEVICE_OVERFLOW  l2kv_append_evict had no row left for an append (the row was
- *                             dropped, everything else went ahead);
- *   L2KV_ERR_TIMEOUT          a kernel of l2kv_decode_attention or l2kv_prefix_attention gave up
+ *                             dropped, everything else went ahead),
+ *                             or l2kv_rotary_write none for a new token's;
+ *   L2KV_ERR_TIMEOUT          a kernel of l2kv_decode_attention, l2kv_prefix_attention,
+ *                             l2kv_prompt_attention or l2kv_tree_attention gave up
  *                             waiting for a copy or a tensor-core operation (every such wait
  *                             is bounded so that a fault cannot hang the GPU).  The kernel
  *                             also sets a mark in the status block at which the rest of its
- *                             grid, and EVERY LATER decode / prefix call on this workspace,
+ *                             grid, and EVERY LATER decode / prefix / prompt / tree call on this workspace,
  *                             leaves at once without writing its output;
+ *   L2KV_ERR_OUT_OF_RANGE     l2kv_tree_commit met a path that leaves its tree (cut there);
  *   L2KV_ERR_DEBUG_BOUNDS     only from a library built with -DL2KV_DEBUG: an index check
  *                             failed (the access was skipped).
  * The word keeps the last anomaly until the workspace is cleared: after any non-zero status,
@@ -311,6 +314,124 @@ int l2kv_prefix_attention_flags(const void* q, const void* K_c, const void* V_c,
                                 int32_t n_queries, float scale, uint32_t flags, float* out,
                                 float* lse_out, void* workspace, size_t workspace_bytes,
                                 void* stream);
+
+/* ---- New tokens: a packed list --------------------------------------------------------------
+ * The calls below take the new tokens of all sequences as one list of n_tokens tokens: token i
+ * belongs to sequence b with tok_off_dev[b] <= i < tok_off_dev[b + 1] (DEVICE int32 [batch + 1],
+ * not decreasing), and is its token number s = i - tok_off_dev[b].  A sequence may have none.
+ * Tokens before tok_off_dev[0] or from tok_off_dev[batch] on belong to no sequence (the padding
+ * of a captured call): their rows are neither used nor written.  n_tokens is a host upper bound;
+ * device offsets are clamped to it.  Tensors of tokens are described by l2kv_tokens: logical shape
+ * [layers, n_tokens, heads, head_dim] in the cache's dtype, head_dim contiguous, the other strides
+ * in elements, with the alignment rules of caches (a query that is a slice of a fused projection
+ * is described as it lies).  Strides of dimensions longer than one are at least head_dim.
+ * The paper has no counterpart to these calls: they are the steps around its cache that a model
+ * with prompts of different lengths, or with drafted tokens, goes through. */
+typedef struct {
+  void* data;                                        /* DEVICE; outputs are written through it */
+  int64_t stride_l, stride_t, stride_h;
+} l2kv_tokens;
+
+/* Flags of the calls on new tokens. */
+#define L2KV_TOKENS_LEN_PER_HEAD 1u   /* lengths are [batch, layers, kv_heads], not [batch, layers] */
+#define L2KV_TOKENS_ROTARY_INTERLEAVED 2u /* l2kv_rotary_write: pairs are (2p, 2p + 1)              */
+
+/* Rotary frequencies for l2kv_rotary_write: freq_out[p], p < rot_dim / 2, in radians per position,
+ * and scale_out, the factor on cosine and sine.  Host only, fp64.  With f_p = base^(-2p / rot_dim):
+ *   NONE    f_p
+ *   LINEAR  f_p / factor
+ *   NTK     f_p for the base  base * factor^(rot_dim / (rot_dim - 2))      (rot_dim > 2)
+ *   LLAMA3  f_p k + f_p / factor (1 - k),  k = clamp((original_len f_p / 2 pi - low) / (high - low), 0, 1)
+ *   YARN    the same mixture with k = 1 - clamp((p - a) / max(z - a, 0.001), 0, 1), where a is
+ *           d(high) rounded down (at least 0) and z is d(low) rounded up (at most rot_dim - 1),
+ *           d(turns) = rot_dim ln(original_len / (2 pi turns)) / (2 ln base); and
+ *           scale = 0.1 ln(factor) + 1 for factor > 1.  scale is 1 for every other kind.
+ * low and high are used by LLAMA3 (usually 1 and 4) and YARN (usually 1 and 32) only. */
+typedef enum {
+  L2KV_ROTARY_NONE = 0, L2KV_ROTARY_LINEAR = 1, L2KV_ROTARY_NTK = 2, L2KV_ROTARY_LLAMA3 = 3,
+  L2KV_ROTARY_YARN = 4
+} l2kv_rotary_scaling;
+int l2kv_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double low,
+                            double high, double original_len, double* freq_out, double* scale_out);
+
+/* Rotary positions and the cache write of new tokens, in one pass.  For token i (number s of
+ * sequence b), with a = pos_dev[i] * freq_dev[p] (DEVICE fp64 [rot_dim / 2]; the product, its
+ * cosine and its sine are formed in fp64), every pair p of every query and key head becomes
+ *   (x, y) -> (x cos a - y sin a, y cos a + x sin a) * rot_scale                  in fp32,
+ * the pair being dimensions p and p + rot_dim / 2, or 2p and 2p + 1 with
+ * L2KV_TOKENS_ROTARY_INTERLEAVED; dimensions from rot_dim on are copied.  Rotated queries go to
+ * q_out (which may be q); rotated keys and the values go to cache row t = start_dev[b, l] + s of
+ * every (b, l, h), and with them idx[..t] = pos_dev[i] and sumsq_c[..t] = the ordering key of the
+ * key row as stored (what l2kv_select_compact takes as sumsq_in).  cur_len_dev[b, l] = start + number of
+ * new tokens.  idx and sumsq_c may be NULL.  start_dev and cur_len_dev must be different arrays
+ * ([batch, layers], or [batch, layers, kv_heads] with L2KV_TOKENS_LEN_PER_HEAD).
+ * rot_dim: 0 (nothing is rotated; freq_dev may be NULL) or a multiple of 16 up to head_dim.
+ * Negative frequencies turn backwards.  Any q_heads, a multiple of kv_heads or not; with
+ * q_heads == 0, q and q_out may be NULL.  A row at or beyond the capacity is not written (its query
+ * still is), cur_len_dev stops there, and the device status word becomes
+ * L2KV_ERR_DEVICE_OVERFLOW.  workspace: any of at least 256 bytes whose first 256 were zeroed. */
+int l2kv_rotary_write(const l2kv_tokens* q, const l2kv_tokens* k, const l2kv_tokens* v,
+                      const int32_t* tok_off_dev, int32_t n_tokens, const int32_t* pos_dev,
+                      const double* freq_dev, int32_t rot_dim, double rot_scale,
+                      const l2kv_tokens* q_out, void* K_c, void* V_c, int32_t* idx, float* sumsq_c,
+                      const l2kv_layout* lay, const int32_t* start_dev, int32_t* cur_len_dev,
+                      uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Causal attention of whole prompts, or of the next pieces of prompts, of different lengths
+ * (Eq. 2 with the mask of a model's prefill).  The keys and values of the new tokens are already in
+ * the cache: they are the last n_b rows of every (b, l), n_b = tok_off_dev[b + 1] - tok_off_dev[b],
+ * in order (as l2kv_rotary_write leaves them; K and V of a projection, [tokens, heads, head_dim], are
+ * such a cache themselves: packed, with stride_h = head_dim).  Token s of sequence b attends to rows
+ *   t < cur_len_dev[b, l] - n_b + s + 1,
+ * so everything cached before is visible, and the new tokens up to the token itself:
+ *   out[l,i,j,:] = sum_t softmax_t( scale * q[l,i,j,:] . K_c[b,l,j/G,t,:] ) * V_c[b,l,j/G,t,:]
+ * out is in the cache's dtype; lse_out (may be NULL) is dense fp32 [layers, n_tokens, q_heads], the
+ * natural-log sum of exponentials of the scaled scores.  A token that sees no row gives zeros and
+ * -inf.  Rows that no token of the call may see can hold anything, NaN included; a
+ * non-finite value that one token may see can also reach tokens near it that may not.
+ * bf16 caches: products are exact, sums fp32, the softmax weights are rounded to bf16 before they
+ * multiply V and the result is rounded once more to bf16.  fp32 caches: fp32 throughout (a path for
+ * correctness, on the CUDA cores).  head_dim 64 and 128; every row address of K_c, V_c and (bf16) q
+ * has to be expressible as a tensor map (no zero strides; L2KV_ERR_UNSUPPORTED otherwise).
+ * flags: L2KV_TOKENS_LEN_PER_HEAD.  workspace: NULL, or of at least 256 bytes of which the first 256 were
+ * zeroed (its status word then reports a wait that gave up); with
+ * l2kv_prompt_attention_workspace_bytes bytes, calls with little work per SM split their caches over
+ * the SMs and merge the pieces.  Beyond its first 256 bytes it needs no initial contents, and two
+ * calls that can overlap on the GPU need one each. */
+int l2kv_prompt_attention_workspace_bytes(const l2kv_layout* lay, int32_t n_tokens, int32_t max_len,
+                                          size_t* bytes);
+int l2kv_prompt_attention(const l2kv_tokens* q, const int32_t* tok_off_dev, int32_t n_tokens,
+                          const void* K_c, const void* V_c, const l2kv_layout* lay,
+                          const int32_t* cur_len_dev, int32_t max_len, float scale, uint32_t flags,
+                          const l2kv_tokens* out, float* lse_out, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* The same for a tree of drafted tokens (several continuations at once, verified in one pass): the
+ * rows before the last n_b are visible to every token; of the last n_b, the tree's own, token i sees
+ * row t where bit c = t - (cur_len_dev[b, l] - n_b) of tree_mask_dev[i, :] is set (DEVICE
+ * uint64 [n_tokens, mask_words], bit c in word c / 64; no bit at or beyond 64 * mask_words).  For a
+ * tree these are the token's ancestors and itself; any other pattern will do, a token that sees
+ * nothing gives zeros and -inf.  mask_words >= 1.  Workspace and errors as for l2kv_prompt_attention. */
+int l2kv_tree_attention(const l2kv_tokens* q, const int32_t* tok_off_dev, int32_t n_tokens,
+                        const uint64_t* tree_mask_dev, int32_t mask_words, const void* K_c,
+                        const void* V_c, const l2kv_layout* lay, const int32_t* cur_len_dev,
+                        int32_t max_len, float scale, uint32_t flags, const l2kv_tokens* out,
+                        float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Keeps the accepted path of a drafted tree: for every (b, l, h) and j < n_path_dev[b], the row
+ * start_dev[b,l] + path_dev[b, j] moves to start_dev[b,l] + j (K, V, idx, sumsq_c), and
+ * len_out_dev[b, l] = start + number of rows kept.  path_dev: DEVICE int32 [batch, path_cap], the
+ * accepted tokens' numbers within their sequence, strictly increasing (a tree's parents come before
+ * their children); n_path_dev int32 [batch].  cur_len_dev[b, l] is the length with the whole tree in
+ * place: a path ends before the first entry that is not greater than the one before it or does
+ * not lie in [0, cur_len - start), and the status word becomes L2KV_ERR_OUT_OF_RANGE.
+ * len_out_dev may be start_dev or cur_len_dev, or another array; with
+ * L2KV_TOKENS_LEN_PER_HEAD all three are [batch, layers, kv_heads].  Rows beyond the kept ones hold what
+ * they held.  idx and sumsq_c may be NULL.  Any workspace of at least 256 bytes, the first 256 zeroed. */
+int l2kv_tree_commit(void* K_c, void* V_c, int32_t* idx, float* sumsq_c, const l2kv_layout* lay,
+                     const int32_t* start_dev, const int32_t* cur_len_dev, const int32_t* path_dev,
+                     int32_t path_cap, const int32_t* n_path_dev, int32_t* len_out_dev, uint32_t flags,
+                     void* workspace, size_t workspace_bytes, void* stream);
 
 /* Attention loss of the norm-based compression against the ideal one (Section 3,
  * Eqs. 5-7), for one query per query head over the cached keys i < cur_len_dev[b,l]:

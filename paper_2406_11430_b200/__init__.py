@@ -9,4 +9,6 @@ from .binding import (L2KVError, Layout, Rows, key_norms, select_compact, decode
                       decode_attention_per_head, append_evict_per_head, prefix_attention_per_head, prefix_attention_workspace, prefix_attention_causal, prefix_attention_flags, PREFIX_CAUSAL, PREFIX_LEN_PER_HEAD, PREFIX_SPLIT_WEIGHTS, attention_loss, prefix_attention, keep_count, workspace_bytes, new_workspace,
                       read_device_status, workspace_reset, selftest_wait_timeout,
                       decode_attention_static_status, status_string, library_path, lib,
-                      KEEP_LOWEST_NORM, KEEP_HIGHEST_NORM, KEEP_RANDOM)
+                      rotary_frequencies, rotary_write, prompt_attention, tree_attention, tree_commit,
+                      prompt_attention_workspace_bytes, ROTARY_NONE, ROTARY_LINEAR, ROTARY_NTK, ROTARY_LLAMA3,
+                      ROTARY_YARN, KEEP_LOWEST_NORM, KEEP_HIGHEST_NORM, KEEP_RANDOM)

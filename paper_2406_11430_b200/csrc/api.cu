@@ -3,7 +3,7 @@
 
 #include <nvtx3/nvToolsExt.h>
 
-#include "common.cuh"
+#include "tokens.cuh"
 
 namespace {
 
@@ -59,6 +59,22 @@ int make_mask(const int32_t* layers, int n, int n_layers, LayerMask* m) {
   for (int i = 0; i < n; ++i) {
     if (layers[i] < 0 || layers[i] >= n_layers) return L2KV_ERR_OUT_OF_RANGE;
     m->w[layers[i] >> 5] |= 1u << (layers[i] & 31);
+  }
+  return L2KV_OK;
+}
+
+// Rows of new tokens, [layers, n_tokens, heads, head_dim]; a stride counts where its dimension is
+// longer than one.
+int check_tokens(const l2kv_tokens* t, const l2kv_layout* lay, int heads, int n_tokens) {
+  if (!t || !t->data) return L2KV_ERR_INVALID_ARG;
+  if (!aligned16(t->data)) return L2KV_ERR_MISALIGNED;
+  const int64_t per16 = 16 / elem_bytes(lay->dtype);
+  const int64_t stride[3] = {t->stride_l, t->stride_t, t->stride_h};
+  const int extent[3] = {lay->layers, n_tokens, heads};
+  for (int i = 0; i < 3; ++i) {
+    if (extent[i] <= 1) continue;
+    if (stride[i] < lay->head_dim) return L2KV_ERR_INVALID_ARG;
+    if (stride[i] % per16) return L2KV_ERR_MISALIGNED;
   }
   return L2KV_OK;
 }
@@ -434,6 +450,160 @@ int l2kv_attention_loss_per_head(const void* q, const void* K, const l2kv_layout
                                  void* stream) {
   return attention_loss_impl(true, q, K, lay, cur_len_unit_dev, max_len, scale, sumsq, alr_out, loss_out,
                              loss_ref_out, workspace, workspace_bytes, stream);
+}
+
+int l2kv_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double low,
+                            double high, double original_len, double* freq_out, double* scale_out) {
+  const double two_pi = 6.283185307179586;
+  if (!freq_out || !scale_out || rot_dim < 2 || rot_dim % 2 || !(base > 1.0) || !std::isfinite(base))
+    return L2KV_ERR_INVALID_ARG;
+  if (scaling < L2KV_ROTARY_NONE || scaling > L2KV_ROTARY_YARN) return L2KV_ERR_INVALID_ARG;
+  if (scaling != L2KV_ROTARY_NONE && !(factor > 0.0 && std::isfinite(factor))) return L2KV_ERR_INVALID_ARG;
+  const bool mixes = scaling == L2KV_ROTARY_LLAMA3 || scaling == L2KV_ROTARY_YARN;
+  if (mixes && !(low > 0.0 && high > low && std::isfinite(high) && original_len > 0.0 && std::isfinite(original_len)))
+    return L2KV_ERR_INVALID_ARG;
+  if (scaling == L2KV_ROTARY_NTK) {
+    if (rot_dim < 4) return L2KV_ERR_INVALID_ARG;
+    base *= std::pow(factor, (double)rot_dim / (rot_dim - 2));
+  }
+  double first = 0.0, width = 1.0;                       // YARN: the ramp's first pair and its width
+  if (scaling == L2KV_ROTARY_YARN) {
+    auto pair_of = [&](double turns) {
+      return rot_dim * std::log(original_len / (turns * two_pi)) / (2.0 * std::log(base));
+    };
+    first = std::fmax(std::floor(pair_of(high)), 0.0);
+    width = std::fmax(std::fmin(std::ceil(pair_of(low)), rot_dim - 1.0) - first, 1e-3);
+  }
+  for (int p = 0; p < rot_dim / 2; ++p) {
+    const double f = std::pow(base, -2.0 * p / rot_dim);
+    double keep = 1.0;
+    if (scaling == L2KV_ROTARY_LINEAR) keep = 0.0;
+    if (scaling == L2KV_ROTARY_LLAMA3)
+      keep = std::fmin(std::fmax((original_len * f / two_pi - low) / (high - low), 0.0), 1.0);
+    if (scaling == L2KV_ROTARY_YARN) keep = 1.0 - std::fmin(std::fmax((p - first) / width, 0.0), 1.0);
+    freq_out[p] = keep == 1.0 ? f : f * keep + f / factor * (1.0 - keep);
+  }
+  *scale_out = scaling == L2KV_ROTARY_YARN && factor > 1.0 ? 0.1 * std::log(factor) + 1.0 : 1.0;
+  return L2KV_OK;
+}
+
+int l2kv_rotary_write(const l2kv_tokens* q, const l2kv_tokens* k, const l2kv_tokens* v,
+                      const int32_t* tok_off_dev, int32_t n_tokens, const int32_t* pos_dev,
+                      const double* freq_dev, int32_t rot_dim, double rot_scale,
+                      const l2kv_tokens* q_out, void* K_c, void* V_c, int32_t* idx, float* sumsq_c,
+                      const l2kv_layout* lay, const int32_t* start_dev, int32_t* cur_len_dev,
+                      uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+  const Range nvtx_range("l2kv_rotary_write");
+  int rc = check_layout(lay);
+  if (rc != L2KV_OK) return rc;
+  if (flags & ~(uint32_t)(L2KV_TOKENS_LEN_PER_HEAD | L2KV_TOKENS_ROTARY_INTERLEAVED)) return L2KV_ERR_INVALID_ARG;
+  if (n_tokens < 0 || rot_dim < 0 || !std::isfinite(rot_scale)) return L2KV_ERR_INVALID_ARG;
+  if (rot_dim > lay->head_dim || rot_dim % 16) return L2KV_ERR_UNSUPPORTED;
+  if (empty(lay)) return L2KV_OK;
+  if (!tok_off_dev || !start_dev || !cur_len_dev || start_dev == cur_len_dev || !K_c || !V_c || !workspace)
+    return L2KV_ERR_INVALID_ARG;
+  if (n_tokens > 0) {
+    if (!pos_dev || (rot_dim > 0 && !freq_dev)) return L2KV_ERR_INVALID_ARG;
+    if (lay->q_heads > 0) {
+      if ((rc = check_tokens(q, lay, lay->q_heads, n_tokens)) != L2KV_OK) return rc;
+      if ((rc = check_tokens(q_out, lay, lay->q_heads, n_tokens)) != L2KV_OK) return rc;
+    }
+    if ((rc = check_tokens(k, lay, lay->kv_heads, n_tokens)) != L2KV_OK) return rc;
+    if ((rc = check_tokens(v, lay, lay->kv_heads, n_tokens)) != L2KV_OK) return rc;
+  }
+  if (!aligned16(K_c) || !aligned16(V_c) || !aligned16(workspace)) return L2KV_ERR_MISALIGNED;
+  if (workspace_bytes < (size_t)kStatusBytes) return L2KV_ERR_WORKSPACE_TOO_SMALL;
+  return launch_rotary_write(make_view(q), make_view(k), make_view(v), make_view(q_out), tok_off_dev, n_tokens,
+                             pos_dev, freq_dev, rot_dim, rot_scale, (flags & L2KV_TOKENS_ROTARY_INTERLEAVED) != 0,
+                             K_c, V_c, idx, sumsq_c, make_geom(*lay), lay->dtype, start_dev, cur_len_dev,
+                             (flags & L2KV_TOKENS_LEN_PER_HEAD) != 0, static_cast<int32_t*>(workspace),
+                             static_cast<cudaStream_t>(stream));
+}
+
+int l2kv_tree_commit(void* K_c, void* V_c, int32_t* idx, float* sumsq_c, const l2kv_layout* lay,
+                     const int32_t* start_dev, const int32_t* cur_len_dev, const int32_t* path_dev,
+                     int32_t path_cap, const int32_t* n_path_dev, int32_t* len_out_dev, uint32_t flags,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  const Range nvtx_range("l2kv_tree_commit");
+  const int rc = check_layout(lay);
+  if (rc != L2KV_OK) return rc;
+  if ((flags & ~(uint32_t)L2KV_TOKENS_LEN_PER_HEAD) || path_cap < 0) return L2KV_ERR_INVALID_ARG;
+  if (empty(lay)) return L2KV_OK;
+  if (!K_c || !V_c || !start_dev || !cur_len_dev || (!path_dev && path_cap > 0) || !n_path_dev || !len_out_dev ||
+      !workspace)
+    return L2KV_ERR_INVALID_ARG;
+  if (!aligned16(K_c) || !aligned16(V_c) || !aligned16(workspace)) return L2KV_ERR_MISALIGNED;
+  if (workspace_bytes < (size_t)kStatusBytes) return L2KV_ERR_WORKSPACE_TOO_SMALL;
+  return launch_tree_commit(K_c, V_c, idx, sumsq_c, make_geom(*lay), lay->dtype, start_dev, cur_len_dev, path_dev,
+                            path_cap, n_path_dev, len_out_dev, (flags & L2KV_TOKENS_LEN_PER_HEAD) != 0,
+                            static_cast<int32_t*>(workspace), static_cast<cudaStream_t>(stream));
+}
+
+// Both masks of attention over a packed list of new tokens (tree: a bit per token and tail row).
+static int token_attention_impl(bool tree, const l2kv_tokens* q, const int32_t* tok_off_dev, int32_t n_tokens,
+                                const uint64_t* tree_mask_dev, int32_t mask_words, const void* K_c,
+                                const void* V_c, const l2kv_layout* lay, const int32_t* cur_len_dev,
+                                int32_t max_len, float scale, uint32_t flags, const l2kv_tokens* out,
+                                float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_layout(lay);
+  if (rc != L2KV_OK) return rc;
+  rc = check_groups(lay);
+  if (rc != L2KV_OK) return rc;
+  if ((flags & ~(uint32_t)L2KV_TOKENS_LEN_PER_HEAD) || n_tokens < 0 || max_len < 0 || !(scale == scale))
+    return L2KV_ERR_INVALID_ARG;
+  if (tree && mask_words < 1) return L2KV_ERR_INVALID_ARG;
+  if (tree && mask_words > (1 << 24)) return L2KV_ERR_OUT_OF_RANGE;
+  if (max_len > lay->t_cap) return L2KV_ERR_OUT_OF_RANGE;
+  if (empty(lay) || n_tokens == 0) return L2KV_OK;
+  if ((rc = check_tokens(q, lay, lay->q_heads, n_tokens)) != L2KV_OK) return rc;
+  if ((rc = check_tokens(out, lay, lay->q_heads, n_tokens)) != L2KV_OK) return rc;
+  if (!tok_off_dev || !K_c || !V_c || !cur_len_dev || (tree && !tree_mask_dev)) return L2KV_ERR_INVALID_ARG;
+  if (!aligned16(K_c) || !aligned16(V_c) || !aligned16(workspace)) return L2KV_ERR_MISALIGNED;
+  if (tree && (reinterpret_cast<uintptr_t>(tree_mask_dev) & 7u)) return L2KV_ERR_MISALIGNED;
+  if (workspace && workspace_bytes < (size_t)kStatusBytes) return L2KV_ERR_WORKSPACE_TOO_SMALL;
+  const float sc = scale > 0.f ? scale : 1.0f / std::sqrt((float)lay->head_dim);
+  const TokenAttention a{make_view(q), make_view(out), tok_off_dev, n_tokens, make_geom(*lay),
+                         LenView{cur_len_dev, (flags & L2KV_TOKENS_LEN_PER_HEAD) ? 1 : 0}, max_len,
+                         sc * 1.4426950408889634f, lse_out,
+                         tree ? reinterpret_cast<const uint32_t*>(tree_mask_dev) : nullptr, mask_words,
+                         static_cast<int32_t*>(workspace)};
+  const size_t room = workspace ? workspace_bytes - kStatusBytes : 0;
+  return launch_token_attention(a, K_c, V_c, lay->dtype, room ? static_cast<char*>(workspace) + kStatusBytes : nullptr,
+                                room, static_cast<cudaStream_t>(stream));
+}
+
+int l2kv_prompt_attention_workspace_bytes(const l2kv_layout* lay, int32_t n_tokens, int32_t max_len,
+                                          size_t* bytes) {
+  if (!bytes) return L2KV_ERR_INVALID_ARG;
+  int rc = check_layout(lay);
+  if (rc != L2KV_OK) return rc;
+  rc = check_groups(lay);
+  if (rc != L2KV_OK) return rc;
+  if (n_tokens < 0 || max_len < 0) return L2KV_ERR_INVALID_ARG;
+  if (max_len > lay->t_cap) return L2KV_ERR_OUT_OF_RANGE;
+  *bytes = (size_t)kStatusBytes;
+  if (!empty(lay) && n_tokens > 0) *bytes += token_attention_scratch(make_geom(*lay), lay->dtype, n_tokens, max_len);
+  return L2KV_OK;
+}
+
+int l2kv_prompt_attention(const l2kv_tokens* q, const int32_t* tok_off_dev, int32_t n_tokens,
+                          const void* K_c, const void* V_c, const l2kv_layout* lay,
+                          const int32_t* cur_len_dev, int32_t max_len, float scale, uint32_t flags,
+                          const l2kv_tokens* out, float* lse_out, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  const Range nvtx_range("l2kv_prompt_attention");
+  return token_attention_impl(false, q, tok_off_dev, n_tokens, nullptr, 0, K_c, V_c, lay, cur_len_dev, max_len,
+                              scale, flags, out, lse_out, workspace, workspace_bytes, stream);
+}
+
+int l2kv_tree_attention(const l2kv_tokens* q, const int32_t* tok_off_dev, int32_t n_tokens,
+                        const uint64_t* tree_mask_dev, int32_t mask_words, const void* K_c,
+                        const void* V_c, const l2kv_layout* lay, const int32_t* cur_len_dev,
+                        int32_t max_len, float scale, uint32_t flags, const l2kv_tokens* out,
+                        float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {
+  const Range nvtx_range("l2kv_tree_attention");
+  return token_attention_impl(true, q, tok_off_dev, n_tokens, tree_mask_dev, mask_words, K_c, V_c, lay,
+                              cur_len_dev, max_len, scale, flags, out, lse_out, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"
