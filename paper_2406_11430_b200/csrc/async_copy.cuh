@@ -39,10 +39,10 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map
                : "memory");
 }
 
-// Builds the rank-5 tensor map (head_dim, token, kv head, layer, batch) of a bf16, head_dim-128
-// cache with a box of 64 elements x box_rows tokens and the 128-byte swizzle.  Returns false
-// when the encoder is unavailable or rejects the geometry (callers then use another path).
-inline bool make_cache_map(CUtensorMap* map, const void* base, const Geom& g, int box_rows) {
+// Tensor map of bf16 elements with the 128-byte swizzle (dims and box innermost first, strides in bytes from
+// the second dimension on).  Returns false when the encoder is unavailable or rejects the geometry.
+inline bool encode_bf16_map(CUtensorMap* map, int rank, const void* base, const cuuint64_t* dims,
+                            const cuuint64_t* strides, const cuuint32_t* box) {
   using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
                                 const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -56,7 +56,16 @@ inline bool make_cache_map(CUtensorMap* map, const void* base, const Geom& g, in
     return reinterpret_cast<EncodeFn>(fn);
   }();
   if (!encode) return false;
-  cuuint64_t dims[5] = {128, (cuuint64_t)g.t_cap, (cuuint64_t)g.H, (cuuint64_t)g.L, (cuuint64_t)g.B};
+  const cuuint32_t elem[5] = {1, 1, 1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), dims, strides,
+                box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The rank-5 tensor map (head_dim, token, kv head, layer, batch) of a bf16 cache with a box of 64
+// elements x box_rows tokens.  Returns false as above (callers then use another path).
+inline bool make_cache_map(CUtensorMap* map, const void* base, const Geom& g, int box_rows) {
+  cuuint64_t dims[5] = {(cuuint64_t)g.D, (cuuint64_t)g.t_cap, (cuuint64_t)g.H, (cuuint64_t)g.L, (cuuint64_t)g.B};
   cuuint64_t strides[4] = {(cuuint64_t)g.st * 2, (cuuint64_t)g.sh * 2, (cuuint64_t)g.sl * 2,
                            (cuuint64_t)g.sb * 2};
   if (g.row_off) {
@@ -68,10 +77,7 @@ inline bool make_cache_map(CUtensorMap* map, const void* base, const Geom& g, in
     return false;                                                       // broadcast views
   }
   const cuuint32_t box[5] = {64, (cuuint32_t)box_rows, 1, 1, 1};
-  const cuuint32_t elem[5] = {1, 1, 1, 1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides,
-                box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return encode_bf16_map(map, 5, base, dims, strides, box);
 }
 
 }  // namespace l2kv

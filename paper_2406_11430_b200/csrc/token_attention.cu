@@ -1,0 +1,858 @@
+// Prompt and tree attention over bf16 caches: packed new tokens, each sequence against its own cached
+// rows, on the tensor cores (tcgen05.mma, operands by TMA in shared memory, accumulators in tensor
+// memory).
+//
+// A query tile is 128 rows: the (token, head-of-the-group) pairs of 128 / G tokens that share a KV
+// head.  Cached rows are taken in blocks of 128; for each one
+//   S = Q K^T  (128 x 128, fp32, tensor memory)  ->  softmax threads: masks, running maximum,
+//   P = 2^(s - m) as bf16 over the score columns  ->  O += P V  (tensor memory).
+// A CTA always works on two such chains at a time, so that one's matrix products run under the other's
+// softmax: two neighbouring query tiles that share every K and V block ("pair"), or, where a sequence
+// has no more tokens than one tile holds, the even and the odd blocks of one query tile ("alternate"),
+// joined at the end.  A chain has one score tile, and the weights overwrite it in place, so per
+// chain Q K^T(j + 1) follows P V(j), and what bounds a long prompt is
+// max(softmax, both products) per block and chain; N = 128 in both products keeps the shared-memory
+// reads of an instruction (A and B operands, 8 KB) within its 64 cycles.
+//
+// Roles: 4 softmax warps per chain (one thread per query row), one thread that issues all matrix
+// products, one warp that works out the items and fetches tiles through a ring of four.  A fixed grid
+// of CTAs walks a list of items (tile or pair of one sequence, layer and KV head), longest first, or,
+// where a call has fewer items than SMs, equal chunks of them that a second kernel joins.
+// Every wait is bounded; one that gives up ends the CTA and marks the workspace.
+#include <algorithm>
+#include <climits>
+#include <cstring>
+
+#include "tokens.cuh"
+#include "umma.cuh"
+
+namespace l2kv {
+
+constexpr int kTaRows = 128;                    // query rows per tile, cached rows per block
+constexpr int kTaHalf = kTaRows * 128;          // [128 rows][64 bf16], swizzled: 16 KB
+constexpr int kTaSlots = 4;                     // K and V tiles in flight
+constexpr int kTaStage = 4096;                  // bytes per softmax warp on the way out
+constexpr int kTaThreads = 320;                 // softmax chain 0, chain 1, issuing warp, fetching warp
+constexpr int kTaGrid = 148;                    // one CTA per SM (512 tensor-memory columns each)
+constexpr int kTaCtrl = 3072;                   // barriers, items, row statistics
+constexpr int kTaPolls = 18;                    // log2 of the polls a wait may take
+constexpr int kTaMaxGroups = 2 * kTaGrid;       // calls with at most so many items are cut into chunks
+constexpr int kTaMinChunk = 8;                  // blocks per chunk at least
+constexpr float kTaRescaleGap = 8.f;            // log2 units a maximum may drift before O is rescaled
+
+template <int D> constexpr int kTaTile = D / 64 * kTaHalf;
+template <int D> constexpr int kTaSmem = (2 + kTaSlots) * kTaTile<D> + 8 * kTaStage + kTaCtrl;
+// as in the other kernels: fp32 accumulators, bf16 operands, N / 8 from bit 17, M / 16 from bit 24; V is
+// N-major
+constexpr uint32_t kTaIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+template <int D> constexpr uint32_t kTaIdescPV =
+    (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
+
+// One unit of a CTA's work.
+struct TaItem {
+  int b, l, h;
+  int tok0, s0, nq;      // first token in the list and in its sequence, tokens of the item
+  int base, end;         // row of the sequence's first new token; rows that some token of the item sees
+  int blk0, nb, nb0;     // first block, blocks of the item (pair: of chain 1 and of chain 0)
+  int pair;              // two query tiles; else one whose blocks the chains take in turn
+  int slot;              // where the partial result of a chunk goes; -1: the result itself
+  int stop;              // no more items
+};
+
+struct TaPlan {
+  int chunk_blocks;      // 0: whole items, longest first; else the chunk length
+  long long items;
+};
+
+struct TaArgs {
+  TokenAttention a;
+  int G, QT;             // query heads per KV head, tokens per tile
+  int chunked;
+  int32_t* plan;         // chunk length for the joining kernel
+  float* part;           // [slots][slot_rows][D] rows, then [slots][slot_rows] log2-sum-exps
+  float* part_lse;
+  int slot_rows, slots;
+};
+
+// ---- the items, worked out by a warp from the device's lengths ------------------------------------
+
+struct TaEntry { int n, cur, base; };
+__device__ __forceinline__ TaEntry ta_entry(const TokenAttention& a, int b, int l, int h) {
+  const long long bl = (long long)b * a.g.L + l;
+  const int n = tokens_of(a.tok_off, b, a.n_tokens).n;
+  const int cur = max(0, min(a.lens.at(bl, h, a.g.H), min(a.max_len, a.g.cap(bl))));
+  return {n, cur, cur - n};
+}
+// Rows that the first `upto` tokens of the sequence see at most.
+__device__ __forceinline__ int ta_end(const TokenAttention& a, const TaEntry& e, int upto) {
+  return a.mask ? e.cur : max(0, min(e.cur, e.base + min(upto, e.n)));
+}
+// An entry as the plan sees it: with a length per head, the longest head's.
+__device__ __forceinline__ TaEntry ta_plan_entry(const TokenAttention& a, int b, int l) {
+  TaEntry e = ta_entry(a, b, l, 0);
+  if (a.lens.per_head && e.n > 0) {
+    for (int h = 1; h < a.g.H; ++h) e.cur = max(e.cur, ta_entry(a, b, l, h).cur);
+    e.base = e.cur - e.n;
+  }
+  return e;
+}
+__device__ __forceinline__ int ta_chunks(const TokenAttention& a, const TaEntry& e, int p, int QP, int C) {
+  const int nb = (ta_end(a, e, (p + 1) * QP) + kTaRows - 1) / kTaRows;
+  return max(1, (nb + C - 1) / C);
+}
+// Chunks of one head of every item of (b, l).
+__device__ __forceinline__ int ta_entry_chunks(const TokenAttention& a, const TaEntry& e, int QP, int C) {
+  int sum = 0;
+  for (int p = 0; p * QP < e.n; ++p) sum += ta_chunks(a, e, p, QP, C);
+  return sum;
+}
+
+// The shortest chunk length with which all chunks fit the grid (as many times as whole items need).
+__device__ __forceinline__ TaPlan ta_plan(const TaArgs& A) {
+  const TokenAttention& a = A.a;
+  const int lane = threadIdx.x & 31, QP = 2 * A.QT;
+  long long groups = 0;
+  const int entries = A.chunked ? a.g.B * a.g.L : a.g.B;
+  for (int e = lane; e < entries; e += 32)
+    groups += (tokens_of(a.tok_off, A.chunked ? e / a.g.L : e, a.n_tokens).n + QP - 1) / QP;
+  for (int off = 16; off; off >>= 1) groups += __shfl_xor_sync(0xffffffffu, groups, off);
+  if (!A.chunked) return {0, groups * a.g.L * a.g.H};
+  const int target = (int)min((long long)A.slots, (groups * a.g.H + kTaGrid - 1) / kTaGrid * kTaGrid);
+  auto count = [&](int C) {
+    int sum = 0;
+    for (int e = lane; e < entries; e += 32) {
+      const TaEntry x = ta_plan_entry(a, e / a.g.L, e % a.g.L);
+      if (x.n > 0) sum += ta_entry_chunks(a, x, QP, C);
+    }
+    return (int)__reduce_add_sync(0xffffffffu, (unsigned)sum) * a.g.H;
+  };
+  int lo = kTaMinChunk, hi = max(kTaMinChunk, (a.max_len + kTaRows - 1) / kTaRows);
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (count(mid) <= target) hi = mid; else lo = mid + 1;
+  }
+  return {lo, (long long)count(lo)};
+}
+
+// Where number k of the chunks (by_group false), or of the whole items, of a chunked call lies.
+struct TaPlace { int b, l, p, h, c, n_chunks, first; bool ok; };
+__device__ __forceinline__ TaPlace ta_place(const TaArgs& A, int C, int k, bool by_group) {
+  const TokenAttention& a = A.a;
+  const int lane = threadIdx.x & 31, QP = 2 * A.QT, entries = a.g.B * a.g.L, H = a.g.H;
+  int before = 0, chunks_before = 0;
+  for (int e0 = 0; e0 < entries; e0 += 32) {
+    const int e = e0 + lane;
+    TaEntry x{0, 0, 0};
+    if (e < entries) x = ta_plan_entry(a, e / a.g.L, e % a.g.L);
+    const int n_ch = x.n > 0 ? ta_entry_chunks(a, x, QP, C) * H : 0;
+    const int mine = by_group ? (x.n + QP - 1) / QP * H : n_ch;
+    int incl = mine, incl_ch = n_ch;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, incl, off), o2 = __shfl_up_sync(0xffffffffu, incl_ch, off);
+      if (lane >= off) { incl += o; incl_ch += o2; }
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, k < before + incl);
+    if (hit) {
+      const int who = __ffs(hit) - 1;
+      int rest = k - before - __shfl_sync(0xffffffffu, incl - mine, who);
+      int first = chunks_before + __shfl_sync(0xffffffffu, incl_ch - n_ch, who);
+      const int ee = e0 + who;
+      const TaEntry y = ta_plan_entry(a, ee / a.g.L, ee % a.g.L);
+      for (int p = 0; p * QP < y.n; ++p) {
+        const int nc = ta_chunks(a, y, p, QP, C), each = by_group ? 1 : nc;
+        if (rest < each * H) return {ee / a.g.L, ee % a.g.L, p, rest / each, rest % each, nc, first + rest / each * nc, true};
+        rest -= each * H;
+        first += nc * H;
+      }
+    }
+    before += __shfl_sync(0xffffffffu, incl, 31);
+    chunks_before += __shfl_sync(0xffffffffu, incl_ch, 31);
+  }
+  return {0, 0, 0, 0, 0, 0, 0, false};
+}
+
+// Whole items, longest first: layer by layer, and within a layer by level, an item's number of tile
+// pairs' worth of visible rows.  The causal items of a sequence are one per level, a tree's are all at one.
+__device__ __forceinline__ TaPlace ta_place_by_level(const TaArgs& A, long long k, long long items) {
+  const TokenAttention& a = A.a;
+  const int lane = threadIdx.x & 31, QP = 2 * A.QT, B = a.g.B, H = a.g.H;
+  const long long per_layer = items / a.g.L;
+  const int l = (int)(k / per_layer);
+  const int rank = (int)(k % per_layer / H), h = (int)(k % per_layer % H);
+  auto at_or_above = [&](int b, int t) {                 // items of sequence b at level t or higher
+    const TaEntry e = ta_entry(a, b, l, 0);
+    const int pairs = (e.n + QP - 1) / QP;
+    if (a.mask) return e.cur / QP >= t ? pairs : 0;
+    return max(0, min(pairs, pairs + max(0, e.base) / QP - t));
+  };
+  auto count = [&](int t) {
+    int sum = 0;
+    for (int b = lane; b < B; b += 32) sum += at_or_above(b, t);
+    return (int)__reduce_add_sync(0xffffffffu, (unsigned)sum);
+  };
+  int lo = 0, hi = (a.max_len + a.n_tokens) / QP + 2;    // the highest level with more than `rank` items at or above
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (count(mid) > rank) lo = mid; else hi = mid - 1;
+  }
+  int rest = rank - count(lo + 1);
+  for (int b0 = 0; b0 < B; b0 += 32) {
+    const int b = b0 + lane;
+    const int mine = b < B ? at_or_above(b, lo) - at_or_above(b, lo + 1) : 0;
+    int incl = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, incl, off);
+      if (lane >= off) incl += o;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, rest < incl);
+    if (hit) {
+      const int who = __ffs(hit) - 1;
+      const int within = rest - __shfl_sync(0xffffffffu, incl - mine, who);
+      const TaEntry e = ta_entry(a, b0 + who, l, 0);
+      const int p = a.mask ? within : lo - max(0, e.base) / QP;
+      return {b0 + who, l, p, h, 0, 1, -1, p * QP < e.n && p >= 0};
+    }
+    rest -= __shfl_sync(0xffffffffu, incl, 31);
+  }
+  return {0, 0, 0, 0, 0, 0, 0, false};
+}
+
+// The item at a place (its chunk's blocks; a chunk can be empty where heads differ in length).
+__device__ __forceinline__ TaItem ta_item(const TaArgs& A, const TaPlace& w, int C) {
+  const TokenAttention& a = A.a;
+  const int QP = 2 * A.QT;
+  const TaEntry e = ta_entry(a, w.b, w.l, w.h);
+  TaItem it;
+  it.b = w.b; it.l = w.l; it.h = w.h;
+  it.s0 = w.p * QP;
+  it.tok0 = tokens_of(a.tok_off, w.b, a.n_tokens).first + it.s0;
+  it.nq = min(QP, e.n - it.s0);
+  it.base = e.base;
+  it.end = ta_end(a, e, it.s0 + QP);
+  it.pair = it.nq > A.QT;
+  const int nb = (it.end + kTaRows - 1) / kTaRows;
+  const int nb0 = (ta_end(a, e, it.s0 + A.QT) + kTaRows - 1) / kTaRows;
+  it.blk0 = w.n_chunks > 1 ? w.c * C : 0;
+  it.nb = max(0, nb - it.blk0);
+  it.nb0 = max(0, nb0 - it.blk0);
+  if (w.n_chunks > 1) { it.nb = min(it.nb, C); it.nb0 = min(it.nb0, C); }
+  it.slot = w.n_chunks > 1 ? w.first + w.c : -1;
+  it.stop = 0;
+  return it;
+}
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1,
+                                            int c2, int c3) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+               "[%0], [%1, {%3, %4, %5, %6}], [%2];"
+               :: "r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+               : "memory");
+}
+// The lowest x bits.
+__device__ __forceinline__ uint32_t low_bits(int x) { return x >= 32 ? 0xffffffffu : x <= 0 ? 0u : (1u << x) - 1u; }
+
+// 32 columns of this warp's 32 rows, one row per lane, to `dst` (the lane's own row at these columns;
+// null: no such row) through this warp's stage: a thread that stored its own row would put 16 bytes
+// into each of 32 different lines per instruction.
+__device__ __forceinline__ void ta_store_bf16(const float (&v)[32], __nv_bfloat16* dst, uint4* stage) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    stage[lane * 4 + (i ^ ((lane >> 1) & 3))] =
+        make_uint4(pack_bf16(v[8 * i], v[8 * i + 1]), pack_bf16(v[8 * i + 2], v[8 * i + 3]),
+                   pack_bf16(v[8 * i + 4], v[8 * i + 5]), pack_bf16(v[8 * i + 6], v[8 * i + 7]));
+  __syncwarp();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = 8 * k + (lane >> 2);
+    __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(
+        __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), r));
+    const uint4 x = stage[r * 4 + ((lane & 3) ^ ((r >> 1) & 3))];
+    if (to) reinterpret_cast<uint4*>(to)[lane & 3] = x;
+  }
+  __syncwarp();
+}
+__device__ __forceinline__ void ta_store_f32(const float (&v)[32], float* dst, uint4* stage) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    stage[lane * 8 + (i ^ (lane & 7))] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+                                                    __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+  __syncwarp();
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = 4 * k + (lane >> 3);
+    float* to = reinterpret_cast<float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), r));
+    const uint4 x = stage[r * 8 + ((lane & 7) ^ (r & 7))];
+    if (to) reinterpret_cast<uint4*>(to)[lane & 7] = x;
+  }
+  __syncwarp();
+}
+
+template <int D, bool TREE>
+__global__ void __launch_bounds__(kTaThreads, 1)
+token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__ CUtensorMap map_q,
+                       const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  constexpr int TILE = kTaTile<D>;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const TokenAttention& a = A.a;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // A wait that gave up in an earlier call marks the workspace; nothing runs until it is cleared.
+  if (a.status && *reinterpret_cast<volatile int32_t*>(a.status + 2) != 0) return;
+
+  const uint32_t base = smem_u32(smem);
+  const uint32_t s_q = base, s_ring = base + 2 * TILE;
+  unsigned char* const stage_base = smem + (2 + kTaSlots) * TILE;
+  unsigned char* const ctrl = stage_base + 8 * kTaStage;
+  const uint32_t bars = smem_u32(ctrl);
+  TaItem* const items = reinterpret_cast<TaItem*>(ctrl + 256);            // [2]
+  volatile int* const s_fail = reinterpret_cast<volatile int*>(ctrl + 512);
+  uint32_t* const s_tmem = reinterpret_cast<uint32_t*>(ctrl + 516);
+  float2* const s_stat = reinterpret_cast<float2*>(ctrl + 1024);          // [2][128]: maximum, sum
+  auto full = [&](uint32_t pos) { return bars + 8u * (pos % kTaSlots); };
+  auto empty = [&](uint32_t pos) { return bars + 32u + 8u * (pos % kTaSlots); };
+  const uint32_t q_full = bars + 64u, q_free = bars + 72u, sync256 = bars + 80u;
+  auto item_full = [&](uint32_t i) { return bars + 88u + 8u * (i & 1u); };
+  auto item_free = [&](uint32_t i) { return bars + 104u + 8u * (i & 1u); };
+  auto s_full = [&](int c) { return bars + 120u + 8u * (uint32_t)c; };
+  auto p_full = [&](int c) { return bars + 136u + 8u * (uint32_t)c; };
+  auto o_full = [&](int c) { return bars + 152u + 8u * (uint32_t)c; };
+  const uint32_t drained = bars + 168u;
+
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 :: "r"(smem_u32(s_tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (tid == 0) {
+    for (int i = 0; i < 2 * kTaSlots; ++i) mbar_init(bars + 8u * i, 1);
+    mbar_init(q_full, 1); mbar_init(q_free, 1); mbar_init(sync256, 8);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(item_full(i), 1); mbar_init(item_free(i), 9);
+      mbar_init(s_full(i), 1); mbar_init(p_full(i), 4); mbar_init(o_full(i), 1);
+    }
+    mbar_init(drained, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    *s_fail = 0;
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *s_tmem;
+  // A wait that another role's failure ends too.
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    if (mbar_test(bar, parity)) return true;
+    return *s_fail == 0 && mbar_wait<kTaPolls>(bar, parity);
+  };
+  uint32_t pos = 0;                                      // ring position of the item's first tile
+
+  if (warp == 9) {
+    // ---- items and tiles ---------------------------------------------------------------------------
+    const TaPlan plan = ta_plan(A);
+    if (A.chunked && blockIdx.x == 0 && lane == 0) *A.plan = plan.chunk_blocks;
+    bool ok = true;
+    uint32_t n_pub = 0, n_q = 0;
+    for (int round = 0; ok; ++round) {
+      // every other round backwards: the CTA that had the longest item of one gets the shortest of the next
+      const long long k = (long long)round * gridDim.x +
+                          (round & 1 ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x);
+      TaItem it;
+      it.stop = 1;
+      it.nb = 0;
+      if (k < plan.items) {
+        const TaPlace w = A.chunked ? ta_place(A, plan.chunk_blocks, (int)k, false) : ta_place_by_level(A, k, plan.items);
+        // (offsets that decrease can describe more items than there is room for: those stay undone)
+        if (w.ok && (!A.chunked || w.first + w.c < A.slots)) it = ta_item(A, w, plan.chunk_blocks);
+      }
+      if (n_pub >= 2) ok = wait(item_free(n_pub), (n_pub / 2 - 1) & 1u);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      if (lane == 0) {
+        items[n_pub & 1] = it;
+        mbar_arrive(item_full(n_pub));
+      }
+      ++n_pub;
+      if (it.stop) break;
+      if (it.nb == 0) continue;
+      if (lane == 0) {
+        const int tiles = it.pair ? 2 : 1;
+        if (n_q > 0) ok = wait(q_free, (n_q - 1) & 1u);
+        if (ok) {
+          mbar_expect_tx(q_full, tiles * TILE);
+          for (int t = 0; t < tiles; ++t)
+            for (int c = 0; c < D / 64; ++c)
+              tma_load_4d(s_q + t * TILE + c * kTaHalf, &map_q, q_full, c * 64, it.h * A.G, it.tok0 + t * A.QT, it.l);
+        }
+        const int row0 = (int)a.g.row0((long long)it.b * a.g.L + it.l);
+        const int tm_l = a.g.row_off ? 0 : it.l, tm_b = a.g.row_off ? 0 : it.b;
+        for (int i = 0; ok && i < 2 * it.nb; ++i) {
+          // in the order the issuing thread uses them.  Pair: K0 V0 K1 V1 ..; alternate: K0 K1 V0 K2 V1 ..
+          bool is_k;
+          int j;
+          if (it.pair) { is_k = !(i & 1); j = i >> 1; }
+          else if (i == 0 || i == 2 * it.nb - 1) { is_k = i == 0; j = is_k ? 0 : it.nb - 1; }
+          else { is_k = i & 1; j = is_k ? (i + 1) >> 1 : (i - 2) >> 1; }
+          const uint32_t at = pos + i;
+          if (at >= kTaSlots) ok = wait(empty(at), (at / kTaSlots - 1) & 1u);
+          if (!ok) break;
+          mbar_expect_tx(full(at), TILE);
+          for (int c = 0; c < D / 64; ++c)
+            tma_load_5d(s_ring + (at % kTaSlots) * TILE + c * kTaHalf, is_k ? &map_k : &map_v, full(at), c * 64,
+                        row0 + (it.blk0 + j) * kTaRows, it.h, tm_l, tm_b);
+        }
+      }
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      pos += 2 * it.nb;
+      ++n_q;
+    }
+    if (!ok) {
+      *s_fail = 1;
+      // copies that may still be in flight: the last ones of every slot, and the query tiles
+      if (lane == 0) {
+        for (int i = 0; i < kTaSlots; ++i) { mbar_wait<12>(bars + 8u * i, 0); mbar_wait<12>(bars + 8u * i, 1); }
+        mbar_wait<12>(q_full, 0); mbar_wait<12>(q_full, 1);
+      }
+    }
+  } else if (warp == 8) {
+    // ---- matrix products ----------------------------------------------------------------------------
+    if (lane == 0) {
+      bool ok = true;
+      uint32_t n_item = 0, n_q = 0, np[2] = {0, 0};
+      while (ok) {
+        ok = wait(item_full(n_item), (n_item / 2) & 1u);
+        if (!ok) break;
+        const TaItem it = items[n_item & 1];
+        mbar_arrive(item_free(n_item));
+        ++n_item;
+        if (it.stop) break;
+        if (it.nb == 0) continue;
+        auto qk = [&](int c, uint32_t at) {              // S[c] = Q K^T
+          const uint32_t sq = s_q + (it.pair ? c * TILE : 0), sk = s_ring + (at % kTaSlots) * TILE;
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+            umma_bf16(tmem + c * 256, umma_desc(sq + (k >> 2) * kTaHalf + (k & 3) * 32, 16, 1024),
+                      umma_desc(sk + (k >> 2) * kTaHalf + (k & 3) * 32, 16, 1024), kTaIdescQK, k > 0);
+          umma_commit(s_full(c));
+        };
+        auto pv = [&](int c, uint32_t at, bool first) {  // O[c] += P V
+          const uint32_t sv = s_ring + (at % kTaSlots) * TILE;
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            umma_bf16_ts(tmem + c * 256 + 128, tmem + c * 256 + k * 8, umma_desc(sv + k * 2048, kTaHalf, 1024),
+                         kTaIdescPV<D>, (!first || k > 0) ? 1u : 0u);
+        };
+        auto landed = [&](uint32_t at) {
+          ok = ok && wait(full(at), (at / kTaSlots) & 1u);
+          if (ok) tc_fence_after();
+          return ok;
+        };
+        auto weights = [&](int c) {
+          ok = ok && wait(p_full(c), np[c] & 1u);
+          ++np[c];
+          if (ok) tc_fence_after();
+          return ok;
+        };
+        ok = wait(q_full, n_q & 1u);
+        ++n_q;
+        if (!ok) break;
+        tc_fence_after();
+        if (it.pair) {
+          // chain 0's tokens come first, so it never has more blocks than chain 1
+          if (!landed(pos)) break;
+          if (it.nb0 > 0) qk(0, pos);
+          qk(1, pos);
+          umma_commit(empty(pos));
+          if (it.nb == 1) umma_commit(q_free);
+          for (int j = 0; ok && j < it.nb; ++j) {
+            const uint32_t v = pos + 2 * j + 1, kn = v + 1;
+            const bool more = j + 1 < it.nb;
+            if (!landed(v) || (more && !landed(kn))) break;
+            if (j < it.nb0) {
+              if (!weights(0)) break;
+              pv(0, v, j == 0);
+              if (j + 1 < it.nb0) qk(0, kn); else umma_commit(o_full(0));
+            }
+            if (!weights(1)) break;
+            pv(1, v, j == 0);
+            umma_commit(empty(v));
+            if (more) {
+              qk(1, kn);
+              umma_commit(empty(kn));
+              if (j + 2 == it.nb) umma_commit(q_free);
+            } else {
+              umma_commit(o_full(1));
+            }
+          }
+        } else {
+          const int nb = it.nb;
+          auto k_at = [&](int j) { return pos + (j == 0 ? 0 : 2 * j - 1); };
+          auto v_at = [&](int j) { return pos + (j == nb - 1 ? 2 * nb - 1 : 2 * j + 2); };
+          for (int j = 0; j < 2 && j < nb; ++j) {
+            if (!landed(k_at(j))) break;
+            qk(j, k_at(j));
+            umma_commit(empty(k_at(j)));
+          }
+          if (nb <= 2) umma_commit(q_free);
+          for (int j = 0; ok && j < nb; ++j) {
+            const int c = j & 1;
+            if (!landed(v_at(j)) || !weights(c)) break;
+            pv(c, v_at(j), j < 2);
+            umma_commit(empty(v_at(j)));
+            if (j + 2 < nb) {
+              if (!landed(k_at(j + 2))) break;
+              qk(c, k_at(j + 2));
+              umma_commit(empty(k_at(j + 2)));
+              if (j + 3 == nb) umma_commit(q_free);
+            } else {
+              umma_commit(o_full(c));
+            }
+          }
+        }
+        pos += 2 * it.nb;
+      }
+      if (!ok) {
+        *s_fail = 1;
+        umma_commit(drained);                            // products in flight read this CTA's shared memory
+        mbar_wait<14>(drained, 0);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---- softmax: one thread per query row of its chain -----------------------------------------------
+    const int chain = warp >> 2, row = tid & (kTaRows - 1);
+    const uint32_t t_s = tmem + chain * 256 + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_s + 128;
+    const uint32_t t_o0 = tmem + 128 + ((uint32_t)((warp & 3) * 32) << 16), t_o1 = t_o0 + 256;
+    uint4* const stage = reinterpret_cast<uint4*>(stage_base + warp * kTaStage);
+    const int tok_in_tile = row / A.G, head_in_group = row % A.G;
+    uint32_t n_item = 0, n_s = 0, n_o = 0, n_sync = 0;
+    bool ok = true;
+    auto sync_chains = [&]() {                           // all eight softmax warps, bounded
+      __syncwarp();
+      if (lane == 0) mbar_arrive(sync256);
+      ok = ok && wait(sync256, n_sync & 1u);
+      ++n_sync;
+      ok = __all_sync(0xffffffffu, ok);
+      return ok;
+    };
+    while (true) {
+      ok = __all_sync(0xffffffffu, wait(item_full(n_item), (n_item / 2) & 1u));
+      if (!ok) break;
+      const TaItem it = items[n_item & 1];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(item_free(n_item));
+      ++n_item;
+      if (it.stop) break;
+      const int q = (it.pair ? chain * A.QT : 0) + tok_in_tile;             // token within the item
+      const bool valid = q < it.nq;
+      const bool warp_valid = __any_sync(0xffffffffu, valid);
+      // rows this token sees: all below `limit`, and, from row `base` on, those of its mask
+      const int limit = !valid ? 0 : TREE ? it.end : min(it.end, it.base + it.s0 + q + 1);
+      const uint32_t* mask = TREE ? a.mask + (long long)(it.tok0 + (valid ? q : 0)) * 2 * a.mask_words : nullptr;
+      const int nb_mine = it.pair ? (chain ? it.nb : it.nb0) : (it.nb + 1 - chain) / 2;
+      float m_ref = -INFINITY, sum = 0.f;
+
+      for (int jj = 0; jj < nb_mine; ++jj) {
+        const int j = it.pair ? jj : 2 * jj + chain;                         // block within the item
+        const int r0 = (it.blk0 + j) * kTaRows;                              // its first row
+        ok = __all_sync(0xffffffffu, wait(s_full(chain), n_s & 1u));
+        ++n_s;
+        if (!ok) break;
+        tc_fence_after();
+        if (warp_valid) {
+          float s[128];
+          {
+            uint32_t x[32], y[32];
+            tmem_ld64(t_s, x, y);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) { s[i] = __uint_as_float(x[i]); s[32 + i] = __uint_as_float(y[i]); }
+            tmem_ld64(t_s + 64, x, y);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) { s[64 + i] = __uint_as_float(x[i]); s[96 + i] = __uint_as_float(y[i]); }
+          }
+          const bool masked = TREE ? r0 + kTaRows > it.base : __any_sync(0xffffffffu, limit < r0 + kTaRows);
+          if (masked) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              uint32_t bits = low_bits(limit - r0 - 32 * w);
+              if constexpr (TREE) {
+                const int c = r0 + 32 * w - it.base;     // mask column of the word's first row
+                if (c > -32 && bits) {
+                  const int i = c >= 0 ? c >> 5 : 0, n_words = 2 * a.mask_words;
+                  const uint32_t lo = c < 0 || i < n_words ? mask[i] : 0u;
+                  bits &= c < 0 ? low_bits(-c) | lo << -c
+                                : __funnelshift_r(lo, i + 1 < n_words ? mask[i + 1] : 0u, c & 31);
+                }
+              }
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (!(bits >> i & 1u)) s[32 * w + i] = -INFINITY;
+            }
+          }
+          float t0 = fmaxf(s[0], s[1]), t1 = fmaxf(s[2], s[3]);
+#pragma unroll
+          for (int i = 4; i < 128; i += 4) {
+            t0 = fmaxf(t0, fmaxf(s[i], s[i + 1]));
+            t1 = fmaxf(t1, fmaxf(s[i + 2], s[i + 3]));
+          }
+          const float m_new = fmaxf(m_ref, fmaxf(t0, t1) * a.scale_log2e);
+          if (jj == 0) m_ref = m_new;
+          // O is quiet here: these scores were issued behind the last P V of this chain
+          const bool need = m_new > m_ref + kTaRescaleGap;
+          if (__any_sync(0xffffffffu, need)) {
+            const float factor = need ? fast_exp2(m_ref - m_new) : 1.f;
+#pragma unroll 1
+            for (int c = 0; c < D; c += 8) tmem_scale8(t_o + c, factor);
+            if (need) { sum *= factor; m_ref = m_new; }
+          }
+          const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;             // a row that has seen nothing yet
+          float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            uint32_t pk[32];
+#pragma unroll
+            for (int i = 0; i < 64; i += 2) {
+              const float p0 = fast_exp2(__fmaf_rn(s[64 * hh + i], a.scale_log2e, neg_m));
+              const float p1 = fast_exp2(__fmaf_rn(s[64 * hh + i + 1], a.scale_log2e, neg_m));
+              sum0 += p0;
+              sum1 += p1;
+              pk[i >> 1] = pack_bf16(p0, p1);
+            }
+            tmem_st32(t_s + 32 * hh, pk);
+          }
+          tmem_wait_st();
+          sum += sum0 + sum1;
+        }
+        // Rows of the V tile that no token of the item sees can hold anything; clear them, so that a zero
+        // weight times Inf or NaN cannot reach O (in a pair both chains write the same zeros).
+        if (it.end - r0 < kTaRows) {
+          const uint32_t v = pos + (it.pair ? 2 * j + 1 : j == it.nb - 1 ? 2 * it.nb - 1 : 2 * j + 2);
+          ok = __all_sync(0xffffffffu, wait(full(v), (v / kTaSlots) & 1u));
+          if (!ok) break;
+          if (row >= it.end - r0) {
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c)
+              st_shared16(s_ring + (v % kTaSlots) * TILE + (c >> 3) * kTaHalf + row * 128 + ((c & 7) << 4), 0, 0, 0, 0);
+          }
+          proxy_fence();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(chain));
+      }
+      if (!ok) break;
+      pos += 2 * it.nb;
+
+      // ---- the item's rows go out --------------------------------------------------------------------
+      if (nb_mine > 0) {
+        ok = __all_sync(0xffffffffu, wait(o_full(chain), n_o & 1u));
+        ++n_o;
+        if (!ok) break;
+      }
+      tc_fence_after();
+      const int tok = it.tok0 + q, head = it.h * A.G + head_in_group;
+      const long long part_row = (long long)it.slot * A.slot_rows + (it.pair ? chain * kTaRows : 0) + row;
+      __nv_bfloat16* const out = valid ? a.out.row<__nv_bfloat16>(it.l, tok, head) : nullptr;
+      float* const part = valid && it.slot >= 0 ? A.part + part_row * D : nullptr;
+      float f0 = 1.f, f1 = 0.f, total = sum, m = m_ref;
+      int c_lo = 0, c_hi = D;
+      if (!it.pair) {
+        // one query tile, two chains: each joins half of the columns of both
+        s_stat[chain * kTaRows + row] = make_float2(m_ref, sum);
+        tc_fence_before();                               // the other chain's warps have seen its O complete
+        if (!sync_chains()) break;
+        tc_fence_after();
+        const float2 st0 = s_stat[row], st1 = s_stat[kTaRows + row];
+        m = fmaxf(st0.x, st1.x);
+        const float low = m == -INFINITY ? 0.f : m;
+        f0 = fast_exp2(st0.x - low);
+        f1 = it.nb > 1 ? fast_exp2(st1.x - low) : 0.f;
+        total = st0.y * f0 + st1.y * f1;
+        c_lo = chain * (D / 2);
+        c_hi = c_lo + D / 2;
+      }
+      const bool any = warp_valid && it.nb > 0 && (it.pair ? nb_mine > 0 : true);
+      const float inv = total == 0.f ? 0.f : 1.f / total;
+      f0 *= inv;
+      f1 *= inv;
+      if (warp_valid) {
+        for (int c = c_lo; c < c_hi; c += 32) {
+          float v[32];
+          if (any) {
+            uint32_t x[32];
+            tmem_ld32((it.pair ? t_o : t_o0) + c, x);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(x[i]) * f0;
+            if (!it.pair && it.nb > 1) {
+              tmem_ld32(t_o1 + c, x);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = __fmaf_rn(__uint_as_float(x[i]), f1, v[i]);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+          }
+          if (it.slot >= 0) ta_store_f32(v, part ? part + c : nullptr, stage);
+          else ta_store_bf16(v, out ? out + c : nullptr, stage);
+        }
+        if (valid && (it.pair || chain == 0)) {
+          const float lse2 = total == 0.f ? -INFINITY : m + log2f(total);
+          if (it.slot >= 0) A.part_lse[part_row] = lse2;
+          else if (a.lse) a.lse[((long long)it.l * a.n_tokens + tok) * a.g.Hq + head] = lse2 * 0.6931471805599453f;
+        }
+      }
+      tc_fence_before();
+      // the next item's first products overwrite what both chains have just read
+      if (!it.pair && !sync_chains()) break;
+    }
+    if (!ok) *s_fail = 1;
+  }
+  __syncthreads();
+  tc_fence_after();
+  if (*s_fail && tid == 0) record_timeout(a.status);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512) : "memory");
+}
+
+// Joins the chunks of items that were cut: out = sum_c w_c O_c / sum_c w_c, w_c = 2^(lse_c - max lse), chunk
+// by chunk in order.  A block per item and 32 of its rows, a warp per row at a time.
+constexpr int kTaJoinWarps = 8;
+template <int D>
+__global__ void __launch_bounds__(32 * kTaJoinWarps)
+token_attention_join_kernel(const __grid_constant__ TaArgs A) {
+  constexpr int V = D / 32;
+  __shared__ TaItem s_it;
+  __shared__ int s_first, s_chunks;
+  const TokenAttention& a = A.a;
+  if (a.status && a.status[2] != 0) return;              // a wait gave up: no output
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (warp == 0) {
+    const int C = *A.plan;
+    const TaPlace w = ta_place(A, C, (int)blockIdx.x, true);
+    if (lane == 0) {
+      s_chunks = w.ok ? w.n_chunks : 0;
+      s_first = w.first;
+      if (w.ok) s_it = ta_item(A, w, C);
+    }
+  }
+  __syncthreads();
+  const int nc = s_chunks, first = s_first;
+  if (nc <= 1 || first + nc > A.slots) return;           // written by the kernel that computed it
+  const TaItem& it = s_it;
+  const int rows = it.nq * A.G;
+  for (int r = (int)blockIdx.y * 32 + warp; r < min(rows, (int)blockIdx.y * 32 + 32); r += kTaJoinWarps) {
+    const long long row = (long long)first * A.slot_rows + r;
+    float top = -INFINITY;
+    for (int c = lane; c < nc; c += 32) top = fmaxf(top, A.part_lse[row + (long long)c * A.slot_rows]);
+#pragma unroll
+    for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    const float low = top == -INFINITY ? 0.f : top;
+    float den = 0.f, num[V] = {};
+#pragma unroll 4
+    for (int c = 0; c < nc; ++c) {
+      const long long at = row + (long long)c * A.slot_rows;
+      const float lse2 = A.part_lse[at];
+      const float w = lse2 == -INFINITY ? 0.f : exp2f(lse2 - low);
+      den += w;
+      float x[V];
+      if constexpr (V == 4) *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(A.part + at * D + lane * V);
+      else *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(A.part + at * D + lane * V);
+#pragma unroll
+      for (int e = 0; e < V; ++e) num[e] = w == 0.f ? num[e] : fmaf(w, x[e], num[e]);
+    }
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    const int tok = it.tok0 + r / A.G, head = it.h * A.G + r % A.G;
+    uint32_t y[V / 2];
+#pragma unroll
+    for (int e = 0; e < V; e += 2) y[e / 2] = pack_bf16(num[e] * inv, num[e + 1] * inv);
+    uint32_t* to = reinterpret_cast<uint32_t*>(a.out.row<__nv_bfloat16>(it.l, tok, head)) + lane * (V / 2);
+    if constexpr (V == 4) *reinterpret_cast<uint2*>(to) = make_uint2(y[0], y[1]);
+    else *to = y[0];
+    if (a.lse && lane == 0)
+      a.lse[((long long)it.l * a.n_tokens + tok) * a.g.Hq + head] =
+          den == 0.f ? -INFINITY : (top + log2f(den)) * 0.6931471805599453f;
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+
+// Room for chunks: calls that have few items, whatever the sequences' lengths turn out to be.
+struct TaRoom {
+  long long groups;       // items at most
+  int slots, slot_rows;   // 0 slots: items are never cut
+  size_t bytes;
+};
+static TaRoom ta_room(const Geom& g, int n_tokens, int max_len) {
+  const int G = g.Hq / g.H, QP = 2 * (kTaRows / G);
+  TaRoom r{((long long)n_tokens / QP + std::min(g.B, n_tokens)) * g.L * g.H, 0, 0, 0};
+  if (r.groups <= kTaMaxGroups && max_len > kTaMinChunk * kTaRows) {
+    r.slots = (int)((r.groups + kTaGrid - 1) / kTaGrid * kTaGrid);
+    r.slot_rows = (long long)n_tokens * G <= kTaRows ? kTaRows : 2 * kTaRows;
+    r.bytes = 256 + (size_t)r.slots * r.slot_rows * (g.D + 1) * sizeof(float);
+  }
+  return r;
+}
+
+size_t token_attention_scratch(const Geom& g, int dtype, int n_tokens, int max_len) {
+  return dtype == L2KV_BF16 ? ta_room(g, n_tokens, max_len).bytes : 0;
+}
+
+// Rank-4 map of the queries (head_dim, head, token, layer); a box is one half row of a tile's rows.
+static bool make_query_map(CUtensorMap* map, const TokenAttention& a) {
+  const Geom& g = a.g;
+  const int G = g.Hq / g.H;
+  const long long tight = g.D;
+  const cuuint64_t dims[4] = {(cuuint64_t)g.D, (cuuint64_t)g.Hq, (cuuint64_t)a.n_tokens, (cuuint64_t)g.L};
+  const cuuint64_t strides[3] = {(cuuint64_t)(g.Hq > 1 ? a.q.sh : tight) * 2, (cuuint64_t)(a.n_tokens > 1 ? a.q.st : tight) * 2,
+                                 (cuuint64_t)(g.L > 1 ? a.q.sl : tight) * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)G, (cuuint32_t)(kTaRows / G), 1};
+  return encode_bf16_map(map, 4, a.q.p, dims, strides, box);
+}
+
+template <int D, bool TREE>
+static int launch_ta(const TaArgs& A, const void* K, const void* V, long long groups, cudaStream_t s) {
+  const TokenAttention& a = A.a;
+  alignas(64) CUtensorMap map_q, map_k, map_v;
+  std::memset(&map_q, 0, sizeof map_q);
+  std::memset(&map_k, 0, sizeof map_k);
+  std::memset(&map_v, 0, sizeof map_v);
+  if (!make_query_map(&map_q, a) || !make_cache_map(&map_k, K, a.g, kTaRows) || !make_cache_map(&map_v, V, a.g, kTaRows))
+    return L2KV_ERR_UNSUPPORTED;
+  auto kern = token_attention_kernel<D, TREE>;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTaSmem<D>) != cudaSuccess)
+    return L2KV_ERR_CUDA;
+  const unsigned grid = (unsigned)std::min<long long>(kTaGrid, A.chunked ? kTaGrid : groups);
+  kern<<<grid, kTaThreads, kTaSmem<D>, s>>>(A, map_q, map_k, map_v);
+  if (cudaGetLastError() != cudaSuccess) return L2KV_ERR_CUDA;
+  if (A.chunked) {
+    token_attention_join_kernel<D><<<dim3((unsigned)groups, (unsigned)(A.slot_rows / 32)), 32 * kTaJoinWarps, 0, s>>>(A);
+    if (cudaGetLastError() != cudaSuccess) return L2KV_ERR_CUDA;
+  }
+  return L2KV_OK;
+}
+
+int launch_token_attention(const TokenAttention& a, const void* K, const void* V, int dtype, char* scratch,
+                           size_t scratch_bytes, cudaStream_t s) {
+  if (dtype != L2KV_BF16) return launch_token_attention_simple(a, K, V, dtype, s);
+  const TaRoom room = ta_room(a.g, a.n_tokens, a.max_len);
+  TaArgs A{};
+  A.a = a;
+  A.G = a.g.Hq / a.g.H;
+  A.QT = kTaRows / A.G;
+  A.slot_rows = room.slot_rows;
+  if (room.slots > 0 && scratch && scratch_bytes >= room.bytes) {
+    A.chunked = 1;
+    A.slots = room.slots;
+    A.plan = reinterpret_cast<int32_t*>(scratch);
+    A.part = reinterpret_cast<float*>(scratch + 256);
+    A.part_lse = A.part + (size_t)room.slots * room.slot_rows * a.g.D;
+  }
+  if (a.g.D == 128)
+    return a.mask ? launch_ta<128, true>(A, K, V, room.groups, s) : launch_ta<128, false>(A, K, V, room.groups, s);
+  return a.mask ? launch_ta<64, true>(A, K, V, room.groups, s) : launch_ta<64, false>(A, K, V, room.groups, s);
+}
+
+}  // namespace l2kv

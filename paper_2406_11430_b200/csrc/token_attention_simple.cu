@@ -109,10 +109,4 @@ int launch_token_attention_simple(const TokenAttention& a, const void* K, const 
   return cudaGetLastError() == cudaSuccess ? L2KV_OK : L2KV_ERR_CUDA;
 }
 
-size_t token_attention_scratch(const Geom&, int, int, int) { return 0; }
-int launch_token_attention(const TokenAttention& a, const void* K, const void* V, int dtype, char*, size_t,
-                           cudaStream_t s) {
-  return launch_token_attention_simple(a, K, V, dtype, s);
-}
-
 }  // namespace l2kv
