@@ -32,7 +32,11 @@ constexpr int kTaRows = 128;                    // query rows per tile, cached r
 constexpr int kTaHalf = kTaRows * 128;          // [128 rows][64 bf16], swizzled: 16 KB
 constexpr int kTaSlots = 4;                     // K and V tiles in flight
 constexpr int kTaStage = 4096;                  // bytes per softmax warp on the way out
-constexpr int kTaThreads = 320;                 // softmax chain 0, chain 1, issuing warp, fetching warp
+constexpr int kTaThreads = 384;                 // softmax chain 0, chain 1, issuing warp, fetching warp, two idle ones
+#ifndef L2KV_TA_POLY
+#define L2KV_TA_POLY 0
+#endif
+constexpr int kTaPolyEvery = L2KV_TA_POLY;      // of so many weight pairs one is computed on the FMA pipe (0: none)
 constexpr int kTaGrid = 148;                    // one CTA per SM (512 tensor-memory columns each)
 constexpr int kTaCtrl = 3072;                   // barriers, items, row statistics
 constexpr int kTaPolls = 18;                    // log2 of the polls a wait may take
@@ -291,6 +295,37 @@ __device__ __forceinline__ void ta_store_f32(const float (&v)[32], float* dst, u
   __syncwarp();
 }
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{ .reg .b64 x, y, z, w; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%6, %7}; "
+      "fma.rn.f32x2 w, x, y, z; mov.b64 {%0, %1}, w; }"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{ .reg .b64 x, y, w; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 w, x, y; mov.b64 {%0, %1}, w; }"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+// 2^x on the FMA pipe: x = n + f with n the nearest whole number (adding 1.5 2^23 leaves it in the low
+// bits), 2^f on [-1/2, 1/2] by a polynomial of degree 4 fitted for the smallest relative error (2.6e-6),
+// n added to the exponent.  For x in [-126, 126]; below, 2^-126.
+__device__ __forceinline__ float2 poly_exp2(float2 x) {
+  const float2 magic = make_float2(12582912.f, 12582912.f), back = make_float2(-12582912.f, -12582912.f);
+  x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
+  const float2 t = add2(x, magic), n = add2(t, back);
+  const float2 f = add2(x, make_float2(-n.x, -n.y));
+  auto k = [](float c) { return make_float2(c, c); };
+  float2 p = fma2(f, k(0.009570102207362652f), k(0.05591786280274391f));
+  p = fma2(f, p, k(0.240247443318367f));
+  p = fma2(f, p, k(0.6931217908859253f));
+  p = fma2(f, p, k(0.9999992847442627f));
+  return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
+                     __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+}
+
 template <int D, bool TREE>
 __global__ void __launch_bounds__(kTaThreads, 1)
 token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__ CUtensorMap map_q,
@@ -320,6 +355,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   auto p_full = [&](int c) { return bars + 136u + 8u * (uint32_t)c; };
   auto o_full = [&](int c) { return bars + 152u + 8u * (uint32_t)c; };
   const uint32_t drained = bars + 168u;
+  auto p_half = [&](int c) { return bars + 176u + 8u * (uint32_t)c; };
 
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
@@ -331,7 +367,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
     mbar_init(q_full, 1); mbar_init(q_free, 1); mbar_init(sync256, 8);
     for (int i = 0; i < 2; ++i) {
       mbar_init(item_full(i), 1); mbar_init(item_free(i), 9);
-      mbar_init(s_full(i), 1); mbar_init(p_full(i), 4); mbar_init(o_full(i), 1);
+      mbar_init(s_full(i), 1); mbar_init(p_full(i), 4); mbar_init(p_half(i), 4); mbar_init(o_full(i), 1);
     }
     mbar_init(drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -349,7 +385,11 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   };
   uint32_t pos = 0;                                      // ring position of the item's first tile
 
-  if (warp == 9) {
+  // Registers: the softmax threads hold a block's 128 scores; the launch's 384 x 168 registers are dealt out
+  // as 256 x 208 + 128 x 88.
+  if (warp >= 8) {
+   asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+   if (warp == 9) {
     // ---- items and tiles ---------------------------------------------------------------------------
     const TaPlan plan = ta_plan(A);
     if (A.chunked && blockIdx.x == 0 && lane == 0) *A.plan = plan.chunk_blocks;
@@ -415,111 +455,127 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
         mbar_wait<12>(q_full, 0); mbar_wait<12>(q_full, 1);
       }
     }
-  } else if (warp == 8) {
-    // ---- matrix products ----------------------------------------------------------------------------
-    if (lane == 0) {
-      bool ok = true;
-      uint32_t n_item = 0, n_q = 0, np[2] = {0, 0};
-      while (ok) {
-        ok = wait(item_full(n_item), (n_item / 2) & 1u);
-        if (!ok) break;
-        const TaItem it = items[n_item & 1];
-        mbar_arrive(item_free(n_item));
-        ++n_item;
-        if (it.stop) break;
-        if (it.nb == 0) continue;
-        auto qk = [&](int c, uint32_t at) {              // S[c] = Q K^T
-          const uint32_t sq = s_q + (it.pair ? c * TILE : 0), sk = s_ring + (at % kTaSlots) * TILE;
+   } else if (warp == 8) {
+    // ---- matrix products: the whole warp walks the items, one elected lane issues -------------------
+    bool ok = true;
+    uint32_t n_item = 0, n_q = 0, np0 = 0, np1 = 0;
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    auto commit = [&](uint32_t bar) { if (elect_one()) umma_commit(bar); };
+    while (true) {
+      ok = __all_sync(0xffffffffu, wait(item_full(n_item), (n_item / 2) & 1u));
+      if (!ok) break;
+      const bool stop = __shfl_sync(0xffffffffu, items[n_item & 1].stop, 0);
+      const bool pair = __shfl_sync(0xffffffffu, items[n_item & 1].pair, 0);
+      const int nb = __shfl_sync(0xffffffffu, items[n_item & 1].nb, 0);
+      const int nb0 = __shfl_sync(0xffffffffu, items[n_item & 1].nb0, 0);
+      if (lane == 0) mbar_arrive(item_free(n_item));
+      __syncwarp();
+      ++n_item;
+      if (stop) break;
+      if (nb == 0) continue;
+      auto qk = [&](int c, uint32_t at) {                // S[c] = Q K^T
+        const uint64_t dq = umma_desc(s_q + (pair ? c * TILE : 0), 16, 1024);
+        const uint64_t dk = umma_desc(s_ring + (at % kTaSlots) * TILE, 16, 1024);
+        if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k)
-            umma_bf16(tmem + c * 256, umma_desc(sq + (k >> 2) * kTaHalf + (k & 3) * 32, 16, 1024),
-                      umma_desc(sk + (k >> 2) * kTaHalf + (k & 3) * 32, 16, 1024), kTaIdescQK, k > 0);
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t off = ((k >> 2) * kTaHalf + (k & 3) * 32) >> 4;   // the address field counts 16 bytes
+            umma_ss(tm + c * 256, dq + off, dk + off, kTaIdescQK, k > 0);
+          }
           umma_commit(s_full(c));
-        };
-        auto pv = [&](int c, uint32_t at, bool first) {  // O[c] += P V
-          const uint32_t sv = s_ring + (at % kTaSlots) * TILE;
+        }
+      };
+      auto pv = [&](int c, uint32_t at, int half, bool first) {              // O[c] += P V, 64 rows of the block
+        const uint64_t dv = umma_desc(s_ring + (at % kTaSlots) * TILE, kTaHalf, 1024);
+        if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            umma_bf16_ts(tmem + c * 256 + 128, tmem + c * 256 + k * 8, umma_desc(sv + k * 2048, kTaHalf, 1024),
-                         kTaIdescPV<D>, (!first || k > 0) ? 1u : 0u);
-        };
-        auto landed = [&](uint32_t at) {
-          ok = ok && wait(full(at), (at / kTaSlots) & 1u);
-          if (ok) tc_fence_after();
-          return ok;
-        };
-        auto weights = [&](int c) {
-          ok = ok && wait(p_full(c), np[c] & 1u);
-          ++np[c];
-          if (ok) tc_fence_after();
-          return ok;
-        };
-        ok = wait(q_full, n_q & 1u);
-        ++n_q;
-        if (!ok) break;
+          for (int k = 0; k < 4; ++k)
+            umma_ts(tm + c * 256 + 128, tm + c * 256 + 32 * half + k * 8, dv + ((half * 4 + k) * 2048 >> 4),
+                    kTaIdescPV<D>, first && half == 0 && k == 0 ? 0u : 1u);
+        }
+      };
+      auto landed = [&](uint32_t at) { ok = wait(full(at), (at / kTaSlots) & 1u) && ok; };
+      // both halves of a block's weights, each multiplied as soon as it is there
+      auto weights_v = [&](int c, uint32_t at, bool first) {
+        const uint32_t parity = (c ? np1 : np0) & 1u;
+        if (c) ++np1; else ++np0;
+        ok = wait(p_half(c), parity) && ok;
         tc_fence_after();
-        if (it.pair) {
-          // chain 0's tokens come first, so it never has more blocks than chain 1
-          if (!landed(pos)) break;
-          if (it.nb0 > 0) qk(0, pos);
-          qk(1, pos);
-          umma_commit(empty(pos));
-          if (it.nb == 1) umma_commit(q_free);
-          for (int j = 0; ok && j < it.nb; ++j) {
-            const uint32_t v = pos + 2 * j + 1, kn = v + 1;
-            const bool more = j + 1 < it.nb;
-            if (!landed(v) || (more && !landed(kn))) break;
-            if (j < it.nb0) {
-              if (!weights(0)) break;
-              pv(0, v, j == 0);
-              if (j + 1 < it.nb0) qk(0, kn); else umma_commit(o_full(0));
-            }
-            if (!weights(1)) break;
-            pv(1, v, j == 0);
-            umma_commit(empty(v));
-            if (more) {
-              qk(1, kn);
-              umma_commit(empty(kn));
-              if (j + 2 == it.nb) umma_commit(q_free);
-            } else {
-              umma_commit(o_full(1));
-            }
+        pv(c, at, 0, first);
+        ok = wait(p_full(c), parity) && ok;
+        tc_fence_after();
+        pv(c, at, 1, false);
+      };
+      ok = wait(q_full, n_q & 1u);
+      ++n_q;
+      if (pair) {
+        // chain 0's tokens come first, so it never has more blocks than chain 1
+        landed(pos);
+        tc_fence_after();
+        if (nb0 > 0) qk(0, pos);
+        qk(1, pos);
+        commit(empty(pos));
+        if (nb == 1) commit(q_free);
+        for (int j = 0; j < nb; ++j) {
+          const uint32_t v = pos + 2 * j + 1, kn = v + 1;
+          const bool more = j + 1 < nb;
+          landed(v);
+          if (more) landed(kn);
+          if (!__all_sync(0xffffffffu, ok)) break;
+          if (j < nb0) {
+            weights_v(0, v, j == 0);
+            if (j + 1 < nb0) qk(0, kn); else commit(o_full(0));
           }
-        } else {
-          const int nb = it.nb;
-          auto k_at = [&](int j) { return pos + (j == 0 ? 0 : 2 * j - 1); };
-          auto v_at = [&](int j) { return pos + (j == nb - 1 ? 2 * nb - 1 : 2 * j + 2); };
-          for (int j = 0; j < 2 && j < nb; ++j) {
-            if (!landed(k_at(j))) break;
-            qk(j, k_at(j));
-            umma_commit(empty(k_at(j)));
-          }
-          if (nb <= 2) umma_commit(q_free);
-          for (int j = 0; ok && j < nb; ++j) {
-            const int c = j & 1;
-            if (!landed(v_at(j)) || !weights(c)) break;
-            pv(c, v_at(j), j < 2);
-            umma_commit(empty(v_at(j)));
-            if (j + 2 < nb) {
-              if (!landed(k_at(j + 2))) break;
-              qk(c, k_at(j + 2));
-              umma_commit(empty(k_at(j + 2)));
-              if (j + 3 == nb) umma_commit(q_free);
-            } else {
-              umma_commit(o_full(c));
-            }
+          weights_v(1, v, j == 0);
+          commit(empty(v));
+          if (more) {
+            qk(1, kn);
+            commit(empty(kn));
+            if (j + 2 == nb) commit(q_free);
+          } else {
+            commit(o_full(1));
           }
         }
-        pos += 2 * it.nb;
+      } else {
+        auto k_at = [&](int j) { return pos + (j == 0 ? 0 : 2 * j - 1); };
+        auto v_at = [&](int j) { return pos + (j == nb - 1 ? 2 * nb - 1 : 2 * j + 2); };
+        for (int j = 0; j < 2 && j < nb; ++j) {
+          landed(k_at(j));
+          tc_fence_after();
+          qk(j, k_at(j));
+          commit(empty(k_at(j)));
+        }
+        if (nb <= 2) commit(q_free);
+        for (int j = 0; j < nb; ++j) {
+          const int c = j & 1;
+          landed(v_at(j));
+          if (!__all_sync(0xffffffffu, ok)) break;
+          weights_v(c, v_at(j), j < 2);
+          commit(empty(v_at(j)));
+          if (j + 2 < nb) {
+            landed(k_at(j + 2));
+            tc_fence_after();
+            qk(c, k_at(j + 2));
+            commit(empty(k_at(j + 2)));
+            if (j + 3 == nb) commit(q_free);
+          } else {
+            commit(o_full(c));
+          }
+        }
       }
-      if (!ok) {
-        *s_fail = 1;
-        umma_commit(drained);                            // products in flight read this CTA's shared memory
-        mbar_wait<14>(drained, 0);
-      }
+      pos += 2 * nb;
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+    }
+    if (!ok) {
+      *s_fail = 1;
+      commit(drained);                                   // products in flight read this CTA's shared memory
+      mbar_wait<14>(drained, 0);
     }
     __syncwarp();
+   }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ---- softmax: one thread per query row of its chain -----------------------------------------------
     const int chain = warp >> 2, row = tid & (kTaRows - 1);
     const uint32_t t_s = tmem + chain * 256 + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_s + 128;
@@ -560,70 +616,6 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
         ++n_s;
         if (!ok) break;
         tc_fence_after();
-        if (warp_valid) {
-          float s[128];
-          {
-            uint32_t x[32], y[32];
-            tmem_ld64(t_s, x, y);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) { s[i] = __uint_as_float(x[i]); s[32 + i] = __uint_as_float(y[i]); }
-            tmem_ld64(t_s + 64, x, y);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) { s[64 + i] = __uint_as_float(x[i]); s[96 + i] = __uint_as_float(y[i]); }
-          }
-          const bool masked = TREE ? r0 + kTaRows > it.base : __any_sync(0xffffffffu, limit < r0 + kTaRows);
-          if (masked) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              uint32_t bits = low_bits(limit - r0 - 32 * w);
-              if constexpr (TREE) {
-                const int c = r0 + 32 * w - it.base;     // mask column of the word's first row
-                if (c > -32 && bits) {
-                  const int i = c >= 0 ? c >> 5 : 0, n_words = 2 * a.mask_words;
-                  const uint32_t lo = c < 0 || i < n_words ? mask[i] : 0u;
-                  bits &= c < 0 ? low_bits(-c) | lo << -c
-                                : __funnelshift_r(lo, i + 1 < n_words ? mask[i + 1] : 0u, c & 31);
-                }
-              }
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (!(bits >> i & 1u)) s[32 * w + i] = -INFINITY;
-            }
-          }
-          float t0 = fmaxf(s[0], s[1]), t1 = fmaxf(s[2], s[3]);
-#pragma unroll
-          for (int i = 4; i < 128; i += 4) {
-            t0 = fmaxf(t0, fmaxf(s[i], s[i + 1]));
-            t1 = fmaxf(t1, fmaxf(s[i + 2], s[i + 3]));
-          }
-          const float m_new = fmaxf(m_ref, fmaxf(t0, t1) * a.scale_log2e);
-          if (jj == 0) m_ref = m_new;
-          // O is quiet here: these scores were issued behind the last P V of this chain
-          const bool need = m_new > m_ref + kTaRescaleGap;
-          if (__any_sync(0xffffffffu, need)) {
-            const float factor = need ? fast_exp2(m_ref - m_new) : 1.f;
-#pragma unroll 1
-            for (int c = 0; c < D; c += 8) tmem_scale8(t_o + c, factor);
-            if (need) { sum *= factor; m_ref = m_new; }
-          }
-          const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;             // a row that has seen nothing yet
-          float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll
-          for (int hh = 0; hh < 2; ++hh) {
-            uint32_t pk[32];
-#pragma unroll
-            for (int i = 0; i < 64; i += 2) {
-              const float p0 = fast_exp2(__fmaf_rn(s[64 * hh + i], a.scale_log2e, neg_m));
-              const float p1 = fast_exp2(__fmaf_rn(s[64 * hh + i + 1], a.scale_log2e, neg_m));
-              sum0 += p0;
-              sum1 += p1;
-              pk[i >> 1] = pack_bf16(p0, p1);
-            }
-            tmem_st32(t_s + 32 * hh, pk);
-          }
-          tmem_wait_st();
-          sum += sum0 + sum1;
-        }
         // Rows of the V tile that no token of the item sees can hold anything; clear them, so that a zero
         // weight times Inf or NaN cannot reach O (in a pair both chains write the same zeros).
         if (it.end - r0 < kTaRows) {
@@ -636,6 +628,89 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
               st_shared16(s_ring + (v % kTaSlots) * TILE + (c >> 3) * kTaHalf + row * 128 + ((c & 7) << 4), 0, 0, 0, 0);
           }
           proxy_fence();
+        }
+        if (warp_valid) {
+          uint32_t x[64], y[64];
+          tmem_ld64_issue(t_s, x);
+          tmem_ld64_wait(x);
+          tmem_ld64_issue(t_s + 64, y);
+          // the bits of a word of 32 columns that this thread's row sees
+          const bool masked = TREE ? r0 + kTaRows > it.base : __any_sync(0xffffffffu, limit < r0 + kTaRows);
+          auto seen = [&](int w) {
+            uint32_t bits = low_bits(limit - r0 - 32 * w);
+            if constexpr (TREE) {
+              const int c = r0 + 32 * w - it.base;       // mask column of the word's first row
+              if (c > -32 && bits) {
+                const int i = c >= 0 ? c >> 5 : 0, n_words = 2 * a.mask_words;
+                const uint32_t lo = c < 0 || i < n_words ? mask[i] : 0u;
+                bits &= c < 0 ? low_bits(-c) | lo << -c
+                              : __funnelshift_r(lo, i + 1 < n_words ? mask[i + 1] : 0u, c & 31);
+              }
+            }
+            return bits;
+          };
+          auto hide = [&](uint32_t (&v)[64], int w0) {
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              const uint32_t bits = seen(w0 + w);
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (!(bits >> i & 1u)) v[32 * w + i] = 0xff800000u;          // -inf
+            }
+          };
+          auto top_of = [&](const uint32_t (&v)[64]) {
+            float t0 = __uint_as_float(v[0]), t1 = __uint_as_float(v[1]);
+#pragma unroll
+            for (int i = 2; i < 62; i += 4) {
+              t0 = fmaxf(t0, fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 1])));
+              t1 = fmaxf(t1, fmaxf(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])));
+            }
+            return fmaxf(t0, fmaxf(t1, fmaxf(__uint_as_float(v[62]), __uint_as_float(v[63]))));
+          };
+          if (masked) hide(x, 0);
+          float top = top_of(x);
+          tmem_ld64_wait(y);
+          if (masked) hide(y, 2);
+          top = fmaxf(top, top_of(y));
+          const float m_new = fmaxf(m_ref, top * a.scale_log2e);
+          if (jj == 0) m_ref = m_new;
+          // O is quiet here: these scores were issued behind the last P V of this chain
+          const bool need = m_new > m_ref + kTaRescaleGap;
+          if (__any_sync(0xffffffffu, need)) {
+            const float factor = need ? fast_exp2(m_ref - m_new) : 1.f;
+#pragma unroll 1
+            for (int c = 0; c < D; c += 8) tmem_scale8(t_o + c, factor);
+            if (need) { sum *= factor; m_ref = m_new; }
+          }
+          const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;             // a row that has seen nothing yet
+          const float2 sc2 = make_float2(a.scale_log2e, a.scale_log2e), nm2 = make_float2(neg_m, neg_m);
+          float2 sums = make_float2(0.f, 0.f);
+          auto weights = [&](const uint32_t (&v)[64], uint32_t to, auto mixed) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {                // 32 columns: 16 words of bf16 pairs
+              uint32_t pk[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const float2 e = fma2(make_float2(__uint_as_float(v[32 * c + 2 * i]), __uint_as_float(v[32 * c + 2 * i + 1])), sc2, nm2);
+                float2 w;
+                if (decltype(mixed)::value && kTaPolyEvery && i % (kTaPolyEvery ? kTaPolyEvery : 1) == 0) w = poly_exp2(e);
+                else w = make_float2(fast_exp2(e.x), fast_exp2(e.y));
+                sums = add2(sums, w);
+                pk[i] = pack_bf16(w.x, w.y);
+              }
+              tmem_st16(to + 16 * c, pk);
+            }
+          };
+          if (masked) weights(x, t_s, std::false_type{}); else weights(x, t_s, std::true_type{});
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_half(chain));
+          if (masked) weights(y, t_s + 32, std::false_type{}); else weights(y, t_s + 32, std::true_type{});
+          tmem_wait_st();
+          sum += sums.x + sums.y;
+        } else if (lane == 0) {
+          mbar_arrive(p_half(chain));
         }
         tc_fence_before();
         __syncwarp();
