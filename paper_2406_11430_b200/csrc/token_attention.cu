@@ -29,10 +29,17 @@
 namespace l2kv {
 
 constexpr int kTaRows = 128;                    // query rows per tile, cached rows per block
-constexpr int kTaHalf = kTaRows * 128;          // [128 rows][64 bf16], swizzled: 16 KB
-constexpr int kTaSlots = 4;                     // K and V tiles in flight
+constexpr int kTaSub = 64;                      // cached rows per sub-block: one K tile, one V tile
+constexpr int kTaHalf = kTaRows * 128;          // query rows, [128][64 bf16], swizzled: 16 KB
+constexpr int kTaSubHalf = kTaSub * 128;        // cached rows, [64][64 bf16]: 8 KB
 constexpr int kTaStage = 4096;                  // bytes per softmax warp on the way out
-constexpr int kTaThreads = 384;                 // softmax chain 0, chain 1, issuing warp, fetching warp, two idle ones
+constexpr int kTaThreads = 352;                 // 2 x 4 softmax warps, issuing warps 8 and 10, fetching warp 9
+#ifndef L2KV_TA_TURN
+#define L2KV_TA_TURN 1
+#endif
+#ifndef L2KV_TA_TURN_AT
+#define L2KV_TA_TURN_AT 20
+#endif
 #ifndef L2KV_TA_POLY
 #define L2KV_TA_POLY 0
 #endif
@@ -44,11 +51,13 @@ constexpr int kTaMaxGroups = 2 * kTaGrid;       // calls with at most so many it
 constexpr int kTaMinChunk = 8;                  // blocks per chunk at least
 constexpr float kTaRescaleGap = 8.f;            // log2 units a maximum may drift before O is rescaled
 
-template <int D> constexpr int kTaTile = D / 64 * kTaHalf;
-template <int D> constexpr int kTaSmem = (2 + kTaSlots) * kTaTile<D> + 8 * kTaStage + kTaCtrl;
+template <int D> constexpr int kTaQTile = D / 64 * kTaHalf;
+template <int D> constexpr int kTaTile = D / 64 * kTaSubHalf;
+template <int D> constexpr int kTaSlots = 1024 / D;   // K and V tiles in flight: 128 KB
+template <int D> constexpr int kTaSmem = 2 * kTaQTile<D> + kTaSlots<D> * kTaTile<D> + 8 * kTaStage + kTaCtrl;
 // as in the other kernels: fp32 accumulators, bf16 operands, N / 8 from bit 17, M / 16 from bit 24; V is
 // N-major
-constexpr uint32_t kTaIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+constexpr uint32_t kTaIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((64u >> 3) << 17) | ((128u >> 4) << 24);
 template <int D> constexpr uint32_t kTaIdescPV =
     (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
 
@@ -57,8 +66,8 @@ struct TaItem {
   int b, l, h;
   int tok0, s0, nq;      // first token in the list and in its sequence, tokens of the item
   int base, end;         // row of the sequence's first new token; rows that some token of the item sees
-  int blk0, nb, nb0;     // first block, blocks of the item (pair: of chain 1 and of chain 0)
-  int pair;              // two query tiles; else one whose blocks the chains take in turn
+  int row0, n, n0;       // first row, sub-blocks of the item (pair: of chain 1 and of chain 0)
+  int pair;              // two query tiles; else one whose sub-blocks the chains take in turn
   int slot;              // where the partial result of a chunk goes; -1: the result itself
   int stop;              // no more items
 };
@@ -236,16 +245,24 @@ __device__ __forceinline__ TaItem ta_item(const TaArgs& A, const TaPlace& w, int
   it.base = e.base;
   it.end = ta_end(a, e, it.s0 + QP);
   it.pair = it.nq > A.QT;
-  const int nb = (it.end + kTaRows - 1) / kTaRows;
-  const int nb0 = (ta_end(a, e, it.s0 + A.QT) + kTaRows - 1) / kTaRows;
-  it.blk0 = w.n_chunks > 1 ? w.c * C : 0;
-  it.nb = max(0, nb - it.blk0);
-  it.nb0 = max(0, nb0 - it.blk0);
-  if (w.n_chunks > 1) { it.nb = min(it.nb, C); it.nb0 = min(it.nb0, C); }
+  const int end0 = ta_end(a, e, it.s0 + A.QT);           // what the first tile's tokens see
+  it.row0 = w.n_chunks > 1 ? w.c * C * kTaRows : 0;
+  const int most = w.n_chunks > 1 ? C * (kTaRows / kTaSub) : INT_MAX;
+  it.n = min(most, max(0, (it.end - it.row0 + kTaSub - 1) / kTaSub));
+  it.n0 = min(most, max(0, (end0 - it.row0 + kTaSub - 1) / kTaSub));
   it.slot = w.n_chunks > 1 ? w.first + w.c : -1;
   it.stop = 0;
   return it;
 }
+
+// Where the ring holds the tiles of an item's sub-block g: K tiles run `ahead` of V tiles, the order of use
+// being K(0) .. K(ahead - 1), V(0), K(ahead), V(1), K(ahead + 1), ...
+struct TaRing {
+  uint32_t pos;
+  int n, ahead;
+  __device__ __forceinline__ uint32_t k_at(int g) const { return pos + (g < ahead ? g : 2 * g - ahead + 1); }
+  __device__ __forceinline__ uint32_t v_at(int g) const { return pos + min(ahead, n) + g + max(0, min(g, n - ahead)); }
+};
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1,
                                             int c2, int c3) {
@@ -330,7 +347,7 @@ template <int D, bool TREE>
 __global__ void __launch_bounds__(kTaThreads, 1)
 token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__ CUtensorMap map_q,
                        const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
-  constexpr int TILE = kTaTile<D>;
+  constexpr int QTILE = kTaQTile<D>, TILE = kTaTile<D>, SLOTS = kTaSlots<D>;
   extern __shared__ __align__(1024) unsigned char smem[];
   const TokenAttention& a = A.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -338,24 +355,28 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   if (a.status && *reinterpret_cast<volatile int32_t*>(a.status + 2) != 0) return;
 
   const uint32_t base = smem_u32(smem);
-  const uint32_t s_q = base, s_ring = base + 2 * TILE;
-  unsigned char* const stage_base = smem + (2 + kTaSlots) * TILE;
+  const uint32_t s_q = base, s_ring = base + 2 * QTILE;
+  unsigned char* const stage_base = smem + 2 * QTILE + SLOTS * TILE;
   unsigned char* const ctrl = stage_base + 8 * kTaStage;
   const uint32_t bars = smem_u32(ctrl);
-  TaItem* const items = reinterpret_cast<TaItem*>(ctrl + 256);            // [2]
-  volatile int* const s_fail = reinterpret_cast<volatile int*>(ctrl + 512);
-  uint32_t* const s_tmem = reinterpret_cast<uint32_t*>(ctrl + 516);
+  TaItem* const items = reinterpret_cast<TaItem*>(ctrl + 512);            // [2]
+  volatile int* const s_fail = reinterpret_cast<volatile int*>(ctrl + 768);
+  uint32_t* const s_tmem = reinterpret_cast<uint32_t*>(ctrl + 772);
+  volatile int* const s_turn = reinterpret_cast<volatile int*>(ctrl + 896);   // [2][4]: exponentials done, by chain and lane quarter
   float2* const s_stat = reinterpret_cast<float2*>(ctrl + 1024);          // [2][128]: maximum, sum
-  auto full = [&](uint32_t pos) { return bars + 8u * (pos % kTaSlots); };
-  auto empty = [&](uint32_t pos) { return bars + 32u + 8u * (pos % kTaSlots); };
-  const uint32_t q_full = bars + 64u, q_free = bars + 72u, sync256 = bars + 80u;
-  auto item_full = [&](uint32_t i) { return bars + 88u + 8u * (i & 1u); };
-  auto item_free = [&](uint32_t i) { return bars + 104u + 8u * (i & 1u); };
-  auto s_full = [&](int c) { return bars + 120u + 8u * (uint32_t)c; };
-  auto p_full = [&](int c) { return bars + 136u + 8u * (uint32_t)c; };
-  auto o_full = [&](int c) { return bars + 152u + 8u * (uint32_t)c; };
-  const uint32_t drained = bars + 168u;
-  auto p_half = [&](int c) { return bars + 176u + 8u * (uint32_t)c; };
+  auto full = [&](uint32_t pos) { return bars + 8u * (pos % SLOTS); };
+  auto empty = [&](uint32_t pos) { return bars + 128u + 8u * (pos % SLOTS); };
+  const uint32_t more = bars + 256u;
+  const uint32_t q_full = more, q_free = more + 8u, sync256 = more + 16u;
+  auto item_full = [&](uint32_t i) { return more + 24u + 8u * (i & 1u); };
+  auto item_free = [&](uint32_t i) { return more + 40u + 8u * (i & 1u); };
+  auto s_full = [&](int c, uint32_t i) { return more + 56u + 16u * (uint32_t)c + 8u * (i & 1u); };
+  auto p_full = [&](int c, uint32_t i) { return more + 88u + 16u * (uint32_t)c + 8u * (i & 1u); };
+  // Complete once per P V, by the parity of its running number: a wait tells a phase from its two neighbours
+  // only, and the one rescaling waits for can be two products behind.
+  auto pv_done = [&](int c, uint32_t i) { return more + 120u + 16u * (uint32_t)c + 8u * (i & 1u); };
+  auto o_full = [&](int c) { return more + 152u + 8u * (uint32_t)c; };
+  auto drained = [&](int c) { return more + 168u + 8u * (uint32_t)c; };
 
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
@@ -363,15 +384,19 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (tid == 0) {
-    for (int i = 0; i < 2 * kTaSlots; ++i) mbar_init(bars + 8u * i, 1);
-    mbar_init(q_full, 1); mbar_init(q_free, 1); mbar_init(sync256, 8);
+    // a tile and the query rows are given back once per chain
+    for (int i = 0; i < SLOTS; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 2); }
+    mbar_init(q_full, 1); mbar_init(q_free, 2); mbar_init(sync256, 8);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(item_full(i), 1); mbar_init(item_free(i), 9);
-      mbar_init(s_full(i), 1); mbar_init(p_full(i), 4); mbar_init(p_half(i), 4); mbar_init(o_full(i), 1);
+      mbar_init(item_full(i), 1); mbar_init(item_free(i), 10);
+      mbar_init(s_full(0, i), 1); mbar_init(s_full(1, i), 1);
+      mbar_init(p_full(0, i), 4); mbar_init(p_full(1, i), 4);
+      mbar_init(pv_done(0, i), 1); mbar_init(pv_done(1, i), 1);
+      mbar_init(o_full(i), 1); mbar_init(drained(i), 1);
     }
-    mbar_init(drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     *s_fail = 0;
+    for (int i = 0; i < 8; ++i) s_turn[i] = 0;
   }
   __syncwarp();
   tc_fence_before();
@@ -383,13 +408,10 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
     if (mbar_test(bar, parity)) return true;
     return *s_fail == 0 && mbar_wait<kTaPolls>(bar, parity);
   };
+  auto landed = [&](uint32_t at) { return wait(full(at), (at / SLOTS) & 1u); };
   uint32_t pos = 0;                                      // ring position of the item's first tile
 
-  // Registers: the softmax threads hold a block's 128 scores; the launch's 384 x 168 registers are dealt out
-  // as 256 x 208 + 128 x 88.
-  if (warp >= 8) {
-   asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-   if (warp == 9) {
+  if (warp == 9) {
     // ---- items and tiles ---------------------------------------------------------------------------
     const TaPlan plan = ta_plan(A);
     if (A.chunked && blockIdx.x == 0 && lane == 0) *A.plan = plan.chunk_blocks;
@@ -401,7 +423,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
                           (round & 1 ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x);
       TaItem it;
       it.stop = 1;
-      it.nb = 0;
+      it.n = 0;
       if (k < plan.items) {
         const TaPlace w = A.chunked ? ta_place(A, plan.chunk_blocks, (int)k, false) : ta_place_by_level(A, k, plan.items);
         // (offsets that decrease can describe more items than there is room for: those stay undone)
@@ -415,174 +437,143 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       }
       ++n_pub;
       if (it.stop) break;
-      if (it.nb == 0) continue;
+      if (it.n == 0) continue;
       if (lane == 0) {
         const int tiles = it.pair ? 2 : 1;
         if (n_q > 0) ok = wait(q_free, (n_q - 1) & 1u);
         if (ok) {
-          mbar_expect_tx(q_full, tiles * TILE);
+          mbar_expect_tx(q_full, tiles * QTILE);
           for (int t = 0; t < tiles; ++t)
             for (int c = 0; c < D / 64; ++c)
-              tma_load_4d(s_q + t * TILE + c * kTaHalf, &map_q, q_full, c * 64, it.h * A.G, it.tok0 + t * A.QT, it.l);
+              tma_load_4d(s_q + t * QTILE + c * kTaHalf, &map_q, q_full, c * 64, it.h * A.G, it.tok0 + t * A.QT, it.l);
         }
-        const int row0 = (int)a.g.row0((long long)it.b * a.g.L + it.l);
+        const int row0 = (int)a.g.row0((long long)it.b * a.g.L + it.l) + it.row0;
         const int tm_l = a.g.row_off ? 0 : it.l, tm_b = a.g.row_off ? 0 : it.b;
-        for (int i = 0; ok && i < 2 * it.nb; ++i) {
-          // in the order the issuing thread uses them.  Pair: K0 V0 K1 V1 ..; alternate: K0 K1 V0 K2 V1 ..
+        // in the order of use: the first `ahead` tiles of K, then V(g), K(g + ahead), V(g + 1), ...
+        const int ahead = min(it.pair ? 2 : 4, it.n);
+        for (int i = 0; ok && i < 2 * it.n; ++i) {
+          const int after = i - ahead;
           bool is_k;
-          int j;
-          if (it.pair) { is_k = !(i & 1); j = i >> 1; }
-          else if (i == 0 || i == 2 * it.nb - 1) { is_k = i == 0; j = is_k ? 0 : it.nb - 1; }
-          else { is_k = i & 1; j = is_k ? (i + 1) >> 1 : (i - 2) >> 1; }
+          int g;
+          if (after < 0) { is_k = true; g = i; }
+          else if (after < 2 * (it.n - ahead)) { is_k = after & 1; g = (after >> 1) + (is_k ? ahead : 0); }
+          else { is_k = false; g = after - (it.n - ahead); }
           const uint32_t at = pos + i;
-          if (at >= kTaSlots) ok = wait(empty(at), (at / kTaSlots - 1) & 1u);
+          if (at >= SLOTS) ok = wait(empty(at), (at / SLOTS - 1) & 1u);
           if (!ok) break;
+          if (!it.pair) mbar_arrive(empty(at));          // for the chain that does not use it
           mbar_expect_tx(full(at), TILE);
           for (int c = 0; c < D / 64; ++c)
-            tma_load_5d(s_ring + (at % kTaSlots) * TILE + c * kTaHalf, is_k ? &map_k : &map_v, full(at), c * 64,
-                        row0 + (it.blk0 + j) * kTaRows, it.h, tm_l, tm_b);
+            tma_load_5d(s_ring + (at % SLOTS) * TILE + c * kTaSubHalf, is_k ? &map_k : &map_v, full(at), c * 64,
+                        row0 + g * kTaSub, it.h, tm_l, tm_b);
         }
       }
       ok = __shfl_sync(0xffffffffu, ok, 0);
-      pos += 2 * it.nb;
+      pos += 2 * it.n;
       ++n_q;
     }
     if (!ok) {
       *s_fail = 1;
       // copies that may still be in flight: the last ones of every slot, and the query tiles
       if (lane == 0) {
-        for (int i = 0; i < kTaSlots; ++i) { mbar_wait<12>(bars + 8u * i, 0); mbar_wait<12>(bars + 8u * i, 1); }
+        for (int i = 0; i < SLOTS; ++i) { mbar_wait<12>(full(i), 0); mbar_wait<12>(full(i), 1); }
         mbar_wait<12>(q_full, 0); mbar_wait<12>(q_full, 1);
       }
     }
-   } else if (warp == 8) {
-    // ---- matrix products: the whole warp walks the items, one elected lane issues -------------------
+  } else if (warp == 8 || warp == 10) {
+    // ---- matrix products of one chain: the whole warp walks the items, one elected lane issues --------
+    const int c = warp == 10;
     bool ok = true;
-    uint32_t n_item = 0, n_q = 0, np0 = 0, np1 = 0;
-    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    uint32_t n_item = 0, n_q = 0, n_s = 0, n_p = 0;      // running numbers: items, scores issued, weights used
+    const uint32_t t_c = __shfl_sync(0xffffffffu, tmem, 0) + c * 256;
     auto commit = [&](uint32_t bar) { if (elect_one()) umma_commit(bar); };
     while (true) {
       ok = __all_sync(0xffffffffu, wait(item_full(n_item), (n_item / 2) & 1u));
       if (!ok) break;
       const bool stop = __shfl_sync(0xffffffffu, items[n_item & 1].stop, 0);
       const bool pair = __shfl_sync(0xffffffffu, items[n_item & 1].pair, 0);
-      const int nb = __shfl_sync(0xffffffffu, items[n_item & 1].nb, 0);
-      const int nb0 = __shfl_sync(0xffffffffu, items[n_item & 1].nb0, 0);
-      if (lane == 0) mbar_arrive(item_free(n_item));
+      const int n = __shfl_sync(0xffffffffu, items[n_item & 1].n, 0);
+      const int n0 = __shfl_sync(0xffffffffu, items[n_item & 1].n0, 0);
       __syncwarp();
+      if (lane == 0) mbar_arrive(item_free(n_item));
       ++n_item;
       if (stop) break;
-      if (nb == 0) continue;
-      auto qk = [&](int c, uint32_t at) {                // S[c] = Q K^T
-        const uint64_t dq = umma_desc(s_q + (pair ? c * TILE : 0), 16, 1024);
-        const uint64_t dk = umma_desc(s_ring + (at % kTaSlots) * TILE, 16, 1024);
-        if (elect_one()) {
+      if (n == 0) continue;
+      const int mine = pair ? (c ? n : n0) : (n + 1 - c) / 2;
+      const TaRing ring{pos, n, pair ? 2 : 4};
+      const uint64_t dq = umma_desc(s_q + (pair ? c * QTILE : 0), 16, 1024);
+      auto qk = [&](uint32_t at) {                       // S[n_s & 1] = Q K^T; elected lane only
+        const uint64_t dk = umma_desc(s_ring + (at % SLOTS) * TILE, 16, 1024);
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            const uint32_t off = ((k >> 2) * kTaHalf + (k & 3) * 32) >> 4;   // the address field counts 16 bytes
-            umma_ss(tm + c * 256, dq + off, dk + off, kTaIdescQK, k > 0);
-          }
-          umma_commit(s_full(c));
-        }
-      };
-      auto pv = [&](int c, uint32_t at, int half, bool first) {              // O[c] += P V, 64 rows of the block
-        const uint64_t dv = umma_desc(s_ring + (at % kTaSlots) * TILE, kTaHalf, 1024);
-        if (elect_one()) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            umma_ts(tm + c * 256 + 128, tm + c * 256 + 32 * half + k * 8, dv + ((half * 4 + k) * 2048 >> 4),
-                    kTaIdescPV<D>, first && half == 0 && k == 0 ? 0u : 1u);
-        }
-      };
-      auto landed = [&](uint32_t at) { ok = wait(full(at), (at / kTaSlots) & 1u) && ok; };
-      // both halves of a block's weights, each multiplied as soon as it is there
-      auto weights_v = [&](int c, uint32_t at, bool first) {
-        const uint32_t parity = (c ? np1 : np0) & 1u;
-        if (c) ++np1; else ++np0;
-        ok = wait(p_half(c), parity) && ok;
-        tc_fence_after();
-        pv(c, at, 0, first);
-        ok = wait(p_full(c), parity) && ok;
-        tc_fence_after();
-        pv(c, at, 1, false);
+        for (int k = 0; k < D / 16; ++k)                 // (the address fields count 16 bytes)
+          umma_ss(t_c + (n_s & 1) * 64, dq + (((k >> 2) * kTaHalf + (k & 3) * 32) >> 4),
+                  dk + (((k >> 2) * kTaSubHalf + (k & 3) * 32) >> 4), kTaIdescQK, k > 0);
+        umma_commit(s_full(c, n_s));
+        umma_commit(empty(at));
       };
       ok = wait(q_full, n_q & 1u);
       ++n_q;
-      if (pair) {
-        // chain 0's tokens come first, so it never has more blocks than chain 1
-        landed(pos);
+      for (int u = 0; u < min(2, mine); ++u, ++n_s) {
+        const uint32_t at = ring.k_at(pair ? u : 2 * u + c);
+        ok = landed(at) && ok;
         tc_fence_after();
-        if (nb0 > 0) qk(0, pos);
-        qk(1, pos);
-        commit(empty(pos));
-        if (nb == 1) commit(q_free);
-        for (int j = 0; j < nb; ++j) {
-          const uint32_t v = pos + 2 * j + 1, kn = v + 1;
-          const bool more = j + 1 < nb;
-          landed(v);
-          if (more) landed(kn);
-          if (!__all_sync(0xffffffffu, ok)) break;
-          if (j < nb0) {
-            weights_v(0, v, j == 0);
-            if (j + 1 < nb0) qk(0, kn); else commit(o_full(0));
-          }
-          weights_v(1, v, j == 0);
-          commit(empty(v));
-          if (more) {
-            qk(1, kn);
-            commit(empty(kn));
-            if (j + 2 == nb) commit(q_free);
-          } else {
-            commit(o_full(1));
-          }
-        }
-      } else {
-        auto k_at = [&](int j) { return pos + (j == 0 ? 0 : 2 * j - 1); };
-        auto v_at = [&](int j) { return pos + (j == nb - 1 ? 2 * nb - 1 : 2 * j + 2); };
-        for (int j = 0; j < 2 && j < nb; ++j) {
-          landed(k_at(j));
-          tc_fence_after();
-          qk(j, k_at(j));
-          commit(empty(k_at(j)));
-        }
-        if (nb <= 2) commit(q_free);
-        for (int j = 0; j < nb; ++j) {
-          const int c = j & 1;
-          landed(v_at(j));
-          if (!__all_sync(0xffffffffu, ok)) break;
-          weights_v(c, v_at(j), j < 2);
-          commit(empty(v_at(j)));
-          if (j + 2 < nb) {
-            landed(k_at(j + 2));
-            tc_fence_after();
-            qk(c, k_at(j + 2));
-            commit(empty(k_at(j + 2)));
-            if (j + 3 == nb) commit(q_free);
-          } else {
-            commit(o_full(c));
-          }
-        }
+        if (elect_one()) qk(at);
       }
-      pos += 2 * nb;
+      if (mine <= 2) commit(q_free);
+      for (int u = 0; u < mine; ++u, ++n_p) {
+        // Everything that will be there anyway is checked before the weights are waited for: a check costs
+        // about 100 cycles, and the softmax waits for what is issued behind the weights.
+        const uint32_t v = ring.v_at(pair ? u : 2 * u + c), kn = ring.k_at(pair ? u + 2 : 2 * u + 4 + c);
+        const bool next = u + 2 < mine;
+        ok = landed(v) && ok;
+        if (next) ok = landed(kn) && ok;
+        ok = wait(p_full(c, n_p), (n_p >> 1) & 1u) && ok;
+        if (!__all_sync(0xffffffffu, ok)) break;
+        tc_fence_after();
+        const uint64_t dv = umma_desc(s_ring + (v % SLOTS) * TILE, kTaSubHalf, 1024);
+        if (elect_one()) {                               // O += P V(u)
+#pragma unroll
+          for (int k = 0; k < kTaSub / 16; ++k)
+            umma_ts(t_c + 128, t_c + (n_p & 1) * 64 + k * 8, dv + (k * 2048 >> 4), kTaIdescPV<D>, u > 0 || k > 0);
+          umma_commit(empty(v));
+          // The score columns that P V(u) reads its weights from take scores u + 2: both products come
+          // from one thread and run on one tensor core, which takes them in the order of issue.
+          if (next) qk(kn);
+          umma_commit(pv_done(c, n_p));
+          if (u + 1 == mine) umma_commit(o_full(c));
+          if (u + 3 == mine) umma_commit(q_free);
+        }
+        if (next) ++n_s;
+      }
+      // tiles behind the last that chain 0 of a pair has a use for
+      if (pair && c == 0)
+        for (int g = mine; ok && g < n; ++g) {
+          ok = landed(ring.k_at(g));
+          if (lane == 0) mbar_arrive(empty(ring.k_at(g)));
+          ok = landed(ring.v_at(g)) && ok;
+          if (lane == 0) mbar_arrive(empty(ring.v_at(g)));
+          __syncwarp();
+        }
+      pos += 2 * n;
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
     }
     if (!ok) {
       *s_fail = 1;
-      commit(drained);                                   // products in flight read this CTA's shared memory
-      mbar_wait<14>(drained, 0);
+      commit(drained(c));                                // products in flight read this CTA's shared memory
+      mbar_wait<14>(drained(c), 0);
     }
-    __syncwarp();
-   }
-  } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+  } else if (warp < 8) {
     // ---- softmax: one thread per query row of its chain -----------------------------------------------
     const int chain = warp >> 2, row = tid & (kTaRows - 1);
-    const uint32_t t_s = tmem + chain * 256 + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_s + 128;
+    const uint32_t t_c = tmem + chain * 256 + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_c + 128;
     const uint32_t t_o0 = tmem + 128 + ((uint32_t)((warp & 3) * 32) << 16), t_o1 = t_o0 + 256;
     uint4* const stage = reinterpret_cast<uint4*>(stage_base + warp * kTaStage);
     const int tok_in_tile = row / A.G, head_in_group = row % A.G;
     uint32_t n_item = 0, n_s = 0, n_o = 0, n_sync = 0;
+    int other_s = 0;                                     // the other chain's n_s at the start of the item
+    volatile int* const my_turn = s_turn + chain * 4 + (warp & 3);
+    volatile int* const other_turn = s_turn + (1 - chain) * 4 + (warp & 3);
     bool ok = true;
     auto sync_chains = [&]() {                           // all eight softmax warps, bounded
       __syncwarp();
@@ -606,77 +597,70 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       // rows this token sees: all below `limit`, and, from row `base` on, those of its mask
       const int limit = !valid ? 0 : TREE ? it.end : min(it.end, it.base + it.s0 + q + 1);
       const uint32_t* mask = TREE ? a.mask + (long long)(it.tok0 + (valid ? q : 0)) * 2 * a.mask_words : nullptr;
-      const int nb_mine = it.pair ? (chain ? it.nb : it.nb0) : (it.nb + 1 - chain) / 2;
+      const int mine = it.pair ? (chain ? it.n : it.n0) : (it.n + 1 - chain) / 2;
+      const int others = it.pair ? (chain ? it.n0 : it.n) : (it.n + chain) / 2;
+      const TaRing ring{pos, it.n, it.pair ? 2 : 4};
       float m_ref = -INFINITY, sum = 0.f;
 
-      for (int jj = 0; jj < nb_mine; ++jj) {
-        const int j = it.pair ? jj : 2 * jj + chain;                         // block within the item
-        const int r0 = (it.blk0 + j) * kTaRows;                              // its first row
-        ok = __all_sync(0xffffffffu, wait(s_full(chain), n_s & 1u));
-        ++n_s;
+      for (int u = 0; u < mine; ++u, ++n_s) {
+        const int g = it.pair ? u : 2 * u + chain;                           // sub-block within the item
+        const int r0 = it.row0 + g * kTaSub;                                 // its first row
+        const uint32_t t_s = t_c + (n_s & 1) * 64;
+        ok = __all_sync(0xffffffffu, wait(s_full(chain, n_s), (n_s >> 1) & 1u));
         if (!ok) break;
         tc_fence_after();
         // Rows of the V tile that no token of the item sees can hold anything; clear them, so that a zero
         // weight times Inf or NaN cannot reach O (in a pair both chains write the same zeros).
-        if (it.end - r0 < kTaRows) {
-          const uint32_t v = pos + (it.pair ? 2 * j + 1 : j == it.nb - 1 ? 2 * it.nb - 1 : 2 * j + 2);
-          ok = __all_sync(0xffffffffu, wait(full(v), (v / kTaSlots) & 1u));
+        if (it.end - r0 < kTaSub) {
+          const uint32_t v = ring.v_at(g);
+          ok = __all_sync(0xffffffffu, landed(v));
           if (!ok) break;
-          if (row >= it.end - r0) {
+          if (row < kTaSub && row >= it.end - r0) {
 #pragma unroll
             for (int c = 0; c < D / 8; ++c)
-              st_shared16(s_ring + (v % kTaSlots) * TILE + (c >> 3) * kTaHalf + row * 128 + ((c & 7) << 4), 0, 0, 0, 0);
+              st_shared16(s_ring + (v % SLOTS) * TILE + (c >> 3) * kTaSubHalf + row * 128 + ((c & 7) << 4), 0, 0, 0, 0);
           }
           proxy_fence();
         }
         if (warp_valid) {
-          uint32_t x[64], y[64];
+          uint32_t x[64];
           tmem_ld64_issue(t_s, x);
-          tmem_ld64_wait(x);
-          tmem_ld64_issue(t_s + 64, y);
           // the bits of a word of 32 columns that this thread's row sees
-          const bool masked = TREE ? r0 + kTaRows > it.base : __any_sync(0xffffffffu, limit < r0 + kTaRows);
-          auto seen = [&](int w) {
-            uint32_t bits = low_bits(limit - r0 - 32 * w);
-            if constexpr (TREE) {
-              const int c = r0 + 32 * w - it.base;       // mask column of the word's first row
-              if (c > -32 && bits) {
-                const int i = c >= 0 ? c >> 5 : 0, n_words = 2 * a.mask_words;
-                const uint32_t lo = c < 0 || i < n_words ? mask[i] : 0u;
-                bits &= c < 0 ? low_bits(-c) | lo << -c
-                              : __funnelshift_r(lo, i + 1 < n_words ? mask[i + 1] : 0u, c & 31);
-              }
-            }
-            return bits;
-          };
-          auto hide = [&](uint32_t (&v)[64], int w0) {
+          const bool masked = TREE ? r0 + kTaSub > it.base : __any_sync(0xffffffffu, limit < r0 + kTaSub);
+          tmem_ld64_wait(x);
+          if (masked) {
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-              const uint32_t bits = seen(w0 + w);
+              uint32_t bits = low_bits(limit - r0 - 32 * w);
+              if constexpr (TREE) {
+                const int c = r0 + 32 * w - it.base;     // mask column of the word's first row
+                if (c > -32 && bits) {
+                  const int i = c >= 0 ? c >> 5 : 0, n_words = 2 * a.mask_words;
+                  const uint32_t lo = c < 0 || i < n_words ? mask[i] : 0u;
+                  bits &= c < 0 ? low_bits(-c) | lo << -c
+                                : __funnelshift_r(lo, i + 1 < n_words ? mask[i + 1] : 0u, c & 31);
+                }
+              }
 #pragma unroll
               for (int i = 0; i < 32; ++i)
-                if (!(bits >> i & 1u)) v[32 * w + i] = 0xff800000u;          // -inf
+                if (!(bits >> i & 1u)) x[32 * w + i] = 0xff800000u;          // -inf
             }
-          };
-          auto top_of = [&](const uint32_t (&v)[64]) {
-            float t0 = __uint_as_float(v[0]), t1 = __uint_as_float(v[1]);
+          }
+          float t0 = __uint_as_float(x[0]), t1 = __uint_as_float(x[1]);
 #pragma unroll
-            for (int i = 2; i < 62; i += 4) {
-              t0 = fmaxf(t0, fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 1])));
-              t1 = fmaxf(t1, fmaxf(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])));
-            }
-            return fmaxf(t0, fmaxf(t1, fmaxf(__uint_as_float(v[62]), __uint_as_float(v[63]))));
-          };
-          if (masked) hide(x, 0);
-          float top = top_of(x);
-          tmem_ld64_wait(y);
-          if (masked) hide(y, 2);
-          top = fmaxf(top, top_of(y));
+          for (int i = 2; i < 62; i += 4) {
+            t0 = fmaxf(t0, fmaxf(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
+            t1 = fmaxf(t1, fmaxf(__uint_as_float(x[i + 2]), __uint_as_float(x[i + 3])));
+          }
+          const float top = fmaxf(t0, fmaxf(t1, fmaxf(__uint_as_float(x[62]), __uint_as_float(x[63]))));
           const float m_new = fmaxf(m_ref, top * a.scale_log2e);
-          if (jj == 0) m_ref = m_new;
-          // O is quiet here: these scores were issued behind the last P V of this chain
+          if (u == 0) m_ref = m_new;
           const bool need = m_new > m_ref + kTaRescaleGap;
           if (__any_sync(0xffffffffu, need)) {
+            // O is quiet once these scores' predecessors, and with them P V(u - 2), and P V(u - 1) are done
+            ok = __all_sync(0xffffffffu, wait(pv_done(chain, n_s - 1), ((n_s - 1) >> 1) & 1u));
+            if (!ok) break;
+            tc_fence_after();
             const float factor = need ? fast_exp2(m_ref - m_new) : 1.f;
 #pragma unroll 1
             for (int c = 0; c < D; c += 8) tmem_scale8(t_o + c, factor);
@@ -685,42 +669,47 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
           const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;             // a row that has seen nothing yet
           const float2 sc2 = make_float2(a.scale_log2e, a.scale_log2e), nm2 = make_float2(neg_m, neg_m);
           float2 sums = make_float2(0.f, 0.f);
-          auto weights = [&](const uint32_t (&v)[64], uint32_t to, auto mixed) {
+#if L2KV_TA_TURN
+          // The two warps of a scheduler, one per chain, take turns in the exponentials: side by side both would
+          // be slowed to half speed and then wait for the tensor core together, in step for good.
+          // (Only the pace depends on it: a turn that does not come is not waited for.)
+          if (chain ? u < others : u <= others) {
+            const int until = other_s + u + chain;
+            for (int spin = 0; spin < 128 && *other_turn - until < 0; ++spin) {}
+          }
+#endif
+          auto weights = [&](auto mixed) {
+            uint32_t pk[32];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {                // 32 columns: 16 words of bf16 pairs
-              uint32_t pk[16];
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const float2 e = fma2(make_float2(__uint_as_float(v[32 * c + 2 * i]), __uint_as_float(v[32 * c + 2 * i + 1])), sc2, nm2);
-                float2 w;
-                if (decltype(mixed)::value && kTaPolyEvery && i % (kTaPolyEvery ? kTaPolyEvery : 1) == 0) w = poly_exp2(e);
-                else w = make_float2(fast_exp2(e.x), fast_exp2(e.y));
-                sums = add2(sums, w);
-                pk[i] = pack_bf16(w.x, w.y);
-              }
-              tmem_st16(to + 16 * c, pk);
+            for (int i = 0; i < 32; ++i) {
+              const float2 e = fma2(make_float2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), sc2, nm2);
+              float2 w;
+              if (decltype(mixed)::value && kTaPolyEvery && i % (kTaPolyEvery ? kTaPolyEvery : 1) == 0) w = poly_exp2(e);
+              else w = make_float2(fast_exp2(e.x), fast_exp2(e.y));
+              sums = add2(sums, w);
+              pk[i] = pack_bf16(w.x, w.y);
+#if L2KV_TA_TURN
+              if (i == L2KV_TA_TURN_AT) { __syncwarp(); if (lane == 0) *my_turn = (int)n_s + 1; }
+#endif
             }
+            tmem_st32(t_s, pk);
           };
-          if (masked) weights(x, t_s, std::false_type{}); else weights(x, t_s, std::true_type{});
-          tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(p_half(chain));
-          if (masked) weights(y, t_s + 32, std::false_type{}); else weights(y, t_s + 32, std::true_type{});
+          if (masked) weights(std::false_type{}); else weights(std::true_type{});
           tmem_wait_st();
           sum += sums.x + sums.y;
         } else if (lane == 0) {
-          mbar_arrive(p_half(chain));
+          *my_turn = (int)n_s + 1;
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(chain));
+        if (lane == 0) mbar_arrive(p_full(chain, n_s));
       }
       if (!ok) break;
-      pos += 2 * it.nb;
+      pos += 2 * it.n;
+      other_s += others;
 
       // ---- the item's rows go out --------------------------------------------------------------------
-      if (nb_mine > 0) {
+      if (mine > 0) {
         ok = __all_sync(0xffffffffu, wait(o_full(chain), n_o & 1u));
         ++n_o;
         if (!ok) break;
@@ -742,12 +731,12 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
         m = fmaxf(st0.x, st1.x);
         const float low = m == -INFINITY ? 0.f : m;
         f0 = fast_exp2(st0.x - low);
-        f1 = it.nb > 1 ? fast_exp2(st1.x - low) : 0.f;
+        f1 = it.n > 1 ? fast_exp2(st1.x - low) : 0.f;
         total = st0.y * f0 + st1.y * f1;
         c_lo = chain * (D / 2);
         c_hi = c_lo + D / 2;
       }
-      const bool any = warp_valid && it.nb > 0 && (it.pair ? nb_mine > 0 : true);
+      const bool any = it.pair ? mine > 0 : it.n > 0;
       const float inv = total == 0.f ? 0.f : 1.f / total;
       f0 *= inv;
       f1 *= inv;
@@ -759,7 +748,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
             tmem_ld32((it.pair ? t_o : t_o0) + c, x);
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(x[i]) * f0;
-            if (!it.pair && it.nb > 1) {
+            if (!it.pair && it.n > 1) {
               tmem_ld32(t_o1 + c, x);
 #pragma unroll
               for (int i = 0; i < 32; ++i) v[i] = __fmaf_rn(__uint_as_float(x[i]), f1, v[i]);
@@ -894,7 +883,7 @@ static int launch_ta(const TaArgs& A, const void* K, const void* V, long long gr
   std::memset(&map_q, 0, sizeof map_q);
   std::memset(&map_k, 0, sizeof map_k);
   std::memset(&map_v, 0, sizeof map_v);
-  if (!make_query_map(&map_q, a) || !make_cache_map(&map_k, K, a.g, kTaRows) || !make_cache_map(&map_v, V, a.g, kTaRows))
+  if (!make_query_map(&map_q, a) || !make_cache_map(&map_k, K, a.g, kTaSub) || !make_cache_map(&map_v, V, a.g, kTaSub))
     return L2KV_ERR_UNSUPPORTED;
   auto kern = token_attention_kernel<D, TREE>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTaSmem<D>) != cudaSuccess)
