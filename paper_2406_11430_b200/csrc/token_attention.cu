@@ -47,8 +47,8 @@ constexpr int kTaPolyEvery = L2KV_TA_POLY;      // of so many weight pairs one i
 constexpr int kTaGrid = 148;                    // one CTA per SM (512 tensor-memory columns each)
 constexpr int kTaCtrl = 3072;                   // barriers, items, row statistics
 constexpr int kTaPolls = 18;                    // log2 of the polls a wait may take
-constexpr int kTaMaxGroups = 2 * kTaGrid;       // calls with at most so many items are cut into chunks
-constexpr int kTaMinChunk = 8;                  // blocks per chunk at least
+constexpr int kTaItemCost = 6;                  // what starting and finishing an item costs, in sub-blocks
+constexpr int kTaMinShare = 24;                 // items that cost less on average are not cut
 constexpr float kTaRescaleGap = 8.f;            // log2 units a maximum may drift before O is rescaled
 
 template <int D> constexpr int kTaQTile = D / 64 * kTaHalf;
@@ -72,19 +72,14 @@ struct TaItem {
   int stop;              // no more items
 };
 
-struct TaPlan {
-  int chunk_blocks;      // 0: whole items, longest first; else the chunk length
-  long long items;
-};
-
+struct TaSpot;
 struct TaArgs {
   TokenAttention a;
   int G, QT;             // query heads per KV head, tokens per tile
-  int chunked;
-  int32_t* plan;         // chunk length for the joining kernel
-  float* part;           // [slots][slot_rows][D] rows, then [slots][slot_rows] log2-sum-exps
+  TaSpot* plan;          // [kTaGrid] where each CTA's share begins, for the joining kernel; null: items stay whole
+  float* part;           // [2 kTaGrid][slot_rows][D] rows, then [2 kTaGrid][slot_rows] log2-sum-exps
   float* part_lse;
-  int slot_rows, slots;
+  int slot_rows;
 };
 
 // ---- the items, worked out by a warp from the device's lengths ------------------------------------
@@ -96,95 +91,119 @@ __device__ __forceinline__ TaEntry ta_entry(const TokenAttention& a, int b, int 
   const int cur = max(0, min(a.lens.at(bl, h, a.g.H), min(a.max_len, a.g.cap(bl))));
   return {n, cur, cur - n};
 }
-// Rows that the first `upto` tokens of the sequence see at most.
+// Rows that the first `upto` tokens of the sequence see at most, and their sub-blocks.
 __device__ __forceinline__ int ta_end(const TokenAttention& a, const TaEntry& e, int upto) {
   return a.mask ? e.cur : max(0, min(e.cur, e.base + min(upto, e.n)));
 }
-// An entry as the plan sees it: with a length per head, the longest head's.
-__device__ __forceinline__ TaEntry ta_plan_entry(const TokenAttention& a, int b, int l) {
-  TaEntry e = ta_entry(a, b, l, 0);
-  if (a.lens.per_head && e.n > 0) {
-    for (int h = 1; h < a.g.H; ++h) e.cur = max(e.cur, ta_entry(a, b, l, h).cur);
-    e.base = e.cur - e.n;
+__device__ __forceinline__ int ta_subs(int rows) { return (rows + kTaSub - 1) / kTaSub; }
+// An entry as the shares see it: with a length per head, the longest head's.
+__device__ __forceinline__ TaEntry ta_plan_entry(const TokenAttention& a, int e) {
+  const int b = e / a.g.L, l = e % a.g.L;
+  TaEntry x = ta_entry(a, b, l, 0);
+  if (a.lens.per_head && x.n > 0) {
+    for (int h = 1; h < a.g.H; ++h) x.cur = max(x.cur, ta_entry(a, b, l, h).cur);
+    x.base = x.cur - x.n;
   }
-  return e;
+  return x;
 }
-__device__ __forceinline__ int ta_chunks(const TokenAttention& a, const TaEntry& e, int p, int QP, int C) {
-  const int nb = (ta_end(a, e, (p + 1) * QP) + kTaRows - 1) / kTaRows;
-  return max(1, (nb + C - 1) / C);
-}
-// Chunks of one head of every item of (b, l).
-__device__ __forceinline__ int ta_entry_chunks(const TokenAttention& a, const TaEntry& e, int QP, int C) {
-  int sum = 0;
-  for (int p = 0; p * QP < e.n; ++p) sum += ta_chunks(a, e, p, QP, C);
+// Cost of the first m items (pairs of tiles, one head) of an entry: their sub-blocks, and kTaItemCost for each.
+__device__ __forceinline__ long long ta_cost(const TokenAttention& a, const TaEntry& e, int QP, int m) {
+  const int pairs = (e.n + QP - 1) / QP;
+  if (m <= 0) return 0;
+  if (a.mask) return (long long)m * (ta_subs(e.cur) + kTaItemCost);
+  long long sum = (long long)m * kTaItemCost;
+  if (m >= pairs) { sum += ta_subs(e.cur); m = pairs - 1; }                  // the last one ends where the cache does
+  // the others see base + k QP rows, k = 1 .. m
+  if (e.base < 0) {
+    for (int k = 1; k <= m; ++k) sum += ta_subs(max(0, e.base + k * QP));
+  } else if (QP % kTaSub == 0) {
+    sum += (long long)m * ta_subs(e.base) + (long long)(QP / kTaSub) * m * (m + 1) / 2;
+  } else {                                               // QP is half a sub-block: odd and even k
+    const long long even = m / 2, odd = (m + 1) / 2;
+    sum += even * ta_subs(e.base) + even * (even + 1) / 2 + odd * ta_subs(e.base + QP) + odd * (odd - 1) / 2;
+  }
   return sum;
 }
 
-// The shortest chunk length with which all chunks fit the grid (as many times as whole items need).
+// A place in the list of all items, (b, l) by (b, l), within it tile pair by tile pair, within that head by
+// head: an item, the cost of everything before it, and a number of its sub-blocks.
+struct TaSpot {
+  long long at;
+  int e, p, h, off;
+};
+
+struct TaPlan {
+  long long items, share;    // share 0: whole items, longest first; else what a CTA takes, in cost
+};
 __device__ __forceinline__ TaPlan ta_plan(const TaArgs& A) {
   const TokenAttention& a = A.a;
-  const int lane = threadIdx.x & 31, QP = 2 * A.QT;
-  long long groups = 0;
-  const int entries = A.chunked ? a.g.B * a.g.L : a.g.B;
-  for (int e = lane; e < entries; e += 32)
-    groups += (tokens_of(a.tok_off, A.chunked ? e / a.g.L : e, a.n_tokens).n + QP - 1) / QP;
-  for (int off = 16; off; off >>= 1) groups += __shfl_xor_sync(0xffffffffu, groups, off);
-  if (!A.chunked) return {0, groups * a.g.L * a.g.H};
-  const int target = (int)min((long long)A.slots, (groups * a.g.H + kTaGrid - 1) / kTaGrid * kTaGrid);
-  auto count = [&](int C) {
-    int sum = 0;
-    for (int e = lane; e < entries; e += 32) {
-      const TaEntry x = ta_plan_entry(a, e / a.g.L, e % a.g.L);
-      if (x.n > 0) sum += ta_entry_chunks(a, x, QP, C);
-    }
-    return (int)__reduce_add_sync(0xffffffffu, (unsigned)sum) * a.g.H;
-  };
-  int lo = kTaMinChunk, hi = max(kTaMinChunk, (a.max_len + kTaRows - 1) / kTaRows);
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (count(mid) <= target) hi = mid; else lo = mid + 1;
+  const int lane = threadIdx.x & 31, QP = 2 * A.QT, L = a.g.L;
+  long long items = 0, cost = 0;
+  for (int e = lane; e < a.g.B * L; e += 32) {
+    const int n = tokens_of(a.tok_off, e / L, a.n_tokens).n, pairs = (n + QP - 1) / QP;
+    items += pairs;
+    if (A.plan && n > 0) cost += ta_cost(a, ta_plan_entry(a, e), QP, pairs);
   }
-  return {lo, (long long)count(lo)};
+#pragma unroll
+  for (int off = 16; off; off >>= 1) {
+    items += __shfl_xor_sync(0xffffffffu, items, off);
+    cost += __shfl_xor_sync(0xffffffffu, cost, off);
+  }
+  items *= a.g.H;
+  cost *= a.g.H;
+  if (!A.plan || cost < items * kTaMinShare) return {items, 0};
+  return {items, max((long long)kTaMinShare, (cost + kTaGrid - 1) / kTaGrid)};
 }
 
-// Where number k of the chunks (by_group false), or of the whole items, of a chunked call lies.
-struct TaPlace { int b, l, p, h, c, n_chunks, first; bool ok; };
-__device__ __forceinline__ TaPlace ta_place(const TaArgs& A, int C, int k, bool by_group) {
+// The spot at cost x; a spot close to an item's start or end is moved there, so that no sliver is cut off.
+__device__ __forceinline__ TaSpot ta_spot(const TaArgs& A, long long x, long long share) {
   const TokenAttention& a = A.a;
   const int lane = threadIdx.x & 31, QP = 2 * A.QT, entries = a.g.B * a.g.L, H = a.g.H;
-  int before = 0, chunks_before = 0;
+  long long before = 0;
   for (int e0 = 0; e0 < entries; e0 += 32) {
     const int e = e0 + lane;
-    TaEntry x{0, 0, 0};
-    if (e < entries) x = ta_plan_entry(a, e / a.g.L, e % a.g.L);
-    const int n_ch = x.n > 0 ? ta_entry_chunks(a, x, QP, C) * H : 0;
-    const int mine = by_group ? (x.n + QP - 1) / QP * H : n_ch;
-    int incl = mine, incl_ch = n_ch;
+    TaEntry y{0, 0, 0};
+    if (e < entries) y = ta_plan_entry(a, e);
+    const long long mine = y.n > 0 ? ta_cost(a, y, QP, (y.n + QP - 1) / QP) * H : 0;
+    long long incl = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, incl, off), o2 = __shfl_up_sync(0xffffffffu, incl_ch, off);
-      if (lane >= off) { incl += o; incl_ch += o2; }
+      const long long o = __shfl_up_sync(0xffffffffu, incl, off);
+      if (lane >= off) incl += o;
     }
-    const unsigned hit = __ballot_sync(0xffffffffu, k < before + incl);
+    const unsigned hit = __ballot_sync(0xffffffffu, x < before + incl);
     if (hit) {
       const int who = __ffs(hit) - 1;
-      int rest = k - before - __shfl_sync(0xffffffffu, incl - mine, who);
-      int first = chunks_before + __shfl_sync(0xffffffffu, incl_ch - n_ch, who);
-      const int ee = e0 + who;
-      const TaEntry y = ta_plan_entry(a, ee / a.g.L, ee % a.g.L);
-      for (int p = 0; p * QP < y.n; ++p) {
-        const int nc = ta_chunks(a, y, p, QP, C), each = by_group ? 1 : nc;
-        if (rest < each * H) return {ee / a.g.L, ee % a.g.L, p, rest / each, rest % each, nc, first + rest / each * nc, true};
-        rest -= each * H;
-        first += nc * H;
+      const long long start = before + __shfl_sync(0xffffffffu, incl - mine, who), rest = x - start;
+      const TaEntry z = ta_plan_entry(a, e0 + who);
+      int lo = 0, hi = (z.n + QP - 1) / QP - 1;          // the last tile pair that begins at or before rest
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (ta_cost(a, z, QP, mid) * H <= rest) lo = mid; else hi = mid - 1;
       }
+      const long long first = ta_cost(a, z, QP, lo), each = ta_cost(a, z, QP, lo + 1) - first;
+      const long long inside = rest - first * H;
+      const int n = (int)each - kTaItemCost, near = 4 + (int)min(share / 64, 64ll);
+      TaSpot s{start + first * H + inside / each * each, e0 + who, lo, (int)(inside / each), 0};
+      s.off = max(0, (int)(inside % each) - kTaItemCost);
+      if (s.off < near) s.off = 0;
+      if (n - s.off < near && s.off > 0) {               // on to the next item
+        s.off = 0;
+        s.at += each;
+        if (++s.h == H) { s.h = 0; ++s.p; }
+        if (s.p * QP >= z.n) {
+          s.p = 0;
+          do ++s.e; while (s.e < entries && tokens_of(a.tok_off, s.e / a.g.L, a.n_tokens).n == 0);
+        }
+      }
+      return s;
     }
     before += __shfl_sync(0xffffffffu, incl, 31);
-    chunks_before += __shfl_sync(0xffffffffu, incl_ch, 31);
   }
-  return {0, 0, 0, 0, 0, 0, 0, false};
+  return {before, entries, 0, 0, 0};                     // behind everything
 }
 
+struct TaPlace { int b, l, p, h; bool ok; };
 // Whole items, longest first: layer by layer, and within a layer by level, an item's number of tile
 // pairs' worth of visible rows.  The causal items of a sequence are one per level, a tree's are all at one.
 __device__ __forceinline__ TaPlace ta_place_by_level(const TaArgs& A, long long k, long long items) {
@@ -225,32 +244,30 @@ __device__ __forceinline__ TaPlace ta_place_by_level(const TaArgs& A, long long 
       const int within = rest - __shfl_sync(0xffffffffu, incl - mine, who);
       const TaEntry e = ta_entry(a, b0 + who, l, 0);
       const int p = a.mask ? within : lo - max(0, e.base) / QP;
-      return {b0 + who, l, p, h, 0, 1, -1, p * QP < e.n && p >= 0};
+      return {b0 + who, l, p, h, p * QP < e.n && p >= 0};
     }
     rest -= __shfl_sync(0xffffffffu, incl, 31);
   }
-  return {0, 0, 0, 0, 0, 0, 0, false};
+  return {0, 0, 0, 0, false};
 }
 
-// The item at a place (its chunk's blocks; a chunk can be empty where heads differ in length).
-__device__ __forceinline__ TaItem ta_item(const TaArgs& A, const TaPlace& w, int C) {
+// Sub-blocks [from, to) of the item of (b, l), tile pair p, head h.
+__device__ __forceinline__ TaItem ta_item(const TaArgs& A, int b, int l, int p, int h, int from, int to, int slot) {
   const TokenAttention& a = A.a;
   const int QP = 2 * A.QT;
-  const TaEntry e = ta_entry(a, w.b, w.l, w.h);
+  const TaEntry e = ta_entry(a, b, l, h);
   TaItem it;
-  it.b = w.b; it.l = w.l; it.h = w.h;
-  it.s0 = w.p * QP;
-  it.tok0 = tokens_of(a.tok_off, w.b, a.n_tokens).first + it.s0;
+  it.b = b; it.l = l; it.h = h;
+  it.s0 = p * QP;
+  it.tok0 = tokens_of(a.tok_off, b, a.n_tokens).first + it.s0;
   it.nq = min(QP, e.n - it.s0);
   it.base = e.base;
   it.end = ta_end(a, e, it.s0 + QP);
   it.pair = it.nq > A.QT;
-  const int end0 = ta_end(a, e, it.s0 + A.QT);           // what the first tile's tokens see
-  it.row0 = w.n_chunks > 1 ? w.c * C * kTaRows : 0;
-  const int most = w.n_chunks > 1 ? C * (kTaRows / kTaSub) : INT_MAX;
-  it.n = min(most, max(0, (it.end - it.row0 + kTaSub - 1) / kTaSub));
-  it.n0 = min(most, max(0, (end0 - it.row0 + kTaSub - 1) / kTaSub));
-  it.slot = w.n_chunks > 1 ? w.first + w.c : -1;
+  it.row0 = from * kTaSub;
+  it.n = max(0, min(to, ta_subs(it.end)) - from);
+  it.n0 = max(0, min(to, ta_subs(ta_end(a, e, it.s0 + A.QT))) - from);       // what the first tile's tokens see
+  it.slot = slot;
   it.stop = 0;
   return it;
 }
@@ -414,20 +431,43 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   if (warp == 9) {
     // ---- items and tiles ---------------------------------------------------------------------------
     const TaPlan plan = ta_plan(A);
-    if (A.chunked && blockIdx.x == 0 && lane == 0) *A.plan = plan.chunk_blocks;
+    const int QP = 2 * A.QT, L = a.g.L, H = a.g.H;
+    TaSpot spot{0, 0, 0, 0, 0}, end{0, 0, 0, 0, 0};
+    if (plan.share > 0) {
+      spot = ta_spot(A, blockIdx.x * plan.share, plan.share);
+      end = ta_spot(A, (blockIdx.x + 1) * plan.share, plan.share);
+    }
+    if (A.plan && lane == 0) A.plan[blockIdx.x] = spot;
     bool ok = true;
     uint32_t n_pub = 0, n_q = 0;
     for (int round = 0; ok; ++round) {
-      // every other round backwards: the CTA that had the longest item of one gets the shortest of the next
-      const long long k = (long long)round * gridDim.x +
-                          (round & 1 ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x);
       TaItem it;
       it.stop = 1;
       it.n = 0;
-      if (k < plan.items) {
-        const TaPlace w = A.chunked ? ta_place(A, plan.chunk_blocks, (int)k, false) : ta_place_by_level(A, k, plan.items);
-        // (offsets that decrease can describe more items than there is room for: those stay undone)
-        if (w.ok && (!A.chunked || w.first + w.c < A.slots)) it = ta_item(A, w, plan.chunk_blocks);
+      if (plan.share > 0) {
+        if (spot.at < end.at || spot.off < (spot.at == end.at ? end.off : 0)) {
+          const TaEntry e = ta_plan_entry(a, spot.e);
+          const int n = ta_subs(ta_end(a, e, (spot.p + 1) * QP));
+          const int to = spot.at == end.at ? end.off : n;
+          // a piece that does not begin its item goes to this CTA's first slot, one that does to its second
+          const int slot = spot.off > 0 ? 2 * (int)blockIdx.x : to < n ? 2 * (int)blockIdx.x + 1 : -1;
+          it = ta_item(A, spot.e / L, spot.e % L, spot.p, spot.h, spot.off, to, slot);
+          spot.at += n + kTaItemCost;
+          spot.off = 0;
+          if (++spot.h == H) { spot.h = 0; ++spot.p; }
+          if (spot.p * QP >= e.n) {
+            spot.p = 0;
+            do ++spot.e; while (spot.e < a.g.B * L && tokens_of(a.tok_off, spot.e / L, a.n_tokens).n == 0);
+          }
+        }
+      } else {
+        // every other round backwards: the CTA that had the longest item of one gets the shortest of the next
+        const long long k = (long long)round * gridDim.x +
+                            (round & 1 ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x);
+        if (k < plan.items) {
+          const TaPlace w = ta_place_by_level(A, k, plan.items);
+          if (w.ok) it = ta_item(A, w.b, w.l, w.p, w.h, 0, INT_MAX, -1);
+        }
       }
       if (n_pub >= 2) ok = wait(item_free(n_pub), (n_pub / 2 - 1) & 1u);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
@@ -781,43 +821,35 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512) : "memory");
 }
 
-// Joins the chunks of items that were cut: out = sum_c w_c O_c / sum_c w_c, w_c = 2^(lse_c - max lse), chunk
-// by chunk in order.  A block per item and 32 of its rows, a warp per row at a time.
+// Joins the pieces of items that were cut: out = sum_c w_c O_c / sum_c w_c, w_c = 2^(lse_c - max lse), piece by
+// piece in order.  A block per CTA share and 32 rows of the item that the share's start cuts, a warp per row at
+// a time; an item that several starts cut is the first one's.
 constexpr int kTaJoinWarps = 8;
 template <int D>
 __global__ void __launch_bounds__(32 * kTaJoinWarps)
 token_attention_join_kernel(const __grid_constant__ TaArgs A) {
   constexpr int V = D / 32;
-  __shared__ TaItem s_it;
-  __shared__ int s_first, s_chunks;
   const TokenAttention& a = A.a;
   if (a.status && a.status[2] != 0) return;              // a wait gave up: no output
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (warp == 0) {
-    const int C = *A.plan;
-    const TaPlace w = ta_place(A, C, (int)blockIdx.x, true);
-    if (lane == 0) {
-      s_chunks = w.ok ? w.n_chunks : 0;
-      s_first = w.first;
-      if (w.ok) s_it = ta_item(A, w, C);
-    }
-  }
-  __syncthreads();
-  const int nc = s_chunks, first = s_first;
-  if (nc <= 1 || first + nc > A.slots) return;           // written by the kernel that computed it
-  const TaItem& it = s_it;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = (int)blockIdx.x + 1;
+  const TaSpot s = A.plan[c0];
+  if (s.off == 0 || (A.plan[c0 - 1].at == s.at && A.plan[c0 - 1].off > 0)) return;
+  int c1 = c0 + 1;                                       // shares [c0, c1) begin inside the item
+  while (c1 < kTaGrid && A.plan[c1].at == s.at && A.plan[c1].off > 0) ++c1;
+  const int nc = c1 - c0 + 1;
+  const TaItem it = ta_item(A, s.e / a.g.L, s.e % a.g.L, s.p, s.h, 0, INT_MAX, 0);
+  auto slot = [&](int c) { return c == 0 ? 2 * c0 - 1 : 2 * (c0 + c - 1); };
   const int rows = it.nq * A.G;
   for (int r = (int)blockIdx.y * 32 + warp; r < min(rows, (int)blockIdx.y * 32 + 32); r += kTaJoinWarps) {
-    const long long row = (long long)first * A.slot_rows + r;
     float top = -INFINITY;
-    for (int c = lane; c < nc; c += 32) top = fmaxf(top, A.part_lse[row + (long long)c * A.slot_rows]);
+    for (int c = lane; c < nc; c += 32) top = fmaxf(top, A.part_lse[(long long)slot(c) * A.slot_rows + r]);
 #pragma unroll
     for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
     const float low = top == -INFINITY ? 0.f : top;
     float den = 0.f, num[V] = {};
 #pragma unroll 4
     for (int c = 0; c < nc; ++c) {
-      const long long at = row + (long long)c * A.slot_rows;
+      const long long at = (long long)slot(c) * A.slot_rows + r;
       const float lse2 = A.part_lse[at];
       const float w = lse2 == -INFINITY ? 0.f : exp2f(lse2 - low);
       den += w;
@@ -843,19 +875,19 @@ token_attention_join_kernel(const __grid_constant__ TaArgs A) {
 
 // ---- host ------------------------------------------------------------------------------------------
 
-// Room for chunks: calls that have few items, whatever the sequences' lengths turn out to be.
+// Room for the pieces of items that are cut; none where no item can be long enough to be (see ta_plan).
 struct TaRoom {
-  long long groups;       // items at most
-  int slots, slot_rows;   // 0 slots: items are never cut
+  long long items;        // at most
+  int slot_rows;          // 0: items are never cut
   size_t bytes;
 };
+constexpr size_t kTaPlanBytes = (kTaGrid * sizeof(TaSpot) + 255) / 256 * 256;
 static TaRoom ta_room(const Geom& g, int n_tokens, int max_len) {
   const int G = g.Hq / g.H, QP = 2 * (kTaRows / G);
-  TaRoom r{((long long)n_tokens / QP + std::min(g.B, n_tokens)) * g.L * g.H, 0, 0, 0};
-  if (r.groups <= kTaMaxGroups && max_len > kTaMinChunk * kTaRows) {
-    r.slots = (int)((r.groups + kTaGrid - 1) / kTaGrid * kTaGrid);
+  TaRoom r{((long long)n_tokens / QP + std::min(g.B, n_tokens)) * g.L * g.H, 0, 0};
+  if (max_len > (kTaMinShare - kTaItemCost - 1) * kTaSub) {
     r.slot_rows = (long long)n_tokens * G <= kTaRows ? kTaRows : 2 * kTaRows;
-    r.bytes = 256 + (size_t)r.slots * r.slot_rows * (g.D + 1) * sizeof(float);
+    r.bytes = kTaPlanBytes + (size_t)2 * kTaGrid * r.slot_rows * (g.D + 1) * sizeof(float);
   }
   return r;
 }
@@ -877,7 +909,7 @@ static bool make_query_map(CUtensorMap* map, const TokenAttention& a) {
 }
 
 template <int D, bool TREE>
-static int launch_ta(const TaArgs& A, const void* K, const void* V, long long groups, cudaStream_t s) {
+static int launch_ta(const TaArgs& A, const void* K, const void* V, long long items, cudaStream_t s) {
   const TokenAttention& a = A.a;
   alignas(64) CUtensorMap map_q, map_k, map_v;
   std::memset(&map_q, 0, sizeof map_q);
@@ -888,11 +920,11 @@ static int launch_ta(const TaArgs& A, const void* K, const void* V, long long gr
   auto kern = token_attention_kernel<D, TREE>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTaSmem<D>) != cudaSuccess)
     return L2KV_ERR_CUDA;
-  const unsigned grid = (unsigned)std::min<long long>(kTaGrid, A.chunked ? kTaGrid : groups);
+  const unsigned grid = (unsigned)std::min<long long>(kTaGrid, A.plan ? kTaGrid : items);
   kern<<<grid, kTaThreads, kTaSmem<D>, s>>>(A, map_q, map_k, map_v);
   if (cudaGetLastError() != cudaSuccess) return L2KV_ERR_CUDA;
-  if (A.chunked) {
-    token_attention_join_kernel<D><<<dim3((unsigned)groups, (unsigned)(A.slot_rows / 32)), 32 * kTaJoinWarps, 0, s>>>(A);
+  if (A.plan) {
+    token_attention_join_kernel<D><<<dim3(kTaGrid - 1, (unsigned)(A.slot_rows / 32)), 32 * kTaJoinWarps, 0, s>>>(A);
     if (cudaGetLastError() != cudaSuccess) return L2KV_ERR_CUDA;
   }
   return L2KV_OK;
@@ -907,16 +939,14 @@ int launch_token_attention(const TokenAttention& a, const void* K, const void* V
   A.G = a.g.Hq / a.g.H;
   A.QT = kTaRows / A.G;
   A.slot_rows = room.slot_rows;
-  if (room.slots > 0 && scratch && scratch_bytes >= room.bytes) {
-    A.chunked = 1;
-    A.slots = room.slots;
-    A.plan = reinterpret_cast<int32_t*>(scratch);
-    A.part = reinterpret_cast<float*>(scratch + 256);
-    A.part_lse = A.part + (size_t)room.slots * room.slot_rows * a.g.D;
+  if (room.slot_rows > 0 && scratch && scratch_bytes >= room.bytes) {
+    A.plan = reinterpret_cast<TaSpot*>(scratch);
+    A.part = reinterpret_cast<float*>(scratch + kTaPlanBytes);
+    A.part_lse = A.part + (size_t)2 * kTaGrid * room.slot_rows * a.g.D;
   }
   if (a.g.D == 128)
-    return a.mask ? launch_ta<128, true>(A, K, V, room.groups, s) : launch_ta<128, false>(A, K, V, room.groups, s);
-  return a.mask ? launch_ta<64, true>(A, K, V, room.groups, s) : launch_ta<64, false>(A, K, V, room.groups, s);
+    return a.mask ? launch_ta<128, true>(A, K, V, room.items, s) : launch_ta<128, false>(A, K, V, room.items, s);
+  return a.mask ? launch_ta<64, true>(A, K, V, room.items, s) : launch_ta<64, false>(A, K, V, room.items, s);
 }
 
 }  // namespace l2kv
