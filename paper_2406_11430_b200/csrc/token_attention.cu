@@ -47,7 +47,7 @@ constexpr int kTaPolyEvery = L2KV_TA_POLY;      // of so many weight pairs one i
 constexpr int kTaGrid = 148;                    // one CTA per SM (512 tensor-memory columns each)
 constexpr int kTaCtrl = 3072;                   // barriers, items, row statistics
 constexpr int kTaPolls = 18;                    // log2 of the polls a wait may take
-constexpr int kTaItemCost = 6;                  // what starting and finishing an item costs, in sub-blocks
+constexpr int kTaItemCost = 4;                  // what starting and finishing an item costs, in sub-blocks
 constexpr int kTaMinShare = 24;                 // items that cost less on average are not cut
 constexpr float kTaRescaleGap = 8.f;            // log2 units a maximum may drift before O is rescaled
 
@@ -132,124 +132,99 @@ struct TaSpot {
   int e, p, h, off;
 };
 
-struct TaPlan {
-  long long items, share;    // share 0: whole items, longest first; else what a CTA takes, in cost
-};
-__device__ __forceinline__ TaPlan ta_plan(const TaArgs& A) {
-  const TokenAttention& a = A.a;
-  const int lane = threadIdx.x & 31, QP = 2 * A.QT, L = a.g.L;
-  long long items = 0, cost = 0;
-  for (int e = lane; e < a.g.B * L; e += 32) {
-    const int n = tokens_of(a.tok_off, e / L, a.n_tokens).n, pairs = (n + QP - 1) / QP;
-    items += pairs;
-    if (A.plan && n > 0) cost += ta_cost(a, ta_plan_entry(a, e), QP, pairs);
+// The shares of the CTAs: stretches of the list that cost the same.  Where a share ends inside an item the item
+// is cut, unless items are short on average or there is no room for partial results: then the share ends with
+// the item.  One warp; the first 32 entries stay in registers.
+struct TaShares {
+  const TaArgs& A;
+  TaEntry mine;                // entry number `lane`
+  int entries, QP;
+  long long share;
+  bool cut, one_each;          // one_each: no more items than CTAs, one to each
+  __device__ __forceinline__ TaEntry entry(int e0) const {
+    const int e = e0 + (threadIdx.x & 31);
+    if (e0 == 0) return mine;
+    return e < entries ? ta_plan_entry(A.a, e) : TaEntry{0, 0, 0};
   }
-#pragma unroll
-  for (int off = 16; off; off >>= 1) {
-    items += __shfl_xor_sync(0xffffffffu, items, off);
-    cost += __shfl_xor_sync(0xffffffffu, cost, off);
+  // Cost of the first m items of an entry and one head.
+  __device__ __forceinline__ long long cost(const TaEntry& e, int m) const { return one_each ? m : ta_cost(A.a, e, QP, m); }
+  __device__ __forceinline__ long long cost_of(const TaEntry& e) const {
+    return e.n > 0 ? cost(e, (e.n + QP - 1) / QP) * A.a.g.H : 0;
   }
-  items *= a.g.H;
-  cost *= a.g.H;
-  if (!A.plan || cost < items * kTaMinShare) return {items, 0};
-  return {items, max((long long)kTaMinShare, (cost + kTaGrid - 1) / kTaGrid)};
-}
-
-// The spot at cost x; a spot close to an item's start or end is moved there, so that no sliver is cut off.
-__device__ __forceinline__ TaSpot ta_spot(const TaArgs& A, long long x, long long share) {
-  const TokenAttention& a = A.a;
-  const int lane = threadIdx.x & 31, QP = 2 * A.QT, entries = a.g.B * a.g.L, H = a.g.H;
-  long long before = 0;
-  for (int e0 = 0; e0 < entries; e0 += 32) {
-    const int e = e0 + lane;
-    TaEntry y{0, 0, 0};
-    if (e < entries) y = ta_plan_entry(a, e);
-    const long long mine = y.n > 0 ? ta_cost(a, y, QP, (y.n + QP - 1) / QP) * H : 0;
-    long long incl = mine;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const long long o = __shfl_up_sync(0xffffffffu, incl, off);
-      if (lane >= off) incl += o;
+  __device__ __forceinline__ explicit TaShares(const TaArgs& args) : A(args) {
+    const int lane = threadIdx.x & 31;
+    QP = 2 * A.QT;
+    entries = A.a.g.B * A.a.g.L;
+    mine = lane < entries ? ta_plan_entry(A.a, lane) : TaEntry{0, 0, 0};
+    one_each = false;
+    long long sum = 0;
+    int items = 0;
+    for (int e0 = 0; e0 < entries; e0 += 32) {
+      const TaEntry e = entry(e0);
+      sum += cost_of(e);
+      items += (e.n + QP - 1) / QP;
     }
-    const unsigned hit = __ballot_sync(0xffffffffu, x < before + incl);
-    if (hit) {
-      const int who = __ffs(hit) - 1;
-      const long long start = before + __shfl_sync(0xffffffffu, incl - mine, who), rest = x - start;
-      const TaEntry z = ta_plan_entry(a, e0 + who);
-      int lo = 0, hi = (z.n + QP - 1) / QP - 1;          // the last tile pair that begins at or before rest
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (ta_cost(a, z, QP, mid) * H <= rest) lo = mid; else hi = mid - 1;
+#pragma unroll
+    for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    items = (int)__reduce_add_sync(0xffffffffu, (unsigned)items) * A.a.g.H;
+    cut = A.plan && sum >= (long long)items * kTaMinShare;
+    one_each = !cut && items <= (int)gridDim.x;
+    share = cut ? max((long long)kTaMinShare, (sum + gridDim.x - 1) / gridDim.x)
+                : one_each ? 1 : (sum + gridDim.x - 1) / gridDim.x;
+  }
+  // The next item of the list.
+  __device__ __forceinline__ void next(TaSpot& s, long long cost, int n_tokens) const {
+    s.at += cost;
+    s.off = 0;
+    if (++s.h == A.a.g.H) { s.h = 0; ++s.p; }
+    if (s.p * QP >= n_tokens) {
+      s.p = 0;
+      do ++s.e; while (s.e < entries && tokens_of(A.a.tok_off, s.e / A.a.g.L, A.a.n_tokens).n == 0);
+    }
+  }
+  // Where the share of CTA c begins (c = the number of CTAs: behind everything).  A spot close to an item's
+  // start or end is moved there, so that no sliver is cut off.
+  __device__ __forceinline__ TaSpot begin(int c) const {
+    const int lane = threadIdx.x & 31, H = A.a.g.H;
+    const long long x = c * share;
+    long long before = 0;
+    for (int e0 = 0; e0 < entries; e0 += 32) {
+      const TaEntry y = entry(e0);
+      const long long here = cost_of(y);
+      long long incl = here;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const long long o = __shfl_up_sync(0xffffffffu, incl, off);
+        if (lane >= off) incl += o;
       }
-      const long long first = ta_cost(a, z, QP, lo), each = ta_cost(a, z, QP, lo + 1) - first;
-      const long long inside = rest - first * H;
-      const int n = (int)each - kTaItemCost, near = 4 + (int)min(share / 64, 64ll);
-      TaSpot s{start + first * H + inside / each * each, e0 + who, lo, (int)(inside / each), 0};
-      s.off = max(0, (int)(inside % each) - kTaItemCost);
-      if (s.off < near) s.off = 0;
-      if (n - s.off < near && s.off > 0) {               // on to the next item
-        s.off = 0;
-        s.at += each;
-        if (++s.h == H) { s.h = 0; ++s.p; }
-        if (s.p * QP >= z.n) {
-          s.p = 0;
-          do ++s.e; while (s.e < entries && tokens_of(a.tok_off, s.e / a.g.L, a.n_tokens).n == 0);
+      const unsigned hit = __ballot_sync(0xffffffffu, x < before + incl);
+      if (hit) {
+        const int who = __ffs(hit) - 1;
+        const long long start = before + __shfl_sync(0xffffffffu, incl - here, who), rest = x - start;
+        const TaEntry z{__shfl_sync(0xffffffffu, y.n, who), __shfl_sync(0xffffffffu, y.cur, who),
+                        __shfl_sync(0xffffffffu, y.base, who)};
+        // the last tile pair that begins at or before `rest`: the lanes try 32 of them at a time
+        int lo = 0, step = (z.n + QP - 1) / QP;          // in [lo, lo + step)
+        while (step > 1) {
+          step = (step + 31) / 32;
+          const unsigned m = __ballot_sync(0xffffffffu, cost(z, lo + lane * step) * H <= rest);
+          lo += step * (31 - __clz(m));                  // (costs grow with p; behind the last they stay above rest)
         }
+        const long long first = cost(z, lo);
+        const int each = (int)(cost(z, lo + 1) - first), inside = (int)(rest - first * H);
+        const int n = each - kTaItemCost, near = cut ? 4 + (int)min(share / 64, 64ll) : (n + 1) / 2 + 1;
+        TaSpot s{start + first * H + (long long)(inside / each) * each, e0 + who, lo, inside / each, 0};
+        if (one_each) return s;
+        s.off = max(0, inside % each - kTaItemCost);
+        if (s.off < near) s.off = 0;
+        else if (n - s.off < near) next(s, each, z.n);
+        return s;
       }
-      return s;
+      before += __shfl_sync(0xffffffffu, incl, 31);
     }
-    before += __shfl_sync(0xffffffffu, incl, 31);
+    return {before, entries, 0, 0, 0};
   }
-  return {before, entries, 0, 0, 0};                     // behind everything
-}
-
-struct TaPlace { int b, l, p, h; bool ok; };
-// Whole items, longest first: layer by layer, and within a layer by level, an item's number of tile
-// pairs' worth of visible rows.  The causal items of a sequence are one per level, a tree's are all at one.
-__device__ __forceinline__ TaPlace ta_place_by_level(const TaArgs& A, long long k, long long items) {
-  const TokenAttention& a = A.a;
-  const int lane = threadIdx.x & 31, QP = 2 * A.QT, B = a.g.B, H = a.g.H;
-  const long long per_layer = items / a.g.L;
-  const int l = (int)(k / per_layer);
-  const int rank = (int)(k % per_layer / H), h = (int)(k % per_layer % H);
-  auto at_or_above = [&](int b, int t) {                 // items of sequence b at level t or higher
-    const TaEntry e = ta_entry(a, b, l, 0);
-    const int pairs = (e.n + QP - 1) / QP;
-    if (a.mask) return e.cur / QP >= t ? pairs : 0;
-    return max(0, min(pairs, pairs + max(0, e.base) / QP - t));
-  };
-  auto count = [&](int t) {
-    int sum = 0;
-    for (int b = lane; b < B; b += 32) sum += at_or_above(b, t);
-    return (int)__reduce_add_sync(0xffffffffu, (unsigned)sum);
-  };
-  int lo = 0, hi = (a.max_len + a.n_tokens) / QP + 2;    // the highest level with more than `rank` items at or above
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (count(mid) > rank) lo = mid; else hi = mid - 1;
-  }
-  int rest = rank - count(lo + 1);
-  for (int b0 = 0; b0 < B; b0 += 32) {
-    const int b = b0 + lane;
-    const int mine = b < B ? at_or_above(b, lo) - at_or_above(b, lo + 1) : 0;
-    int incl = mine;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, incl, off);
-      if (lane >= off) incl += o;
-    }
-    const unsigned hit = __ballot_sync(0xffffffffu, rest < incl);
-    if (hit) {
-      const int who = __ffs(hit) - 1;
-      const int within = rest - __shfl_sync(0xffffffffu, incl - mine, who);
-      const TaEntry e = ta_entry(a, b0 + who, l, 0);
-      const int p = a.mask ? within : lo - max(0, e.base) / QP;
-      return {b0 + who, l, p, h, p * QP < e.n && p >= 0};
-    }
-    rest -= __shfl_sync(0xffffffffu, incl, 31);
-  }
-  return {0, 0, 0, 0, false};
-}
+};
 
 // Sub-blocks [from, to) of the item of (b, l), tile pair p, head h.
 __device__ __forceinline__ TaItem ta_item(const TaArgs& A, int b, int l, int p, int h, int from, int to, int slot) {
@@ -291,43 +266,33 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
 // The lowest x bits.
 __device__ __forceinline__ uint32_t low_bits(int x) { return x >= 32 ? 0xffffffffu : x <= 0 ? 0u : (1u << x) - 1u; }
 
-// 32 columns of this warp's 32 rows, one row per lane, to `dst` (the lane's own row at these columns;
-// null: no such row) through this warp's stage: a thread that stored its own row would put 16 bytes
-// into each of 32 different lines per instruction.
-__device__ __forceinline__ void ta_store_bf16(const float (&v)[32], __nv_bfloat16* dst, uint4* stage) {
-  const int lane = threadIdx.x & 31;
+// The way out: columns of this warp's 32 rows, one row per lane, through 4 KB of shared memory, so that a store
+// instruction fills whole sectors of a few rows (a thread that stored its own row would put 16 bytes into each
+// of 32 different lines).  bf16: 64 columns at a time, 4 rows of 128 bytes per instruction; fp32: 32.  Lane i
+// then holds piece i & 7 of the rows 4 k + (i >> 3), whose addresses it asks their owners for once.
+struct TaRows {
+  char* to[8];                                           // null: no such row
+  __device__ __forceinline__ explicit TaRows(void* own) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    stage[lane * 4 + (i ^ ((lane >> 1) & 3))] =
-        make_uint4(pack_bf16(v[8 * i], v[8 * i + 1]), pack_bf16(v[8 * i + 2], v[8 * i + 3]),
-                   pack_bf16(v[8 * i + 4], v[8 * i + 5]), pack_bf16(v[8 * i + 6], v[8 * i + 7]));
-  __syncwarp();
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int r = 8 * k + (lane >> 2);
-    __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(
-        __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), r));
-    const uint4 x = stage[r * 4 + ((lane & 3) ^ ((r >> 1) & 3))];
-    if (to) reinterpret_cast<uint4*>(to)[lane & 3] = x;
+    for (int k = 0; k < 8; ++k)
+      to[k] = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own), 4 * k + (lane >> 3)));
   }
-  __syncwarp();
-}
-__device__ __forceinline__ void ta_store_f32(const float (&v)[32], float* dst, uint4* stage) {
-  const int lane = threadIdx.x & 31;
+  // pieces[i]: bytes [16 i, 16 i + 16) of the lane's own 128
+  __device__ __forceinline__ void store(const uint4 (&pieces)[8], int byte, uint4* stage) const {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    stage[lane * 8 + (i ^ (lane & 7))] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
-                                                    __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
-  __syncwarp();
+    for (int i = 0; i < 8; ++i) stage[lane * 8 + (i ^ (lane & 7))] = pieces[i];
+    __syncwarp();
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const int r = 4 * k + (lane >> 3);
-    float* to = reinterpret_cast<float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), r));
-    const uint4 x = stage[r * 8 + ((lane & 7) ^ (r & 7))];
-    if (to) reinterpret_cast<uint4*>(to)[lane & 7] = x;
+    for (int k = 0; k < 8; ++k) {
+      const int r = 4 * k + (lane >> 3);
+      const uint4 x = stage[r * 8 + ((lane & 7) ^ (r & 7))];
+      if (to[k]) reinterpret_cast<uint4*>(to[k] + byte)[lane & 7] = x;
+    }
+    __syncwarp();
   }
-  __syncwarp();
-}
+};
 
 // Two fp32 operations in one instruction.
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -368,6 +333,8 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   extern __shared__ __align__(1024) unsigned char smem[];
   const TokenAttention& a = A.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // the joining kernel may be set up now; it waits for this one's results by itself
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // A wait that gave up in an earlier call marks the workspace; nothing runs until it is cleared.
   if (a.status && *reinterpret_cast<volatile int32_t*>(a.status + 2) != 0) return;
 
@@ -416,6 +383,21 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
     for (int i = 0; i < 8; ++i) s_turn[i] = 0;
   }
   __syncwarp();
+  // (while the others set up) where this CTA's share of the work begins and ends
+  TaSpot spot{0, 0, 0, 0, 0}, end{0, 0, 0, 0, 0};
+  bool one_each = false;
+  if (warp == 9) {
+    if (lane < 3) {
+      const CUtensorMap* const map = lane == 0 ? &map_q : lane == 1 ? &map_k : &map_v;
+      asm volatile("prefetch.tensormap [%0];" :: "l"(map) : "memory");
+    }
+    __syncwarp();
+    const TaShares shares(A);
+    spot = shares.begin(blockIdx.x);
+    end = shares.begin(blockIdx.x + 1);
+    one_each = shares.one_each;
+    if (A.plan && lane == 0) A.plan[blockIdx.x] = spot;
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -430,43 +412,26 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
 
   if (warp == 9) {
     // ---- items and tiles ---------------------------------------------------------------------------
-    const TaPlan plan = ta_plan(A);
-    const int QP = 2 * A.QT, L = a.g.L, H = a.g.H;
-    TaSpot spot{0, 0, 0, 0, 0}, end{0, 0, 0, 0, 0};
-    if (plan.share > 0) {
-      spot = ta_spot(A, blockIdx.x * plan.share, plan.share);
-      end = ta_spot(A, (blockIdx.x + 1) * plan.share, plan.share);
-    }
-    if (A.plan && lane == 0) A.plan[blockIdx.x] = spot;
+    const int QP = 2 * A.QT, L = a.g.L;
     bool ok = true;
     uint32_t n_pub = 0, n_q = 0;
-    for (int round = 0; ok; ++round) {
+    while (ok) {
       TaItem it;
       it.stop = 1;
       it.n = 0;
-      if (plan.share > 0) {
-        if (spot.at < end.at || spot.off < (spot.at == end.at ? end.off : 0)) {
-          const TaEntry e = ta_plan_entry(a, spot.e);
-          const int n = ta_subs(ta_end(a, e, (spot.p + 1) * QP));
-          const int to = spot.at == end.at ? end.off : n;
-          // a piece that does not begin its item goes to this CTA's first slot, one that does to its second
-          const int slot = spot.off > 0 ? 2 * (int)blockIdx.x : to < n ? 2 * (int)blockIdx.x + 1 : -1;
-          it = ta_item(A, spot.e / L, spot.e % L, spot.p, spot.h, spot.off, to, slot);
-          spot.at += n + kTaItemCost;
-          spot.off = 0;
-          if (++spot.h == H) { spot.h = 0; ++spot.p; }
-          if (spot.p * QP >= e.n) {
-            spot.p = 0;
-            do ++spot.e; while (spot.e < a.g.B * L && tokens_of(a.tok_off, spot.e / L, a.n_tokens).n == 0);
-          }
-        }
-      } else {
-        // every other round backwards: the CTA that had the longest item of one gets the shortest of the next
-        const long long k = (long long)round * gridDim.x +
-                            (round & 1 ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x);
-        if (k < plan.items) {
-          const TaPlace w = ta_place_by_level(A, k, plan.items);
-          if (w.ok) it = ta_item(A, w.b, w.l, w.p, w.h, 0, INT_MAX, -1);
+      if (spot.at < end.at || (spot.at == end.at && spot.off < end.off)) {
+        const TaEntry e = ta_plan_entry(a, spot.e);
+        const int n = ta_subs(ta_end(a, e, (spot.p + 1) * QP));
+        const int to = spot.at == end.at ? end.off : n;
+        // a piece that does not begin its item goes to this CTA's first slot, one that does to its second
+        const int slot = spot.off > 0 ? 2 * (int)blockIdx.x : to < n ? 2 * (int)blockIdx.x + 1 : -1;
+        it = ta_item(A, spot.e / L, spot.e % L, spot.p, spot.h, spot.off, to, slot);
+        spot.at += one_each ? 1 : n + kTaItemCost;
+        spot.off = 0;
+        if (++spot.h == a.g.H) { spot.h = 0; ++spot.p; }
+        if (spot.p * QP >= e.n) {
+          spot.p = 0;
+          do ++spot.e; while (spot.e < a.g.B * L && tokens_of(a.tok_off, spot.e / L, a.n_tokens).n == 0);
         }
       }
       if (n_pub >= 2) ok = wait(item_free(n_pub), (n_pub / 2 - 1) & 1u);
@@ -773,32 +738,56 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
         f0 = fast_exp2(st0.x - low);
         f1 = it.n > 1 ? fast_exp2(st1.x - low) : 0.f;
         total = st0.y * f0 + st1.y * f1;
-        c_lo = chain * (D / 2);
-        c_hi = c_lo + D / 2;
+        c_lo = chain * 64;                               // (64-wide heads: chain 0 has them all)
+        c_hi = min(c_lo + 64, D);
       }
       const bool any = it.pair ? mine > 0 : it.n > 0;
       const float inv = total == 0.f ? 0.f : 1.f / total;
       f0 *= inv;
       f1 *= inv;
       if (warp_valid) {
-        for (int c = c_lo; c < c_hi; c += 32) {
+        const TaRows rows(it.slot >= 0 ? static_cast<void*>(part) : static_cast<void*>(out));
+        // columns [c, c + 32) of the result
+        auto columns = [&](int c, float (&v)[32]) {
+          if (!any) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+            return;
+          }
+          uint32_t x[32];
+          tmem_ld32((it.pair ? t_o : t_o0) + c, x);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(x[i]) * f0;
+          if (!it.pair && it.n > 1) {
+            tmem_ld32(t_o1 + c, x);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __fmaf_rn(__uint_as_float(x[i]), f1, v[i]);
+          }
+        };
+        for (int c = c_lo; c < c_hi; c += 64) {
+          uint4 pieces[8];
           float v[32];
-          if (any) {
-            uint32_t x[32];
-            tmem_ld32((it.pair ? t_o : t_o0) + c, x);
+          if (it.slot >= 0) {
+#pragma unroll 1
+            for (int d = c; d < min(c + 64, c_hi); d += 32) {
+              columns(d, v);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(x[i]) * f0;
-            if (!it.pair && it.n > 1) {
-              tmem_ld32(t_o1 + c, x);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = __fmaf_rn(__uint_as_float(x[i]), f1, v[i]);
+              for (int i = 0; i < 8; ++i)
+                pieces[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+                                       __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+              rows.store(pieces, d * 4, stage);
             }
           } else {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+            for (int d = 0; d < 2; ++d) {
+              columns(c + 32 * d, v);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                pieces[4 * d + i] = make_uint4(pack_bf16(v[8 * i], v[8 * i + 1]), pack_bf16(v[8 * i + 2], v[8 * i + 3]),
+                                               pack_bf16(v[8 * i + 4], v[8 * i + 5]), pack_bf16(v[8 * i + 6], v[8 * i + 7]));
+            }
+            rows.store(pieces, c * 2, stage);
           }
-          if (it.slot >= 0) ta_store_f32(v, part ? part + c : nullptr, stage);
-          else ta_store_bf16(v, out ? out + c : nullptr, stage);
         }
         if (valid && (it.pair || chain == 0)) {
           const float lse2 = total == 0.f ? -INFINITY : m + log2f(total);
@@ -830,6 +819,7 @@ __global__ void __launch_bounds__(32 * kTaJoinWarps)
 token_attention_join_kernel(const __grid_constant__ TaArgs A) {
   constexpr int V = D / 32;
   const TokenAttention& a = A.a;
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // everything of the kernel before is complete and visible
   if (a.status && a.status[2] != 0) return;              // a wait gave up: no output
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = (int)blockIdx.x + 1;
   const TaSpot s = A.plan[c0];
@@ -924,8 +914,17 @@ static int launch_ta(const TaArgs& A, const void* K, const void* V, long long it
   kern<<<grid, kTaThreads, kTaSmem<D>, s>>>(A, map_q, map_k, map_v);
   if (cudaGetLastError() != cudaSuccess) return L2KV_ERR_CUDA;
   if (A.plan) {
-    token_attention_join_kernel<D><<<dim3(kTaGrid - 1, (unsigned)(A.slot_rows / 32)), 32 * kTaJoinWarps, 0, s>>>(A);
-    if (cudaGetLastError() != cudaSuccess) return L2KV_ERR_CUDA;
+    // (set up while the kernel before it runs: a small call would wait for this launch otherwise)
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(kTaGrid - 1, (unsigned)(A.slot_rows / 32));
+    cfg.blockDim = dim3(32 * kTaJoinWarps);
+    cfg.stream = s;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, token_attention_join_kernel<D>, A) != cudaSuccess) return L2KV_ERR_CUDA;
   }
   return L2KV_OK;
 }
@@ -934,6 +933,7 @@ int launch_token_attention(const TokenAttention& a, const void* K, const void* V
                            size_t scratch_bytes, cudaStream_t s) {
   if (dtype != L2KV_BF16) return launch_token_attention_simple(a, K, V, dtype, s);
   const TaRoom room = ta_room(a.g, a.n_tokens, a.max_len);
+  if (room.items > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
   TaArgs A{};
   A.a = a;
   A.G = a.g.Hq / a.g.H;
