@@ -1,5 +1,4 @@
 """ctypes binding of libl2kv.so: argument marshalling only."""
-import contextlib
 import ctypes
 import os
 
@@ -31,11 +30,6 @@ class _CLayout(ctypes.Structure):
                 ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64),
                 ("row_off_dev", ctypes.c_void_p), ("row_cap_dev", ctypes.c_void_p),
                 ("total_rows", ctypes.c_int64)]
-
-
-class _CTokens(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("stride_l", ctypes.c_int64), ("stride_t", ctypes.c_int64),
-                ("stride_h", ctypes.c_int64)]
 
 
 def library_path():
@@ -80,20 +74,10 @@ def lib():
         L.l2kv_decode_attention_static_status.argtypes = [vp, ctypes.POINTER(i32), i32]
         L.l2kv_prefix_attention_flags.argtypes = [vp, vp, vp, lay, vp, i32, i32, ctypes.c_float,
                                                   ctypes.c_uint32, vp, vp, vp, sz, vp]
-        tok, f64, u32 = ctypes.POINTER(_CTokens), ctypes.c_double, ctypes.c_uint32
+        f64 = ctypes.c_double
         L.l2kv_rotary_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, ctypes.POINTER(f64),
                                               ctypes.POINTER(f64)]
-        L.l2kv_rotary_write.argtypes = [tok, tok, tok, vp, i32, vp, vp, i32, f64, tok, vp, vp, vp, vp, lay,
-                                        vp, vp, u32, vp, sz, vp]
-        L.l2kv_tree_commit.argtypes = [vp, vp, vp, vp, lay, vp, vp, vp, i32, vp, vp, u32, vp, sz, vp]
-        L.l2kv_prompt_attention_workspace_bytes.argtypes = [lay, i32, i32, ctypes.POINTER(sz)]
-        L.l2kv_prompt_attention.argtypes = [tok, vp, i32, vp, vp, lay, vp, i32, ctypes.c_float, u32, tok, vp,
-                                            vp, sz, vp]
-        L.l2kv_tree_attention.argtypes = [tok, vp, i32, vp, i32, vp, vp, lay, vp, i32, ctypes.c_float, u32,
-                                          tok, vp, vp, sz, vp]
-        for name in ("l2kv_rotary_frequencies", "l2kv_rotary_write", "l2kv_tree_commit",
-                     "l2kv_prompt_attention_workspace_bytes", "l2kv_prompt_attention", "l2kv_tree_attention",
-                     "l2kv_prefix_attention", "l2kv_attention_loss_workspace_bytes", "l2kv_attention_loss",
+        for name in ("l2kv_rotary_frequencies", "l2kv_prefix_attention", "l2kv_attention_loss_workspace_bytes", "l2kv_attention_loss",
                      "l2kv_keep_count", "l2kv_workspace_bytes", "l2kv_read_device_status",
                      "l2kv_key_norms", "l2kv_select_compact", "l2kv_decode_attention",
                      "l2kv_append_evict", "l2kv_select_compact_per_head",
@@ -165,7 +149,6 @@ def _ptr(t):
     return ctypes.c_void_p(0 if t is None else t.data_ptr())
 
 
-_NO_CONTEXT = contextlib.nullcontext()
 _RAW_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -404,47 +387,41 @@ def prefix_attention_per_head(q, K_c, V_c, cur_len_unit_dev, max_len, out, lse_o
 
 
 ROTARY_NONE, ROTARY_LINEAR, ROTARY_NTK, ROTARY_LLAMA3, ROTARY_YARN = range(5)
-_LEN_PER_HEAD, _INTERLEAVED = 1, 2
+_NATIVE = None
 
 
-def _tokens(t, layout, n_tokens=None, heads=None):
-    """Description of rows of new tokens: [L, N, heads, D], or [N, heads, D] where L is 1."""
-    if t is None:
-        return None
-    if t.dim() == 3:
-        t = t.unsqueeze(0)
-    c = layout.c
-    if t.dim() != 4 or t.stride(3) != 1 or t.shape[0] != c.layers or t.shape[3] != c.head_dim:
-        raise ValueError("tokens must be [L, N, heads, D] (or [N, heads, D] for one layer) with D contiguous")
-    if _DTYPE.get(t.dtype) != c.dtype:
-        raise ValueError(f"tokens of {t.dtype} do not fit the cache's dtype")
-    if (n_tokens is not None and t.shape[1] != n_tokens) or (heads is not None and t.shape[2] != heads):
-        raise ValueError("tokens differ in number or heads")
-    return _CTokens(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+def _token_calls():
+    """The compiled marshalling module of the calls below, bound to the loaded library."""
+    global _NATIVE
+    if _NATIVE is None:
+        try:
+            from . import _token_calls as native
+        except ImportError as e:
+            raise ImportError("_token_calls is missing: run `python -m paper_2406_11430_b200.build`; there is no "
+                              f"fallback path ({e})") from e
+        L = lib()
+        native.bind(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
+            "l2kv_rotary_write", "l2kv_tree_commit", "l2kv_prompt_attention", "l2kv_tree_attention",
+            "l2kv_prompt_attention_workspace_bytes")))
+        _NATIVE = native
+    return _NATIVE
 
 
-def _entries(t, count, what, dtype=torch.int32):
-    if t is not None and (t.dtype != dtype or not t.is_contiguous() or (count is not None and t.numel() != count)):
-        raise ValueError(f"{what} must be contiguous {dtype} with {count} entries")
-
-
-def _one_device(ref, *tensors):
-    """Every tensor of a call lies where `ref` lies: kernels run on one device."""
-    for t in tensors:
-        if t is not None and t.device != ref.device:
-            raise ValueError(f"a tensor on {t.device} in a call on {ref.device}")
-
-
-def _on_device(ref):
-    """The context a call runs in: the device that holds `ref` is the current one."""
-    if ref.is_cuda and ref.device.index != torch.cuda.current_device():
-        return torch.cuda.device(ref.device)
-    return _NO_CONTEXT
-
-
-def _lengths(layout, per_head):
-    c = layout.c
-    return c.batch * c.layers * (c.kv_heads if per_head else 1)
+def _call(fn, name, ref, stream, *args):
+    """One call on the stream given, or on the current one of the device that holds `ref`, which is made the
+    current device for the call (a stream of one device takes no kernel of another)."""
+    device = ref.device
+    if device.type != "cuda":
+        rc = fn(*args, 0)                        # host tensors: checks only
+    else:
+        handle = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+        if torch._C._cuda_getDevice() == device.index:
+            rc = fn(*args, handle)
+        else:
+            with torch.cuda.device(device):
+                rc = fn(*args, handle)
+    if rc != 0:
+        raise L2KVError(rc, name)
 
 
 def rotary_frequencies(rot_dim, base=10000.0, scaling=ROTARY_NONE, factor=1.0, low=1.0, high=4.0,
@@ -463,82 +440,40 @@ def rotary_write(q, k, v, tok_off, pos, freq, q_out, K_c, V_c, idx, sumsq_c, sta
                  interleaved=False, attn_scale=1.0, stream=None, rows=None, per_head=False):
     """Rotates the queries and keys of new tokens (q, k, v: [L, N, heads, D], packed by tok_off) and writes
     keys and values to cache rows start_dev + s, with idx and sumsq_c; see l2kv_rotary_write.  freq: fp64
-    [rot_dim / 2] on the device, or None for no rotation.  q and q_out may be None."""
-    lay = Layout(K_c, q_heads=0 if q is None else q.shape[-2], rows=rows)
-    n = k.shape[-3]
-    _one_device(K_c, q, k, v, tok_off, pos, freq, q_out, V_c, idx, sumsq_c, start_dev, cur_len_dev, workspace)
-    _entries(tok_off, lay.c.batch + 1, "tok_off")
-    _entries(pos, n, "pos")
-    _entries(freq, None, "freq", torch.float64)
-    _entries(start_dev, _lengths(lay, per_head), "start_dev")
-    _entries(cur_len_dev, _lengths(lay, per_head), "cur_len_dev")
-    with _on_device(K_c):
-        _check(lib().l2kv_rotary_write(
-            _tokens(q, lay, n), _tokens(k, lay, n, lay.c.kv_heads), _tokens(v, lay, n, lay.c.kv_heads), _ptr(tok_off),
-            n, _ptr(pos), _ptr(freq), 0 if freq is None else 2 * freq.numel(), float(attn_scale),
-            _tokens(q_out, lay, n, lay.c.q_heads), _ptr(K_c), _ptr(V_c), _ptr(idx), _ptr(sumsq_c), lay.ref(),
-            _ptr(start_dev), _ptr(cur_len_dev), (_LEN_PER_HEAD if per_head else 0) | (_INTERLEAVED if interleaved else 0),
-            _ptr(workspace), workspace.numel(), _stream(stream, K_c)), "l2kv_rotary_write")
+    [rot_dim / 2] on the device, or None for no rotation.  q and q_out may be None, and so may idx and sumsq_c."""
+    _call((_NATIVE or _token_calls()).rotary_write, "l2kv_rotary_write", K_c, stream, q, k, v, tok_off, pos, freq, q_out,
+          K_c, V_c, idx, sumsq_c, start_dev, cur_len_dev, workspace, interleaved, attn_scale, rows, per_head)
 
 
 def tree_commit(K_c, V_c, idx, sumsq_c, start_dev, cur_len_dev, path, n_path, len_out_dev, workspace, stream=None,
                 rows=None, per_head=False):
     """Moves the rows of the accepted path (path: int32 [B, path_cap], n_path: int32 [B]) of a drafted tree down to
     rows start_dev + j; see l2kv_tree_commit.  len_out_dev may be start_dev or cur_len_dev."""
-    lay = Layout(K_c, rows=rows)
-    if path.dim() != 2 or path.shape[0] != lay.c.batch:
-        raise ValueError("path must be [B, path_cap]")
-    _one_device(K_c, V_c, idx, sumsq_c, start_dev, cur_len_dev, path, n_path, len_out_dev, workspace)
-    _entries(path, None, "path")
-    _entries(n_path, lay.c.batch, "n_path")
-    for t, what in ((start_dev, "start_dev"), (cur_len_dev, "cur_len_dev"), (len_out_dev, "len_out_dev")):
-        _entries(t, _lengths(lay, per_head), what)
-    with _on_device(K_c):
-        _check(lib().l2kv_tree_commit(
-            _ptr(K_c), _ptr(V_c), _ptr(idx), _ptr(sumsq_c), lay.ref(), _ptr(start_dev), _ptr(cur_len_dev), _ptr(path),
-            path.shape[1], _ptr(n_path), _ptr(len_out_dev), _LEN_PER_HEAD if per_head else 0, _ptr(workspace),
-            workspace.numel(), _stream(stream, K_c)), "l2kv_tree_commit")
+    _call((_NATIVE or _token_calls()).tree_commit, "l2kv_tree_commit", K_c, stream, K_c, V_c, idx, sumsq_c, start_dev,
+          cur_len_dev, path, n_path, len_out_dev, workspace, rows, per_head)
 
 
 def prompt_attention_workspace_bytes(K_c, q, max_len, rows=None):
     """Bytes with which prompt_attention and tree_attention may split caches over the SMs."""
-    lay = Layout(K_c, q_heads=q.shape[-2], rows=rows)
-    out = ctypes.c_size_t(0)
-    _check(lib().l2kv_prompt_attention_workspace_bytes(lay.ref(), q.shape[-3], int(max_len), ctypes.byref(out)),
-           "l2kv_prompt_attention_workspace_bytes")
-    return out.value
-
-
-def _token_attention(name, q, tok_off, mask, K_c, V_c, cur_len_dev, max_len, out, lse_out, scale, workspace, stream,
-                     rows, per_head):
-    lay = Layout(K_c, q_heads=q.shape[-2], rows=rows)
-    n = q.shape[-3]
-    _entries(tok_off, lay.c.batch + 1, "tok_off")
-    _entries(cur_len_dev, _lengths(lay, per_head), "cur_len_dev")
-    _entries(lse_out, lay.c.layers * n * lay.c.q_heads, "lse_out", torch.float32)
-    _one_device(K_c, q, tok_off, mask, V_c, cur_len_dev, out, lse_out, workspace)
-    masked = () if mask is None else (_ptr(mask), mask.shape[-1])
-    with _on_device(K_c):
-        _check(getattr(lib(), name)(
-            _tokens(q, lay), _ptr(tok_off), n, *masked, _ptr(K_c), _ptr(V_c), lay.ref(), _ptr(cur_len_dev), int(max_len),
-            float(scale), _LEN_PER_HEAD if per_head else 0, _tokens(out, lay, n, lay.c.q_heads), _ptr(lse_out),
-            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream, q)), name)
+    n = (_NATIVE or _token_calls()).workspace_bytes(K_c, q, max_len, rows)
+    if n < 0:
+        raise L2KVError(n, "l2kv_prompt_attention_workspace_bytes")
+    return n
 
 
 def prompt_attention(q, tok_off, K_c, V_c, cur_len_dev, max_len, out, lse_out=None, scale=0.0, workspace=None,
                      stream=None, rows=None, per_head=False):
     """Causal attention of packed prompts (q, out: [L, N, Hq, D]) over caches whose last rows are the prompts'
     own; see l2kv_prompt_attention."""
-    _token_attention("l2kv_prompt_attention", q, tok_off, None, K_c, V_c, cur_len_dev, max_len, out, lse_out, scale,
-                     workspace, stream, rows, per_head)
+    _call((_NATIVE or _token_calls()).attention, "l2kv_prompt_attention", K_c, stream, q, tok_off, None, K_c, V_c,
+          cur_len_dev, max_len, out, lse_out, scale, workspace, rows, per_head)
 
 
 def tree_attention(q, tok_off, tree_mask, K_c, V_c, cur_len_dev, max_len, out, lse_out=None, scale=0.0, workspace=None,
                    stream=None, rows=None, per_head=False):
     """Attention of drafted trees: token i sees everything before the tree, and the tree's row c where bit c of
     tree_mask[i] (int64 or uint64 [N, words]) is set; see l2kv_tree_attention."""
-    if tree_mask.dim() != 2 or tree_mask.shape[0] != q.shape[-3] or tree_mask.dtype not in (torch.int64, torch.uint64) \
-            or not tree_mask.is_contiguous():
-        raise ValueError("tree_mask must be contiguous int64 or uint64 [N, words]")
-    _token_attention("l2kv_tree_attention", q, tok_off, tree_mask, K_c, V_c, cur_len_dev, max_len, out, lse_out, scale,
-                     workspace, stream, rows, per_head)
+    if tree_mask is None:
+        raise ValueError("tree_mask is missing")
+    _call((_NATIVE or _token_calls()).attention, "l2kv_tree_attention", K_c, stream, q, tok_off, tree_mask, K_c, V_c,
+          cur_len_dev, max_len, out, lse_out, scale, workspace, rows, per_head)

@@ -3,6 +3,8 @@
 nvcc cross-compiles without a GPU; the CUDA runtime is linked statically so the
 library has no dependency beyond the driver.  Every source file is compiled to an
 object of its own (in parallel, and only when it or a header changed), then linked.
+The Python binding's marshalling module (csrc/token_calls.cpp) is compiled with the host
+compiler against the installed torch's headers.
 """
 import glob
 import hashlib
@@ -16,6 +18,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libl2kv.so")
 DEBUG_LIB = os.path.join(HERE, "libl2kv_debug.so")      # the same library with index checks
+BINDING = os.path.join(HERE, "_token_calls.so")         # marshalling of the calls on new tokens
 OBJ_DIR = os.path.join(HERE, "_build")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -41,6 +44,8 @@ def _stale(target, deps):
 
 def build(force=False, verbose=False, out=None, defines=()):
     """out / defines: build a variant (e.g. defines=["L2KV_DEBUG"]) into another file."""
+    if out is None:
+        build_binding(force)
     out = out or LIB
     if not force and not _stale(out, sources() + _headers()):
         return out
@@ -59,6 +64,23 @@ def build(force=False, verbose=False, out=None, defines=()):
         objs = list(pool.map(compile_one, sources()))
     subprocess.run([nvcc] + NVCC_FLAGS + ["-shared", "-o", out] + objs, check=True)
     return out
+
+
+def build_binding(force=False):
+    src = os.path.join(CSRC, "token_calls.cpp")
+    if not force and not _stale(BINDING, [src, os.path.join(ROOT, "include", "l2kv.h"), os.path.abspath(__file__)]):
+        return BINDING
+    import sysconfig
+    import torch
+    home = os.path.dirname(torch.__file__)
+    includes = [os.path.join(ROOT, "include"), os.path.join(home, "include"),
+                os.path.join(home, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"]]
+    lib = os.path.join(home, "lib")
+    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[f"-I{i}" for i in includes],
+                    "-o", BINDING, src, f"-L{lib}", f"-Wl,-rpath,{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10"],
+                   check=True)
+    return BINDING
 
 
 def build_debug(force=False):
