@@ -9,12 +9,14 @@
 namespace l2kv {
 
 // ---- rotary positions and cache write ------------------------------------------------------------
-// One block per (token, layer).  A row (one head of q, k or v) belongs to LPR adjacent lanes, a
-// 16-byte piece each, as everywhere in the library; a half-split pair's other element is in another
-// lane of the row, an interleaved pair's in the same piece.  A thread meets the same piece of
-// every row, so it keeps that piece's cosines and sines in registers.
+// A token's rows (the heads of q, k and v of one layer) are one warp's, or, for calls with few tokens, shared by
+// several warps.  A row belongs to LPR adjacent lanes, a 16-byte piece each, as everywhere in the
+// library; a half-split pair's other element is in another lane of the row, an interleaved pair's in the
+// same piece.  A lane meets the same piece of every row, so it keeps that piece's cosines and sines in
+// registers.  Rows are read kRotaryBatch pieces per lane at a time, the first batch before
+// anything is known of the token; angle, sequence and cache row are worked out under those loads.
 constexpr int kRotaryThreads = 256;
-
+constexpr int kRotaryWarps = kRotaryThreads / 32;
 struct RotaryArgs {
   TokView q, k, v, q_out;
   Geom g;
@@ -45,115 +47,181 @@ __device__ __forceinline__ uint4 pack_piece<__nv_bfloat16>(const float (&y)[8]) 
   return make_uint4(two(y[0], y[1]), two(y[2], y[3]), two(y[4], y[5]), two(y[6], y[7]));
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kRotaryThreads)
+// A 16-byte load that leaves no line in L1.  (Not through the read-only path: q_out may be q.)
+__device__ __forceinline__ uint4 ld_once(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+
+// Cosine and sine of the angle a, to about 1e-10, in fp64.  a / 2 pi is formed as a sum of two doubles and the nearest
+// quarter turn taken off it, which leaves the rest exact for any position; at most an eighth of a turn is
+// left, where the Taylor series are short (the terms left out: x^13 / 13! < 1e-11, x^12 / 12! < 2e-10).
+__device__ __forceinline__ void cos_sin(double a, double* c, double* s) {
+  constexpr double kHi = 0.15915494309189535, kLo = -9.839338337591243e-18;   // 1 / 2 pi
+  const double t = a * kHi;
+  const double rest = __fma_rn(a, kLo, __fma_rn(a, kHi, -t));
+  const double quarters = rint(4.0 * t);
+  const double x = (__fma_rn(-0.25, quarters, t) + rest) * 6.283185307179586, z = x * x;
+  double sx = __fma_rn(z, -1.0 / 39916800.0, 1.0 / 362880.0), cx = __fma_rn(z, -1.0 / 3628800.0, 1.0 / 40320.0);
+  sx = __fma_rn(z, sx, -1.0 / 5040.0);
+  cx = __fma_rn(z, cx, -1.0 / 720.0);
+  sx = __fma_rn(z, sx, 1.0 / 120.0);
+  cx = __fma_rn(z, cx, 1.0 / 24.0);
+  sx = __fma_rn(z, sx, -1.0 / 6.0);
+  cx = __fma_rn(z, cx, -0.5);
+  sx = __fma_rn(x * z, sx, x);
+  cx = __fma_rn(z, cx, 1.0);
+  const int q = (int)(long long)quarters;                // only its last two bits count
+  const double u = q & 1 ? sx : cx, v = q & 1 ? cx : sx;
+  *c = (q + 1) & 2 ? -u : u;
+  *s = q & 2 ? -v : v;
+}
+
+// WPT: warps that share a token.  PAIRS: interleaved pairs.
+template <typename T, int D, int WPT, bool PAIRS>
+__global__ void __launch_bounds__(kRotaryThreads, 3)
 rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* __restrict__ K, T* __restrict__ V) {
-  constexpr int EPV = Elem<T>::kPerVec, LPR = D / EPV, RPB = kRotaryThreads / LPR;
+  constexpr int EPV = Elem<T>::kPerVec, LPR = D / EPV, RPW = 32 / LPR;
+  constexpr int U = WPT == 1 ? 8 : 4;                    // pieces per lane in flight
+  constexpr int TPB = kRotaryWarps / WPT;                // tokens per block
+  constexpr int STEP = WPT * RPW;                        // rows that a token's warps take at once
+  __shared__ float2 s_turn[kRotaryWarps][D / 2];
   const Geom& g = a.g;
-  const int tid = threadIdx.x, lane = tid & 31, piece = tid % LPR;
-  const long long n_rows = (long long)a.n_tokens * g.L;
-  if (blockIdx.x >= n_rows) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane % LPR;
+  const unsigned n_rows = (unsigned)a.n_tokens * (unsigned)g.L, token_blocks = (n_rows + TPB - 1) / TPB;
+  if (blockIdx.x >= token_blocks) {
     // trailing blocks: the new lengths (sequences without new tokens have one too)
-    const long long u = (blockIdx.x - n_rows) * kRotaryThreads + tid;
+    const long long u = (long long)(blockIdx.x - token_blocks) * kRotaryThreads + threadIdx.x;
     const long long units = (long long)g.B * g.L * (a.per_head ? g.H : 1);
     if (u >= units) return;
     const long long bl = a.per_head ? u / g.H : u;
-    const int b = (int)(bl / g.L);
-    const int n = tokens_of(a.tok_off, b, a.n_tokens).n;
+    const int n = tokens_of(a.tok_off, (int)(bl / g.L), a.n_tokens).n;
     a.cur_len[u] = (int)min((long long)g.cap(bl), (long long)max(0, a.start[u]) + n);
     return;
   }
-  const int i = (int)(blockIdx.x / g.L), l = (int)(blockIdx.x % g.L);
-  __shared__ float s_cos[D / 2], s_sin[D / 2];
-  const int half = a.rot_dim / 2;
-  if (tid < half) {
-    double s, c;
-    sincos((double)a.pos[i] * a.freq[tid], &s, &c);
-    s_cos[tid] = (float)(c * a.scale);
-    s_sin[tid] = (float)(s * a.scale);
+  const unsigned il = blockIdx.x * TPB + warp / WPT;     // token * layers + layer
+  if (il >= n_rows) return;
+  const int i = (int)(il / (unsigned)g.L), l = (int)(il % (unsigned)g.L);
+  const int group = (warp % WPT) * RPW, row0 = group + lane / LPR;           // this lane's first row of each kind
+
+  // Rows of one kind, U at a time: `from` the lane's piece of row 0, rows `stride` bytes apart.
+  auto load = [&](uint4 (&x)[U], const char* from, long long stride, int r0, int n) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      x[u] = r0 + u * STEP < n ? ld_once(from + (r0 + u * STEP) * stride) : make_uint4(0, 0, 0, 0);
+  };
+  const char* const q_from = reinterpret_cast<const char*>(a.q.row<T>(l, i, 0)) + piece * 16;
+  const long long q_stride = a.q.sh * (long long)sizeof(T);
+  uint4 x[U];
+  load(x, q_from, q_stride, row0, g.Hq);
+
+  const int half = a.rot_dim / 2, pos = a.pos[i];
+  for (int p = lane; p < half; p += 32) {
+    double c, s;
+    cos_sin((double)pos * a.freq[p], &c, &s);
+    s_turn[warp][p] = make_float2((float)(c * a.scale), (float)(s * a.scale));
   }
   const int b = sequence_of(a.tok_off, g.B, a.n_tokens, i);
-  if (b < 0) return;                                    // a token of no sequence (whole block)
+  if (b < 0) return;                                     // a token of no sequence (the whole warp)
   const int at = i - tokens_of(a.tok_off, b, a.n_tokens).first;
-  __syncthreads();
+  __syncwarp();
 
-  const int rot_pieces = a.rot_dim / EPV;
-  float cs[EPV], sn[EPV];                                // y = x * cs + partner * sn
-  int from = lane;                                       // lane that holds the partner's piece
-  if (piece < rot_pieces) {
-    if (a.interleaved) {
+  const int rot_pieces = a.rot_dim / EPV, hp = rot_pieces / 2;
+  const bool turns = piece < rot_pieces, upper = piece >= hp;
+  const int partner = PAIRS || !turns ? lane : upper ? lane - hp : lane + hp;   // lane with the pairs' other elements
+  float cs[EPV], sn[EPV];                                // y = x * cs + other * sn
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) {
-        const int p = (piece * EPV + e) / 2;
-        cs[e] = s_cos[p];
-        sn[e] = e & 1 ? s_sin[p] : -s_sin[p];
-      }
+  for (int e = 0; e < EPV; ++e) {
+    const int p = PAIRS ? (piece * EPV + e) / 2 : (upper ? piece - hp : piece) * EPV + e;
+    const float2 t = s_turn[warp][turns ? p : 0];
+    cs[e] = t.x;
+    sn[e] = (PAIRS ? (e & 1) != 0 : upper) ? t.y : -t.y;
+  }
+  auto rotated = [&](const uint4& v) {                   // whole warps
+    float f[EPV], o[EPV], y[EPV];
+    Elem<T>::unpack(v, f);
+    if constexpr (PAIRS) {
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) o[e] = f[e ^ 1];
     } else {
-      const int hp = rot_pieces / 2;
-      const bool upper = piece >= hp;
-      from = upper ? lane - hp : lane + hp;
+      uint4 w;
+      w.x = __shfl_sync(0xffffffffu, v.x, partner); w.y = __shfl_sync(0xffffffffu, v.y, partner);
+      w.z = __shfl_sync(0xffffffffu, v.z, partner); w.w = __shfl_sync(0xffffffffu, v.w, partner);
+      Elem<T>::unpack(w, o);
+    }
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) {
-        const int p = (upper ? piece - hp : piece) * EPV + e;
-        cs[e] = s_cos[p];
-        sn[e] = upper ? s_sin[p] : -s_sin[p];
-      }
+    for (int e = 0; e < EPV; ++e) y[e] = __fmaf_rn(f[e], cs[e], o[e] * sn[e]);
+    const uint4 r = pack_piece<T>(y);
+    return turns ? r : v;                                // (dimensions from rot_dim on are copied)
+  };
+
+  char* const q_to = reinterpret_cast<char*>(a.q_out.row<T>(l, i, 0)) + piece * 16;
+  const long long q_to_stride = a.q_out.sh * (long long)sizeof(T);
+  for (int r0 = row0; r0 - row0 + group < g.Hq; r0 += U * STEP) {
+    if (r0 != row0) load(x, q_from, q_stride, r0, g.Hq);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint4 y = rotated(x[u]);
+      if (r0 + u * STEP < g.Hq) st_stream(q_to + (r0 + u * STEP) * q_to_stride, y);
     }
   }
 
-  const int rows = g.Hq + 2 * g.H;
-  for (int r0 = 0; r0 < rows; r0 += RPB) {
-    const int r = r0 + tid / LPR;
-    const bool is_q = r < g.Hq, is_k = !is_q && r < g.Hq + g.H, any = r < rows;
-    const int h = is_q ? r : is_k ? r - g.Hq : r - g.Hq - g.H;
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (any) {
-      const TokView& from_t = is_q ? a.q : is_k ? a.k : a.v;
-      x = *reinterpret_cast<const uint4*>(from_t.row<T>(l, i, h) + piece * EPV);
-    }
-    uint4 other;
-    other.x = __shfl_sync(0xffffffffu, x.x, from); other.y = __shfl_sync(0xffffffffu, x.y, from);
-    other.z = __shfl_sync(0xffffffffu, x.z, from); other.w = __shfl_sync(0xffffffffu, x.w, from);
-    if ((is_q || is_k) && piece < rot_pieces) {
-      float f[EPV], o[EPV], y[EPV];
-      Elem<T>::unpack(x, f);
-      Elem<T>::unpack(other, o);
+  // keys and values side by side, half a batch of each
+  const long long bl = (long long)b * g.L + l;
+  const int cap = g.cap(bl);
+  const long long slot_all = a.per_head ? 0 : (long long)max(0, a.start[bl]) + at;
+  const char* const k_from = reinterpret_cast<const char*>(a.k.row<T>(l, i, 0)) + piece * 16;
+  const char* const v_from = reinterpret_cast<const char*>(a.v.row<T>(l, i, 0)) + piece * 16;
+  const long long k_stride = a.k.sh * (long long)sizeof(T), v_stride = a.v.sh * (long long)sizeof(T);
+  const long long cache0 = g.base(b, l, 0) + piece * EPV, meta0 = g.meta(bl * g.H);
+  const long long meta_h = g.row_off ? g.total_rows : (long long)g.t_cap;
+  for (int r0 = row0; r0 - row0 + group < g.H; r0 += U / 2 * STEP) {
 #pragma unroll
-      for (int e = 0; e < EPV; ++e)
-        y[e] = __fmaf_rn(f[e], cs[e], (a.interleaved ? f[e ^ 1] : o[e]) * sn[e]);
-      x = pack_piece<T>(y);
+    for (int u = 0; u < U / 2; ++u) {
+      const int h = r0 + u * STEP;
+      x[2 * u] = h < g.H ? ld_once(k_from + h * k_stride) : make_uint4(0, 0, 0, 0);
+      x[2 * u + 1] = h < g.H ? ld_once(v_from + h * v_stride) : make_uint4(0, 0, 0, 0);
     }
-    // the key of the row as it is stored
-    float key = 0.f;
-    if (__any_sync(0xffffffffu, is_k)) key = piece_sumsq_reduce<T, LPR>(x);
-    if (!any) continue;
-    if (is_q) {
-      *reinterpret_cast<uint4*>(a.q_out.row<T>(l, i, h) + piece * EPV) = x;
-      continue;
-    }
-    const long long bl = (long long)b * g.L + l, unit = bl * g.H + h;
-    const long long slot = (long long)max(0, a.start[a.per_head ? unit : bl]) + at;
-    if (slot >= g.cap(bl)) {
-      if (piece == 0) atomicExch(a.status, (int)L2KV_ERR_DEVICE_OVERFLOW);
-      continue;
-    }
-    const long long to = g.base(b, l, h) + slot * g.st + piece * EPV;
-    *reinterpret_cast<uint4*>((is_k ? K : V) + to) = x;
-    if (is_k && piece == 0) {
-      const long long m = g.meta(unit) + slot;
-      if (a.idx) a.idx[m] = a.pos[i];
-      if (a.sumsq) a.sumsq[m] = key;
+#pragma unroll
+    for (int u = 0; u < U / 2; ++u) {
+      const int h = r0 + u * STEP;
+      const uint4 y = rotated(x[2 * u]);
+      const float key = piece_sumsq_reduce<T, LPR>(y);   // of the row as it is stored
+      if (h >= g.H) continue;
+      const long long slot = a.per_head ? (long long)max(0, a.start[bl * g.H + h]) + at : slot_all;
+      if (slot >= cap) {
+        if (piece == 0) atomicExch(a.status, (int)L2KV_ERR_DEVICE_OVERFLOW);
+        continue;
+      }
+      const long long to = cache0 + h * g.sh + slot * g.st;
+      *reinterpret_cast<uint4*>(K + to) = y;
+      *reinterpret_cast<uint4*>(V + to) = x[2 * u + 1];
+      if (piece == 0) {
+        const long long m = meta0 + h * meta_h + slot;
+        if (a.idx) a.idx[m] = pos;
+        if (a.sumsq) a.sumsq[m] = key;
+      }
     }
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, int WPT, bool PAIRS>
 static int launch_rw(const RotaryArgs& a, void* K, void* V, cudaStream_t s) {
+  constexpr int TPB = kRotaryWarps / WPT;
   const long long units = (long long)a.g.B * a.g.L * (a.per_head ? a.g.H : 1);
-  const long long blocks = (long long)a.n_tokens * a.g.L + (units + kRotaryThreads - 1) / kRotaryThreads;
-  if (blocks > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
-  rotary_write_kernel<T, D><<<(unsigned)blocks, kRotaryThreads, 0, s>>>(a, static_cast<T*>(K), static_cast<T*>(V));
+  const long long blocks = ((long long)a.n_tokens * a.g.L + TPB - 1) / TPB + (units + kRotaryThreads - 1) / kRotaryThreads;
+  if (blocks * TPB > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
+  rotary_write_kernel<T, D, WPT, PAIRS><<<(unsigned)blocks, kRotaryThreads, 0, s>>>(a, static_cast<T*>(K), static_cast<T*>(V));
   return cudaGetLastError() == cudaSuccess ? L2KV_OK : L2KV_ERR_CUDA;
+}
+// One warp per token where that alone fills the GPU (148 SMs, 16 warps each), else a block per token.
+template <typename T, int D>
+static int launch_rw_t(const RotaryArgs& a, void* K, void* V, cudaStream_t s) {
+  const bool many = (long long)a.n_tokens * a.g.L >= 148 * 16;
+  if (a.interleaved) return many ? launch_rw<T, D, 1, true>(a, K, V, s) : launch_rw<T, D, kRotaryWarps, true>(a, K, V, s);
+  return many ? launch_rw<T, D, 1, false>(a, K, V, s) : launch_rw<T, D, kRotaryWarps, false>(a, K, V, s);
 }
 
 int launch_rotary_write(const TokView& q, const TokView& k, const TokView& v, const TokView& q_out,
@@ -163,97 +231,90 @@ int launch_rotary_write(const TokView& q, const TokView& k, const TokView& v, co
                         int per_head, int32_t* status, cudaStream_t s) {
   const RotaryArgs a{q, k, v, q_out, g, tok_off, pos, freq, start, cur_len, idx, sumsq, status,
                      n_tokens, rot_dim, interleaved, per_head, scale};
-  if (dtype == L2KV_BF16) return g.D == 128 ? launch_rw<__nv_bfloat16, 128>(a, K, V, s) : launch_rw<__nv_bfloat16, 64>(a, K, V, s);
-  return g.D == 128 ? launch_rw<float, 128>(a, K, V, s) : launch_rw<float, 64>(a, K, V, s);
+  if (dtype == L2KV_BF16) return g.D == 128 ? launch_rw_t<__nv_bfloat16, 128>(a, K, V, s) : launch_rw_t<__nv_bfloat16, 64>(a, K, V, s);
+  return g.D == 128 ? launch_rw_t<float, 128>(a, K, V, s) : launch_rw_t<float, 64>(a, K, V, s);
 }
 
 // ---- the accepted path of a tree -----------------------------------------------------------------
-// One block per (b, l), all heads: it has read every length before it writes one, so the lengths may
-// be updated in place.  A path is strictly increasing, so path[j] >= j: rows are taken in
-// passes of ascending j, everything a pass moves is loaded before anything is stored, and no store
-// can meet a row that a later pass still needs.  Two rows of K and of V in flight per thread.
-constexpr int kCommitThreads = 512;
-constexpr int kCommitRows = 2;
+// One block per (b, l), a warp per head: it has read every length before it writes one, so the lengths may be
+// updated in place, and no two warps touch the same rows.  A path is strictly increasing, so path[j] >= j:
+// entries are taken in passes of ascending j, everything a pass moves is loaded before anything is stored,
+// and no store can meet a row that a later pass still needs.  What a call takes is a chain of three round
+// trips to memory (path and lengths, rows, stores); kCommitRows rows of K and of V per lane are in flight.
+constexpr int kCommitWarps = 8;
+constexpr int kCommitRows = 4;
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kCommitThreads)
+__global__ void __launch_bounds__(32 * kCommitWarps)
 tree_commit_kernel(T* __restrict__ K, T* __restrict__ V, int32_t* __restrict__ idx,
                    float* __restrict__ sumsq, Geom g, const int32_t* start_dev, const int32_t* cur_dev,
                    const int32_t* __restrict__ path, int path_cap, const int32_t* __restrict__ n_path,
                    int32_t* len_out, int per_head, int32_t* __restrict__ status) {
-  constexpr int EPV = Elem<T>::kPerVec, LPR = D / EPV, RPB = kCommitThreads / LPR;
-  __shared__ int s_ok;                                   // entries before the first that does not increase
+  constexpr int EPV = Elem<T>::kPerVec, LPR = D / EPV, RPW = 32 / LPR;
   const long long bl = blockIdx.x;
   const int b = (int)(bl / g.L), l = (int)(bl % g.L);
-  const int tid = threadIdx.x, piece = tid % LPR;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane % LPR;
   const int32_t* p = path + (long long)b * path_cap;
-  const int want = max(0, min(n_path[b], path_cap));
-  const int cap = g.cap(bl);
-  auto start_of = [&](int h) { return max(0, min(start_dev[per_head ? bl * g.H + h : bl], cap)); };
-  auto tail_of = [&](int h) { return max(0, min(cur_dev[per_head ? bl * g.H + h : bl], cap) - start_of(h)); };
-  if (tid == 0) s_ok = want;
-  __syncthreads();
-  for (int j = tid; j < want; j += kCommitThreads)
-    if (p[j] <= (j ? p[j - 1] : -1)) atomicMin(&s_ok, j);
-  __syncthreads();
-  const int ok = s_ok;
-
-  const long long moves = (long long)ok * g.H;           // move f: entry f / H, head f % H
-  for (long long f0 = 0; f0 < moves; f0 += RPB * kCommitRows) {
-    uint4 vk[kCommitRows], vv[kCommitRows];
-    int32_t vi[kCommitRows];
-    float vs[kCommitRows];
-    bool go[kCommitRows];
+  const int first = lane < path_cap ? p[lane] : 0;       // (asked for before n_path is known)
+  const int want = max(0, min(n_path[b], path_cap)), cap = g.cap(bl);
+  int len = 0;                                           // of the last head this warp took
+  bool bad = false;
+  for (int h = warp; h < g.H; h += kCommitWarps) {
+    const long long u = per_head ? bl * g.H + h : bl;
+    const int start = max(0, min(start_dev[u], cap)), tail = max(0, min(cur_dev[u], cap) - start);
+    const long long base = g.base(b, l, h) + (long long)start * g.st + piece * EPV, meta = g.meta(bl * g.H + h) + start;
+    int kept = 0, last = -1;                             // last: the entry before this group of 32
+    while (kept < want) {
+      const int j0 = kept, mine = j0 == 0 ? first : j0 + lane < want ? p[j0 + lane] : 0;
+      int before = __shfl_up_sync(0xffffffffu, mine, 1);
+      if (lane == 0) before = last;
+      // entries of this group before the first that does not increase or leaves the tree
+      const unsigned wrong = __ballot_sync(0xffffffffu, j0 + lane < want && (mine <= before || mine >= tail));
+      const int n = min(min(32, want - j0), wrong ? __ffs(wrong) - 1 : 32);
+      for (int e0 = 0; e0 < n; e0 += RPW * kCommitRows) {
+        uint4 vk[kCommitRows], vv[kCommitRows];
+        int32_t vi[kCommitRows];
+        float vs[kCommitRows];
+        bool go[kCommitRows];
 #pragma unroll
-    for (int u = 0; u < kCommitRows; ++u) {
-      const long long f = f0 + u * RPB + tid / LPR;
-      const int j = (int)(f / g.H), h = (int)(f % g.H);
-      go[u] = false;
-      if (f >= moves) continue;
-      const int from = p[j];
-      go[u] = from != j && from < tail_of(h);
-      if (!go[u]) continue;
-      const int row0 = start_of(h);
-      const long long at = g.base(b, l, h) + (long long)(row0 + from) * g.st + piece * EPV;
-      vk[u] = *reinterpret_cast<const uint4*>(K + at);
-      vv[u] = *reinterpret_cast<const uint4*>(V + at);
-      if (piece == 0) {
-        const long long m = g.meta(bl * g.H + h) + row0 + from;
-        if (idx) vi[u] = idx[m];
-        if (sumsq) vs[u] = sumsq[m];
-      }
-    }
-    __syncthreads();
+        for (int r = 0; r < kCommitRows; ++r) {
+          const int e = e0 + r * RPW + lane / LPR;
+          const int from = __shfl_sync(0xffffffffu, mine, e & 31);
+          go[r] = e < n && from != j0 + e;
+          if (!go[r]) continue;
+          vk[r] = *reinterpret_cast<const uint4*>(K + base + from * g.st);
+          vv[r] = *reinterpret_cast<const uint4*>(V + base + from * g.st);
+          if (piece == 0) {
+            if (idx) vi[r] = idx[meta + from];
+            if (sumsq) vs[r] = sumsq[meta + from];
+          }
+        }
+        __syncwarp();
 #pragma unroll
-    for (int u = 0; u < kCommitRows; ++u) {
-      if (!go[u]) continue;
-      const long long f = f0 + u * RPB + tid / LPR;
-      const int j = (int)(f / g.H), h = (int)(f % g.H);
-      const int row0 = start_of(h);
-      const long long at = g.base(b, l, h) + (long long)(row0 + j) * g.st + piece * EPV;
-      *reinterpret_cast<uint4*>(K + at) = vk[u];
-      *reinterpret_cast<uint4*>(V + at) = vv[u];
-      if (piece == 0) {
-        const long long m = g.meta(bl * g.H + h) + row0 + j;
-        if (idx) idx[m] = vi[u];
-        if (sumsq) sumsq[m] = vs[u];
+        for (int r = 0; r < kCommitRows; ++r) {
+          if (!go[r]) continue;
+          const int to = j0 + e0 + r * RPW + lane / LPR;
+          *reinterpret_cast<uint4*>(K + base + to * g.st) = vk[r];
+          *reinterpret_cast<uint4*>(V + base + to * g.st) = vv[r];
+          if (piece == 0) {
+            if (idx) idx[meta + to] = vi[r];
+            if (sumsq) sumsq[meta + to] = vs[r];
+          }
+        }
+        __syncwarp();
       }
+      kept += n;
+      last = __shfl_sync(0xffffffffu, mine, 31);
+      if (n < 32) break;
     }
+    bad |= kept < want;
+    len = start + kept;
+    if (per_head && lane == 0) len_out[u] = len;         // (nobody else reads this head's lengths)
   }
-
-  // The new lengths.  Every read of the old ones by another thread lies before this barrier.  Entries
-  // are increasing, so those inside the tail are the first ones.
-  __syncthreads();
-  for (int h = tid; h < (per_head ? g.H : 1); h += kCommitThreads) {
-    const int tail = tail_of(h);
-    int lo = 0, hi = ok;
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (p[mid] < tail) lo = mid + 1; else hi = mid;
-    }
-    if (lo < want) atomicExch(status, (int)L2KV_ERR_OUT_OF_RANGE);
-    len_out[per_head ? bl * g.H + h : bl] = start_of(h) + lo;
-  }
+  if (bad && lane == 0) atomicExch(status, (int)L2KV_ERR_OUT_OF_RANGE);
+  if (per_head) return;
+  __syncthreads();                                       // every warp has read the lengths
+  if (threadIdx.x == 0) len_out[bl] = len;
 }
 
 template <typename T, int D>
@@ -262,7 +323,7 @@ static int launch_tc(void* K, void* V, int32_t* idx, float* sumsq, const Geom& g
                      int32_t* len_out, int per_head, int32_t* status, cudaStream_t s) {
   const long long blocks = (long long)g.B * g.L;
   if (blocks > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
-  tree_commit_kernel<T, D><<<(unsigned)blocks, kCommitThreads, 0, s>>>(
+  tree_commit_kernel<T, D><<<(unsigned)blocks, 32 * kCommitWarps, 0, s>>>(
       static_cast<T*>(K), static_cast<T*>(V), idx, sumsq, g, start, cur, path, path_cap, n_path, len_out,
       per_head, status);
   return cudaGetLastError() == cudaSuccess ? L2KV_OK : L2KV_ERR_CUDA;
