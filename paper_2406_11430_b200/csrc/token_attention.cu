@@ -53,8 +53,8 @@ constexpr float kTaRescaleGap = 8.f;            // log2 units a maximum may drif
 
 template <int D> constexpr int kTaQTile = D / 64 * kTaHalf;
 template <int D> constexpr int kTaTile = D / 64 * kTaSubHalf;
-template <int D> constexpr int kTaSlots = 1024 / D;   // K and V tiles in flight: 128 KB
-template <int D> constexpr int kTaSmem = 2 * kTaQTile<D> + kTaSlots<D> * kTaTile<D> + 8 * kTaStage + kTaCtrl;
+template <int D> constexpr int kTaSlots = 512 / D;    // K tiles, and V tiles, in flight: 64 KB each
+template <int D> constexpr int kTaSmem = 2 * kTaQTile<D> + 2 * kTaSlots<D> * kTaTile<D> + 8 * kTaStage + kTaCtrl;
 // as in the other kernels: fp32 accumulators, bf16 operands, N / 8 from bit 17, M / 16 from bit 24; V is
 // N-major
 constexpr uint32_t kTaIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((64u >> 3) << 17) | ((128u >> 4) << 24);
@@ -270,14 +270,14 @@ __device__ __forceinline__ TaItem ta_item(const TaArgs& A, int b, int l, int p, 
   return it;
 }
 
-// Where the ring holds the tiles of an item's sub-block g: K tiles run `ahead` of V tiles, the order of use
-// being K(0) .. K(ahead - 1), V(0), K(ahead), V(1), K(ahead + 1), ...
-struct TaRing {
-  uint32_t pos;
-  int n, ahead;
-  __device__ __forceinline__ uint32_t k_at(int g) const { return pos + (g < ahead ? g : 2 * g - ahead + 1); }
-  __device__ __forceinline__ uint32_t v_at(int g) const { return pos + min(ahead, n) + g + max(0, min(g, n - ahead)); }
-};
+// K and V tiles come through a ring each.  Sub-block g of an item takes place pos + g of both; an alternate item
+// takes an even number of places (of an odd number of sub-blocks the last stays empty).  A wait on a barrier
+// tells a phase from its neighbours only, so whoever waits for a tile has to know that the tile before it in the same
+// slot has landed.  So it is: within an item that one is a tile the same chain has waited for (an alternate
+// item deals the slots to the chains by turns, and their number is even), and an item begins when all tiles of
+// those before it have landed (a pair's chains wait for all of them, those of an alternate item for each
+// other at its end).
+__device__ __forceinline__ int ta_places(int n, bool pair) { return pair ? n : (n + 1) & ~1; }
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1,
                                             int c2, int c3) {
@@ -362,8 +362,8 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   if (a.status && *reinterpret_cast<volatile int32_t*>(a.status + 2) != 0) return;
 
   const uint32_t base = smem_u32(smem);
-  const uint32_t s_q = base, s_ring = base + 2 * QTILE;
-  unsigned char* const stage_base = smem + 2 * QTILE + SLOTS * TILE;
+  const uint32_t s_q = base, s_k = base + 2 * QTILE, s_v = s_k + SLOTS * TILE;
+  unsigned char* const stage_base = smem + 2 * QTILE + 2 * SLOTS * TILE;
   unsigned char* const ctrl = stage_base + 8 * kTaStage;
   const uint32_t bars = smem_u32(ctrl);
   TaItem* const items = reinterpret_cast<TaItem*>(ctrl + 512);            // [2]
@@ -371,8 +371,10 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   uint32_t* const s_tmem = reinterpret_cast<uint32_t*>(ctrl + 772);
   volatile int* const s_turn = reinterpret_cast<volatile int*>(ctrl + 896);   // [2][4]: exponentials done, by chain and lane quarter
   float2* const s_stat = reinterpret_cast<float2*>(ctrl + 1024);          // [2][128]: maximum, sum
-  auto full = [&](uint32_t pos) { return bars + 8u * (pos % SLOTS); };
-  auto empty = [&](uint32_t pos) { return bars + 128u + 8u * (pos % SLOTS); };
+  auto k_full = [&](uint32_t at) { return bars + 8u * (at % SLOTS); };
+  auto v_full = [&](uint32_t at) { return bars + 64u + 8u * (at % SLOTS); };
+  auto k_empty = [&](uint32_t at) { return bars + 128u + 8u * (at % SLOTS); };
+  auto v_empty = [&](uint32_t at) { return bars + 192u + 8u * (at % SLOTS); };
   const uint32_t more = bars + 256u;
   const uint32_t q_full = more, q_free = more + 8u, sync256 = more + 16u;
   auto item_full = [&](uint32_t i) { return more + 24u + 8u * (i & 1u); };
@@ -383,6 +385,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   // only, and the one rescaling waits for can be two products behind.
   auto pv_done = [&](int c, uint32_t i) { return more + 120u + 16u * (uint32_t)c + 8u * (i & 1u); };
   auto o_full = [&](int c) { return more + 152u + 8u * (uint32_t)c; };
+  const uint32_t issued = more + 184u;
   auto drained = [&](int c) { return more + 168u + 8u * (uint32_t)c; };
 
   if (warp == 0) {
@@ -392,8 +395,11 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   }
   if (tid == 0) {
     // a tile and the query rows are given back once per chain
-    for (int i = 0; i < SLOTS; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 2); }
-    mbar_init(q_full, 1); mbar_init(q_free, 2); mbar_init(sync256, 8);
+    for (int i = 0; i < SLOTS; ++i) {
+      mbar_init(k_full(i), 1); mbar_init(v_full(i), 1);
+      mbar_init(k_empty(i), 2); mbar_init(v_empty(i), 2);
+    }
+    mbar_init(q_full, 1); mbar_init(q_free, 2); mbar_init(sync256, 8); mbar_init(issued, 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(item_full(i), 1); mbar_init(item_free(i), 10);
       mbar_init(s_full(0, i), 1); mbar_init(s_full(1, i), 1);
@@ -433,8 +439,45 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
     if (mbar_test(bar, parity)) return true;
     return *s_fail == 0 && mbar_wait<kTaPolls>(bar, parity);
   };
-  auto landed = [&](uint32_t at) { return wait(full(at), (at / SLOTS) & 1u); };
-  uint32_t pos = 0;                                      // ring position of the item's first tile
+  auto k_landed = [&](uint32_t at) { return wait(k_full(at), (at / SLOTS) & 1u); };
+  auto v_landed = [&](uint32_t at) { return wait(v_full(at), (at / SLOTS) & 1u); };
+  uint32_t pos = 0;                                      // the rings' place of the item's first tiles
+  // The tiles of an item, K `ahead` of V (one thread): the order in which they can be used, so that none waits
+  // for a place behind one that is not needed yet.
+  auto fetch = [&](const TaItem& it) {
+    const int row0 = (int)a.g.row0((long long)it.b * a.g.L + it.l) + it.row0;
+    const int tm_l = a.g.row_off ? 0 : it.l, tm_b = a.g.row_off ? 0 : it.b;
+    const int places = ta_places(it.n, it.pair), ahead = it.pair ? 2 : 4;
+    bool ok = true;
+    auto one = [&](bool is_k, int g) {
+      const uint32_t at = pos + g, full = is_k ? k_full(at) : v_full(at), empty = is_k ? k_empty(at) : v_empty(at);
+      if (at >= SLOTS) ok = wait(empty, (at / SLOTS - 1) & 1u);
+      if (!ok) return;
+      if (!it.pair) mbar_arrive(empty);                  // for the chain that does not use it
+      if (g >= it.n) {                                   // an empty place: landed and given back at once
+        mbar_arrive(full);
+        mbar_arrive(empty);
+        return;
+      }
+      mbar_expect_tx(full, TILE);
+      for (int c = 0; c < D / 64; ++c)
+        tma_load_5d((is_k ? s_k : s_v) + (at % SLOTS) * TILE + c * kTaSubHalf, is_k ? &map_k : &map_v, full, c * 64,
+                    row0 + g * kTaSub, it.h, tm_l, tm_b);
+    };
+    for (int g = 0; ok && g < places + ahead; ++g) {
+      if (g < places) one(true, g);
+      if (ok && g >= ahead) one(false, g - ahead);
+    }
+    return ok;
+  };
+  // After a failure: copies that may still be in flight, the last ones of every slot.
+  auto drain = [&]() {
+    for (int i = 0; i < SLOTS; ++i)
+      for (uint32_t parity = 0; parity < 2; ++parity) {
+        mbar_wait<12>(k_full(i), parity);
+        mbar_wait<12>(v_full(i), parity);
+      }
+  };
 
   if (warp == 9) {
     // ---- items and tiles ---------------------------------------------------------------------------
@@ -478,36 +521,16 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
             for (int c = 0; c < D / 64; ++c)
               tma_load_4d(s_q + t * QTILE + c * kTaHalf, &map_q, q_full, c * 64, it.h * A.G, it.tok0 + t * A.QT, it.l);
         }
-        const int row0 = (int)a.g.row0((long long)it.b * a.g.L + it.l) + it.row0;
-        const int tm_l = a.g.row_off ? 0 : it.l, tm_b = a.g.row_off ? 0 : it.b;
-        // in the order of use: the first `ahead` tiles of K, then V(g), K(g + ahead), V(g + 1), ...
-        const int ahead = min(it.pair ? 2 : 4, it.n);
-        for (int i = 0; ok && i < 2 * it.n; ++i) {
-          const int after = i - ahead;
-          bool is_k;
-          int g;
-          if (after < 0) { is_k = true; g = i; }
-          else if (after < 2 * (it.n - ahead)) { is_k = after & 1; g = (after >> 1) + (is_k ? ahead : 0); }
-          else { is_k = false; g = after - (it.n - ahead); }
-          const uint32_t at = pos + i;
-          if (at >= SLOTS) ok = wait(empty(at), (at / SLOTS - 1) & 1u);
-          if (!ok) break;
-          if (!it.pair) mbar_arrive(empty(at));          // for the chain that does not use it
-          mbar_expect_tx(full(at), TILE);
-          for (int c = 0; c < D / 64; ++c)
-            tma_load_5d(s_ring + (at % SLOTS) * TILE + c * kTaSubHalf, is_k ? &map_k : &map_v, full(at), c * 64,
-                        row0 + g * kTaSub, it.h, tm_l, tm_b);
-        }
+        ok = ok && fetch(it);
       }
       ok = __shfl_sync(0xffffffffu, ok, 0);
-      pos += 2 * it.n;
+      pos += ta_places(it.n, it.pair);
       ++n_q;
     }
     if (!ok) {
       *s_fail = 1;
-      // copies that may still be in flight: the last ones of every slot, and the query tiles
       if (lane == 0) {
-        for (int i = 0; i < SLOTS; ++i) { mbar_wait<12>(full(i), 0); mbar_wait<12>(full(i), 1); }
+        drain();
         mbar_wait<12>(q_full, 0); mbar_wait<12>(q_full, 1);
       }
     }
@@ -515,7 +538,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
     // ---- matrix products of one chain: the whole warp walks the items, one elected lane issues --------
     const int c = warp == 10;
     bool ok = true;
-    uint32_t n_item = 0, n_q = 0, n_s = 0, n_p = 0;      // running numbers: items, scores issued, weights used
+    uint32_t n_item = 0, n_q = 0, n_s = 0, n_p = 0, n_alt = 0;   // running numbers: items, scores issued, weights used, ...
     const uint32_t t_c = __shfl_sync(0xffffffffu, tmem, 0) + c * 256;
     auto commit = [&](uint32_t bar) { if (elect_one()) umma_commit(bar); };
     while (true) {
@@ -531,22 +554,22 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       if (stop) break;
       if (n == 0) continue;
       const int mine = pair ? (c ? n : n0) : (n + 1 - c) / 2;
-      const TaRing ring{pos, n, pair ? 2 : 4};
+      auto place = [&](int u) { return pos + (pair ? u : 2 * u + c); };
       const uint64_t dq = umma_desc(s_q + (pair ? c * QTILE : 0), 16, 1024);
       auto qk = [&](uint32_t at) {                       // S[n_s & 1] = Q K^T; elected lane only
-        const uint64_t dk = umma_desc(s_ring + (at % SLOTS) * TILE, 16, 1024);
+        const uint64_t dk = umma_desc(s_k + (at % SLOTS) * TILE, 16, 1024);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)                 // (the address fields count 16 bytes)
           umma_ss(t_c + (n_s & 1) * 64, dq + (((k >> 2) * kTaHalf + (k & 3) * 32) >> 4),
                   dk + (((k >> 2) * kTaSubHalf + (k & 3) * 32) >> 4), kTaIdescQK, k > 0);
         umma_commit(s_full(c, n_s));
-        umma_commit(empty(at));
+        umma_commit(k_empty(at));
       };
       ok = wait(q_full, n_q & 1u);
       ++n_q;
       for (int u = 0; u < min(2, mine); ++u, ++n_s) {
-        const uint32_t at = ring.k_at(pair ? u : 2 * u + c);
-        ok = landed(at) && ok;
+        const uint32_t at = place(u);
+        ok = k_landed(at) && ok;
         tc_fence_after();
         if (elect_one()) qk(at);
       }
@@ -554,19 +577,19 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       for (int u = 0; u < mine; ++u, ++n_p) {
         // Everything that will be there anyway is checked before the weights are waited for: a check costs
         // about 100 cycles, and the softmax waits for what is issued behind the weights.
-        const uint32_t v = ring.v_at(pair ? u : 2 * u + c), kn = ring.k_at(pair ? u + 2 : 2 * u + 4 + c);
+        const uint32_t v = place(u), kn = place(u + 2);
         const bool next = u + 2 < mine;
-        ok = landed(v) && ok;
-        if (next) ok = landed(kn) && ok;
+        ok = v_landed(v) && ok;
+        if (next) ok = k_landed(kn) && ok;
         ok = wait(p_full(c, n_p), (n_p >> 1) & 1u) && ok;
         if (!__all_sync(0xffffffffu, ok)) break;
         tc_fence_after();
-        const uint64_t dv = umma_desc(s_ring + (v % SLOTS) * TILE, kTaSubHalf, 1024);
+        const uint64_t dv = umma_desc(s_v + (v % SLOTS) * TILE, kTaSubHalf, 1024);
         if (elect_one()) {                               // O += P V(u)
 #pragma unroll
           for (int k = 0; k < kTaSub / 16; ++k)
             umma_ts(t_c + 128, t_c + (n_p & 1) * 64 + k * 8, dv + (k * 2048 >> 4), kTaIdescPV<D>, u > 0 || k > 0);
-          umma_commit(empty(v));
+          umma_commit(v_empty(v));
           // The score columns that P V(u) reads its weights from take scores u + 2: both products come
           // from one thread and run on one tensor core, which takes them in the order of issue.
           if (next) qk(kn);
@@ -579,13 +602,17 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       // tiles behind the last that chain 0 of a pair has a use for
       if (pair && c == 0)
         for (int g = mine; ok && g < n; ++g) {
-          ok = landed(ring.k_at(g));
-          if (lane == 0) mbar_arrive(empty(ring.k_at(g)));
-          ok = landed(ring.v_at(g)) && ok;
-          if (lane == 0) mbar_arrive(empty(ring.v_at(g)));
+          ok = k_landed(pos + g) && v_landed(pos + g);
+          if (lane == 0) { mbar_arrive(k_empty(pos + g)); mbar_arrive(v_empty(pos + g)); }
           __syncwarp();
         }
-      pos += 2 * n;
+      if (!pair) {                                       // until all tiles of the item have landed
+        __syncwarp();
+        if (lane == 0) mbar_arrive(issued);
+        ok = ok && wait(issued, n_alt & 1u);
+        ++n_alt;
+      }
+      pos += ta_places(n, pair);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
     }
@@ -630,7 +657,6 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       const uint32_t* mask = TREE ? a.mask + (long long)(it.tok0 + (valid ? q : 0)) * 2 * a.mask_words : nullptr;
       const int mine = it.pair ? (chain ? it.n : it.n0) : (it.n + 1 - chain) / 2;
       const int others = it.pair ? (chain ? it.n0 : it.n) : (it.n + chain) / 2;
-      const TaRing ring{pos, it.n, it.pair ? 2 : 4};
       float m_ref = -INFINITY, sum = 0.f;
 
       for (int u = 0; u < mine; ++u, ++n_s) {
@@ -643,22 +669,21 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
         // Rows of the V tile that no token of the item sees can hold anything; clear them, so that a zero
         // weight times Inf or NaN cannot reach O (in a pair both chains write the same zeros).
         if (it.end - r0 < kTaSub) {
-          const uint32_t v = ring.v_at(g);
-          ok = __all_sync(0xffffffffu, landed(v));
+          const uint32_t v = pos + g;
+          ok = __all_sync(0xffffffffu, v_landed(v));
           if (!ok) break;
           if (row < kTaSub && row >= it.end - r0) {
 #pragma unroll
             for (int c = 0; c < D / 8; ++c)
-              st_shared16(s_ring + (v % SLOTS) * TILE + (c >> 3) * kTaSubHalf + row * 128 + ((c & 7) << 4), 0, 0, 0, 0);
+              st_shared16(s_v + (v % SLOTS) * TILE + (c >> 3) * kTaSubHalf + row * 128 + ((c & 7) << 4), 0, 0, 0, 0);
           }
           proxy_fence();
         }
         if (warp_valid) {
           uint32_t x[64];
-          tmem_ld64_issue(t_s, x);
+          tmem_ld64(t_s, x);
           // the bits of a word of 32 columns that this thread's row sees
           const bool masked = TREE ? r0 + kTaSub > it.base : __any_sync(0xffffffffu, limit < r0 + kTaSub);
-          tmem_ld64_wait(x);
           if (masked) {
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
@@ -736,7 +761,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
         if (lane == 0) mbar_arrive(p_full(chain, n_s));
       }
       if (!ok) break;
-      pos += 2 * it.n;
+      pos += ta_places(it.n, it.pair);
       other_s += others;
 
       // ---- the item's rows go out --------------------------------------------------------------------
