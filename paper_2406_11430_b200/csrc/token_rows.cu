@@ -55,16 +55,22 @@ __device__ __forceinline__ uint4 ld_once(const void* p) {
   return v;
 }
 
-// Cosine and sine of the angle a, to about 1e-10, in fp64.  a / 2 pi is formed as a sum of two doubles and the nearest
-// quarter turn taken off it, which leaves the rest exact for any position; at most an eighth of a turn is
-// left, where the Taylor series are short (the terms left out: x^13 / 13! < 1e-11, x^12 / 12! < 2e-10).
+// Cosine and sine of the angle a in fp64, to about 1e-15: their fp32 roundings are those of the exact values
+// but for one in some 10^7.  a / 2 pi is formed as a sum of two doubles and the nearest quarter turn taken off it,
+// which leaves the rest exact for any position; at most an eighth of a turn is left, where the Taylor series
+// are short (the first terms left out: x^17 / 17! < 5e-17, x^16 / 16! < 1e-15).
 __device__ __forceinline__ void cos_sin(double a, double* c, double* s) {
   constexpr double kHi = 0.15915494309189535, kLo = -9.839338337591243e-18;   // 1 / 2 pi
   const double t = a * kHi;
   const double rest = __fma_rn(a, kLo, __fma_rn(a, kHi, -t));
   const double quarters = rint(4.0 * t);
   const double x = (__fma_rn(-0.25, quarters, t) + rest) * 6.283185307179586, z = x * x;
-  double sx = __fma_rn(z, -1.0 / 39916800.0, 1.0 / 362880.0), cx = __fma_rn(z, -1.0 / 3628800.0, 1.0 / 40320.0);
+  double sx = __fma_rn(z, -1.0 / 1307674368000.0, 1.0 / 6227020800.0);
+  double cx = __fma_rn(z, -1.0 / 87178291200.0, 1.0 / 479001600.0);
+  sx = __fma_rn(z, sx, -1.0 / 39916800.0);
+  cx = __fma_rn(z, cx, -1.0 / 3628800.0);
+  sx = __fma_rn(z, sx, 1.0 / 362880.0);
+  cx = __fma_rn(z, cx, 1.0 / 40320.0);
   sx = __fma_rn(z, sx, -1.0 / 5040.0);
   cx = __fma_rn(z, cx, -1.0 / 720.0);
   sx = __fma_rn(z, sx, 1.0 / 120.0);
@@ -152,7 +158,9 @@ rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* __restrict__ K, T* 
       Elem<T>::unpack(w, o);
     }
 #pragma unroll
-    for (int e = 0; e < EPV; ++e) y[e] = __fmaf_rn(f[e], cs[e], o[e] * sn[e]);
+    // Two products and a sum, each rounded: the arithmetic of the formula as it is written, so that a stored bf16
+    // key, and with it the ordering key, is the one any plain fp32 form of it stores
+    for (int e = 0; e < EPV; ++e) y[e] = __fadd_rn(__fmul_rn(f[e], cs[e]), __fmul_rn(o[e], sn[e]));
     const uint4 r = pack_piece<T>(y);
     return turns ? r : v;                                // (dimensions from rot_dim on are copied)
   };
