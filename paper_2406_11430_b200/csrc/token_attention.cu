@@ -3,22 +3,31 @@
 // memory).
 //
 // A query tile is 128 rows: the (token, head-of-the-group) pairs of 128 / G tokens that share a KV
-// head.  Cached rows are taken in blocks of 128; for each one
-//   S = Q K^T  (128 x 128, fp32, tensor memory)  ->  softmax threads: masks, running maximum,
+// head.  Cached rows are taken in sub-blocks of 64; for each one
+//   S = Q K^T  (128 x 64, fp32, tensor memory)  ->  softmax threads: masks, running maximum,
 //   P = 2^(s - m) as bf16 over the score columns  ->  O += P V  (tensor memory).
 // A CTA always works on two such chains at a time, so that one's matrix products run under the other's
-// softmax: two neighbouring query tiles that share every K and V block ("pair"), or, where a sequence
-// has no more tokens than one tile holds, the even and the odd blocks of one query tile ("alternate"),
-// joined at the end.  A chain has one score tile, and the weights overwrite it in place, so per
-// chain Q K^T(j + 1) follows P V(j), and what bounds a long prompt is
-// max(softmax, both products) per block and chain; N = 128 in both products keeps the shared-memory
-// reads of an instruction (A and B operands, 8 KB) within its 64 cycles.
+// softmax: two neighbouring query tiles that share every K and V tile ("pair"), or, where a sequence
+// has no more tokens than one tile holds, the even and the odd sub-blocks of one query tile ("alternate"),
+// joined at the end.  Each chain has two score tiles, so S(j + 1) is formed while S(j) is worked on.
 //
-// Roles: 4 softmax warps per chain (one thread per query row), one thread that issues all matrix
-// products, one warp that works out the items and fetches tiles through a ring of four.  A fixed grid
-// of CTAs walks a list of items (tile or pair of one sequence, layer and KV head), longest first, or,
-// where a call has fewer items than SMs, equal chunks of them that a second kernel joins.
+// Roles: 4 softmax warps per chain (one thread per query row), a warp per chain that issues its matrix
+// products, one that works out the items and fetches tiles through a ring each for K and V.  A fixed grid of
+// CTAs takes equal shares of the call's work, a list of items (tile or pair of one sequence, layer and KV
+// head); an item that a share's end cuts leaves partial results that a second kernel joins.
 // Every wait is bounded; one that gives up ends the CTA and marks the workspace.
+//
+// What bounds it (cycle counters and probes; per sub-block, both chains): the exponentials need 1024 cycles of
+// the MUFU pipe, the products 1312 of the tensor core (Q K^T at N = 64 50 cycles per instruction, bound by
+// its operands' way out of shared memory; P V 64), and a sub-block takes about 1650: the exponentials of one
+// chain take 660 with the pipe to themselves, and the chains hand them to each other in turn.  Long prompts
+// run into the GPU's power limit besides: 16 k tokens, 32 heads of 128, take 1.75 ms at 1965 MHz and
+// 1.95 to 2.0 ms (1110 to 1130 TFLOP/s) at the 1600 MHz that are left after a while.  Tree batches that fit one tile
+// are bound by memory (98 us for 478 MB, of which 79 us stream).
+// Tried, correct and not faster: blocks of 128 rows with one score tile per chain (products at N = 128, 10 to
+// 20 % slower: the chain softmax - product - softmax has no slack), two softmax warps for the same 32 rows,
+// a share of the exponentials as a polynomial on the FMA pipe (any share from 1/8 to 1/2), no maxima after the
+// first sub-block.
 #include <algorithm>
 #include <climits>
 #include <cstring>
@@ -34,21 +43,12 @@ constexpr int kTaHalf = kTaRows * 128;          // query rows, [128][64 bf16], s
 constexpr int kTaSubHalf = kTaSub * 128;        // cached rows, [64][64 bf16]: 8 KB
 constexpr int kTaStage = 4096;                  // bytes per softmax warp on the way out
 constexpr int kTaThreads = 352;                 // 2 x 4 softmax warps, issuing warps 8 and 10, fetching warp 9
-#ifndef L2KV_TA_TURN
-#define L2KV_TA_TURN 1
-#endif
-#ifndef L2KV_TA_TURN_AT
-#define L2KV_TA_TURN_AT 15
-#endif
-#ifndef L2KV_TA_POLY
-#define L2KV_TA_POLY 0
-#endif
-constexpr int kTaPolyEvery = L2KV_TA_POLY;      // of so many weight pairs one is computed on the FMA pipe (0: none)
 constexpr int kTaGrid = 148;                    // one CTA per SM (512 tensor-memory columns each)
 constexpr int kTaCtrl = 3072;                   // barriers, items, row statistics
 constexpr int kTaPolls = 18;                    // log2 of the polls a wait may take
 constexpr int kTaItemCost = 4;                  // what starting and finishing an item costs, in sub-blocks
 constexpr int kTaMinShare = 24;                 // items that cost less on average are not cut
+constexpr int kTaGroup = 4;                     // pairs of weights whose exponentials go side by side
 constexpr float kTaRescaleGap = 8.f;            // log2 units a maximum may drift before O is rescaled
 
 template <int D> constexpr int kTaQTile = D / 64 * kTaHalf;
@@ -68,7 +68,7 @@ struct TaItem {
   int base, end;         // row of the sequence's first new token; rows that some token of the item sees
   int row0, n, n0;       // first row, sub-blocks of the item (pair: of chain 1 and of chain 0)
   int pair;              // two query tiles; else one whose sub-blocks the chains take in turn
-  int slot;              // where the partial result of a chunk goes; -1: the result itself
+  int slot;              // where the partial result of a piece goes; -1: the result itself
   int stop;              // no more items
 };
 
@@ -331,23 +331,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return d;
 }
-// 2^x on the FMA pipe: x = n + f with n the nearest whole number (adding 1.5 2^23 leaves it in the low
-// bits), 2^f on [-1/2, 1/2] by a polynomial of degree 4 fitted for the smallest relative error (2.6e-6),
-// n added to the exponent.  For x in [-126, 126]; below, 2^-126.
-__device__ __forceinline__ float2 poly_exp2(float2 x) {
-  const float2 magic = make_float2(12582912.f, 12582912.f), back = make_float2(-12582912.f, -12582912.f);
-  x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
-  const float2 t = add2(x, magic), n = add2(t, back);
-  const float2 f = add2(x, make_float2(-n.x, -n.y));
-  auto k = [](float c) { return make_float2(c, c); };
-  float2 p = fma2(f, k(0.009570102207362652f), k(0.05591786280274391f));
-  p = fma2(f, p, k(0.240247443318367f));
-  p = fma2(f, p, k(0.6931217908859253f));
-  p = fma2(f, p, k(0.9999992847442627f));
-  return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
-                     __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
-}
-
 template <int D, bool TREE>
 __global__ void __launch_bounds__(kTaThreads, 1)
 token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__ CUtensorMap map_q,
@@ -424,8 +407,11 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
     one_each = ta_small_call(A, spot, end);
     if (!one_each) {
       const TaShares shares(A);
-      spot = shares.begin(blockIdx.x);
-      end = shares.begin(blockIdx.x + 1);
+#pragma unroll 1                                         // (the second time its instructions are at hand)
+      for (int k = 0; k < 2; ++k) {
+        spot = end;
+        end = shares.begin(blockIdx.x + k);
+      }
       one_each = shares.one_each;
     }
     if (A.plan && lane == 0) A.plan[blockIdx.x] = spot;
@@ -657,21 +643,21 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       const uint32_t* mask = TREE ? a.mask + (long long)(it.tok0 + (valid ? q : 0)) * 2 * a.mask_words : nullptr;
       const int mine = it.pair ? (chain ? it.n : it.n0) : (it.n + 1 - chain) / 2;
       const int others = it.pair ? (chain ? it.n0 : it.n) : (it.n + chain) / 2;
+      // rows below `clear` are seen by all rows of the warp
+      const int clear = TREE ? it.base : (int)__reduce_min_sync(0xffffffffu, (unsigned)max(0, limit));
       float m_ref = -INFINITY, sum = 0.f;
 
       for (int u = 0; u < mine; ++u, ++n_s) {
         const int g = it.pair ? u : 2 * u + chain;                           // sub-block within the item
         const int r0 = it.row0 + g * kTaSub;                                 // its first row
         const uint32_t t_s = t_c + (n_s & 1) * 64;
-        ok = __all_sync(0xffffffffu, wait(s_full(chain, n_s), (n_s >> 1) & 1u));
-        if (!ok) break;
+        ok = wait(s_full(chain, n_s), (n_s >> 1) & 1u);  // (voted on below)
         tc_fence_after();
         // Rows of the V tile that no token of the item sees can hold anything; clear them, so that a zero
         // weight times Inf or NaN cannot reach O (in a pair both chains write the same zeros).
         if (it.end - r0 < kTaSub) {
           const uint32_t v = pos + g;
-          ok = __all_sync(0xffffffffu, v_landed(v));
-          if (!ok) break;
+          ok = v_landed(v) && ok;
           if (row < kTaSub && row >= it.end - r0) {
 #pragma unroll
             for (int c = 0; c < D / 8; ++c)
@@ -682,9 +668,8 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
         if (warp_valid) {
           uint32_t x[64];
           tmem_ld64(t_s, x);
-          // the bits of a word of 32 columns that this thread's row sees
-          const bool masked = TREE ? r0 + kTaSub > it.base : __any_sync(0xffffffffu, limit < r0 + kTaSub);
-          if (masked) {
+          if (r0 + kTaSub > clear) {
+            // the bits of a word of 32 columns that this thread's row sees
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
               uint32_t bits = low_bits(limit - r0 - 32 * w);
@@ -702,18 +687,22 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
                 if (!(bits >> i & 1u)) x[32 * w + i] = 0xff800000u;          // -inf
             }
           }
-          float t0 = __uint_as_float(x[0]), t1 = __uint_as_float(x[1]);
+          float t[4] = {__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3])};
 #pragma unroll
-          for (int i = 2; i < 62; i += 4) {
-            t0 = fmaxf(t0, fmaxf(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
-            t1 = fmaxf(t1, fmaxf(__uint_as_float(x[i + 2]), __uint_as_float(x[i + 3])));
-          }
-          const float top = fmaxf(t0, fmaxf(t1, fmaxf(__uint_as_float(x[62]), __uint_as_float(x[63]))));
+          for (int i = 4; i < 60; i += 8)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              t[e] = fmaxf(t[e], fmaxf(__uint_as_float(x[i + 2 * e]), __uint_as_float(x[i + 2 * e + 1])));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) t[e] = fmaxf(t[e], __uint_as_float(x[60 + e]));
+          const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
           const float m_new = fmaxf(m_ref, top * a.scale_log2e);
           if (u == 0) m_ref = m_new;
           const bool need = m_new > m_ref + kTaRescaleGap;
-          if (__any_sync(0xffffffffu, need)) {
-            // O is quiet once these scores' predecessors, and with them P V(u - 2), and P V(u - 1) are done
+          if (__any_sync(0xffffffffu, need || !ok)) {
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            // O is quiet once P V(u - 1) is done (P V(u) waits for this warp)
             ok = __all_sync(0xffffffffu, wait(pv_done(chain, n_s - 1), ((n_s - 1) >> 1) & 1u));
             if (!ok) break;
             tc_fence_after();
@@ -725,36 +714,55 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
           const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;             // a row that has seen nothing yet
           const float2 sc2 = make_float2(a.scale_log2e, a.scale_log2e), nm2 = make_float2(neg_m, neg_m);
           float2 sums = make_float2(0.f, 0.f);
-#if L2KV_TA_TURN
-          // The two warps of a scheduler, one per chain, take turns in the exponentials: side by side both would
-          // be slowed to half speed and then wait for the tensor core together, in step for good.
-          // (Only the pace depends on it: a turn that does not come is not waited for.)
+          // The two warps of a scheduler, one per chain, take turns in the exponentials: side by side both are
+          // slowed to half speed and then wait for the tensor core together, in step for good (7 to 10 % slower
+          // on long and on ragged prompts).  Only the pace depends on it: a turn that does not come is not waited for.
           if (chain ? u < others : u <= others) {
             const int until = other_s + u + chain;
             for (int spin = 0; spin < 128 && *other_turn - until < 0; ++spin) {}
           }
-#endif
-          auto weights = [&](auto mixed) {
-            uint32_t pk[32];
+          // Four pairs at a time, one stage apart: the exponentials of one group beside the arguments of the next
+          // and the sums and roundings of the one before.  Left to itself the compiler does each kind of
+          // instruction for all pairs before the next, and the exponentials' pipe idles meanwhile (4 to 10 %
+          // slower; groups of 2 or 8 pairs: 4 % slower, the same).
+          uint32_t pk[32];
+          float2 arg[kTaGroup], w[kTaGroup], done[kTaGroup];
+          auto args_of = [&](int g) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const float2 e = fma2(make_float2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), sc2, nm2);
-              float2 w;
-              if (decltype(mixed)::value && kTaPolyEvery && i % (kTaPolyEvery ? kTaPolyEvery : 1) == 0) w = poly_exp2(e);
-              else w = make_float2(fast_exp2(e.x), fast_exp2(e.y));
-              sums = add2(sums, w);
-              pk[i] = pack_bf16(w.x, w.y);
-#if L2KV_TA_TURN
-              if (i == L2KV_TA_TURN_AT) { __syncwarp(); if (lane == 0) *my_turn = (int)n_s + 1; }
-#endif
+            for (int i = 0; i < kTaGroup; ++i) {
+              const int k = 2 * (kTaGroup * g + i);
+              arg[i] = fma2(make_float2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), sc2, nm2);
             }
-            tmem_st32(t_s, pk);
           };
-          if (masked) weights(std::false_type{}); else weights(std::true_type{});
+          auto finish = [&](int g) {
+#pragma unroll
+            for (int i = 0; i < kTaGroup; ++i) {
+              sums = add2(sums, done[i]);
+              pk[kTaGroup * g + i] = pack_bf16(done[i].x, done[i].y);
+            }
+          };
+          args_of(0);
+#pragma unroll
+          for (int g = 0; g < 32 / kTaGroup; ++g) {
+            __syncwarp();                                // (a fence for the compiler's scheduling)
+#pragma unroll
+            for (int i = 0; i < kTaGroup; ++i) w[i] = make_float2(fast_exp2(arg[i].x), fast_exp2(arg[i].y));
+            if (g + 1 < 32 / kTaGroup) args_of(g + 1);
+            if (g > 0) finish(g - 1);
+#pragma unroll
+            for (int i = 0; i < kTaGroup; ++i) done[i] = w[i];
+          }
+          finish(32 / kTaGroup - 1);
+          if (lane == 0)                                 // the turn; the store takes the last weights as an operand, so it comes behind them
+            asm volatile("{ .reg .b32 t; mov.b32 t, %2; st.volatile.shared.b32 [%0], %1; }"
+                         :: "r"(smem_u32(const_cast<int*>(my_turn))), "r"(n_s + 1), "r"(pk[31]) : "memory");
+          tmem_st32(t_s, pk);
           tmem_wait_st();
           sum += sums.x + sums.y;
-        } else if (lane == 0) {
-          *my_turn = (int)n_s + 1;
+        } else {
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          if (lane == 0) *my_turn = (int)n_s + 1;
         }
         tc_fence_before();
         __syncwarp();
