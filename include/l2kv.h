@@ -335,6 +335,8 @@ typedef struct {
 /* Flags of the calls on new tokens. */
 #define L2KV_TOKENS_LEN_PER_HEAD 1u   /* lengths are [batch, layers, kv_heads], not [batch, layers] */
 #define L2KV_TOKENS_ROTARY_INTERLEAVED 2u /* l2kv_rotary_write: pairs are (2p, 2p + 1)              */
+#define L2KV_TOKENS_NO_LAUNCH 4u     /* checks only: L2KV_ERR_INVALID_ARG where a kernel would run, as
+                                        for pointers to host memory (the Python binding sets it then) */
 
 /* Rotary frequencies for l2kv_rotary_write: freq_out[p], p < rot_dim / 2, in radians per position,
  * and scale_out, the factor on cosine and sine.  Host only, fp64.  With f_p = base^(-2p / rot_dim):
@@ -396,8 +398,9 @@ int l2kv_rotary_write(const l2kv_tokens* q, const l2kv_tokens* k, const l2kv_tok
  * flags: L2KV_TOKENS_LEN_PER_HEAD.  workspace: NULL, or of at least 256 bytes of which the first 256 were
  * zeroed (its status word then reports a wait that gave up); with
  * l2kv_prompt_attention_workspace_bytes bytes, calls with little work per SM split their caches over
- * the SMs and merge the pieces.  Beyond its first 256 bytes it needs no initial contents, and two
- * calls that can overlap on the GPU need one each. */
+ * the SMs and merge the pieces.  Beyond its first 256 bytes it needs no initial contents, two calls that
+ * can overlap on the GPU need one each, and one that the other calls of this layout use will do if it is large
+ * enough (their completion counters are left alone). */
 int l2kv_prompt_attention_workspace_bytes(const l2kv_layout* lay, int32_t n_tokens, int32_t max_len,
                                           size_t* bytes);
 int l2kv_prompt_attention(const l2kv_tokens* q, const int32_t* tok_off_dev, int32_t n_tokens,

@@ -412,7 +412,7 @@ def _call(fn, name, ref, stream, *args):
     current device for the call (a stream of one device takes no kernel of another)."""
     device = ref.device
     if device.type != "cuda":
-        rc = fn(*args, 0)                        # host tensors: checks only
+        rc = fn(*args, 0)                        # host tensors: checks only (nothing is launched)
     else:
         handle = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
         if torch._C._cuda_getDevice() == device.index:

@@ -496,7 +496,7 @@ int l2kv_rotary_write(const l2kv_tokens* q, const l2kv_tokens* k, const l2kv_tok
   const Range nvtx_range("l2kv_rotary_write");
   int rc = check_layout(lay);
   if (rc != L2KV_OK) return rc;
-  if (flags & ~(uint32_t)(L2KV_TOKENS_LEN_PER_HEAD | L2KV_TOKENS_ROTARY_INTERLEAVED)) return L2KV_ERR_INVALID_ARG;
+  if (flags & ~(uint32_t)(L2KV_TOKENS_LEN_PER_HEAD | L2KV_TOKENS_ROTARY_INTERLEAVED | L2KV_TOKENS_NO_LAUNCH)) return L2KV_ERR_INVALID_ARG;
   if (n_tokens < 0 || rot_dim < 0 || !std::isfinite(rot_scale)) return L2KV_ERR_INVALID_ARG;
   if (rot_dim > lay->head_dim || rot_dim % 16) return L2KV_ERR_UNSUPPORTED;
   if (empty(lay)) return L2KV_OK;
@@ -513,6 +513,7 @@ int l2kv_rotary_write(const l2kv_tokens* q, const l2kv_tokens* k, const l2kv_tok
   }
   if (!aligned16(K_c) || !aligned16(V_c) || !aligned16(workspace)) return L2KV_ERR_MISALIGNED;
   if (workspace_bytes < (size_t)kStatusBytes) return L2KV_ERR_WORKSPACE_TOO_SMALL;
+  if (flags & L2KV_TOKENS_NO_LAUNCH) return L2KV_ERR_INVALID_ARG;
   return launch_rotary_write(make_view(q), make_view(k), make_view(v), make_view(q_out), tok_off_dev, n_tokens,
                              pos_dev, freq_dev, rot_dim, rot_scale, (flags & L2KV_TOKENS_ROTARY_INTERLEAVED) != 0,
                              K_c, V_c, idx, sumsq_c, make_geom(*lay), lay->dtype, start_dev, cur_len_dev,
@@ -527,13 +528,14 @@ int l2kv_tree_commit(void* K_c, void* V_c, int32_t* idx, float* sumsq_c, const l
   const Range nvtx_range("l2kv_tree_commit");
   const int rc = check_layout(lay);
   if (rc != L2KV_OK) return rc;
-  if ((flags & ~(uint32_t)L2KV_TOKENS_LEN_PER_HEAD) || path_cap < 0) return L2KV_ERR_INVALID_ARG;
+  if ((flags & ~(uint32_t)(L2KV_TOKENS_LEN_PER_HEAD | L2KV_TOKENS_NO_LAUNCH)) || path_cap < 0) return L2KV_ERR_INVALID_ARG;
   if (empty(lay)) return L2KV_OK;
   if (!K_c || !V_c || !start_dev || !cur_len_dev || (!path_dev && path_cap > 0) || !n_path_dev || !len_out_dev ||
       !workspace)
     return L2KV_ERR_INVALID_ARG;
   if (!aligned16(K_c) || !aligned16(V_c) || !aligned16(workspace)) return L2KV_ERR_MISALIGNED;
   if (workspace_bytes < (size_t)kStatusBytes) return L2KV_ERR_WORKSPACE_TOO_SMALL;
+  if (flags & L2KV_TOKENS_NO_LAUNCH) return L2KV_ERR_INVALID_ARG;
   return launch_tree_commit(K_c, V_c, idx, sumsq_c, make_geom(*lay), lay->dtype, start_dev, cur_len_dev, path_dev,
                             path_cap, n_path_dev, len_out_dev, (flags & L2KV_TOKENS_LEN_PER_HEAD) != 0,
                             static_cast<int32_t*>(workspace), static_cast<cudaStream_t>(stream));
@@ -549,7 +551,7 @@ static int token_attention_impl(bool tree, const l2kv_tokens* q, const int32_t* 
   if (rc != L2KV_OK) return rc;
   rc = check_groups(lay);
   if (rc != L2KV_OK) return rc;
-  if ((flags & ~(uint32_t)L2KV_TOKENS_LEN_PER_HEAD) || n_tokens < 0 || max_len < 0 || !(scale == scale))
+  if ((flags & ~(uint32_t)(L2KV_TOKENS_LEN_PER_HEAD | L2KV_TOKENS_NO_LAUNCH)) || n_tokens < 0 || max_len < 0 || !(scale == scale))
     return L2KV_ERR_INVALID_ARG;
   if (tree && mask_words < 1) return L2KV_ERR_INVALID_ARG;
   if (tree && mask_words > (1 << 24)) return L2KV_ERR_OUT_OF_RANGE;
@@ -561,15 +563,18 @@ static int token_attention_impl(bool tree, const l2kv_tokens* q, const int32_t* 
   if (!aligned16(K_c) || !aligned16(V_c) || !aligned16(workspace)) return L2KV_ERR_MISALIGNED;
   if (tree && (reinterpret_cast<uintptr_t>(tree_mask_dev) & 7u)) return L2KV_ERR_MISALIGNED;
   if (workspace && workspace_bytes < (size_t)kStatusBytes) return L2KV_ERR_WORKSPACE_TOO_SMALL;
+  if (flags & L2KV_TOKENS_NO_LAUNCH) return L2KV_ERR_INVALID_ARG;
   const float sc = scale > 0.f ? scale : 1.0f / std::sqrt((float)lay->head_dim);
   const TokenAttention a{make_view(q), make_view(out), tok_off_dev, n_tokens, make_geom(*lay),
                          LenView{cur_len_dev, (flags & L2KV_TOKENS_LEN_PER_HEAD) ? 1 : 0}, max_len,
                          sc * 1.4426950408889634f, lse_out,
                          tree ? reinterpret_cast<const uint32_t*>(tree_mask_dev) : nullptr, mask_words,
                          static_cast<int32_t*>(workspace)};
-  const size_t room = workspace ? workspace_bytes - kStatusBytes : 0;
-  return launch_token_attention(a, K_c, V_c, lay->dtype, room ? static_cast<char*>(workspace) + kStatusBytes : nullptr,
-                                room, static_cast<cudaStream_t>(stream));
+  // scratch begins behind the status block and the completion counters of the other calls on this layout
+  const size_t head = plan_workspace(*lay, 0).sumsq_off;
+  const size_t room = workspace && workspace_bytes > head ? workspace_bytes - head : 0;
+  return launch_token_attention(a, K_c, V_c, lay->dtype, room ? static_cast<char*>(workspace) + head : nullptr, room,
+                                static_cast<cudaStream_t>(stream));
 }
 
 int l2kv_prompt_attention_workspace_bytes(const l2kv_layout* lay, int32_t n_tokens, int32_t max_len,
@@ -582,7 +587,9 @@ int l2kv_prompt_attention_workspace_bytes(const l2kv_layout* lay, int32_t n_toke
   if (n_tokens < 0 || max_len < 0) return L2KV_ERR_INVALID_ARG;
   if (max_len > lay->t_cap) return L2KV_ERR_OUT_OF_RANGE;
   *bytes = (size_t)kStatusBytes;
-  if (!empty(lay) && n_tokens > 0) *bytes += token_attention_scratch(make_geom(*lay), lay->dtype, n_tokens, max_len);
+  if (empty(lay) || n_tokens == 0) return L2KV_OK;
+  const size_t scratch = token_attention_scratch(make_geom(*lay), lay->dtype, n_tokens, max_len);
+  if (scratch) *bytes = plan_workspace(*lay, 0).sumsq_off + scratch;
   return L2KV_OK;
 }
 

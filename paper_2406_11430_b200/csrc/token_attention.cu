@@ -44,7 +44,7 @@ constexpr int kTaSubHalf = kTaSub * 128;        // cached rows, [64][64 bf16]: 8
 constexpr int kTaStage = 4096;                  // bytes per softmax warp on the way out
 constexpr int kTaThreads = 352;                 // 2 x 4 softmax warps, issuing warps 8 and 10, fetching warp 9
 constexpr int kTaGrid = 148;                    // one CTA per SM (512 tensor-memory columns each)
-constexpr int kTaCtrl = 3072;                   // barriers, items, row statistics
+constexpr int kTaCtrl = 1024 + 2 * kTaRows * 8;  // barriers and items; row statistics
 constexpr int kTaPolls = 18;                    // log2 of the polls a wait may take
 constexpr int kTaItemCost = 4;                  // what starting and finishing an item costs, in sub-blocks
 constexpr int kTaMinShare = 24;                 // items that cost less on average are not cut
@@ -990,7 +990,7 @@ static int launch_ta(const TaArgs& A, const void* K, const void* V, long long it
 
 int launch_token_attention(const TokenAttention& a, const void* K, const void* V, int dtype, char* scratch,
                            size_t scratch_bytes, cudaStream_t s) {
-  if (dtype != L2KV_BF16) return launch_token_attention_simple(a, K, V, dtype, s);
+  if (dtype != L2KV_BF16) return launch_token_attention_simple(a, K, V, s);
   const TaRoom room = ta_room(a.g, a.n_tokens, a.max_len);
   if (room.items > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
   TaArgs A{};

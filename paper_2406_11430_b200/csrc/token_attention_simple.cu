@@ -12,12 +12,12 @@ namespace l2kv {
 
 constexpr int kTsWarps = 4;
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(32 * kTsWarps)
-token_attention_simple_kernel(const __grid_constant__ TokenAttention a, const T* __restrict__ K,
-                              const T* __restrict__ V) {
-  constexpr int EPV = Elem<T>::kPerVec, DPL = D / 32;
-  __shared__ float s_q[kTsWarps][D];
+token_attention_simple_kernel(const __grid_constant__ TokenAttention a, const float* __restrict__ K,
+                              const float* __restrict__ V) {
+  constexpr int DPL = D / 32;
+  __shared__ __align__(16) float s_q[kTsWarps][D];
   const Geom& g = a.g;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int groups = (g.Hq + kTsWarps - 1) / kTsWarps;
@@ -36,11 +36,11 @@ token_attention_simple_kernel(const __grid_constant__ TokenAttention a, const T*
   const int base = cur - r.n;                            // row of the sequence's first new token
   const int end = a.mask ? cur : max(0, min(cur, base + (i - r.first) + 1));
 
-  const T* q = a.q.row<T>(l, i, j);
-  for (int d = lane; d < D; d += 32) s_q[warp][d] = (float)q[d];
+  const float* q = a.q.row<float>(l, i, j);
+  for (int d = lane; d < D; d += 32) s_q[warp][d] = q[d];
   __syncwarp();
-  const T* Ku = K + g.base(b, l, h);
-  const T* Vu = V + g.base(b, l, h);
+  const float* Ku = K + g.base(b, l, h);
+  const float* Vu = V + g.base(b, l, h);
   float m = -INFINITY, sum = 0.f, o[DPL] = {};
   for (int t0 = 0; t0 < end; t0 += 32) {
     const int t = t0 + lane;
@@ -51,14 +51,15 @@ token_attention_simple_kernel(const __grid_constant__ TokenAttention a, const T*
     }
     float s = -INFINITY;
     if (sees) {
-      const T* row = Ku + (long long)t * g.st;
+      const float* row = Ku + (long long)t * g.st;
       float acc = 0.f;
 #pragma unroll 4
-      for (int d = 0; d < D; d += EPV) {
-        float x[EPV];
-        Elem<T>::unpack(*reinterpret_cast<const uint4*>(row + d), x);
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) acc = fmaf(x[e], s_q[warp][d + e], acc);
+      for (int d = 0; d < D; d += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(row + d), y = *reinterpret_cast<const float4*>(&s_q[warp][d]);
+        acc = fmaf(x.x, y.x, acc);
+        acc = fmaf(x.y, y.y, acc);
+        acc = fmaf(x.z, y.z, acc);
+        acc = fmaf(x.w, y.w, acc);
       }
       s = acc * a.scale_log2e;
     }
@@ -78,34 +79,26 @@ token_attention_simple_kernel(const __grid_constant__ TokenAttention a, const T*
       const int k = __ffs(who) - 1;
       who &= who - 1;
       const float w = __shfl_sync(0xffffffffu, p, k);
-      const T* row = Vu + (long long)(t0 + k) * g.st + lane * DPL;
+      const float* row = Vu + (long long)(t0 + k) * g.st + lane * DPL;
 #pragma unroll
-      for (int e = 0; e < DPL; ++e) o[e] = fmaf(w, (float)row[e], o[e]);
+      for (int e = 0; e < DPL; ++e) o[e] = fmaf(w, row[e], o[e]);
     }
   }
 #pragma unroll
   for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  T* out = a.out.row<T>(l, i, j) + lane * DPL;
+  float* out = a.out.row<float>(l, i, j) + lane * DPL;
 #pragma unroll
-  for (int e = 0; e < DPL; ++e) out[e] = (T)(sum == 0.f ? 0.f : o[e] * inv);
+  for (int e = 0; e < DPL; ++e) out[e] = sum == 0.f ? 0.f : o[e] * inv;
   if (a.lse && lane == 0)
     a.lse[((long long)l * a.n_tokens + i) * g.Hq + j] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
 }
 
-int launch_token_attention_simple(const TokenAttention& a, const void* K, const void* V, int dtype,
-                                  cudaStream_t s) {
+int launch_token_attention_simple(const TokenAttention& a, const void* K, const void* V, cudaStream_t s) {
   const long long blocks = (long long)a.n_tokens * a.g.L * ((a.g.Hq + kTsWarps - 1) / kTsWarps);
   if (blocks > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
-#define L2KV_TS(T, D)                                                                                  \
-  token_attention_simple_kernel<T, D><<<(unsigned)blocks, 32 * kTsWarps, 0, s>>>(                       \
-      a, static_cast<const T*>(K), static_cast<const T*>(V))
-  if (dtype == L2KV_BF16) {
-    if (a.g.D == 128) L2KV_TS(__nv_bfloat16, 128); else L2KV_TS(__nv_bfloat16, 64);
-  } else {
-    if (a.g.D == 128) L2KV_TS(float, 128); else L2KV_TS(float, 64);
-  }
-#undef L2KV_TS
+  auto kern = a.g.D == 128 ? token_attention_simple_kernel<128> : token_attention_simple_kernel<64>;
+  kern<<<(unsigned)blocks, 32 * kTsWarps, 0, s>>>(a, static_cast<const float*>(K), static_cast<const float*>(V));
   return cudaGetLastError() == cudaSuccess ? L2KV_OK : L2KV_ERR_CUDA;
 }
 

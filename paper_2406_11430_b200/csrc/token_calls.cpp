@@ -37,6 +37,12 @@ double real(PyObject* o) {
   if (v == -1.0 && PyErr_Occurred()) throw Bad{""};
   return v;
 }
+// An argument that is an int32 of the library's.
+int32_t integer32(PyObject* o, const char* what) {
+  const int64_t v = integer(o);
+  if (v != (int32_t)v) throw Bad{std::string(what) + " is out of range"};
+  return (int32_t)v;
+}
 bool truth(PyObject* o) { return PyObject_IsTrue(o) == 1; }
 
 int dtype_of(const at::Tensor& t) {
@@ -83,6 +89,11 @@ void one_device(const at::Tensor& ref, const T*... ts) {
   for (const at::Tensor* t : {static_cast<const at::Tensor*>(ts)...})
     if (t && t->device() != ref.device())
       throw Bad{"a tensor on " + t->device().str() + " in a call on " + ref.device().str()};
+}
+
+// Host tensors are checked like others, but no kernel may see them.
+uint32_t flags_of(const at::Tensor& K, bool per_head) {
+  return (per_head ? L2KV_TOKENS_LEN_PER_HEAD : 0) | (K.is_cuda() ? 0 : L2KV_TOKENS_NO_LAUNCH);
 }
 
 // V has K's geometry: one set of strides describes both.
@@ -165,7 +176,7 @@ PyObject* rotary_write(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
         static_cast<const double*>(ptr(freq)), freq ? (int32_t)(2 * freq->numel()) : 0, real(v[15]), q_out ? &to : nullptr,
         ptr(K), ptr(V), static_cast<int32_t*>(ptr(idx)), static_cast<float*>(ptr(key)), &a,
         static_cast<const int32_t*>(ptr(start)), static_cast<int32_t*>(ptr(cur)),
-        (per_head ? L2KV_TOKENS_LEN_PER_HEAD : 0) | (interleaved ? L2KV_TOKENS_ROTARY_INTERLEAVED : 0), ptr(ws),
+        flags_of(*K, per_head) | (interleaved ? L2KV_TOKENS_ROTARY_INTERLEAVED : 0), ptr(ws),
         (size_t)ws->numel(), reinterpret_cast<void*>(integer(v[18]))));
   });
 }
@@ -194,7 +205,7 @@ PyObject* tree_commit(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
         ptr(K), ptr(V), static_cast<int32_t*>(ptr(idx)), static_cast<float*>(ptr(key)), &a,
         static_cast<const int32_t*>(ptr(start)), static_cast<const int32_t*>(ptr(cur)), static_cast<const int32_t*>(ptr(path)),
         (int32_t)path->size(1), static_cast<const int32_t*>(ptr(n_path)), static_cast<int32_t*>(ptr(out)),
-        per_head ? L2KV_TOKENS_LEN_PER_HEAD : 0, ptr(ws), (size_t)ws->numel(), reinterpret_cast<void*>(integer(v[12]))));
+        flags_of(*K, per_head), ptr(ws), (size_t)ws->numel(), reinterpret_cast<void*>(integer(v[12]))));
   });
 }
 
@@ -215,9 +226,9 @@ PyObject* attention(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     entries(ws, -1, "workspace", at::kByte);
     const l2kv_tokens tq = tokens(*q, a, n, a.q_heads), to = tokens(*out, a, n, a.q_heads);
     void* stream = reinterpret_cast<void*>(integer(v[13]));
-    const int32_t max_len = (int32_t)integer(v[6]);
+    const int32_t max_len = integer32(v[6], "max_len");
     const float scale = (float)real(v[9]);
-    const uint32_t flags = per_head ? L2KV_TOKENS_LEN_PER_HEAD : 0;
+    const uint32_t flags = flags_of(*K, per_head);
     const size_t ws_bytes = ws ? (size_t)ws->numel() : 0;
     if (!mask)
       return PyLong_FromLong(fn_prompt_attention(
@@ -240,7 +251,7 @@ PyObject* workspace_bytes(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     const at::Tensor *K = tensor(v[0], "K_c"), *q = tensor(v[1], "q");
     const l2kv_layout a = layout(*K, heads_of(*q), v[3]);
     size_t bytes = 0;
-    const int rc = fn_workspace_bytes(&a, (int32_t)q->size(-3), (int32_t)integer(v[2]), &bytes);
+    const int rc = fn_workspace_bytes(&a, (int32_t)q->size(-3), integer32(v[2], "max_len"), &bytes);
     return PyLong_FromLongLong(rc == L2KV_OK ? (long long)bytes : rc);
   });
 }

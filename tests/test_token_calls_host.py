@@ -198,3 +198,22 @@ def test_frequencies_refuse(bad):
     with pytest.raises(l2.L2KVError) as e:
         l2.rotary_frequencies(**dict(dict(rot_dim=64), **bad))
     assert e.value.status == -1
+
+
+@pytest.mark.parametrize("call", [_rotary, _prompt, _tree, _commit])
+def test_host_tensors_that_fit_launch_nothing(call):
+    """A call whose arguments are all in order, but in host memory: no kernel may be given such pointers."""
+    with pytest.raises(l2.L2KVError) as e:
+        call(_inputs())
+    assert e.value.status == -1
+
+
+@pytest.mark.parametrize("max_len", [1 << 31, (1 << 32) + 5, -(1 << 40)])
+def test_lengths_beyond_32_bits_are_refused(max_len):
+    a = _inputs()
+    a["max_len"] = max_len
+    for call in (_prompt, _tree):
+        with pytest.raises(ValueError):
+            call(a)
+    with pytest.raises(ValueError):
+        l2.prompt_attention_workspace_bytes(a["K"], a["q"], max_len)
