@@ -870,56 +870,59 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
 }
 
 // Joins the pieces of items that were cut: out = sum_c w_c O_c / sum_c w_c, w_c = 2^(lse_c - max lse), piece by
-// piece in order.  A block per CTA share and 32 rows of the item that the share's start cuts, a warp per row at
-// a time; an item that several starts cut is the first one's.
+// piece in order.  A block per CTA share and 32 rows of the item that the share's start cuts, eight lanes per row,
+// so that a warp's four rows are loaded together; an item that several starts cut is the first one's.  What it
+// takes is the chain plan - sums - rows of loads.
 constexpr int kTaJoinWarps = 8;
 template <int D>
 __global__ void __launch_bounds__(32 * kTaJoinWarps)
 token_attention_join_kernel(const __grid_constant__ TaArgs A) {
-  constexpr int V = D / 32;
+  constexpr int V = D / 8;                               // columns per lane: four at a time, 32 apart
   const TokenAttention& a = A.a;
   asm volatile("griddepcontrol.wait;" ::: "memory");     // everything of the kernel before is complete and visible
   if (a.status && a.status[2] != 0) return;              // a wait gave up: no output
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = (int)blockIdx.x + 1;
-  const TaSpot s = A.plan[c0];
-  if (s.off == 0 || (A.plan[c0 - 1].at == s.at && A.plan[c0 - 1].off > 0)) return;
+  const int piece = threadIdx.x & 7, r = (int)blockIdx.y * 32 + ((int)threadIdx.x >> 3), c0 = (int)blockIdx.x + 1;
+  const TaSpot s = A.plan[c0], before = A.plan[c0 - 1];
+  if (s.off == 0 || (before.at == s.at && before.off > 0)) return;
   int c1 = c0 + 1;                                       // shares [c0, c1) begin inside the item
   while (c1 < kTaGrid && A.plan[c1].at == s.at && A.plan[c1].off > 0) ++c1;
   const int nc = c1 - c0 + 1;
+  auto row = [&](int c) { return (long long)(c == 0 ? 2 * c0 - 1 : 2 * (c0 + c - 1)) * A.slot_rows + r; };
   const TaItem it = ta_item(A, s.e / a.g.L, s.e % a.g.L, s.p, s.h, 0, INT_MAX, 0);
-  auto slot = [&](int c) { return c == 0 ? 2 * c0 - 1 : 2 * (c0 + c - 1); };
-  const int rows = it.nq * A.G;
-  for (int r = (int)blockIdx.y * 32 + warp; r < min(rows, (int)blockIdx.y * 32 + 32); r += kTaJoinWarps) {
-    float top = -INFINITY;
-    for (int c = lane; c < nc; c += 32) top = fmaxf(top, A.part_lse[(long long)slot(c) * A.slot_rows + r]);
-#pragma unroll
-    for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    const float low = top == -INFINITY ? 0.f : top;
-    float den = 0.f, num[V] = {};
+  if (r >= it.nq * A.G) return;
+  float top = -INFINITY;
 #pragma unroll 4
-    for (int c = 0; c < nc; ++c) {
-      const long long at = (long long)slot(c) * A.slot_rows + r;
-      const float lse2 = A.part_lse[at];
-      const float w = lse2 == -INFINITY ? 0.f : exp2f(lse2 - low);
-      den += w;
-      float x[V];
-      if constexpr (V == 4) *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(A.part + at * D + lane * V);
-      else *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(A.part + at * D + lane * V);
+  for (int c = 0; c < nc; ++c) top = fmaxf(top, A.part_lse[row(c)]);
+  const float low = top == -INFINITY ? 0.f : top;
+  float den = 0.f, num[V] = {};
+#pragma unroll 2
+  for (int c = 0; c < nc; ++c) {
+    const float lse2 = A.part_lse[row(c)];
+    const float w = lse2 == -INFINITY ? 0.f : exp2f(lse2 - low);
+    const float4* const from = reinterpret_cast<const float4*>(A.part + row(c) * D) + piece;
+    float4 x[V / 4];
 #pragma unroll
-      for (int e = 0; e < V; ++e) num[e] = w == 0.f ? num[e] : fmaf(w, x[e], num[e]);
+    for (int i = 0; i < V / 4; ++i) x[i] = from[8 * i];
+    den += w;
+    if (w == 0.f) continue;                              // (rows of a piece that sees nothing are zeros)
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) {
+      num[4 * i] = fmaf(w, x[i].x, num[4 * i]);
+      num[4 * i + 1] = fmaf(w, x[i].y, num[4 * i + 1]);
+      num[4 * i + 2] = fmaf(w, x[i].z, num[4 * i + 2]);
+      num[4 * i + 3] = fmaf(w, x[i].w, num[4 * i + 3]);
     }
-    const float inv = den == 0.f ? 0.f : 1.f / den;
-    const int tok = it.tok0 + r / A.G, head = it.h * A.G + r % A.G;
-    uint32_t y[V / 2];
-#pragma unroll
-    for (int e = 0; e < V; e += 2) y[e / 2] = pack_bf16(num[e] * inv, num[e + 1] * inv);
-    uint32_t* to = reinterpret_cast<uint32_t*>(a.out.row<__nv_bfloat16>(it.l, tok, head)) + lane * (V / 2);
-    if constexpr (V == 4) *reinterpret_cast<uint2*>(to) = make_uint2(y[0], y[1]);
-    else *to = y[0];
-    if (a.lse && lane == 0)
-      a.lse[((long long)it.l * a.n_tokens + tok) * a.g.Hq + head] =
-          den == 0.f ? -INFINITY : (top + log2f(den)) * 0.6931471805599453f;
   }
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  const int tok = it.tok0 + r / A.G, head = it.h * A.G + r % A.G;
+  uint2* const to = reinterpret_cast<uint2*>(a.out.row<__nv_bfloat16>(it.l, tok, head)) + piece;
+#pragma unroll
+  for (int i = 0; i < V / 4; ++i)
+    to[8 * i] = make_uint2(pack_bf16(num[4 * i] * inv, num[4 * i + 1] * inv),
+                           pack_bf16(num[4 * i + 2] * inv, num[4 * i + 3] * inv));
+  if (a.lse && piece == 0)
+    a.lse[((long long)it.l * a.n_tokens + tok) * a.g.Hq + head] =
+        den == 0.f ? -INFINITY : (top + log2f(den)) * 0.6931471805599453f;
 }
 
 // ---- host ------------------------------------------------------------------------------------------
