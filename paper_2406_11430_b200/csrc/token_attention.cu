@@ -339,11 +339,6 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   extern __shared__ __align__(1024) unsigned char smem[];
   const TokenAttention& a = A.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  // the joining kernel may be set up now; it waits for this one's results by itself
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  // A wait that gave up in an earlier call marks the workspace; nothing runs until it is cleared.
-  if (a.status && *reinterpret_cast<volatile int32_t*>(a.status + 2) != 0) return;
-
   const uint32_t base = smem_u32(smem);
   const uint32_t s_q = base, s_k = base + 2 * QTILE, s_v = s_k + SLOTS * TILE;
   unsigned char* const stage_base = smem + 2 * QTILE + 2 * SLOTS * TILE;
@@ -352,6 +347,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   TaItem* const items = reinterpret_cast<TaItem*>(ctrl + 512);            // [2]
   volatile int* const s_fail = reinterpret_cast<volatile int*>(ctrl + 768);
   uint32_t* const s_tmem = reinterpret_cast<uint32_t*>(ctrl + 772);
+  volatile int* const s_marked = reinterpret_cast<volatile int*>(ctrl + 776);
   volatile int* const s_turn = reinterpret_cast<volatile int*>(ctrl + 896);   // [2][4]: exponentials done, by chain and lane quarter
   float2* const s_stat = reinterpret_cast<float2*>(ctrl + 1024);          // [2][128]: maximum, sum
   auto k_full = [&](uint32_t at) { return bars + 8u * (at % SLOTS); };
@@ -371,11 +367,6 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   const uint32_t issued = more + 184u;
   auto drained = [&](int c) { return more + 168u + 8u * (uint32_t)c; };
 
-  if (warp == 0) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                 :: "r"(smem_u32(s_tmem)), "r"(512) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
   if (tid == 0) {
     // a tile and the query rows are given back once per chain
     for (int i = 0; i < SLOTS; ++i) {
@@ -395,15 +386,24 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
     for (int i = 0; i < 8; ++i) s_turn[i] = 0;
   }
   __syncwarp();
+  if (warp == 9 && lane < 3) {
+    const CUtensorMap* const map = lane == 0 ? &map_q : lane == 1 ? &map_k : &map_v;
+    asm volatile("prefetch.tensormap [%0];" :: "l"(map) : "memory");
+  }
+  __syncwarp();
+  wait_for_previous();
+  // (tensor memory is taken behind the kernel before, which may need it, and before the next one may start)
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 :: "r"(smem_u32(s_tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // A wait that gave up in an earlier call marks the workspace; nothing runs until it is cleared.
+  if (tid == 32) *s_marked = a.status ? *reinterpret_cast<volatile int32_t*>(a.status + 2) : 0;
   // (while the others set up) where this CTA's share of the work begins and ends
   TaSpot spot{0, 0, 0, 0, 0}, end{0, 0, 0, 0, 0};
   bool one_each = false;
   if (warp == 9) {
-    if (lane < 3) {
-      const CUtensorMap* const map = lane == 0 ? &map_q : lane == 1 ? &map_k : &map_v;
-      asm volatile("prefetch.tensormap [%0];" :: "l"(map) : "memory");
-    }
-    __syncwarp();
     one_each = ta_small_call(A, spot, end);
     if (!one_each) {
       const TaShares shares(A);
@@ -420,6 +420,12 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
+  auto free_tmem = [&]() {
+    if (warp == 0)
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512) : "memory");
+  };
+  next_may_start();
+  if (*s_marked) { free_tmem(); return; }
   // A wait that another role's failure ends too.
   auto wait = [&](uint32_t bar, uint32_t parity) {
     if (mbar_test(bar, parity)) return true;
@@ -865,8 +871,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   if (*s_fail && tid == 0) record_timeout(a.status);
   tc_fence_before();
   __syncthreads();
-  if (warp == 0)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512) : "memory");
+  free_tmem();
 }
 
 // Joins the pieces of items that were cut: out = sum_c w_c O_c / sum_c w_c, w_c = 2^(lse_c - max lse), piece by
@@ -879,7 +884,8 @@ __global__ void __launch_bounds__(32 * kTaJoinWarps)
 token_attention_join_kernel(const __grid_constant__ TaArgs A) {
   constexpr int V = D / 8;                               // columns per lane: four at a time, 32 apart
   const TokenAttention& a = A.a;
-  asm volatile("griddepcontrol.wait;" ::: "memory");     // everything of the kernel before is complete and visible
+  next_may_start();
+  wait_for_previous();
   if (a.status && a.status[2] != 0) return;              // a wait gave up: no output
   const int piece = threadIdx.x & 7, r = (int)blockIdx.y * 32 + ((int)threadIdx.x >> 3), c0 = (int)blockIdx.x + 1;
   const TaSpot s = A.plan[c0], before = A.plan[c0 - 1];
@@ -973,22 +979,10 @@ static int launch_ta(const TaArgs& A, const void* K, const void* V, long long it
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTaSmem<D>) != cudaSuccess)
     return L2KV_ERR_CUDA;
   const unsigned grid = (unsigned)std::min<long long>(kTaGrid, A.plan ? kTaGrid : items);
-  kern<<<grid, kTaThreads, kTaSmem<D>, s>>>(A, map_q, map_k, map_v);
-  if (cudaGetLastError() != cudaSuccess) return L2KV_ERR_CUDA;
-  if (A.plan) {
-    // (set up while the kernel before it runs: a small call would wait for this launch otherwise)
-    cudaLaunchAttribute early{};
-    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    early.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(kTaGrid - 1, (unsigned)(A.slot_rows / 32));
-    cfg.blockDim = dim3(32 * kTaJoinWarps);
-    cfg.stream = s;
-    cfg.attrs = &early;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, token_attention_join_kernel<D>, A) != cudaSuccess) return L2KV_ERR_CUDA;
-  }
-  return L2KV_OK;
+  const int rc = launch_early(kern, dim3(grid), kTaThreads, kTaSmem<D>, s, A, map_q, map_k, map_v);
+  if (rc != L2KV_OK || !A.plan) return rc;
+  return launch_early(token_attention_join_kernel<D>, dim3(kTaGrid - 1, (unsigned)(A.slot_rows / 32)), 32 * kTaJoinWarps, 0,
+                      s, A);
 }
 
 int launch_token_attention(const TokenAttention& a, const void* K, const void* V, int dtype, char* scratch,

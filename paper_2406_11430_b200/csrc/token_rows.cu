@@ -96,6 +96,8 @@ rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* __restrict__ K, T* 
   __shared__ float2 s_turn[kRotaryWarps][D / 2];
   const Geom& g = a.g;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane % LPR;
+  next_may_start();
+  wait_for_previous();
   const unsigned n_rows = (unsigned)a.n_tokens * (unsigned)g.L, token_blocks = (n_rows + TPB - 1) / TPB;
   if (blockIdx.x >= token_blocks) {
     // trailing blocks: the new lengths (sequences without new tokens have one too)
@@ -221,8 +223,8 @@ static int launch_rw(const RotaryArgs& a, void* K, void* V, cudaStream_t s) {
   const long long units = (long long)a.g.B * a.g.L * (a.per_head ? a.g.H : 1);
   const long long blocks = ((long long)a.n_tokens * a.g.L + TPB - 1) / TPB + (units + kRotaryThreads - 1) / kRotaryThreads;
   if (blocks * TPB > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
-  rotary_write_kernel<T, D, WPT, PAIRS><<<(unsigned)blocks, kRotaryThreads, 0, s>>>(a, static_cast<T*>(K), static_cast<T*>(V));
-  return cudaGetLastError() == cudaSuccess ? L2KV_OK : L2KV_ERR_CUDA;
+  return launch_early(rotary_write_kernel<T, D, WPT, PAIRS>, dim3((unsigned)blocks), kRotaryThreads, 0, s, a,
+                      static_cast<T*>(K), static_cast<T*>(V));
 }
 // One warp per token where that alone fills the GPU (148 SMs, 16 warps each), else a block per token.
 template <typename T, int D>
@@ -263,6 +265,8 @@ tree_commit_kernel(T* __restrict__ K, T* __restrict__ V, int32_t* __restrict__ i
   const int b = (int)(bl / g.L), l = (int)(bl % g.L);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane % LPR;
   const int32_t* p = path + (long long)b * path_cap;
+  next_may_start();
+  wait_for_previous();
   const int first = lane < path_cap ? p[lane] : 0;       // (asked for before n_path is known)
   const int want = max(0, min(n_path[b], path_cap)), cap = g.cap(bl);
   int len = 0;                                           // of the last head this warp took
@@ -331,10 +335,8 @@ static int launch_tc(void* K, void* V, int32_t* idx, float* sumsq, const Geom& g
                      int32_t* len_out, int per_head, int32_t* status, cudaStream_t s) {
   const long long blocks = (long long)g.B * g.L;
   if (blocks > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
-  tree_commit_kernel<T, D><<<(unsigned)blocks, 32 * kCommitWarps, 0, s>>>(
-      static_cast<T*>(K), static_cast<T*>(V), idx, sumsq, g, start, cur, path, path_cap, n_path, len_out,
-      per_head, status);
-  return cudaGetLastError() == cudaSuccess ? L2KV_OK : L2KV_ERR_CUDA;
+  return launch_early(tree_commit_kernel<T, D>, dim3((unsigned)blocks), 32 * kCommitWarps, 0, s, static_cast<T*>(K),
+                      static_cast<T*>(V), idx, sumsq, g, start, cur, path, path_cap, n_path, len_out, per_head, status);
 }
 
 int launch_tree_commit(void* K, void* V, int32_t* idx, float* sumsq, const Geom& g, int dtype,

@@ -44,6 +44,28 @@ __device__ __forceinline__ int sequence_of(const int32_t* tok_off, int B, int n_
   return -1;
 }
 
+// These calls follow one another step after step, most of them for a few microseconds, so a kernel may be set
+// up on the SMs while the one before it in the stream runs: it is launched with launch_early, says at its start
+// that the next one may do the same, and waits for everything before it -- complete, and visible -- before its first
+// access to global memory.  A kernel that is launched without asking for this waits as always.
+__device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... P, typename... A>
+inline int launch_early(void (*kern)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, A&&... args) {
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<A&&>(args)...) == cudaSuccess ? L2KV_OK : L2KV_ERR_CUDA;
+}
+
 int launch_rotary_write(const TokView& q, const TokView& k, const TokView& v, const TokView& q_out,
                         const int32_t* tok_off, int n_tokens, const int32_t* pos, const double* freq,
                         int rot_dim, double scale, int interleaved, void* K, void* V, int32_t* idx,

@@ -173,3 +173,61 @@ def test_captured_writes_and_commits_with_other_lengths(l2):
             have[b] += len(p)
         assert start.flatten().tolist() == have
     assert l2.read_device_status(ws) == 0
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_calls_wait_for_whatever_is_before_them(l2, captured):
+    """A call may be set up while the work before it runs, but reads and writes only behind it: large copies, fills,
+    other streams' kernels and the calls themselves, eager and in one graph."""
+    c = Case(l2, [30, 200], [[300], [100]], 1, 2, 4, 128, seed=9, room=8192)
+    meta, freq = c.meta, l2.rotary_frequencies(128)[0].to(DEV)
+    idx, key = torch.zeros(meta, dtype=torch.int32, device=DEV), torch.zeros(meta, device=DEV)
+    start, cur, kept = c.lens(c.ctx), c.lens(c.cur), c.lens(c.ctx)
+    pos, path, n_path = torch.arange(c.N, dtype=torch.int32, device=DEV), i32([[1, 5, 8], [0, 100, 150]]), i32([3, 3])
+    K, V = torch.zeros_like(c.K), torch.zeros_like(c.V)
+    q, out, out2 = (c.empty_out() for _ in range(3))
+    ws = torch.zeros(l2.prompt_attention_workspace_bytes(K, q, c.max_len), dtype=torch.uint8, device=DEV)
+    big = torch.zeros(1 << 27, device=DEV)
+    host_off, other = c.tok_off.cpu().pin_memory(), torch.cuda.Stream()
+    off, lens, work = torch.zeros_like(c.tok_off), torch.zeros_like(start), torch.zeros_like(start)
+
+    def step():
+        big.fill_(1.0)                                       # half a gigabyte, so that what follows is all queued up
+        K.copy_(c.K), V.copy_(c.V)
+        off.copy_(host_off, non_blocking=True)
+        lens.zero_()
+        l2.rotary_write(c.q, c.k, c.v, off, pos, freq, q, K, V, idx, key, start, lens, ws)
+        l2.prompt_attention(q, off, K, V, lens, c.max_len, out, workspace=ws)
+        l2.tree_commit(K, V, idx, key, start, lens, path, n_path, kept, ws)
+        here = torch.cuda.current_stream()
+        other.wait_stream(here)
+        with torch.cuda.stream(other):
+            big.mul_(2.0)
+            work.copy_(kept)
+            work.add_(torch.tensor([[27], [197]], dtype=torch.int32, device=DEV) if not captured else add)
+        here.wait_stream(other)
+        l2.prompt_attention(q, off, K, V, work, c.max_len, out2, workspace=ws)      # the 3 kept rows as context
+    add = i32([[27], [197]])
+    step()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in (out, out2, q, kept)]
+    check_q = Case(l2, [30, 200], [[300], [100]], 1, 2, 4, 128, seed=9, room=8192)
+    check_q.q, check_q.K, check_q.V = q, c.K.clone(), c.V.clone()
+    l2.rotary_write(c.q, c.k, c.v, c.tok_off, pos, freq, torch.empty_like(q), check_q.K, check_q.V, None, None, start, cur, ws)
+    torch.cuda.synchronize()
+    check_attention(check_q, out, None, causal(c))
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        run = graph.replay
+    else:
+        run = step
+    for _ in range(10):
+        for x in (out, out2, q, K, V):
+            x.zero_()
+        kept.zero_(), off.zero_(), lens.zero_()
+        run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (out, out2, q, kept)))
+    assert l2.read_device_status(ws) == 0
