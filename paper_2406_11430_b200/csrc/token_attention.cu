@@ -345,6 +345,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   unsigned char* const ctrl = stage_base + 8 * kTaStage;
   const uint32_t bars = smem_u32(ctrl);
   TaItem* const items = reinterpret_cast<TaItem*>(ctrl + 512);            // [2]
+  TaSpot* const s_end = reinterpret_cast<TaSpot*>(ctrl + 640);
   volatile int* const s_fail = reinterpret_cast<volatile int*>(ctrl + 768);
   uint32_t* const s_tmem = reinterpret_cast<uint32_t*>(ctrl + 772);
   volatile int* const s_marked = reinterpret_cast<volatile int*>(ctrl + 776);
@@ -400,21 +401,21 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   }
   // A wait that gave up in an earlier call marks the workspace; nothing runs until it is cleared.
   if (tid == 32) *s_marked = a.status ? *reinterpret_cast<volatile int32_t*>(a.status + 2) : 0;
-  // (while the others set up) where this CTA's share of the work begins and ends
-  TaSpot spot{0, 0, 0, 0, 0}, end{0, 0, 0, 0, 0};
+  // (while the others set up) where this CTA's share of the work begins (warp 9) and ends (warp 10)
+  TaSpot spot{0, 0, 0, 0, 0};
   bool one_each = false;
-  if (warp == 9) {
+  if (warp == 9 || warp == 10) {
+    TaSpot end;
     one_each = ta_small_call(A, spot, end);
     if (!one_each) {
       const TaShares shares(A);
-#pragma unroll 1                                         // (the second time its instructions are at hand)
-      for (int k = 0; k < 2; ++k) {
-        spot = end;
-        end = shares.begin(blockIdx.x + k);
-      }
+      spot = end = shares.begin((int)blockIdx.x + (warp == 10));
       one_each = shares.one_each;
     }
-    if (A.plan && lane == 0) A.plan[blockIdx.x] = spot;
+    if (lane == 0) {
+      if (warp == 10) *s_end = end;
+      else if (A.plan) A.plan[blockIdx.x] = spot;
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -474,6 +475,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   if (warp == 9) {
     // ---- items and tiles ---------------------------------------------------------------------------
     const int QP = 2 * A.QT, L = a.g.L;
+    const TaSpot end = *s_end;
     bool ok = true;
     uint32_t n_pub = 0, n_q = 0;
     while (ok) {
