@@ -22,8 +22,8 @@
 // its operands' way out of shared memory; P V 64), and a sub-block takes about 1650: the exponentials of one
 // chain take 660 with the pipe to themselves, and the chains hand them to each other in turn.  Long prompts
 // run into the GPU's power limit besides: 16 k tokens, 32 heads of 128, take 1.75 ms at 1965 MHz and
-// 1.95 to 2.0 ms (1110 to 1130 TFLOP/s) at the 1600 MHz that are left after a while.  Tree batches that fit one tile
-// are bound by memory (98 us for 478 MB, of which 79 us stream).
+// 1.97 ms (1117 TFLOP/s) at the 1570 MHz that are left after a while; ragged prompts to 2048 0.31 ms (850 TFLOP/s).
+// Tree batches that fit one tile are bound by memory (88 us for 478 MB, 74 at the copy rate).
 // Tried, correct and not faster: blocks of 128 rows with one score tile per chain (products at N = 128, 10 to
 // 20 % slower: the chain softmax - product - softmax has no slack), two softmax warps for the same 32 rows,
 // a share of the exponentials as a polynomial on the FMA pipe (any share from 1/8 to 1/2), no maxima after the
@@ -47,7 +47,9 @@ constexpr int kTaGrid = 148;                    // one CTA per SM (512 tensor-me
 constexpr int kTaCtrl = 1024 + 2 * kTaRows * 8;  // barriers and items; row statistics
 constexpr int kTaPolls = 18;                    // log2 of the polls a wait may take
 constexpr int kTaItemCost = 4;                  // what starting and finishing an item costs, in sub-blocks
-constexpr int kTaMinShare = 24;                 // items that cost less on average are not cut
+constexpr int kTaMinShare = 12;                 // no shorter shares where items are cut, in sub-blocks
+constexpr int kTaJoinCost = 12;                 // what cutting items costs a call, in sub-blocks
+constexpr int kTaWholeLen = 1216;               // caches up to this length are never cut
 constexpr int kTaGroup = 4;                     // pairs of weights whose exponentials go side by side
 constexpr float kTaRescaleGap = 8.f;            // log2 units a maximum may drift before O is rescaled
 
@@ -133,8 +135,8 @@ struct TaSpot {
 };
 
 // The shares of the CTAs: stretches of the list that cost the same.  Where a share ends inside an item the item
-// is cut, unless items are short on average or there is no room for partial results: then the share ends with
-// the item.  One warp; the first 32 entries stay in registers.
+// is cut, unless there is no room for partial results or cutting would not pay: then the share ends with the
+// item.  One warp; the first 32 entries stay in registers.
 struct TaShares {
   const TaArgs& A;
   TaEntry mine;                // entry number `lane`
@@ -158,19 +160,35 @@ struct TaShares {
     mine = lane < entries ? ta_plan_entry(A.a, lane) : TaEntry{0, 0, 0};
     one_each = false;
     long long sum = 0;
-    int items = 0;
+    int items = 0, longest = 0;
     for (int e0 = 0; e0 < entries; e0 += 32) {
       const TaEntry e = entry(e0);
       sum += cost_of(e);
       items += (e.n + QP - 1) / QP;
+      if (e.n > 0) longest = max(longest, ta_subs(e.cur) + kTaItemCost);
     }
 #pragma unroll
     for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
     items = (int)__reduce_add_sync(0xffffffffu, (unsigned)items) * A.a.g.H;
-    cut = A.plan && sum >= (long long)items * kTaMinShare;
-    one_each = !cut && items <= (int)gridDim.x;
-    share = cut ? max((long long)kTaMinShare, (sum + gridDim.x - 1) / gridDim.x)
-                : one_each ? 1 : (sum + gridDim.x - 1) / gridDim.x;
+    longest = (int)__reduce_max_sync(0xffffffffu, (unsigned)longest);
+    const int grid = (int)gridDim.x;
+    const long long fair = (sum + grid - 1) / grid;
+    share = fair;
+    cut = false;
+    if (A.plan) {
+      // With an item each at most, the longest one decides, or, where that is more, memory: with all SMs at it a
+      // sub-block takes 0.77 us instead of 0.57.  Cut, it is the share or memory, and the partial rows and their
+      // joining.  (8 heads of trees of 12 to 24 tokens, whole / cut in us: 1 tree behind 1.1k rows 16.4 / 19.7,
+      // 3k 34 / 21, 16k 136 / 35; 16 trees behind 3k 42 / 48, 16k 175 / 177; 12 trees behind 3k 39 / 41, 16k
+      // 147 / 136.)  With more items shares end up to half an item late, or, at equal lengths, after a number of
+      // items.  (24 trees behind 1.1k 40 / 36, 16k 319 / 258; a prompt of 2k tokens 65 / 52; 32 pieces of 128 tokens
+      // behind 2k 159 / 160.)
+      const long long memory = fair * 27 / 20, least = max((long long)kTaMinShare, fair);
+      cut = items <= grid ? max((long long)longest, memory) > max(least, memory) + kTaJoinCost
+                          : max(longest / 2ll, (items + grid - 1) / grid * (sum / items) - fair) > kTaJoinCost * 3 / 4;
+      if (cut) share = least;
+    }
+    if (!cut && items <= grid) { one_each = true; share = 1; }
   }
   // The next item of the list.
   __device__ __forceinline__ void next(TaSpot& s, long long cost, int n_tokens) const {
@@ -945,7 +963,7 @@ constexpr size_t kTaPlanBytes = (kTaGrid * sizeof(TaSpot) + 255) / 256 * 256;
 static TaRoom ta_room(const Geom& g, int n_tokens, int max_len) {
   const int G = g.Hq / g.H, QP = 2 * (kTaRows / G);
   TaRoom r{((long long)n_tokens / QP + std::min(g.B, n_tokens)) * g.L * g.H, 0, 0};
-  if (max_len > (kTaMinShare - kTaItemCost - 1) * kTaSub) {
+  if (max_len > kTaWholeLen) {
     r.slot_rows = (long long)n_tokens * G <= kTaRows ? kTaRows : 2 * kTaRows;
     r.bytes = kTaPlanBytes + (size_t)2 * kTaGrid * r.slot_rows * (g.D + 1) * sizeof(float);
   }
