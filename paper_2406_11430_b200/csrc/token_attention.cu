@@ -953,7 +953,7 @@ token_attention_join_kernel(const __grid_constant__ TaArgs A) {
 
 // ---- host ------------------------------------------------------------------------------------------
 
-// Room for the pieces of items that are cut; none where no item can be long enough to be (see ta_plan).
+// Room for the pieces of items that are cut; none where caches are too short for it to pay.
 struct TaRoom {
   long long items;        // at most
   int slot_rows;          // 0: items are never cut
