@@ -41,7 +41,7 @@ constexpr int kTaRows = 128;                    // query rows per tile, cached r
 constexpr int kTaSub = 64;                      // cached rows per sub-block: one K tile, one V tile
 constexpr int kTaHalf = kTaRows * 128;          // query rows, [128][64 bf16], swizzled: 16 KB
 constexpr int kTaSubHalf = kTaSub * 128;        // cached rows, [64][64 bf16]: 8 KB
-constexpr int kTaStage = 4096;                  // bytes per softmax warp on the way out
+constexpr int kTaStage = 2048;                  // bytes per softmax warp on the way out
 constexpr int kTaThreads = 352;                 // 2 x 4 softmax warps, issuing warps 8 and 10, fetching warp 9
 constexpr int kTaGrid = 148;                    // one CTA per SM (512 tensor-memory columns each)
 constexpr int kTaCtrl = 1024 + 2 * kTaRows * 8;  // barriers and items; row statistics
@@ -307,31 +307,33 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
 // The lowest x bits.
 __device__ __forceinline__ uint32_t low_bits(int x) { return x >= 32 ? 0xffffffffu : x <= 0 ? 0u : (1u << x) - 1u; }
 
-// The way out: columns of this warp's 32 rows, one row per lane, through 4 KB of shared memory, so that a store
-// instruction fills whole sectors of a few rows (a thread that stored its own row would put 16 bytes into each
-// of 32 different lines).  bf16: 64 columns at a time, 4 rows of 128 bytes per instruction; fp32: 32.  Lane i
-// then holds piece i & 7 of the rows 4 k + (i >> 3), whose addresses it asks their owners for once.
+// The way out: columns of this warp's 32 rows, one row per lane, through 2 KB of shared memory, so that a store
+// instruction fills whole sectors of eight rows (a thread that stored its own row would put 16 bytes into each
+// of 32 different lines).  64 bytes of each row at a time: lane i holds piece i & 3 of the rows 8 k + (i >> 2), whose
+// addresses it asks their owners for once.
 struct TaRows {
-  char* to[8];                                           // null: no such row
+  char* to[4];                                           // null: no such row
   __device__ __forceinline__ explicit TaRows(void* own) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      to[k] = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own), 4 * k + (lane >> 3)));
-  }
-  // pieces[i]: bytes [16 i, 16 i + 16) of the lane's own 128
-  __device__ __forceinline__ void store(const uint4 (&pieces)[8], int byte, uint4* stage) const {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) stage[lane * 8 + (i ^ (lane & 7))] = pieces[i];
-    __syncwarp();
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int r = 4 * k + (lane >> 3);
-      const uint4 x = stage[r * 8 + ((lane & 7) ^ (r & 7))];
-      if (to[k]) reinterpret_cast<uint4*>(to[k] + byte)[lane & 7] = x;
+    for (int k = 0; k < 4; ++k) {
+      char* const row = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(own), 8 * k + (lane >> 2)));
+      to[k] = row ? row + (lane & 3) * 16 : row;
     }
+  }
+  // pieces[i]: bytes [16 i, 16 i + 16) of the lane's own 64
+  __device__ __forceinline__ void store(const uint4 (&pieces)[4], int byte, uint4* stage) const {
+    const int lane = threadIdx.x & 31;
     __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) stage[lane * 4 + (i ^ (lane >> 1 & 3))] = pieces[i];
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = 8 * k + (lane >> 2);
+      const uint4 x = stage[r * 4 + ((lane & 3) ^ (r >> 1 & 3))];
+      if (to[k]) *reinterpret_cast<uint4*>(to[k] + byte) = x;
+    }
   }
 };
 
@@ -832,14 +834,12 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       f1 *= inv;
       if (warp_valid) {
         const TaRows rows(it.slot >= 0 ? static_cast<void*>(part) : static_cast<void*>(out));
-        // columns [c, c + 32) of the result
-        auto columns = [&](int c, float (&v)[32]) {
-          if (!any) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = 0.f;
-            return;
-          }
+        // 32 columns at a time, in a loop that stays one: this is run once per item, and what it takes is the fetching
+        // of its instructions (unrolled: 3300 cycles per item, of 6400 that an item costs beyond its sub-blocks)
+#pragma unroll 1
+        for (int c = c_lo; c < c_hi; c += 32) {
           uint32_t x[32];
+          float v[32];
           tmem_ld32((it.pair ? t_o : t_o0) + c, x);
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(x[i]) * f0;
@@ -848,29 +848,25 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = __fmaf_rn(__uint_as_float(x[i]), f1, v[i]);
           }
-        };
-        for (int c = c_lo; c < c_hi; c += 64) {
-          uint4 pieces[8];
-          float v[32];
-          if (it.slot >= 0) {
-#pragma unroll 1
-            for (int d = c; d < min(c + 64, c_hi); d += 32) {
-              columns(d, v);
+          if (!any) {                                    // (tensor memory holds whatever it held)
 #pragma unroll
-              for (int i = 0; i < 8; ++i)
-                pieces[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
-                                       __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
-              rows.store(pieces, d * 4, stage);
+            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+          }
+          uint4 pieces[4];
+          if (it.slot >= 0) {
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                pieces[i] = make_uint4(__float_as_uint(v[16 * d + 4 * i]), __float_as_uint(v[16 * d + 4 * i + 1]),
+                                       __float_as_uint(v[16 * d + 4 * i + 2]), __float_as_uint(v[16 * d + 4 * i + 3]));
+              rows.store(pieces, c * 4 + 64 * d, stage);
             }
           } else {
 #pragma unroll
-            for (int d = 0; d < 2; ++d) {
-              columns(c + 32 * d, v);
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                pieces[4 * d + i] = make_uint4(pack_bf16(v[8 * i], v[8 * i + 1]), pack_bf16(v[8 * i + 2], v[8 * i + 3]),
-                                               pack_bf16(v[8 * i + 4], v[8 * i + 5]), pack_bf16(v[8 * i + 6], v[8 * i + 7]));
-            }
+            for (int i = 0; i < 4; ++i)
+              pieces[i] = make_uint4(pack_bf16(v[8 * i], v[8 * i + 1]), pack_bf16(v[8 * i + 2], v[8 * i + 3]),
+                                     pack_bf16(v[8 * i + 4], v[8 * i + 5]), pack_bf16(v[8 * i + 6], v[8 * i + 7]));
             rows.store(pieces, c * 2, stage);
           }
         }
