@@ -834,8 +834,9 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       f1 *= inv;
       if (warp_valid) {
         const TaRows rows(it.slot >= 0 ? static_cast<void*>(part) : static_cast<void*>(out));
-        // 32 columns at a time, in a loop that stays one: this is run once per item, and what it takes is the fetching
-        // of its instructions (unrolled: 3300 cycles per item, of 6400 that an item costs beyond its sub-blocks)
+        // 32 columns at a time, in a loop that stays one: unrolled, the kernel spilled (a prompt of 2k tokens 66 us
+        // instead of 56).  An item costs about 6000 cycles beyond its sub-blocks, 3600 of them here; exchanging pieces
+        // by shuffles instead of shared memory, or two columns per instruction, changed nothing.
 #pragma unroll 1
         for (int c = c_lo; c < c_hi; c += 32) {
           uint32_t x[32];
