@@ -389,8 +389,9 @@ int l2kv_rotary_write(const l2kv_tokens* q, const l2kv_tokens* k, const l2kv_tok
  *   out[l,i,j,:] = sum_t softmax_t( scale * q[l,i,j,:] . K_c[b,l,j/G,t,:] ) * V_c[b,l,j/G,t,:]
  * out is in the cache's dtype; lse_out (may be NULL) is dense fp32 [layers, n_tokens, q_heads], the
  * natural-log sum of exponentials of the scaled scores.  A token that sees no row gives zeros and
- * -inf.  Rows that no token of the call may see can hold anything, NaN included; a
- * non-finite value that one token may see can also reach tokens near it that may not.
+ * -inf.  Rows at or beyond cur_len_dev can hold anything, NaN included.  Before it, keys a token does not see do
+ * not matter to it, whatever they hold; a non-finite VALUE among the sequence's new rows can reach its other new
+ * tokens too (bf16 caches: a weight of zero times it).
  * bf16 caches: products are exact, sums fp32, the softmax weights are rounded to bf16 before they
  * multiply V and the result is rounded once more to bf16.  fp32 caches: fp32 throughout (a path for
  * correctness, on the CUDA cores).  head_dim 64 and 128; every row address of K_c, V_c and (bf16) q

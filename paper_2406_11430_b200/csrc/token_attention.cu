@@ -1004,7 +1004,7 @@ static int launch_ta(const TaArgs& A, const void* K, const void* V, long long it
 
 int launch_token_attention(const TokenAttention& a, const void* K, const void* V, int dtype, char* scratch,
                            size_t scratch_bytes, cudaStream_t s) {
-  if (dtype != L2KV_BF16) return launch_token_attention_simple(a, K, V, s);
+  if (dtype != L2KV_BF16) return launch_token_attention_fp32(a, K, V, s);
   const TaRoom room = ta_room(a.g, a.n_tokens, a.max_len);
   if (room.items > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
   TaArgs A{};

@@ -92,6 +92,6 @@ struct TokenAttention {
 size_t token_attention_scratch(const Geom& g, int dtype, int n_tokens, int max_len);
 int launch_token_attention(const TokenAttention& a, const void* K, const void* V, int dtype, char* scratch,
                            size_t scratch_bytes, cudaStream_t s);
-int launch_token_attention_simple(const TokenAttention& a, const void* K, const void* V, cudaStream_t s);
+int launch_token_attention_fp32(const TokenAttention& a, const void* K, const void* V, cudaStream_t s);
 
 }  // namespace l2kv

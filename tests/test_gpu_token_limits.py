@@ -231,3 +231,37 @@ def test_calls_wait_for_whatever_is_before_them(l2, captured):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, (out, out2, q, kept)))
     assert l2.read_device_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_keys_that_a_token_does_not_see_may_be_anything(l2, dtype):
+    c = Case(l2, [40, 7], [[200], [30]], 1, 2, 4, 128, dtype, seed=14)
+    cur = c.lens(c.cur)
+    trees = [torch.tril(torch.ones((m, m), dtype=torch.bool)) for m in c.n]
+    for t in trees:
+        t[:, 3] = False                                      # nobody sees the fourth new row, itself included
+    mask = mask_words(c, trees)
+
+    def both():
+        a, b = c.empty_out(), c.empty_out()
+        l2.tree_attention(c.q, c.tok_off, mask, c.K, c.V, cur, c.max_len, a)
+        l2.prompt_attention(c.q, c.tok_off, c.K, c.V, cur, c.max_len, b)
+        torch.cuda.synchronize()
+        return a, b
+    tree, causal_out = both()
+    check_attention(c, tree, None, trees)
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        saved = c.K.clone(), c.V.clone()
+        for b, m in enumerate(c.n):
+            for h in range(2):
+                at = int(c.ctx[b, 0, h]) + 3
+                c.K[b, 0, h, at] = bad
+                if dtype == "fp32":
+                    c.V[b, 0, h, at] = bad
+                c.K[b, 0, h, int(c.cur[b, 0, h]) - 1] = bad       # and the last token's own
+        got, got_causal = both()
+        for b, m in enumerate(c.n):
+            first = int(c.off[b])
+            assert torch.equal(got[:, first:first + m - 1], tree[:, first:first + m - 1])
+            assert torch.equal(got_causal[:, first:first + 3], causal_out[:, first:first + 3])   # tokens before the bad row
+        c.K, c.V = saved
