@@ -88,7 +88,7 @@ __device__ __forceinline__ void cos_sin(double a, double* c, double* s) {
 // WPT: warps that share a token.  PAIRS: interleaved pairs.
 template <typename T, int D, int WPT, bool PAIRS>
 __global__ void __launch_bounds__(kRotaryThreads, 3)
-rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* __restrict__ K, T* __restrict__ V) {
+rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* K, T* V) {
   constexpr int EPV = Elem<T>::kPerVec, LPR = D / EPV, RPW = 32 / LPR;
   constexpr int U = WPT == 1 ? 8 : 4;                    // pieces per lane in flight
   constexpr int TPB = kRotaryWarps / WPT;                // tokens per block
@@ -257,10 +257,9 @@ constexpr int kCommitRows = 4;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * kCommitWarps)
-tree_commit_kernel(T* __restrict__ K, T* __restrict__ V, int32_t* __restrict__ idx,
-                   float* __restrict__ sumsq, Geom g, const int32_t* start_dev, const int32_t* cur_dev,
-                   const int32_t* __restrict__ path, int path_cap, const int32_t* __restrict__ n_path,
-                   int32_t* len_out, int per_head, int32_t* __restrict__ status) {
+tree_commit_kernel(T* K, T* V, int32_t* idx, float* sumsq, Geom g, const int32_t* start_dev, const int32_t* cur_dev,
+                   const int32_t* path, int path_cap, const int32_t* n_path, int32_t* len_out, int per_head,
+                   int32_t* status) {
   constexpr int EPV = Elem<T>::kPerVec, LPR = D / EPV, RPW = 32 / LPR;
   const long long bl = blockIdx.x;
   const int b = (int)(bl / g.L), l = (int)(bl % g.L);

@@ -47,7 +47,9 @@ __device__ __forceinline__ int sequence_of(const int32_t* tok_off, int B, int n_
 // These calls follow one another step after step, most of them for a few microseconds, so a kernel may be set
 // up on the SMs while the one before it in the stream runs: it is launched with launch_early, says at its start
 // that the next one may do the same, and waits for everything before it -- complete, and visible -- before its first
-// access to global memory.  A kernel that is launched without asking for this waits as always.
+// access to global memory.  A kernel that is launched without asking for this waits as always.  None of the early
+// ones has a __restrict__ parameter: that would promise that nobody else writes the memory while the kernel lives, and
+// would let the compiler read it before the wait, while the kernel before is still writing it.
 __device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
