@@ -51,6 +51,12 @@ int dtype_of(const at::Tensor& t) {
   throw Bad{"unsupported dtype " + std::string(c10::toString(t.scalar_type()))};
 }
 
+void entries(const at::Tensor* t, int64_t count, const char* what, at::ScalarType type = at::kInt) {
+  if (t && (t->scalar_type() != type || !t->is_contiguous() || (count >= 0 && t->numel() != count)))
+    throw Bad{std::string(what) + " must be contiguous " + c10::toString(type) +
+              (count >= 0 ? " with " + std::to_string(count) + " entries" : "")};
+}
+
 struct Attr {                                            // an attribute of the rows object, held for the call
   PyObject* o;
   Attr(PyObject* of, const char* name) : o(PyObject_GetAttrString(of, name)) { if (!o) throw Bad{""}; }
@@ -70,6 +76,9 @@ l2kv_layout layout(const at::Tensor& K, int64_t q_heads, PyObject* rows) {
     const at::Tensor *o = tensor(off.o, "rows.off"), *c = tensor(cap.o, "rows.cap");
     if (o->device() != K.device() || c->device() != K.device()) throw Bad{"rows on another device than the cache"};
     a.batch = (int32_t)integer(B.o); a.layers = (int32_t)integer(L.o); a.t_cap = (int32_t)integer(t_cap.o);
+    // the kernels read these as int64 and int32 arrays and write where they say
+    entries(o, (int64_t)a.batch * a.layers, "rows.off", at::kLong);
+    entries(c, (int64_t)a.batch * a.layers, "rows.cap");
     a.kv_heads = (int32_t)K.size(0); a.head_dim = (int32_t)K.size(2);
     a.stride_h = K.stride(0); a.stride_t = K.stride(1);
     a.row_off_dev = static_cast<const int64_t*>(o->data_ptr());
@@ -117,11 +126,6 @@ l2kv_tokens tokens(const at::Tensor& t, const l2kv_layout& a, int64_t n, int64_t
   return {t.data_ptr(), d == 4 ? t.stride(0) : 0, t.stride(d - 3), t.stride(d - 2)};
 }
 
-void entries(const at::Tensor* t, int64_t count, const char* what, at::ScalarType type = at::kInt) {
-  if (t && (t->scalar_type() != type || !t->is_contiguous() || (count >= 0 && t->numel() != count)))
-    throw Bad{std::string(what) + " must be contiguous " + c10::toString(type) +
-              (count >= 0 ? " with " + std::to_string(count) + " entries" : "")};
-}
 int64_t n_lengths(const l2kv_layout& a, bool per_head) { return (int64_t)a.batch * a.layers * (per_head ? a.kv_heads : 1); }
 // What lies along the cache's rows: one entry per row and head (-1, any number, for a cache without rows).
 int64_t n_rows(const l2kv_layout& a) {
