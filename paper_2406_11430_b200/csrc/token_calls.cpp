@@ -37,12 +37,12 @@ double real(PyObject* o) {
   if (v == -1.0 && PyErr_Occurred()) throw Bad{""};
   return v;
 }
-// An argument that is an int32 of the library's.
-int32_t integer32(PyObject* o, const char* what) {
-  const int64_t v = integer(o);
+// What is an int32 of the library's: a size, or an argument.
+int32_t narrow(int64_t v, const char* what) {
   if (v != (int32_t)v) throw Bad{std::string(what) + " is out of range"};
   return (int32_t)v;
 }
+int32_t integer32(PyObject* o, const char* what) { return narrow(integer(o), what); }
 bool truth(PyObject* o) { return PyObject_IsTrue(o) == 1; }
 
 int dtype_of(const at::Tensor& t) {
@@ -67,7 +67,7 @@ struct Attr {                                            // an attribute of the 
 l2kv_layout layout(const at::Tensor& K, int64_t q_heads, PyObject* rows) {
   l2kv_layout a{};
   a.dtype = dtype_of(K);
-  a.q_heads = (int32_t)q_heads;
+  a.q_heads = narrow(q_heads, "the number of query heads");
   if (rows != Py_None) {
     const Attr off(rows, "off"), cap(rows, "cap"), B(rows, "B"), L(rows, "L"), t_cap(rows, "t_cap"), total(rows, "total_rows");
     a.total_rows = integer(total.o);
@@ -75,19 +75,19 @@ l2kv_layout layout(const at::Tensor& K, int64_t q_heads, PyObject* rows) {
       throw Bad{"packed cache must be [Hkv, total_rows, D] with D contiguous"};
     const at::Tensor *o = tensor(off.o, "rows.off"), *c = tensor(cap.o, "rows.cap");
     if (o->device() != K.device() || c->device() != K.device()) throw Bad{"rows on another device than the cache"};
-    a.batch = (int32_t)integer(B.o); a.layers = (int32_t)integer(L.o); a.t_cap = (int32_t)integer(t_cap.o);
+    a.batch = integer32(B.o, "rows.B"); a.layers = integer32(L.o, "rows.L"); a.t_cap = integer32(t_cap.o, "rows.t_cap");
     // the kernels read these as int64 and int32 arrays and write where they say
     entries(o, (int64_t)a.batch * a.layers, "rows.off", at::kLong);
     entries(c, (int64_t)a.batch * a.layers, "rows.cap");
-    a.kv_heads = (int32_t)K.size(0); a.head_dim = (int32_t)K.size(2);
+    a.kv_heads = narrow(K.size(0), "a cache's size"); a.head_dim = narrow(K.size(2), "a cache's size");
     a.stride_h = K.stride(0); a.stride_t = K.stride(1);
     a.row_off_dev = static_cast<const int64_t*>(o->data_ptr());
     a.row_cap_dev = static_cast<const int32_t*>(c->data_ptr());
     return a;
   }
   if (K.dim() != 5 || K.stride(4) != 1) throw Bad{"cache must be [B, L, Hkv, t_cap, D] with D contiguous"};
-  a.batch = (int32_t)K.size(0); a.layers = (int32_t)K.size(1); a.kv_heads = (int32_t)K.size(2);
-  a.t_cap = (int32_t)K.size(3); a.head_dim = (int32_t)K.size(4);
+  int32_t* const sizes[5] = {&a.batch, &a.layers, &a.kv_heads, &a.t_cap, &a.head_dim};
+  for (int i = 0; i < 5; ++i) *sizes[i] = narrow(K.size(i), "a cache's size");
   a.stride_b = K.stride(0); a.stride_l = K.stride(1); a.stride_h = K.stride(2); a.stride_t = K.stride(3);
   return a;
 }
@@ -162,7 +162,7 @@ PyObject* rotary_write(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     one_device(*K, q, k, val, off, pos, freq, q_out, V, idx, key, start, cur, ws);
     same_geometry(*K, V);
     heads_of(*k);
-    const int64_t n = k->size(-3);
+    const int32_t n = narrow(k->size(-3), "the number of tokens");
     entries(off, (int64_t)a.batch + 1, "tok_off");
     entries(pos, n, "pos");
     entries(freq, -1, "freq", at::kDouble);
@@ -176,8 +176,8 @@ PyObject* rotary_write(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     if (q_out) to = tokens(*q_out, a, n, a.q_heads);
     const l2kv_tokens tk = tokens(*k, a, n, a.kv_heads), tv = tokens(*val, a, n, a.kv_heads);
     return PyLong_FromLong(fn_rotary_write(
-        q ? &tq : nullptr, &tk, &tv, static_cast<const int32_t*>(ptr(off)), (int32_t)n, static_cast<const int32_t*>(ptr(pos)),
-        static_cast<const double*>(ptr(freq)), freq ? (int32_t)(2 * freq->numel()) : 0, real(v[15]), q_out ? &to : nullptr,
+        q ? &tq : nullptr, &tk, &tv, static_cast<const int32_t*>(ptr(off)), n, static_cast<const int32_t*>(ptr(pos)),
+        static_cast<const double*>(ptr(freq)), freq ? narrow(2 * freq->numel(), "the number of frequencies") : 0, real(v[15]), q_out ? &to : nullptr,
         ptr(K), ptr(V), static_cast<int32_t*>(ptr(idx)), static_cast<float*>(ptr(key)), &a,
         static_cast<const int32_t*>(ptr(start)), static_cast<int32_t*>(ptr(cur)),
         flags_of(*K, per_head) | (interleaved ? L2KV_TOKENS_ROTARY_INTERLEAVED : 0), ptr(ws),
@@ -208,7 +208,7 @@ PyObject* tree_commit(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     return PyLong_FromLong(fn_tree_commit(
         ptr(K), ptr(V), static_cast<int32_t*>(ptr(idx)), static_cast<float*>(ptr(key)), &a,
         static_cast<const int32_t*>(ptr(start)), static_cast<const int32_t*>(ptr(cur)), static_cast<const int32_t*>(ptr(path)),
-        (int32_t)path->size(1), static_cast<const int32_t*>(ptr(n_path)), static_cast<int32_t*>(ptr(out)),
+        narrow(path->size(1), "the length of a path"), static_cast<const int32_t*>(ptr(n_path)), static_cast<int32_t*>(ptr(out)),
         flags_of(*K, per_head), ptr(ws), (size_t)ws->numel(), reinterpret_cast<void*>(integer(v[12]))));
   });
 }
@@ -221,7 +221,7 @@ PyObject* attention(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
                      *out = tensor(v[7], "out"), *lse = tensor(v[8], "lse_out", true), *ws = tensor(v[10], "workspace", true);
     const bool per_head = truth(v[12]);
     const l2kv_layout a = layout(*K, heads_of(*q), v[11]);
-    const int64_t n = q->size(-3);
+    const int32_t n = narrow(q->size(-3), "the number of tokens");
     one_device(*K, q, off, mask, V, cur, out, lse, ws);
     same_geometry(*K, V);
     entries(off, (int64_t)a.batch + 1, "tok_off");
@@ -236,13 +236,13 @@ PyObject* attention(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     const size_t ws_bytes = ws ? (size_t)ws->numel() : 0;
     if (!mask)
       return PyLong_FromLong(fn_prompt_attention(
-          &tq, static_cast<const int32_t*>(ptr(off)), (int32_t)n, ptr(K), ptr(V), &a, static_cast<const int32_t*>(ptr(cur)),
+          &tq, static_cast<const int32_t*>(ptr(off)), n, ptr(K), ptr(V), &a, static_cast<const int32_t*>(ptr(cur)),
           max_len, scale, flags, &to, static_cast<float*>(ptr(lse)), ptr(ws), ws_bytes, stream));
     if (mask->dim() != 2 || mask->size(0) != n || (mask->scalar_type() != at::kLong && mask->scalar_type() != at::kUInt64) ||
         !mask->is_contiguous())
       throw Bad{"tree_mask must be contiguous int64 or uint64 [N, words]"};
     return PyLong_FromLong(fn_tree_attention(
-        &tq, static_cast<const int32_t*>(ptr(off)), (int32_t)n, static_cast<const uint64_t*>(ptr(mask)), (int32_t)mask->size(1),
+        &tq, static_cast<const int32_t*>(ptr(off)), n, static_cast<const uint64_t*>(ptr(mask)), narrow(mask->size(1), "the words of a mask"),
         ptr(K), ptr(V), &a, static_cast<const int32_t*>(ptr(cur)), max_len, scale, flags, &to, static_cast<float*>(ptr(lse)),
         ptr(ws), ws_bytes, stream));
   });
@@ -255,7 +255,7 @@ PyObject* workspace_bytes(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     const at::Tensor *K = tensor(v[0], "K_c"), *q = tensor(v[1], "q");
     const l2kv_layout a = layout(*K, heads_of(*q), v[3]);
     size_t bytes = 0;
-    const int rc = fn_workspace_bytes(&a, (int32_t)q->size(-3), integer32(v[2], "max_len"), &bytes);
+    const int rc = fn_workspace_bytes(&a, narrow(q->size(-3), "the number of tokens"), integer32(v[2], "max_len"), &bytes);
     return PyLong_FromLongLong(rc == L2KV_OK ? (long long)bytes : rc);
   });
 }

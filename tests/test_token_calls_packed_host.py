@@ -1,5 +1,5 @@
 """Host side of the calls on new tokens with packed caches: what describes the rows has to have the type, the order
-and the number of entries that the kernels read it with.  No GPU needed."""
+and the number of entries that the kernels read it with, and every size has to fit the library's 32 bits.  No GPU needed."""
 import types
 
 import pytest
@@ -26,7 +26,7 @@ def _call(which, rows, K=None, n=N, path_cap=4):
         l2.rotary_write(tok(HQ), tok(H), tok(H), off, i32(N), None, tok(HQ), K, K, i32(H, TOTAL), torch.zeros((H, TOTAL)), start, cur, ws,
                         rows=rows)
     elif which == "commit":
-        l2.tree_commit(K, K, None, None, start, cur, i32(B, path_cap), i32(B), start, ws, rows=rows)
+        l2.tree_commit(K, K, None, None, start, cur, i32(B, 4) if path_cap == 4 else i32(B, 1).expand(B, path_cap), i32(B), start, ws, rows=rows)
     elif which == "prompt":
         l2.prompt_attention(tok(HQ), off, K, K, cur, CAP, tok(HQ), workspace=ws, rows=rows)
     elif which == "tree":
@@ -58,3 +58,26 @@ def test_rows_that_fit_get_as_far_as_the_launch(which):
 def test_rows_of_another_type_order_or_number_are_refused(which, change):
     with pytest.raises(ValueError):
         _call(which, _rows(**change))
+
+
+@pytest.mark.parametrize("which", CALLS)
+@pytest.mark.parametrize("change", [dict(B=(1 << 32) + B), dict(L=(1 << 32) + L), dict(t_cap=(1 << 32) + CAP), dict(t_cap=1 << 31),
+                                    dict(L=-(1 << 40))])
+def test_row_counts_beyond_32_bits_are_refused(which, change):
+    with pytest.raises(ValueError):
+        _call(which, _rows(**change))
+
+
+@pytest.mark.parametrize("which", ["rotary", "prompt", "tree", "workspace"])
+def test_more_tokens_than_32_bits_count_are_refused(which):
+    with pytest.raises(ValueError):
+        _call(which, _rows(), n=(1 << 32) + N)
+
+
+def test_longer_paths_and_more_heads_than_32_bits_count_are_refused():
+    with pytest.raises(ValueError):
+        _call("commit", _rows(), path_cap=(1 << 32) + 4)
+    K = torch.zeros((1, TOTAL, D), dtype=torch.bfloat16).expand((1 << 32) + H, TOTAL, D)
+    for which in ("commit", "prompt", "workspace"):
+        with pytest.raises(ValueError):
+            _call(which, _rows(), K=K)
