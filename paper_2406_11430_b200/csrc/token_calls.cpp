@@ -43,7 +43,11 @@ int32_t narrow(int64_t v, const char* what) {
   return (int32_t)v;
 }
 int32_t integer32(PyObject* o, const char* what) { return narrow(integer(o), what); }
-bool truth(PyObject* o) { return PyObject_IsTrue(o) == 1; }
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Bad{""};
+  return v != 0;
+}
 
 int dtype_of(const at::Tensor& t) {
   if (t.scalar_type() == at::kBFloat16) return L2KV_BF16;
