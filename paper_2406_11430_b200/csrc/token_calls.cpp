@@ -61,23 +61,40 @@ void entries(const at::Tensor* t, int64_t count, const char* what, at::ScalarTyp
               (count >= 0 ? " with " + std::to_string(count) + " entries" : "")};
 }
 
-struct Attr {                                            // an attribute of the rows object, held for the call
-  PyObject* o;
-  Attr(PyObject* of, const char* name) : o(PyObject_GetAttrString(of, name)) { if (!o) throw Bad{""}; }
-  ~Attr() { Py_DECREF(o); }
+struct Attr {                                            // an attribute of the rows object, held while this lives
+  PyObject* o = nullptr;
+  Attr() = default;
+  Attr(PyObject* of, const char* name) { get(of, name); }
+  Attr(const Attr&) = delete;
+  ~Attr() { Py_XDECREF(o); }
+  void get(PyObject* of, const char* name) { if (!(o = PyObject_GetAttrString(of, name))) throw Bad{""}; }
 };
+// The row ranges of a packed cache, held for a call: other threads run meanwhile.
+struct Ranges { Attr off, cap; };
+
+// A call of the library.  Other Python threads run while it lasts: it can block for as long as the GPU's queue is full.
+// (The arguments are worked out before, and the caller holds the tensors.)
+template <typename... P, typename... A>
+PyObject* unlocked(int (*fn)(P...), A... args) {
+  PyThreadState* const state = PyEval_SaveThread();
+  const int rc = fn(args...);
+  PyEval_RestoreThread(state);
+  return PyLong_FromLong(rc);
+}
 
 // Geometry of a cache, as the binding's Layout takes it from a tensor.
-l2kv_layout layout(const at::Tensor& K, int64_t q_heads, PyObject* rows) {
+l2kv_layout layout(const at::Tensor& K, int64_t q_heads, PyObject* rows, Ranges* held) {
   l2kv_layout a{};
   a.dtype = dtype_of(K);
   a.q_heads = narrow(q_heads, "the number of query heads");
   if (rows != Py_None) {
-    const Attr off(rows, "off"), cap(rows, "cap"), B(rows, "B"), L(rows, "L"), t_cap(rows, "t_cap"), total(rows, "total_rows");
+    held->off.get(rows, "off");
+    held->cap.get(rows, "cap");
+    const Attr B(rows, "B"), L(rows, "L"), t_cap(rows, "t_cap"), total(rows, "total_rows");
     a.total_rows = integer(total.o);
     if (K.dim() != 3 || K.stride(2) != 1 || K.size(1) != a.total_rows)
       throw Bad{"packed cache must be [Hkv, total_rows, D] with D contiguous"};
-    const at::Tensor *o = tensor(off.o, "rows.off"), *c = tensor(cap.o, "rows.cap");
+    const at::Tensor *o = tensor(held->off.o, "rows.off"), *c = tensor(held->cap.o, "rows.cap");
     if (o->device() != K.device() || c->device() != K.device()) throw Bad{"rows on another device than the cache"};
     a.batch = integer32(B.o, "rows.B"); a.layers = integer32(L.o, "rows.L"); a.t_cap = integer32(t_cap.o, "rows.t_cap");
     // the kernels read these as int64 and int32 arrays and write where they say
@@ -162,7 +179,8 @@ PyObject* rotary_write(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
                      *idx = tensor(v[9], "idx", true), *key = tensor(v[10], "sumsq_c", true),
                      *start = tensor(v[11], "start_dev"), *cur = tensor(v[12], "cur_len_dev"), *ws = tensor(v[13], "workspace");
     const bool interleaved = truth(v[14]), per_head = truth(v[17]);
-    const l2kv_layout a = layout(*K, q ? heads_of(*q) : 0, v[16]);
+    Ranges held;
+    const l2kv_layout a = layout(*K, q ? heads_of(*q) : 0, v[16], &held);
     one_device(*K, q, k, val, off, pos, freq, q_out, V, idx, key, start, cur, ws);
     same_geometry(*K, V);
     heads_of(*k);
@@ -179,13 +197,13 @@ PyObject* rotary_write(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     if (q) tq = tokens(*q, a, n, a.q_heads);
     if (q_out) to = tokens(*q_out, a, n, a.q_heads);
     const l2kv_tokens tk = tokens(*k, a, n, a.kv_heads), tv = tokens(*val, a, n, a.kv_heads);
-    return PyLong_FromLong(fn_rotary_write(
+    return unlocked(fn_rotary_write,
         q ? &tq : nullptr, &tk, &tv, static_cast<const int32_t*>(ptr(off)), n, static_cast<const int32_t*>(ptr(pos)),
-        static_cast<const double*>(ptr(freq)), freq ? narrow(2 * freq->numel(), "the number of frequencies") : 0, real(v[15]), q_out ? &to : nullptr,
-        ptr(K), ptr(V), static_cast<int32_t*>(ptr(idx)), static_cast<float*>(ptr(key)), &a,
+        static_cast<const double*>(ptr(freq)), freq ? narrow(2 * freq->numel(), "the number of frequencies") : 0,
+        real(v[15]), q_out ? &to : nullptr, ptr(K), ptr(V), static_cast<int32_t*>(ptr(idx)), static_cast<float*>(ptr(key)), &a,
         static_cast<const int32_t*>(ptr(start)), static_cast<int32_t*>(ptr(cur)),
         flags_of(*K, per_head) | (interleaved ? L2KV_TOKENS_ROTARY_INTERLEAVED : 0), ptr(ws),
-        (size_t)ws->numel(), reinterpret_cast<void*>(integer(v[18]))));
+        (size_t)ws->numel(), reinterpret_cast<void*>(integer(v[18])));
   });
 }
 
@@ -197,7 +215,8 @@ PyObject* tree_commit(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
                      *path = tensor(v[6], "path"), *n_path = tensor(v[7], "n_path"), *out = tensor(v[8], "len_out_dev"),
                      *ws = tensor(v[9], "workspace");
     const bool per_head = truth(v[11]);
-    const l2kv_layout a = layout(*K, K->dim() > 2 ? K->size(v[10] != Py_None ? 0 : 2) : 0, v[10]);
+    Ranges held;
+    const l2kv_layout a = layout(*K, K->dim() > 2 ? K->size(v[10] != Py_None ? 0 : 2) : 0, v[10], &held);
     if (path->dim() != 2 || path->size(0) != a.batch) throw Bad{"path must be [B, path_cap]"};
     one_device(*K, V, idx, key, start, cur, path, n_path, out, ws);
     same_geometry(*K, V);
@@ -209,11 +228,11 @@ PyObject* tree_commit(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     entries(cur, n_lengths(a, per_head), "cur_len_dev");
     entries(out, n_lengths(a, per_head), "len_out_dev");
     entries(ws, -1, "workspace", at::kByte);
-    return PyLong_FromLong(fn_tree_commit(
+    return unlocked(fn_tree_commit,
         ptr(K), ptr(V), static_cast<int32_t*>(ptr(idx)), static_cast<float*>(ptr(key)), &a,
         static_cast<const int32_t*>(ptr(start)), static_cast<const int32_t*>(ptr(cur)), static_cast<const int32_t*>(ptr(path)),
         narrow(path->size(1), "the length of a path"), static_cast<const int32_t*>(ptr(n_path)), static_cast<int32_t*>(ptr(out)),
-        flags_of(*K, per_head), ptr(ws), (size_t)ws->numel(), reinterpret_cast<void*>(integer(v[12]))));
+        flags_of(*K, per_head), ptr(ws), (size_t)ws->numel(), reinterpret_cast<void*>(integer(v[12])));
   });
 }
 
@@ -224,7 +243,8 @@ PyObject* attention(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
                      *K = tensor(v[3], "K_c"), *V = tensor(v[4], "V_c", true), *cur = tensor(v[5], "cur_len_dev"),
                      *out = tensor(v[7], "out"), *lse = tensor(v[8], "lse_out", true), *ws = tensor(v[10], "workspace", true);
     const bool per_head = truth(v[12]);
-    const l2kv_layout a = layout(*K, heads_of(*q), v[11]);
+    Ranges held;
+    const l2kv_layout a = layout(*K, heads_of(*q), v[11], &held);
     const int32_t n = narrow(q->size(-3), "the number of tokens");
     one_device(*K, q, off, mask, V, cur, out, lse, ws);
     same_geometry(*K, V);
@@ -239,16 +259,16 @@ PyObject* attention(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     const uint32_t flags = flags_of(*K, per_head);
     const size_t ws_bytes = ws ? (size_t)ws->numel() : 0;
     if (!mask)
-      return PyLong_FromLong(fn_prompt_attention(
+      return unlocked(fn_prompt_attention,
           &tq, static_cast<const int32_t*>(ptr(off)), n, ptr(K), ptr(V), &a, static_cast<const int32_t*>(ptr(cur)),
-          max_len, scale, flags, &to, static_cast<float*>(ptr(lse)), ptr(ws), ws_bytes, stream));
+          max_len, scale, flags, &to, static_cast<float*>(ptr(lse)), ptr(ws), ws_bytes, stream);
     if (mask->dim() != 2 || mask->size(0) != n || (mask->scalar_type() != at::kLong && mask->scalar_type() != at::kUInt64) ||
         !mask->is_contiguous())
       throw Bad{"tree_mask must be contiguous int64 or uint64 [N, words]"};
-    return PyLong_FromLong(fn_tree_attention(
+    return unlocked(fn_tree_attention,
         &tq, static_cast<const int32_t*>(ptr(off)), n, static_cast<const uint64_t*>(ptr(mask)), narrow(mask->size(1), "the words of a mask"),
         ptr(K), ptr(V), &a, static_cast<const int32_t*>(ptr(cur)), max_len, scale, flags, &to, static_cast<float*>(ptr(lse)),
-        ptr(ws), ws_bytes, stream));
+        ptr(ws), ws_bytes, stream);
   });
 }
 
@@ -257,7 +277,8 @@ PyObject* workspace_bytes(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
   return guarded([&]() -> PyObject* {
     check_count(n_args, 4);
     const at::Tensor *K = tensor(v[0], "K_c"), *q = tensor(v[1], "q");
-    const l2kv_layout a = layout(*K, heads_of(*q), v[3]);
+    Ranges held;
+    const l2kv_layout a = layout(*K, heads_of(*q), v[3], &held);
     size_t bytes = 0;
     const int rc = fn_workspace_bytes(&a, narrow(q->size(-3), "the number of tokens"), integer32(v[2], "max_len"), &bytes);
     return PyLong_FromLongLong(rc == L2KV_OK ? (long long)bytes : rc);
