@@ -36,6 +36,10 @@ struct Geom {
   }
   // rows that (b, l) may hold
   __device__ __forceinline__ int cap(long long bl) const { return row_off ? row_cap[bl] : t_cap; }
+  // whether row t of (b, l) = bl is one of its own, and, in a packed cache, one of the cache (index checks)
+  __device__ __forceinline__ bool holds(long long bl, long long t) const {
+    return t >= 0 && t < cap(bl) && (!row_off || (row_off[bl] >= 0 && row_off[bl] + t < total_rows));
+  }
   // first entry of unit = (b * L + l) * H + h in the index map / key arrays
   __device__ __forceinline__ long long meta(long long unit) const {
     return row_off ? (unit % H) * total_rows + row_off[unit / H] : unit * (long long)t_cap;

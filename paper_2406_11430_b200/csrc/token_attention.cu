@@ -527,6 +527,8 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       if (it.stop) break;
       if (it.n == 0) continue;
       if (lane == 0) {
+        const long long bl = (long long)it.b * L + it.l;
+        (void)L2KV_BOUNDS(a.g.holds(bl, it.row0) && a.g.holds(bl, it.end - 1), a.status);   // (the copies themselves stay inside)
         const int tiles = it.pair ? 2 : 1;
         if (n_q > 0) ok = wait(q_free, (n_q - 1) & 1u);
         if (ok) {
@@ -809,8 +811,10 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       tc_fence_after();
       const int tok = it.tok0 + q, head = it.h * A.G + head_in_group;
       const long long part_row = (long long)it.slot * A.slot_rows + (it.pair ? chain * kTaRows : 0) + row;
-      __nv_bfloat16* const out = valid ? a.out.row<__nv_bfloat16>(it.l, tok, head) : nullptr;
-      float* const part = valid && it.slot >= 0 ? A.part + part_row * D : nullptr;
+      const bool writes = valid && L2KV_BOUNDS(tok >= 0 && tok < a.n_tokens && head < a.g.Hq && it.slot < 2 * (int)gridDim.x &&
+                                                   (it.pair ? chain * kTaRows : 0) + row < (A.plan ? A.slot_rows : 2 * kTaRows), a.status);
+      __nv_bfloat16* const out = writes ? a.out.row<__nv_bfloat16>(it.l, tok, head) : nullptr;
+      float* const part = writes && it.slot >= 0 ? A.part + part_row * D : nullptr;
       float f0 = 1.f, f1 = 0.f, total = sum, m = m_ref;
       int c_lo = 0, c_hi = D;
       if (!it.pair) {
@@ -871,7 +875,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
             rows.store(pieces, c * 2, stage);
           }
         }
-        if (valid && (it.pair || chain == 0)) {
+        if (writes && (it.pair || chain == 0)) {
           const float lse2 = total == 0.f ? -INFINITY : m + log2f(total);
           if (it.slot >= 0) A.part_lse[part_row] = lse2;
           else if (a.lse) a.lse[((long long)it.l * a.n_tokens + tok) * a.g.Hq + head] = lse2 * 0.6931471805599453f;
@@ -911,8 +915,10 @@ token_attention_join_kernel(const __grid_constant__ TaArgs A) {
   while (c1 < kTaGrid && A.plan[c1].at == s.at && A.plan[c1].off > 0) ++c1;
   const int nc = c1 - c0 + 1;
   auto row = [&](int c) { return (long long)(c == 0 ? 2 * c0 - 1 : 2 * (c0 + c - 1)) * A.slot_rows + r; };
+  if (!L2KV_BOUNDS(s.e >= 0 && s.e < a.g.B * a.g.L && s.h >= 0 && s.h < a.g.H && before.at <= s.at, a.status)) return;
   const TaItem it = ta_item(A, s.e / a.g.L, s.e % a.g.L, s.p, s.h, 0, INT_MAX, 0);
   if (r >= it.nq * A.G) return;
+  if (!L2KV_BOUNDS(r < A.slot_rows && it.tok0 >= 0 && it.tok0 + it.nq <= a.n_tokens, a.status)) return;
   float top = -INFINITY;
 #pragma unroll 4
   for (int c = 0; c < nc; ++c) top = fmaxf(top, A.part_lse[row(c)]);

@@ -55,7 +55,8 @@ token_attention_fp32_kernel(const __grid_constant__ TokenAttention a, const floa
   const long long bl = (long long)b * g.L + l;
   const int cur = max(0, min(a.lens.at(bl, h, g.H), min(a.max_len, g.cap(bl))));
   const int base = cur - range.n, first = tile * kTfRows, rows = min(kTfRows, range.n * G - first);
-  const int end = a.mask ? cur : max(0, min(cur, base + (first + rows - 1) / G + 1));
+  int end = a.mask ? cur : max(0, min(cur, base + (first + rows - 1) / G + 1));
+  if (end > 0 && !L2KV_BOUNDS(g.holds(bl, 0) && g.holds(bl, end - 1), a.status)) end = 0;
   const int clear = a.mask ? base : base + first / G + 1;                    // rows below it are seen by all
 
   for (int e = tid; e < kTfRows * D / 4; e += 128) {

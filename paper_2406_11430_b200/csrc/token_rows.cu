@@ -205,6 +205,7 @@ rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* K, T* V) {
         if (piece == 0) atomicExch(a.status, (int)L2KV_ERR_DEVICE_OVERFLOW);
         continue;
       }
+      if (!L2KV_BOUNDS(g.holds(bl, slot), a.status)) continue;
       const long long to = cache0 + h * g.sh + slot * g.st;
       *reinterpret_cast<uint4*>(K + to) = y;
       *reinterpret_cast<uint4*>(V + to) = x[2 * u + 1];
@@ -293,6 +294,7 @@ tree_commit_kernel(T* K, T* V, int32_t* idx, float* sumsq, Geom g, const int32_t
           const int e = e0 + r * RPW + lane / LPR;
           const int from = __shfl_sync(0xffffffffu, mine, e & 31);
           go[r] = e < n && from != j0 + e;
+          if (go[r]) go[r] = L2KV_BOUNDS(from > j0 + e && g.holds(bl, (long long)start + from), status);
           if (!go[r]) continue;
           vk[r] = *reinterpret_cast<const uint4*>(K + base + from * g.st);
           vv[r] = *reinterpret_cast<const uint4*>(V + base + from * g.st);
