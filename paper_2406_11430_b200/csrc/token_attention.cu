@@ -527,8 +527,8 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       if (it.stop) break;
       if (it.n == 0) continue;
       if (lane == 0) {
-        const long long bl = (long long)it.b * L + it.l;
-        (void)L2KV_BOUNDS(a.g.holds(bl, it.row0) && a.g.holds(bl, it.end - 1), a.status);   // (the copies themselves stay inside)
+        // (the copies themselves stay inside)
+        (void)L2KV_BOUNDS(a.g.holds((long long)it.b * L + it.l, it.row0) && a.g.holds((long long)it.b * L + it.l, it.end - 1), a.status);
         const int tiles = it.pair ? 2 : 1;
         if (n_q > 0) ok = wait(q_free, (n_q - 1) & 1u);
         if (ok) {
