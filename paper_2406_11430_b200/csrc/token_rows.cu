@@ -58,7 +58,7 @@ __device__ __forceinline__ uint4 ld_once(const void* p) {
 // Cosine and sine of the angle a in fp64, to about 1e-15: their fp32 roundings are those of the exact values
 // but for one in some 10^7.  a / 2 pi is formed as a sum of two doubles and the nearest quarter turn taken off it,
 // which leaves the rest exact for any position; at most an eighth of a turn is left, where the Taylor series
-// are short (the first terms left out: x^17 / 17! < 5e-17, x^16 / 16! < 1e-15).
+// are short (the first terms left out: x^17 / 17! < 4.7e-17, x^16 / 16! < 1.01e-15).
 __device__ __forceinline__ void cos_sin(double a, double* c, double* s) {
   constexpr double kHi = 0.15915494309189535, kLo = -9.839338337591243e-18;   // 1 / 2 pi
   const double t = a * kHi;

@@ -24,10 +24,9 @@ __device__ __forceinline__ void umma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];"
                :: "r"(bar) : "memory");
 }
-// For a warp that issues as a whole: the operands of tcgen05.mma live in uniform registers, and only where
-// control flow is uniform can the compiler compute them there (a branch on the lane number costs a move
-// per operand and instruction).  So all lanes run the issuing code and one is elected per group of
-// instructions, always the same one.
+// For a warp that issues as a whole: all lanes run the issuing code, so that its control flow and its addresses are
+// the same for all, and one lane is elected per group of instructions, always the same one.  (Issued by one thread
+// behind a branch on the lane number, causal attention of a 16 k-token prompt took 2142 us instead of 1960.)
 __device__ __forceinline__ bool elect_one() {
   uint32_t e;
   asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(e));
@@ -164,7 +163,8 @@ __device__ __forceinline__ uint32_t pack_bf16_rest(float lo, float hi, uint32_t 
   return pack_bf16(lo - __uint_as_float(packed << 16), hi - __uint_as_float(packed & 0xffff0000u));
 }
 
-// 2^x by the hardware approximation (one MUFU instruction; x <= 0 here, -inf gives 0).
+// 2^x by the hardware approximation (one MUFU instruction; -inf gives 0).  x is at most the few units that a running
+// maximum may drift before sums are rescaled, 8 in the kernels here.
 __device__ __forceinline__ float fast_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
