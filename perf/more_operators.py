@@ -287,7 +287,7 @@ def _deal(s, taken, need):
     order = torch.zeros(n_pages + 1, dtype=torch.int64, device=DEV)
     order[torch.where(free, rank, n_pages)] = torch.arange(n_pages, device=DEV)
     upto = need.view(-1).cumsum(0).view(need.shape)
-    return order, upto - need, upto <= free.sum()
+    return order, upto - need, (need == 0) | (upto <= free.sum())
 
 
 def _plain_update(s):
