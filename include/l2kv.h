@@ -125,15 +125,17 @@ int l2kv_workspace_bytes(const l2kv_layout* lay, int32_t max_len, size_t* bytes)
  *   L2KV_OK                   nothing happened;
  *   L2KV_ERR_DEVICE_OVERFLOW  l2kv_append_evict had no row left for an append (the row was
  *                             dropped, everything else went ahead),
- *                             or l2kv_rotary_write none for a new token's;
+ *                             or l2kv_rotary_write (l2kv_norm_rotary_write) none for a new token's; or
+ *                             l2kv_page_update / l2kv_page_compact too few free pages (see there);
  *   L2KV_ERR_TIMEOUT          a kernel of l2kv_decode_attention, l2kv_prefix_attention,
- *                             l2kv_prompt_attention or l2kv_tree_attention gave up
+ *                             l2kv_prompt_attention, l2kv_tree_attention or l2kv_paged_attention gave up
  *                             waiting for a copy or a tensor-core operation (every such wait
  *                             is bounded so that a fault cannot hang the GPU).  The kernel
  *                             also sets a mark in the status block at which the rest of its
  *                             grid, and EVERY LATER decode / prefix / prompt / tree call on this workspace,
  *                             leaves at once without writing its output;
- *   L2KV_ERR_OUT_OF_RANGE     l2kv_tree_commit met a path that leaves its tree (cut there);
+ *   L2KV_ERR_OUT_OF_RANGE     l2kv_tree_commit met a path that leaves its tree (cut there), or a call on a cache
+ *                             in pages a page that the pool does not have (left out);
  *   L2KV_ERR_DEBUG_BOUNDS     only from a library built with -DL2KV_DEBUG: an index check
  *                             failed (the access was skipped).
  * The word keeps the last anomaly until the workspace is cleared: after any non-zero status,
@@ -443,6 +445,95 @@ int l2kv_tree_commit(void* K_c, void* V_c, int32_t* idx, float* sumsq_c, const l
                      const int32_t* start_dev, const int32_t* cur_len_dev, const int32_t* path_dev,
                      int32_t path_cap, const int32_t* n_path_dev, int32_t* len_out_dev, uint32_t flags,
                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Caches in pages ------------------------------------------------------------------------
+ * A dense or packed cache gives every (sequence, layer) a range of rows for good.  Where requests come, fork,
+ * shrink (compression, rejected drafts) and end, rows in pages fit better: K and V are pools
+ * [kv_heads, n_pages * page_rows, head_dim], idx and sumsq [kv_heads, n_pages * page_rows], and row t of (b, l), for every
+ * head, is pool row  table[b, l, t / page_rows] * page_rows + t % page_rows.  In the l2kv_layout of such a cache
+ * row_off_dev is NULL, stride_h and stride_t are the pool's (stride_b and stride_l are ignored), total_rows is
+ * n_pages * page_rows (at most 2^31 - 1) and t_cap is table_cap * page_rows.  A layer has pages of its own, so that layers may
+ * differ in length; a cache whose layers share one table is the same thing with one layer of layers * kv_heads heads for the calls on
+ * tables, and a view of kv_heads of them for each layer's writes and attention.
+ * Table entries are checked on the device: rows of a page outside [0, n_pages) are read as zeros and never written, and the
+ * status word becomes L2KV_ERR_OUT_OF_RANGE.  The tables, with the lengths, are the only state.  A page is free where no table
+ * names it below its sequence's length and it is not pinned.  The paper has no counterpart; l2kv_page_compact
+ * is its method (Section 3) on such a cache. */
+typedef struct {
+  int32_t* table_dev;                 /* DEVICE; entry j of (b, l) at b * stride_b + l * stride_l + j */
+  int64_t stride_b, stride_l;         /* in entries                                            */
+  int32_t table_cap;                  /* entries per (b, l)                                    */
+  int32_t page_rows;                  /* a power of two, 16 to 1024                            */
+  int32_t n_pages;
+  int32_t reserved;
+  int32_t* room_dev;                  /* DEVICE [batch, layers]: rows that (b, l) may hold, as l2kv_page_update
+                                         leaves it; or NULL: table_cap * page_rows            */
+} l2kv_pages;
+
+/* The tables of the next step.  Sequence b of the new tables (batch_out of them) goes on from sequence parent_dev[b] of
+ * `pages` (int32 [batch_out]; negative: from none) with that one's first keep_dev[b, l] rows (int32 [batch_out, layers]),
+ * and gets room for grow_dev[b] rows more (int32 [batch_out]).  So one call lets sequences go on, fork (a parent named
+ * several times; the pages are shared), give rows back (a smaller keep), end (a parent not named) and begin (no
+ * parent), and grows them.  keep must not be above the parent's length.  With have = ceil(keep / page_rows) and
+ * more = ceil((keep + grow) / page_rows), the new table holds the parent's first `have` pages, then free pages up
+ * to `more`, then -1 up to table_cap; entries of `pages_out` are all written.
+ * A page that several (b, l) of the new tables hold stays, for writing, with the one that has most rows in it, the
+ * lowest b * layers + l of several; a pinned page with none.  Any other that grows and whose last kept page is not full
+ * gets a page in its place that the kept rows are copied to (K, V, idx, sumsq of every head).  Free pages are dealt out in
+ * ascending order to (b, l) in ascending order, within one in table order.
+ * room_dev of pages_out (may be NULL) receives  more * page_rows  where grow > 0, else keep: rows the sequence may write
+ * without touching another's.  Where the free pages do not reach (the requests up to (b, l) sum to more than there are, and its own
+ * is not zero), or `more` is above table_cap, (b, l) keeps what it has, its room is keep, and the status word becomes
+ * L2KV_ERR_DEVICE_OVERFLOW.  A parent at or beyond batch counts as none (L2KV_ERR_OUT_OF_RANGE).
+ * n_free_out (may be NULL): int32, pages free after the call.  pin_dev (may be NULL): uint8 [n_pages], pages that are
+ * neither handed out nor written (prompts kept for later requests).  pages_out has tables of its own; table_cap, page_rows
+ * and n_pages agree.  batch_out * layers and batch * layers are at most 2^20.  idx and sumsq_c may be NULL.
+ * workspace: l2kv_page_workspace_bytes(lay, pages, batch_out, 0, ..) bytes, of which the first 256 were zeroed. */
+int l2kv_page_update(void* K_c, void* V_c, int32_t* idx, float* sumsq_c, const l2kv_layout* lay, const l2kv_pages* pages,
+                     const int32_t* parent_dev, const int32_t* keep_dev, const int32_t* grow_dev, int32_t batch_out,
+                     const uint8_t* pin_dev, const l2kv_pages* pages_out, int32_t* n_free_out, uint32_t flags,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* Compression of a cache in pages: for every (b, l) with keep_dev[b, l] < len_dev[b, l], every head keeps its keep rows
+ * that come first in the order (key, row) -- last, for L2KV_KEEP_HIGHEST_NORM, with ties still to the lower row -- and they
+ * move, in row order, to rows 0 .. keep - 1 in ceil(keep / page_rows) free pages, dealt out as above (K, V, idx, sumsq; bit
+ * copies).  The keys are sumsq_c, as l2kv_rotary_write and l2kv_norm_rotary_write leave them.  The old pages are no longer named by the new table;
+ * others that share them keep them.  Any other (b, l) keeps its pages.  len_out_dev[b, l] (may be len_dev) and room_dev of
+ * pages_out (may be NULL) receive the new length.  Where the free pages do not reach, or a page in use is none, (b, l) stays
+ * whole (L2KV_ERR_DEVICE_OVERFLOW, L2KV_ERR_OUT_OF_RANGE).  The pages that a call frees can be handed out by the next one, so a
+ * full pool is compacted some sequences at a time (keep = len for the others).  keep_dev, len_dev: int32 [batch, layers].
+ * L2KV_KEEP_RANDOM is not offered.  idx may be NULL.  workspace: l2kv_page_workspace_bytes(lay, pages, batch, max_len, ..). */
+int l2kv_page_compact(void* K_c, void* V_c, int32_t* idx, float* sumsq_c, const l2kv_layout* lay, const l2kv_pages* pages,
+                      const int32_t* len_dev, const int32_t* keep_dev, int32_t max_len, int32_t policy, const uint8_t* pin_dev,
+                      const l2kv_pages* pages_out, int32_t* len_out_dev, uint32_t flags, void* workspace,
+                      size_t workspace_bytes, void* stream);
+int l2kv_page_workspace_bytes(const l2kv_layout* lay, const l2kv_pages* pages, int32_t batch_out, int32_t max_len, size_t* bytes);
+
+/* l2kv_rotary_write with norms of queries and keys per head before the rotation, and for caches in pages:
+ *   x -> x / sqrt(mean_d x_d^2 + eps) * (weight_d + weight_offset)       in fp32, rounded once, behind the rotation
+ * with L2KV_TOKENS_NORM_Q for the queries and L2KV_TOKENS_NORM_K for the keys.  q_weight, k_weight: DEVICE [head_dim] in
+ * the cache's dtype, 16-byte aligned, or NULL (the factor is then 1).  eps >= 0.  Values are not normed.  pages: NULL (the cache has
+ * rows, as for l2kv_rotary_write), or the tables that rows start + s lie in; rows at or beyond room_dev[b, l], or in a page
+ * that is none, are not written (status word; cur_len_dev stops at the room).  Everything else as for l2kv_rotary_write. */
+#define L2KV_TOKENS_NORM_Q 8u
+#define L2KV_TOKENS_NORM_K 16u
+int l2kv_norm_rotary_write(const l2kv_tokens* q, const l2kv_tokens* k, const l2kv_tokens* v,
+                           const int32_t* tok_off_dev, int32_t n_tokens, const int32_t* pos_dev,
+                           const double* freq_dev, int32_t rot_dim, double rot_scale, const void* q_weight,
+                           const void* k_weight, float eps, float weight_offset, const l2kv_tokens* q_out, void* K_c,
+                           void* V_c, int32_t* idx, float* sumsq_c, const l2kv_layout* lay, const l2kv_pages* pages,
+                           const int32_t* start_dev, int32_t* cur_len_dev, uint32_t flags, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* l2kv_prompt_attention over a cache in pages: single tokens of a decode step, chunks and whole prompts, mixed as they come.
+ * The same arguments, masks, precision, workspace (l2kv_paged_attention_workspace_bytes) and errors; table entries at or
+ * beyond ceil(cur_len / page_rows) are not read.  A page that is none reads as zeros, which are seen like other rows. */
+int l2kv_paged_attention_workspace_bytes(const l2kv_layout* lay, const l2kv_pages* pages, int32_t n_tokens, int32_t max_len,
+                                         size_t* bytes);
+int l2kv_paged_attention(const l2kv_tokens* q, const int32_t* tok_off_dev, int32_t n_tokens, const void* K_c,
+                         const void* V_c, const l2kv_layout* lay, const l2kv_pages* pages, const int32_t* cur_len_dev,
+                         int32_t max_len, float scale, uint32_t flags, const l2kv_tokens* out, float* lse_out, void* workspace,
+                         size_t workspace_bytes, void* stream);
 
 /* Attention loss of the norm-based compression against the ideal one (Section 3,
  * Eqs. 5-7), for one query per query head over the cached keys i < cur_len_dev[b,l]:

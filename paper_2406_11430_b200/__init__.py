@@ -11,4 +11,5 @@ from .binding import (L2KVError, Layout, Rows, key_norms, select_compact, decode
                       decode_attention_static_status, status_string, library_path, lib,
                       rotary_frequencies, rotary_write, prompt_attention, tree_attention, tree_commit,
                       prompt_attention_workspace_bytes, ROTARY_NONE, ROTARY_LINEAR, ROTARY_NTK, ROTARY_LLAMA3,
-                      ROTARY_YARN, KEEP_LOWEST_NORM, KEEP_HIGHEST_NORM, KEEP_RANDOM)
+                      ROTARY_YARN, Pages, norm_rotary_write, paged_attention, paged_attention_workspace_bytes, page_update,
+                      page_compact, page_workspace_bytes, KEEP_LOWEST_NORM, KEEP_HIGHEST_NORM, KEEP_RANDOM)

@@ -118,6 +118,21 @@ class Rows:
         self.cap = torch.from_numpy(cap).to(device)
 
 
+class Pages:
+    """Tables of a paged cache [Hkv, n_pages * page_rows, D]: row t of (b, l), for every head, is row
+    table[b, l, t // page_rows] * page_rows + t % page_rows.  table: int32 [B, L, entries] on the device; room (may be
+    None): int32 [B, L], the rows that (b, l) may hold, as page_update leaves it; see l2kv_pages."""
+
+    def __init__(self, table, page_rows, n_pages, room=None):
+        self.table, self.page_rows, self.n_pages, self.room = table, int(page_rows), int(n_pages), room
+
+    @classmethod
+    def empty(cls, B, L, entries, page_rows, n_pages, device, room=True):
+        """Tables that name no page, to be filled by page_update."""
+        return cls(torch.full((B, L, entries), -1, dtype=torch.int32, device=device), page_rows, n_pages,
+                   torch.zeros((B, L), dtype=torch.int32, device=device) if room else None)
+
+
 class Layout:
     """Geometry of a cache tensor, taken from the tensor: dense [B, L, Hkv, t_cap, D], or,
     with rows (a Rows), packed [Hkv, total_rows, D].  D contiguous."""
@@ -400,9 +415,11 @@ def _token_calls():
             raise ImportError("_token_calls is missing: run `python -m paper_2406_11430_b200.build`; there is no "
                               f"fallback path ({e})") from e
         L = lib()
-        native.bind(*(ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
-            "l2kv_rotary_write", "l2kv_tree_commit", "l2kv_prompt_attention", "l2kv_tree_attention",
-            "l2kv_prompt_attention_workspace_bytes")))
+        address = lambda names: [ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in names]  # noqa: E731
+        native.bind(*address(("l2kv_rotary_write", "l2kv_tree_commit", "l2kv_prompt_attention", "l2kv_tree_attention",
+                              "l2kv_prompt_attention_workspace_bytes")))
+        native.bind_pages(*address(("l2kv_norm_rotary_write", "l2kv_paged_attention", "l2kv_paged_attention_workspace_bytes",
+                                    "l2kv_page_update", "l2kv_page_compact", "l2kv_page_workspace_bytes")))
         _NATIVE = native
     return _NATIVE
 
@@ -455,7 +472,7 @@ def tree_commit(K_c, V_c, idx, sumsq_c, start_dev, cur_len_dev, path, n_path, le
 
 def prompt_attention_workspace_bytes(K_c, q, max_len, rows=None):
     """Bytes with which prompt_attention and tree_attention may split caches over the SMs."""
-    n = (_NATIVE or _token_calls()).workspace_bytes(K_c, q, max_len, rows)
+    n = (_NATIVE or _token_calls()).workspace_bytes(K_c, q, max_len, rows, None)
     if n < 0:
         raise L2KVError(n, "l2kv_prompt_attention_workspace_bytes")
     return n
@@ -466,7 +483,7 @@ def prompt_attention(q, tok_off, K_c, V_c, cur_len_dev, max_len, out, lse_out=No
     """Causal attention of packed prompts (q, out: [L, N, Hq, D]) over caches whose last rows are the prompts'
     own; see l2kv_prompt_attention."""
     _call((_NATIVE or _token_calls()).attention, "l2kv_prompt_attention", K_c, stream, q, tok_off, None, K_c, V_c,
-          cur_len_dev, max_len, out, lse_out, scale, workspace, rows, per_head)
+          cur_len_dev, max_len, out, lse_out, scale, workspace, rows, per_head, None)
 
 
 def tree_attention(q, tok_off, tree_mask, K_c, V_c, cur_len_dev, max_len, out, lse_out=None, scale=0.0, workspace=None,
@@ -476,4 +493,55 @@ def tree_attention(q, tok_off, tree_mask, K_c, V_c, cur_len_dev, max_len, out, l
     if tree_mask is None:
         raise ValueError("tree_mask is missing")
     _call((_NATIVE or _token_calls()).attention, "l2kv_tree_attention", K_c, stream, q, tok_off, tree_mask, K_c, V_c,
-          cur_len_dev, max_len, out, lse_out, scale, workspace, rows, per_head)
+          cur_len_dev, max_len, out, lse_out, scale, workspace, rows, per_head, None)
+
+
+def norm_rotary_write(q, k, v, tok_off, pos, freq, q_out, K_c, V_c, idx, sumsq_c, start_dev, cur_len_dev, workspace,
+                      q_weight=None, k_weight=None, norm_q=True, norm_k=True, eps=1e-6, weight_offset=0.0, interleaved=False,
+                      attn_scale=1.0, stream=None, rows=None, per_head=False, pages=None):
+    """rotary_write with norms of queries and keys per head before the rotation (weights: [D] in the cache's dtype, or
+    None), into a dense cache, a packed one (rows) or one in pages (pages); see l2kv_norm_rotary_write."""
+    _call((_NATIVE or _token_calls()).norm_rotary_write, "l2kv_norm_rotary_write", K_c, stream, q, k, v, tok_off, pos, freq, q_out,
+          K_c, V_c, idx, sumsq_c, start_dev, cur_len_dev, workspace, interleaved, attn_scale, rows, per_head, pages, q_weight,
+          k_weight, norm_q, norm_k, eps, weight_offset)
+
+
+def paged_attention_workspace_bytes(K_c, q, max_len, pages):
+    """Bytes with which paged_attention may split caches over the SMs."""
+    n = (_NATIVE or _token_calls()).workspace_bytes(K_c, q, max_len, None, pages)
+    if n < 0:
+        raise L2KVError(n, "l2kv_paged_attention_workspace_bytes")
+    return n
+
+
+def paged_attention(q, tok_off, K_c, V_c, cur_len_dev, max_len, out, pages, lse_out=None, scale=0.0, workspace=None,
+                    stream=None, per_head=False):
+    """prompt_attention over a cache in pages: single tokens, chunks and whole prompts; see l2kv_paged_attention."""
+    if pages is None:
+        raise ValueError("pages is missing")
+    _call((_NATIVE or _token_calls()).attention, "l2kv_paged_attention", K_c, stream, q, tok_off, None, K_c, V_c,
+          cur_len_dev, max_len, out, lse_out, scale, workspace, None, per_head, pages)
+
+
+def page_workspace_bytes(K_c, pages, max_len=0, batch_out=None):
+    """Bytes of workspace for page_update to batch_out sequences (default: as many as there are) and, with max_len, for
+    page_compact of caches up to that length."""
+    n = (_NATIVE or _token_calls()).page_workspace_bytes(K_c, pages, batch_out, max_len)
+    if n < 0:
+        raise L2KVError(n, "l2kv_page_workspace_bytes")
+    return n
+
+
+def page_update(K_c, V_c, idx, sumsq_c, pages, parent, keep, grow, pages_out, workspace, pin=None, n_free_out=None, stream=None):
+    """The tables of the next step: sequence b goes on from sequence parent[b] of `pages` with its first keep[b, l] rows, and
+    gets room for grow[b] more; see l2kv_page_update.  parent, grow: int32 [B'], keep: int32 [B', L]; pages_out: tables of B'
+    sequences.  pin: uint8 [n_pages] or None; n_free_out: int32 [1] or None."""
+    _call((_NATIVE or _token_calls()).page_update, "l2kv_page_update", K_c, stream, K_c, V_c, idx, sumsq_c, pages, parent, keep,
+          grow, pages_out, pin, n_free_out, workspace)
+
+
+def page_compact(K_c, V_c, idx, sumsq_c, pages, cur_len_dev, keep_dev, max_len, pages_out, len_out_dev, workspace,
+                 policy=KEEP_LOWEST_NORM, pin=None, stream=None):
+    """Moves the keep_dev[b, l] rows of lowest key norm (sumsq_c) of every head into fresh pages; see l2kv_page_compact."""
+    _call((_NATIVE or _token_calls()).page_compact, "l2kv_page_compact", K_c, stream, K_c, V_c, idx, sumsq_c, pages, cur_len_dev,
+          keep_dev, max_len, policy, pin, pages_out, len_out_dev, workspace)

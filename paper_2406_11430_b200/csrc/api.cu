@@ -79,6 +79,20 @@ int check_tokens(const l2kv_tokens* t, const l2kv_layout* lay, int heads, int n_
   return L2KV_OK;
 }
 
+// Tables of a paged cache, and the layout that goes with them.  `batch`: their sequences; `written`: the call writes them.
+int check_pages(const l2kv_layout* lay, const l2kv_pages* p, int batch, bool written) {
+  if (!p) return L2KV_ERR_INVALID_ARG;
+  if (lay->row_off_dev || p->table_cap < 0 || p->n_pages < 0) return L2KV_ERR_INVALID_ARG;
+  if (p->page_rows < 16 || p->page_rows > kMaxPageRows || (p->page_rows & (p->page_rows - 1))) return L2KV_ERR_UNSUPPORTED;
+  if ((int64_t)p->n_pages * p->page_rows > INT32_MAX) return L2KV_ERR_OUT_OF_RANGE;
+  if ((int64_t)p->n_pages * p->page_rows != lay->total_rows || (int64_t)p->table_cap * p->page_rows != lay->t_cap)
+    return L2KV_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(p->table_dev) | reinterpret_cast<uintptr_t>(p->room_dev)) & 3u) return L2KV_ERR_MISALIGNED;
+  const int64_t least = written ? p->table_cap : 0;
+  if ((batch > 1 && p->stride_b < least) || (lay->layers > 1 && p->stride_l < least)) return L2KV_ERR_INVALID_ARG;
+  return L2KV_OK;
+}
+
 bool empty(const l2kv_layout* a) { return a->batch == 0 || a->layers == 0 || a->kv_heads == 0; }
 
 }  // namespace
@@ -487,21 +501,23 @@ int l2kv_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, doubl
   return L2KV_OK;
 }
 
-int l2kv_rotary_write(const l2kv_tokens* q, const l2kv_tokens* k, const l2kv_tokens* v,
-                      const int32_t* tok_off_dev, int32_t n_tokens, const int32_t* pos_dev,
-                      const double* freq_dev, int32_t rot_dim, double rot_scale,
-                      const l2kv_tokens* q_out, void* K_c, void* V_c, int32_t* idx, float* sumsq_c,
-                      const l2kv_layout* lay, const int32_t* start_dev, int32_t* cur_len_dev,
-                      uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
-  const Range nvtx_range("l2kv_rotary_write");
+static int rotary_write_impl(uint32_t known_flags, const NormArgs* norm, const l2kv_pages* pages, const l2kv_tokens* q,
+                             const l2kv_tokens* k, const l2kv_tokens* v, const int32_t* tok_off_dev, int32_t n_tokens,
+                             const int32_t* pos_dev, const double* freq_dev, int32_t rot_dim, double rot_scale,
+                             const l2kv_tokens* q_out, void* K_c, void* V_c, int32_t* idx, float* sumsq_c,
+                             const l2kv_layout* lay, const int32_t* start_dev, int32_t* cur_len_dev, uint32_t flags,
+                             void* workspace, size_t workspace_bytes, void* stream) {
   int rc = check_layout(lay);
   if (rc != L2KV_OK) return rc;
-  if (flags & ~(uint32_t)(L2KV_TOKENS_LEN_PER_HEAD | L2KV_TOKENS_ROTARY_INTERLEAVED | L2KV_TOKENS_NO_LAUNCH)) return L2KV_ERR_INVALID_ARG;
+  if (pages && (rc = check_pages(lay, pages, lay->batch, false)) != L2KV_OK) return rc;
+  if (flags & ~(known_flags | L2KV_TOKENS_LEN_PER_HEAD | L2KV_TOKENS_ROTARY_INTERLEAVED | L2KV_TOKENS_NO_LAUNCH)) return L2KV_ERR_INVALID_ARG;
   if (n_tokens < 0 || rot_dim < 0 || !std::isfinite(rot_scale)) return L2KV_ERR_INVALID_ARG;
+  if (norm && (!(norm->eps >= 0.f) || !std::isfinite(norm->eps) || !std::isfinite(norm->offset))) return L2KV_ERR_INVALID_ARG;
   if (rot_dim > lay->head_dim || rot_dim % 16) return L2KV_ERR_UNSUPPORTED;
   if (empty(lay)) return L2KV_OK;
   if (!tok_off_dev || !start_dev || !cur_len_dev || start_dev == cur_len_dev || !K_c || !V_c || !workspace)
     return L2KV_ERR_INVALID_ARG;
+  if (pages && !pages->table_dev) return L2KV_ERR_INVALID_ARG;
   if (n_tokens > 0) {
     if (!pos_dev || (rot_dim > 0 && !freq_dev)) return L2KV_ERR_INVALID_ARG;
     if (lay->q_heads > 0) {
@@ -512,13 +528,51 @@ int l2kv_rotary_write(const l2kv_tokens* q, const l2kv_tokens* k, const l2kv_tok
     if ((rc = check_tokens(v, lay, lay->kv_heads, n_tokens)) != L2KV_OK) return rc;
   }
   if (!aligned16(K_c) || !aligned16(V_c) || !aligned16(workspace)) return L2KV_ERR_MISALIGNED;
+  if (norm && (!aligned16(norm->q_weight) || !aligned16(norm->k_weight))) return L2KV_ERR_MISALIGNED;
   if (workspace_bytes < (size_t)kStatusBytes) return L2KV_ERR_WORKSPACE_TOO_SMALL;
   if (flags & L2KV_TOKENS_NO_LAUNCH) return L2KV_ERR_INVALID_ARG;
-  return launch_rotary_write(make_view(q), make_view(k), make_view(v), make_view(q_out), tok_off_dev, n_tokens,
-                             pos_dev, freq_dev, rot_dim, rot_scale, (flags & L2KV_TOKENS_ROTARY_INTERLEAVED) != 0,
-                             K_c, V_c, idx, sumsq_c, make_geom(*lay), lay->dtype, start_dev, cur_len_dev,
-                             (flags & L2KV_TOKENS_LEN_PER_HEAD) != 0, static_cast<int32_t*>(workspace),
-                             static_cast<cudaStream_t>(stream));
+  const int interleaved = (flags & L2KV_TOKENS_ROTARY_INTERLEAVED) != 0, per_head = (flags & L2KV_TOKENS_LEN_PER_HEAD) != 0;
+  int32_t* const status = static_cast<int32_t*>(workspace);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (!norm)
+    return launch_rotary_write(make_view(q), make_view(k), make_view(v), make_view(q_out), tok_off_dev, n_tokens, pos_dev,
+                               freq_dev, rot_dim, rot_scale, interleaved, K_c, V_c, idx, sumsq_c, make_geom(*lay), lay->dtype,
+                               start_dev, cur_len_dev, per_head, status, s);
+  return launch_norm_rotary_write(make_view(q), make_view(k), make_view(v), make_view(q_out), tok_off_dev, n_tokens, pos_dev,
+                                  freq_dev, rot_dim, rot_scale, interleaved, *norm, K_c, V_c, idx, sumsq_c, make_geom(*lay),
+                                  lay->dtype, start_dev, cur_len_dev, per_head, status, s);
+}
+
+int l2kv_rotary_write(const l2kv_tokens* q, const l2kv_tokens* k, const l2kv_tokens* v,
+                      const int32_t* tok_off_dev, int32_t n_tokens, const int32_t* pos_dev,
+                      const double* freq_dev, int32_t rot_dim, double rot_scale,
+                      const l2kv_tokens* q_out, void* K_c, void* V_c, int32_t* idx, float* sumsq_c,
+                      const l2kv_layout* lay, const int32_t* start_dev, int32_t* cur_len_dev,
+                      uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+  const Range nvtx_range("l2kv_rotary_write");
+  return rotary_write_impl(0, nullptr, nullptr, q, k, v, tok_off_dev, n_tokens, pos_dev, freq_dev, rot_dim, rot_scale, q_out,
+                           K_c, V_c, idx, sumsq_c, lay, start_dev, cur_len_dev, flags, workspace, workspace_bytes, stream);
+}
+
+int l2kv_norm_rotary_write(const l2kv_tokens* q, const l2kv_tokens* k, const l2kv_tokens* v,
+                           const int32_t* tok_off_dev, int32_t n_tokens, const int32_t* pos_dev,
+                           const double* freq_dev, int32_t rot_dim, double rot_scale, const void* q_weight,
+                           const void* k_weight, float eps, float weight_offset, const l2kv_tokens* q_out, void* K_c,
+                           void* V_c, int32_t* idx, float* sumsq_c, const l2kv_layout* lay, const l2kv_pages* pages,
+                           const int32_t* start_dev, int32_t* cur_len_dev, uint32_t flags, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  const Range nvtx_range("l2kv_norm_rotary_write");
+  NormArgs norm{};
+  if (pages) norm.pages = make_pages(*pages);
+  norm.q_weight = q_weight;
+  norm.k_weight = k_weight;
+  norm.norm_q = (flags & L2KV_TOKENS_NORM_Q) != 0;
+  norm.norm_k = (flags & L2KV_TOKENS_NORM_K) != 0;
+  norm.eps = eps;
+  norm.offset = weight_offset;
+  return rotary_write_impl(L2KV_TOKENS_NORM_Q | L2KV_TOKENS_NORM_K, &norm, pages, q, k, v, tok_off_dev, n_tokens, pos_dev,
+                           freq_dev, rot_dim, rot_scale, q_out, K_c, V_c, idx, sumsq_c, lay, start_dev, cur_len_dev, flags,
+                           workspace, workspace_bytes, stream);
 }
 
 int l2kv_tree_commit(void* K_c, void* V_c, int32_t* idx, float* sumsq_c, const l2kv_layout* lay,
@@ -541,8 +595,8 @@ int l2kv_tree_commit(void* K_c, void* V_c, int32_t* idx, float* sumsq_c, const l
                             static_cast<int32_t*>(workspace), static_cast<cudaStream_t>(stream));
 }
 
-// Both masks of attention over a packed list of new tokens (tree: a bit per token and tail row).
-static int token_attention_impl(bool tree, const l2kv_tokens* q, const int32_t* tok_off_dev, int32_t n_tokens,
+// Both masks of attention over a packed list of new tokens (tree: a bit per token and tail row), and caches in pages.
+static int token_attention_impl(bool tree, const l2kv_pages* pages, const l2kv_tokens* q, const int32_t* tok_off_dev, int32_t n_tokens,
                                 const uint64_t* tree_mask_dev, int32_t mask_words, const void* K_c,
                                 const void* V_c, const l2kv_layout* lay, const int32_t* cur_len_dev,
                                 int32_t max_len, float scale, uint32_t flags, const l2kv_tokens* out,
@@ -551,6 +605,7 @@ static int token_attention_impl(bool tree, const l2kv_tokens* q, const int32_t* 
   if (rc != L2KV_OK) return rc;
   rc = check_groups(lay);
   if (rc != L2KV_OK) return rc;
+  if (pages && (rc = check_pages(lay, pages, lay->batch, false)) != L2KV_OK) return rc;
   if ((flags & ~(uint32_t)(L2KV_TOKENS_LEN_PER_HEAD | L2KV_TOKENS_NO_LAUNCH)) || n_tokens < 0 || max_len < 0 || !(scale == scale))
     return L2KV_ERR_INVALID_ARG;
   if (tree && mask_words < 1) return L2KV_ERR_INVALID_ARG;
@@ -559,7 +614,8 @@ static int token_attention_impl(bool tree, const l2kv_tokens* q, const int32_t* 
   if (empty(lay) || n_tokens == 0) return L2KV_OK;
   if ((rc = check_tokens(q, lay, lay->q_heads, n_tokens)) != L2KV_OK) return rc;
   if ((rc = check_tokens(out, lay, lay->q_heads, n_tokens)) != L2KV_OK) return rc;
-  if (!tok_off_dev || !K_c || !V_c || !cur_len_dev || (tree && !tree_mask_dev)) return L2KV_ERR_INVALID_ARG;
+  if (!tok_off_dev || !K_c || !V_c || !cur_len_dev || (tree && !tree_mask_dev) || (pages && !pages->table_dev))
+    return L2KV_ERR_INVALID_ARG;
   if (!aligned16(K_c) || !aligned16(V_c) || !aligned16(workspace)) return L2KV_ERR_MISALIGNED;
   if (tree && (reinterpret_cast<uintptr_t>(tree_mask_dev) & 7u)) return L2KV_ERR_MISALIGNED;
   if (workspace && workspace_bytes < (size_t)kStatusBytes) return L2KV_ERR_WORKSPACE_TOO_SMALL;
@@ -569,7 +625,7 @@ static int token_attention_impl(bool tree, const l2kv_tokens* q, const int32_t* 
                          LenView{cur_len_dev, (flags & L2KV_TOKENS_LEN_PER_HEAD) ? 1 : 0}, max_len,
                          sc * 1.4426950408889634f, lse_out,
                          tree ? reinterpret_cast<const uint32_t*>(tree_mask_dev) : nullptr, mask_words,
-                         static_cast<int32_t*>(workspace)};
+                         static_cast<int32_t*>(workspace), pages ? make_pages(*pages) : PageView{}};
   // scratch begins behind the status block and the completion counters of the other calls on this layout
   const size_t head = plan_workspace(*lay, 0).sumsq_off;
   const size_t room = workspace && workspace_bytes > head ? workspace_bytes - head : 0;
@@ -599,7 +655,7 @@ int l2kv_prompt_attention(const l2kv_tokens* q, const int32_t* tok_off_dev, int3
                           const l2kv_tokens* out, float* lse_out, void* workspace,
                           size_t workspace_bytes, void* stream) {
   const Range nvtx_range("l2kv_prompt_attention");
-  return token_attention_impl(false, q, tok_off_dev, n_tokens, nullptr, 0, K_c, V_c, lay, cur_len_dev, max_len,
+  return token_attention_impl(false, nullptr, q, tok_off_dev, n_tokens, nullptr, 0, K_c, V_c, lay, cur_len_dev, max_len,
                               scale, flags, out, lse_out, workspace, workspace_bytes, stream);
 }
 
@@ -609,8 +665,97 @@ int l2kv_tree_attention(const l2kv_tokens* q, const int32_t* tok_off_dev, int32_
                         int32_t max_len, float scale, uint32_t flags, const l2kv_tokens* out,
                         float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {
   const Range nvtx_range("l2kv_tree_attention");
-  return token_attention_impl(true, q, tok_off_dev, n_tokens, tree_mask_dev, mask_words, K_c, V_c, lay,
+  return token_attention_impl(true, nullptr, q, tok_off_dev, n_tokens, tree_mask_dev, mask_words, K_c, V_c, lay,
                               cur_len_dev, max_len, scale, flags, out, lse_out, workspace, workspace_bytes, stream);
+}
+
+int l2kv_paged_attention_workspace_bytes(const l2kv_layout* lay, const l2kv_pages* pages, int32_t n_tokens, int32_t max_len,
+                                         size_t* bytes) {
+  const int rc = l2kv_prompt_attention_workspace_bytes(lay, n_tokens, max_len, bytes);
+  return rc != L2KV_OK ? rc : check_pages(lay, pages, lay->batch, false);
+}
+
+int l2kv_paged_attention(const l2kv_tokens* q, const int32_t* tok_off_dev, int32_t n_tokens, const void* K_c,
+                         const void* V_c, const l2kv_layout* lay, const l2kv_pages* pages, const int32_t* cur_len_dev,
+                         int32_t max_len, float scale, uint32_t flags, const l2kv_tokens* out, float* lse_out, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  const Range nvtx_range("l2kv_paged_attention");
+  if (!pages) return L2KV_ERR_INVALID_ARG;
+  return token_attention_impl(false, pages, q, tok_off_dev, n_tokens, nullptr, 0, K_c, V_c, lay, cur_len_dev, max_len,
+                              scale, flags, out, lse_out, workspace, workspace_bytes, stream);
+}
+
+// What the calls that write tables have in common.
+static int check_table_call(const l2kv_layout* lay, const l2kv_pages* pages, int batch_out, const l2kv_pages* pages_out, uint32_t flags) {
+  int rc = check_layout(lay);
+  if (rc != L2KV_OK) return rc;
+  if ((rc = check_pages(lay, pages, lay->batch, false)) != L2KV_OK) return rc;
+  if ((flags & ~(uint32_t)L2KV_TOKENS_NO_LAUNCH) || batch_out < 0) return L2KV_ERR_INVALID_ARG;
+  if ((rc = check_pages(lay, pages_out, batch_out, true)) != L2KV_OK) return rc;
+  if (pages->page_rows != pages_out->page_rows) return L2KV_ERR_INVALID_ARG;
+  const int64_t most = 1ll << kClaimBits;
+  if ((int64_t)lay->batch * lay->layers > most || (int64_t)batch_out * lay->layers > most || lay->kv_heads > (1 << 18))
+    return L2KV_ERR_OUT_OF_RANGE;
+  return L2KV_OK;
+}
+
+static size_t page_scratch_head(const l2kv_layout* lay) { return plan_workspace(*lay, 0).sumsq_off; }
+
+int l2kv_page_workspace_bytes(const l2kv_layout* lay, const l2kv_pages* pages, int32_t batch_out, int32_t max_len, size_t* bytes) {
+  if (!bytes) return L2KV_ERR_INVALID_ARG;
+  int rc = check_layout(lay);
+  if (rc != L2KV_OK) return rc;
+  if ((rc = check_pages(lay, pages, lay->batch, false)) != L2KV_OK) return rc;
+  if (batch_out < 0 || max_len < 0) return L2KV_ERR_INVALID_ARG;
+  if (max_len > lay->t_cap) return L2KV_ERR_OUT_OF_RANGE;
+  const long long in = (long long)lay->batch * lay->layers, out = (long long)batch_out * lay->layers;
+  *bytes = page_scratch_head(lay) + plan_pages(in > out ? in : out, max_len > 0 ? in * lay->kv_heads : 0, pages->n_pages, max_len).total;
+  return L2KV_OK;
+}
+
+int l2kv_page_update(void* K_c, void* V_c, int32_t* idx, float* sumsq_c, const l2kv_layout* lay, const l2kv_pages* pages,
+                     const int32_t* parent_dev, const int32_t* keep_dev, const int32_t* grow_dev, int32_t batch_out,
+                     const uint8_t* pin_dev, const l2kv_pages* pages_out, int32_t* n_free_out, uint32_t flags,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  const Range nvtx_range("l2kv_page_update");
+  const int rc = check_table_call(lay, pages, batch_out, pages_out, flags);
+  if (rc != L2KV_OK) return rc;
+  if (batch_out == 0 || lay->layers == 0) return L2KV_OK;
+  if (!K_c || !V_c || (lay->batch > 0 && !pages->table_dev) || !pages_out->table_dev || pages->table_dev == pages_out->table_dev ||
+      !parent_dev || !keep_dev || !grow_dev || !workspace || pages_out->room_dev == keep_dev)
+    return L2KV_ERR_INVALID_ARG;
+  if (!aligned16(K_c) || !aligned16(V_c) || !aligned16(workspace)) return L2KV_ERR_MISALIGNED;
+  const size_t head = page_scratch_head(lay);
+  if (workspace_bytes < head + plan_pages((long long)batch_out * lay->layers, 0, pages->n_pages, 0).total) return L2KV_ERR_WORKSPACE_TOO_SMALL;
+  if (flags & L2KV_TOKENS_NO_LAUNCH) return L2KV_ERR_INVALID_ARG;
+  const PageUpdate a{make_pages(*pages), make_pages(*pages_out), pages_out->table_dev, pages_out->room_dev, lay->batch, batch_out,
+                     lay->layers, parent_dev, keep_dev, grow_dev, pin_dev, n_free_out, static_cast<int32_t*>(workspace)};
+  return launch_page_update(a, K_c, V_c, idx, sumsq_c, make_geom(*lay), lay->dtype, static_cast<char*>(workspace) + head,
+                            static_cast<cudaStream_t>(stream));
+}
+
+int l2kv_page_compact(void* K_c, void* V_c, int32_t* idx, float* sumsq_c, const l2kv_layout* lay, const l2kv_pages* pages,
+                      const int32_t* len_dev, const int32_t* keep_dev, int32_t max_len, int32_t policy, const uint8_t* pin_dev,
+                      const l2kv_pages* pages_out, int32_t* len_out_dev, uint32_t flags, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+  const Range nvtx_range("l2kv_page_compact");
+  const int rc = check_table_call(lay, pages, lay ? lay->batch : 0, pages_out, flags);
+  if (rc != L2KV_OK) return rc;
+  if (max_len < 0 || (policy != L2KV_KEEP_LOWEST_NORM && policy != L2KV_KEEP_HIGHEST_NORM)) return L2KV_ERR_INVALID_ARG;
+  if (max_len > lay->t_cap) return L2KV_ERR_OUT_OF_RANGE;
+  if (empty(lay)) return L2KV_OK;
+  if (!K_c || !V_c || !sumsq_c || !pages->table_dev || !pages_out->table_dev || pages->table_dev == pages_out->table_dev || !len_dev ||
+      !keep_dev || !len_out_dev || !workspace || pages_out->room_dev == keep_dev || len_out_dev == keep_dev)
+    return L2KV_ERR_INVALID_ARG;
+  if (!aligned16(K_c) || !aligned16(V_c) || !aligned16(workspace)) return L2KV_ERR_MISALIGNED;
+  const size_t head = page_scratch_head(lay);
+  const long long entries = (long long)lay->batch * lay->layers;
+  if (workspace_bytes < head + plan_pages(entries, entries * lay->kv_heads, pages->n_pages, max_len).total) return L2KV_ERR_WORKSPACE_TOO_SMALL;
+  if (flags & L2KV_TOKENS_NO_LAUNCH) return L2KV_ERR_INVALID_ARG;
+  const PageCompact a{make_pages(*pages), make_pages(*pages_out), pages_out->table_dev, pages_out->room_dev, lay->batch, lay->layers,
+                      lay->kv_heads, max_len, policy, len_dev, keep_dev, len_out_dev, pin_dev, static_cast<int32_t*>(workspace)};
+  return launch_page_compact(a, K_c, V_c, idx, sumsq_c, make_geom(*lay), lay->dtype, static_cast<char*>(workspace) + head,
+                             static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -63,12 +63,13 @@ inline bool encode_bf16_map(CUtensorMap* map, int rank, const void* base, const 
 }
 
 // The rank-5 tensor map (head_dim, token, kv head, layer, batch) of a bf16 cache with a box of 64
-// elements x box_rows tokens.  Returns false as above (callers then use another path).
-inline bool make_cache_map(CUtensorMap* map, const void* base, const Geom& g, int box_rows) {
+// elements x box_rows tokens; `pool`: of the rows of all pages of a paged cache, which are laid out as a packed
+// cache's.  Returns false as above (callers then use another path).
+inline bool make_cache_map(CUtensorMap* map, const void* base, const Geom& g, int box_rows, bool pool = false) {
   cuuint64_t dims[5] = {(cuuint64_t)g.D, (cuuint64_t)g.t_cap, (cuuint64_t)g.H, (cuuint64_t)g.L, (cuuint64_t)g.B};
   cuuint64_t strides[4] = {(cuuint64_t)g.st * 2, (cuuint64_t)g.sh * 2, (cuuint64_t)g.sl * 2,
                            (cuuint64_t)g.sb * 2};
-  if (g.row_off) {
+  if (g.row_off || pool) {
     // packed cache: one [H, total_rows, 128] plane; the two outer dimensions have extent 1
     if (g.st <= 0 || g.sh <= 0 || g.total_rows <= 0 || g.total_rows > 0x7fffffffLL) return false;
     dims[1] = (cuuint64_t)g.total_rows; dims[3] = 1; dims[4] = 1;

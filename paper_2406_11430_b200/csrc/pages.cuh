@@ -1,0 +1,74 @@
+// Caches in pages: where a row lies, and the calls that work on the tables.
+#pragma once
+
+#include "common.cuh"
+
+namespace l2kv {
+
+constexpr int kMaxPageRows = 1024;
+constexpr int kClaimBits = 20;                           // (b, l) pairs of a call that works on tables: 2^20 at most
+
+// The tables of a paged cache: row t of (b, l) is row  table[b, l][t >> shift] << shift | t & (page rows - 1)  of the
+// pool, for every head.  Entries come from device memory: whoever uses one checks it against n.
+struct PageView {
+  const int32_t* table;
+  long long sb, sl;                                      // strides of the table, in entries
+  int cap, shift, n;                                     // entries per (b, l); log2 of a page's rows; pages of the pool
+  const int32_t* room;                                   // [B, L] rows that (b, l) may write, or null: all of its table
+  __device__ __forceinline__ const int32_t* of(int b, int l) const { return table + b * sb + l * sl; }
+  __device__ __forceinline__ int rows() const { return 1 << shift; }
+  __device__ __forceinline__ bool valid(int page) const { return page >= 0 && page < n; }
+};
+
+inline PageView make_pages(const l2kv_pages& p) {
+  int shift = 0;
+  while ((1 << shift) < p.page_rows) ++shift;
+  return PageView{p.table_dev, p.stride_b, p.stride_l, p.table_cap, shift, p.n_pages, p.room_dev};
+}
+
+// What page_update and page_compact share: which pages are held, and which free ones each (b, l) gets.
+struct PagePlan {
+  size_t mark_off;       // uint32 [n_pages]            highest claim on a page; 0: free
+  size_t used_off;       // int32  [groups]             pages held, per group of pages
+  size_t order_off;      // int32  [n_pages]            the free pages in ascending order
+  size_t need_off;       // int2   [entries]            what (b, l) gets: where its pages begin in that order, or -1; a number more
+  size_t key_off;        // float  [units][ld]          page_compact: keys in row order
+  size_t unit_off;       // UnitRec [units]
+  size_t chunk_off;      // int2   [units][n_chunks]
+  size_t total;
+  long long ld;
+  int n_chunks;
+};
+constexpr int kPageBlock = 4096;                         // pages per block of the scan
+PagePlan plan_pages(long long entries, long long units, int n_pages, int max_len);
+
+struct PageUpdate {
+  PageView in, out;                                      // out.table is written through out_table
+  int32_t* out_table;
+  int32_t* out_room;
+  int B_in, B, L;
+  const int32_t* parent;
+  const int32_t* keep;                                   // [B, L]
+  const int32_t* grow;                                   // [B]
+  const uint8_t* pin;                                    // [n_pages] or null
+  int32_t* n_free;                                       // or null
+  int32_t* status;
+};
+int launch_page_update(const PageUpdate& a, void* K, void* V, int32_t* idx, float* sumsq, const Geom& g, int dtype,
+                       char* scratch, cudaStream_t s);
+
+struct PageCompact {
+  PageView in, out;
+  int32_t* out_table;
+  int32_t* out_room;
+  int B, L, H, max_len, policy;
+  const int32_t* len;                                    // [B, L]
+  const int32_t* keep;                                   // [B, L]
+  int32_t* len_out;                                      // [B, L]
+  const uint8_t* pin;
+  int32_t* status;
+};
+int launch_page_compact(const PageCompact& a, void* K, void* V, int32_t* idx, float* sumsq, const Geom& g, int dtype,
+                        char* scratch, cudaStream_t s);
+
+}  // namespace l2kv

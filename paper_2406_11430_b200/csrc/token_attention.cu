@@ -356,7 +356,7 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return d;
 }
-template <int D, bool TREE>
+template <int D, bool TREE, bool PAGED = false>
 __global__ void __launch_bounds__(kTaThreads, 1)
 token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__ CUtensorMap map_q,
                        const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
@@ -488,6 +488,65 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
     }
     return ok;
   };
+  // The same over pages, by the whole warp: lane i holds entry i of 32 of the table's, for K and, behind it, for V,
+  // and asked for the 32 after them when it got these, so that no copy waits for an entry.  A tile is one box or, of pages
+  // shorter than it, several, a lane's each; what lies behind the item's rows, or in a page that is none, is filled with zeros
+  // (a box outside the pool), and such pages are told.
+  [[maybe_unused]] auto fetch_pages = [&](const TaItem& it) {
+    const PageView& pages = a.pages;
+    const int32_t* const table = pages.of(it.b, it.l);
+    const int places = ta_places(it.n, it.pair), ahead = it.pair ? 2 : 4;
+    const int box = min(kTaSub, pages.rows()), n_boxes = kTaSub / box;          // boxes of a tile's half row
+    const int n_ids = (it.end + pages.rows() - 1) >> pages.shift;              // pages with rows that a token sees
+    const int of_half = lane / n_boxes, of_box = lane % n_boxes;
+    auto ids = [&](int chunk) {
+      const int p = chunk * 32 + lane;
+      const int id = p < n_ids ? table[p] : -1;
+      const bool bad = p < n_ids && !pages.valid(id);
+      if (bad && a.status) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
+      return bad ? -1 : id;
+    };
+    int k_chunk = it.row0 >> pages.shift >> 5, v_chunk = k_chunk;
+    int k_ids = ids(k_chunk), v_ids = k_ids, more_ids = ids(k_chunk + 1);
+    bool ok = true;
+    auto one = [&](bool is_k, int g) {
+      const uint32_t at = pos + g, full = is_k ? k_full(at) : v_full(at), empty = is_k ? k_empty(at) : v_empty(at);
+      if (at >= SLOTS) ok = __all_sync(0xffffffffu, wait(empty, (at / SLOTS - 1) & 1u));
+      if (!ok) return;
+      if (g >= it.n) {                                   // an empty place: landed and given back at once
+        if (lane == 0) {
+          mbar_arrive(empty);
+          mbar_arrive(full);
+          mbar_arrive(empty);
+        }
+        __syncwarp();
+        return;
+      }
+      const int t = it.row0 + g * kTaSub, page = t >> pages.shift;
+      if (is_k) {
+        if (page >> 5 != k_chunk) { ++k_chunk; k_ids = more_ids; more_ids = ids(k_chunk + 1); }
+      } else if (page >> 5 != v_chunk) {                 // (V is at most 16 pages behind K)
+        ++v_chunk;
+        v_ids = k_ids;
+      }
+      if (lane == 0) {
+        if (!it.pair) mbar_arrive(empty);                // for the chain that does not use it
+        mbar_expect_tx(full, TILE);
+      }
+      const int id = __shfl_sync(0xffffffffu, is_k ? k_ids : v_ids, (page + of_box) & 31);
+      __syncwarp();
+      if (of_half < D / 64) {
+        const int row = id < 0 ? pages.n << pages.shift : (id << pages.shift) + (t & (pages.rows() - 1));
+        tma_load_5d((is_k ? s_k : s_v) + (at % SLOTS) * TILE + of_half * kTaSubHalf + of_box * box * 128, is_k ? &map_k : &map_v, full,
+                    of_half * 64, row, it.h, 0, 0);
+      }
+    };
+    for (int g = 0; ok && g < places + ahead; ++g) {
+      if (g < places) one(true, g);
+      if (ok && g >= ahead) one(false, g - ahead);
+    }
+    return ok;
+  };
   // After a failure: copies that may still be in flight, the last ones of every slot.
   auto drain = [&]() {
     for (int i = 0; i < SLOTS; ++i)
@@ -542,9 +601,10 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
             for (int c = 0; c < D / 64; ++c)
               tma_load_4d(s_q + t * QTILE + c * kTaHalf, &map_q, q_full, c * 64, it.h * A.G, it.tok0 + t * A.QT, it.l);
         }
-        ok = ok && fetch(it);
+        if constexpr (!PAGED) ok = ok && fetch(it);
       }
       ok = __shfl_sync(0xffffffffu, ok, 0);
+      if constexpr (PAGED) ok = ok && fetch_pages(it);
       pos += ta_places(it.n, it.pair);
       ++n_q;
     }
@@ -993,16 +1053,17 @@ static bool make_query_map(CUtensorMap* map, const TokenAttention& a) {
   return encode_bf16_map(map, 4, a.q.p, dims, strides, box);
 }
 
-template <int D, bool TREE>
+template <int D, bool TREE, bool PAGED = false>
 static int launch_ta(const TaArgs& A, const void* K, const void* V, long long items, cudaStream_t s) {
   const TokenAttention& a = A.a;
   alignas(64) CUtensorMap map_q, map_k, map_v;
   std::memset(&map_q, 0, sizeof map_q);
   std::memset(&map_k, 0, sizeof map_k);
   std::memset(&map_v, 0, sizeof map_v);
-  if (!make_query_map(&map_q, a) || !make_cache_map(&map_k, K, a.g, kTaSub) || !make_cache_map(&map_v, V, a.g, kTaSub))
+  const int box = PAGED ? std::min(kTaSub, 1 << a.pages.shift) : kTaSub;
+  if (!make_query_map(&map_q, a) || !make_cache_map(&map_k, K, a.g, box, PAGED) || !make_cache_map(&map_v, V, a.g, box, PAGED))
     return L2KV_ERR_UNSUPPORTED;
-  auto kern = token_attention_kernel<D, TREE>;
+  auto kern = token_attention_kernel<D, TREE, PAGED>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTaSmem<D>) != cudaSuccess)
     return L2KV_ERR_CUDA;
   const unsigned grid = (unsigned)std::min<long long>(kTaGrid, A.plan ? kTaGrid : items);
@@ -1027,6 +1088,8 @@ int launch_token_attention(const TokenAttention& a, const void* K, const void* V
     A.part = reinterpret_cast<float*>(scratch + kTaPlanBytes);
     A.part_lse = A.part + (size_t)2 * kTaGrid * room.slot_rows * a.g.D;
   }
+  if (a.pages.table)
+    return a.g.D == 128 ? launch_ta<128, false, true>(A, K, V, room.items, s) : launch_ta<64, false, true>(A, K, V, room.items, s);
   if (a.g.D == 128)
     return a.mask ? launch_ta<128, true>(A, K, V, room.items, s) : launch_ta<128, false>(A, K, V, room.items, s);
   return a.mask ? launch_ta<64, true>(A, K, V, room.items, s) : launch_ta<64, false>(A, K, V, room.items, s);

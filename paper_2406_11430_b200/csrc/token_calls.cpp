@@ -18,6 +18,12 @@ decltype(&l2kv_tree_commit) fn_tree_commit;
 decltype(&l2kv_prompt_attention) fn_prompt_attention;
 decltype(&l2kv_tree_attention) fn_tree_attention;
 decltype(&l2kv_prompt_attention_workspace_bytes) fn_workspace_bytes;
+decltype(&l2kv_norm_rotary_write) fn_norm_rotary_write;
+decltype(&l2kv_paged_attention) fn_paged_attention;
+decltype(&l2kv_paged_attention_workspace_bytes) fn_paged_workspace_bytes;
+decltype(&l2kv_page_update) fn_page_update;
+decltype(&l2kv_page_compact) fn_page_compact;
+decltype(&l2kv_page_workspace_bytes) fn_page_workspace_bytes;
 
 // A tensor argument; null for None.
 const at::Tensor* tensor(PyObject* o, const char* what, bool may_be_none = false) {
@@ -170,26 +176,74 @@ PyObject* guarded(F&& f) {
   return nullptr;
 }
 
-PyObject* rotary_write(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
+// The tables of a paged cache, held for a call, and as the library takes them.
+struct Tables {
+  Attr table, room;
+  const at::Tensor *t = nullptr, *r = nullptr;
+  l2kv_pages c{};
+  void get(PyObject* pages) {
+    table.get(pages, "table");
+    room.get(pages, "room");
+    const Attr rows(pages, "page_rows"), n(pages, "n_pages");
+    t = tensor(table.o, "pages.table");
+    r = tensor(room.o, "pages.room", true);
+    if (t->scalar_type() != at::kInt || t->dim() != 3 || (t->size(2) > 1 && t->stride(2) != 1))
+      throw Bad{"pages.table must be int32 [B, L, entries] with the entries contiguous"};
+    entries(r, t->size(0) * t->size(1), "pages.room");
+    c.table_dev = static_cast<int32_t*>(t->data_ptr());
+    c.stride_b = t->stride(0); c.stride_l = t->stride(1);
+    c.table_cap = narrow(t->size(2), "the entries of a table");
+    c.page_rows = integer32(rows.o, "pages.page_rows");
+    c.n_pages = integer32(n.o, "pages.n_pages");
+    c.room_dev = static_cast<int32_t*>(ptr(r));
+  }
+};
+
+// Geometry of a pool of pages, as its tables describe it.
+l2kv_layout layout(const at::Tensor& K, int64_t q_heads, PyObject* pages, Tables* held) {
+  held->get(pages);
+  const l2kv_pages& p = held->c;
+  l2kv_layout a{};
+  a.dtype = dtype_of(K);
+  a.q_heads = narrow(q_heads, "the number of query heads");
+  a.total_rows = (int64_t)p.n_pages * p.page_rows;
+  if (K.dim() != 3 || K.stride(2) != 1 || K.size(1) != a.total_rows)
+    throw Bad{"paged cache must be [Hkv, n_pages * page_rows, D] with D contiguous"};
+  a.batch = narrow(held->t->size(0), "the sequences of a table"); a.layers = narrow(held->t->size(1), "the layers of a table");
+  a.kv_heads = narrow(K.size(0), "a cache's size"); a.head_dim = narrow(K.size(2), "a cache's size");
+  a.t_cap = narrow((int64_t)p.table_cap * p.page_rows, "the rows of a table");
+  a.stride_h = K.stride(0); a.stride_t = K.stride(1);
+  return a;
+}
+int64_t pool_rows(const l2kv_layout& a) { return a.kv_heads > 0 && a.total_rows > 0 ? (int64_t)a.kv_heads * a.total_rows : -1; }
+
+// rotary_write, and, with 7 arguments more, norm_rotary_write.
+PyObject* rotary_write_of(bool norm, PyObject* const* v, Py_ssize_t n_args) {
   return guarded([&]() -> PyObject* {
-    check_count(n_args, 19);
+    check_count(n_args, norm ? 26 : 19);
     const at::Tensor *q = tensor(v[0], "q", true), *k = tensor(v[1], "k"), *val = tensor(v[2], "v"),
                      *off = tensor(v[3], "tok_off"), *pos = tensor(v[4], "pos", true), *freq = tensor(v[5], "freq", true),
                      *q_out = tensor(v[6], "q_out", true), *K = tensor(v[7], "K_c"), *V = tensor(v[8], "V_c", true),
                      *idx = tensor(v[9], "idx", true), *key = tensor(v[10], "sumsq_c", true),
                      *start = tensor(v[11], "start_dev"), *cur = tensor(v[12], "cur_len_dev"), *ws = tensor(v[13], "workspace");
     const bool interleaved = truth(v[14]), per_head = truth(v[17]);
+    PyObject* const pages = norm ? v[18] : Py_None;
+    void* const stream = reinterpret_cast<void*>(integer(v[n_args - 1]));
     Ranges held;
-    const l2kv_layout a = layout(*K, q ? heads_of(*q) : 0, v[16], &held);
-    one_device(*K, q, k, val, off, pos, freq, q_out, V, idx, key, start, cur, ws);
+    Tables tables;
+    const bool paged = pages != Py_None;
+    if (paged && v[16] != Py_None) throw Bad{"a cache has rows or pages, not both"};
+    const int64_t q_heads = q ? heads_of(*q) : 0;
+    const l2kv_layout a = paged ? layout(*K, q_heads, pages, &tables) : layout(*K, q_heads, v[16], &held);
+    one_device(*K, q, k, val, off, pos, freq, q_out, V, idx, key, start, cur, ws, tables.t, tables.r);
     same_geometry(*K, V);
     heads_of(*k);
     const int32_t n = narrow(k->size(-3), "the number of tokens");
     entries(off, (int64_t)a.batch + 1, "tok_off");
     entries(pos, n, "pos");
     entries(freq, -1, "freq", at::kDouble);
-    entries(idx, n_rows(a), "idx");
-    entries(key, n_rows(a), "sumsq_c", at::kFloat);
+    entries(idx, paged ? pool_rows(a) : n_rows(a), "idx");
+    entries(key, paged ? pool_rows(a) : n_rows(a), "sumsq_c", at::kFloat);
     entries(start, n_lengths(a, per_head), "start_dev");
     entries(cur, n_lengths(a, per_head), "cur_len_dev");
     entries(ws, -1, "workspace", at::kByte);
@@ -197,13 +251,96 @@ PyObject* rotary_write(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     if (q) tq = tokens(*q, a, n, a.q_heads);
     if (q_out) to = tokens(*q_out, a, n, a.q_heads);
     const l2kv_tokens tk = tokens(*k, a, n, a.kv_heads), tv = tokens(*val, a, n, a.kv_heads);
-    return unlocked(fn_rotary_write,
-        q ? &tq : nullptr, &tk, &tv, static_cast<const int32_t*>(ptr(off)), n, static_cast<const int32_t*>(ptr(pos)),
-        static_cast<const double*>(ptr(freq)), freq ? narrow(2 * freq->numel(), "the number of frequencies") : 0,
-        real(v[15]), q_out ? &to : nullptr, ptr(K), ptr(V), static_cast<int32_t*>(ptr(idx)), static_cast<float*>(ptr(key)), &a,
-        static_cast<const int32_t*>(ptr(start)), static_cast<int32_t*>(ptr(cur)),
-        flags_of(*K, per_head) | (interleaved ? L2KV_TOKENS_ROTARY_INTERLEAVED : 0), ptr(ws),
-        (size_t)ws->numel(), reinterpret_cast<void*>(integer(v[18])));
+    const int32_t rot_dim = freq ? narrow(2 * freq->numel(), "the number of frequencies") : 0;
+    const double scale = real(v[15]);
+    const uint32_t flags = flags_of(*K, per_head) | (interleaved ? L2KV_TOKENS_ROTARY_INTERLEAVED : 0);
+    const int32_t *p_off = static_cast<const int32_t*>(ptr(off)), *p_pos = static_cast<const int32_t*>(ptr(pos)),
+                  *p_start = static_cast<const int32_t*>(ptr(start));
+    const double* const p_freq = static_cast<const double*>(ptr(freq));
+    int32_t *const p_idx = static_cast<int32_t*>(ptr(idx)), *const p_cur = static_cast<int32_t*>(ptr(cur));
+    float* const p_key = static_cast<float*>(ptr(key));
+    if (!norm)
+      return unlocked(fn_rotary_write, q ? &tq : nullptr, &tk, &tv, p_off, n, p_pos, p_freq, rot_dim, scale, q_out ? &to : nullptr,
+                      ptr(K), ptr(V), p_idx, p_key, &a, p_start, p_cur, flags, ptr(ws), (size_t)ws->numel(), stream);
+    const at::Tensor *qw = tensor(v[19], "q_weight", true), *kw = tensor(v[20], "k_weight", true);
+    const bool norm_q = truth(v[21]), norm_k = truth(v[22]);
+    const float eps = (float)real(v[23]), offset = (float)real(v[24]);
+    one_device(*K, qw, kw);
+    entries(qw, a.head_dim, "q_weight", K->scalar_type());
+    entries(kw, a.head_dim, "k_weight", K->scalar_type());
+    return unlocked(fn_norm_rotary_write, q ? &tq : nullptr, &tk, &tv, p_off, n, p_pos, p_freq, rot_dim, scale,
+                    static_cast<const void*>(ptr(qw)), static_cast<const void*>(ptr(kw)), eps, offset, q_out ? &to : nullptr, ptr(K), ptr(V),
+                    p_idx, p_key, &a, paged ? &tables.c : nullptr, p_start, p_cur,
+                    flags | (norm_q ? L2KV_TOKENS_NORM_Q : 0) | (norm_k ? L2KV_TOKENS_NORM_K : 0), ptr(ws), (size_t)ws->numel(), stream);
+  });
+}
+PyObject* rotary_write(PyObject*, PyObject* const* v, Py_ssize_t n) { return rotary_write_of(false, v, n); }
+PyObject* norm_rotary_write(PyObject*, PyObject* const* v, Py_ssize_t n) { return rotary_write_of(true, v, n); }
+
+// (K, V, idx, sumsq, pages, parent, keep, grow, pages_out, pin, n_free, workspace, stream)
+PyObject* page_update(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
+  return guarded([&]() -> PyObject* {
+    check_count(n_args, 13);
+    const at::Tensor *K = tensor(v[0], "K_c"), *V = tensor(v[1], "V_c", true), *idx = tensor(v[2], "idx", true),
+                     *key = tensor(v[3], "sumsq_c", true), *parent = tensor(v[5], "parent"), *keep = tensor(v[6], "keep"),
+                     *grow = tensor(v[7], "grow"), *pin = tensor(v[9], "pin", true), *n_free = tensor(v[10], "n_free_out", true),
+                     *ws = tensor(v[11], "workspace");
+    Tables in, out;
+    const l2kv_layout a = layout(*K, 0, v[4], &in);
+    out.get(v[8]);
+    one_device(*K, V, idx, key, parent, keep, grow, pin, n_free, ws, in.t, in.r, out.t, out.r);
+    same_geometry(*K, V);
+    if (out.t->size(1) != a.layers) throw Bad{"tables differ in layers"};
+    const int32_t B = narrow(out.t->size(0), "the sequences of a table");
+    entries(idx, pool_rows(a), "idx");
+    entries(key, pool_rows(a), "sumsq_c", at::kFloat);
+    entries(parent, B, "parent");
+    entries(keep, (int64_t)B * a.layers, "keep");
+    entries(grow, B, "grow");
+    entries(pin, in.c.n_pages, "pin", at::kByte);
+    entries(n_free, 1, "n_free_out");
+    entries(ws, -1, "workspace", at::kByte);
+    return unlocked(fn_page_update, ptr(K), ptr(V), static_cast<int32_t*>(ptr(idx)), static_cast<float*>(ptr(key)), &a, &in.c,
+                    static_cast<const int32_t*>(ptr(parent)), static_cast<const int32_t*>(ptr(keep)), static_cast<const int32_t*>(ptr(grow)),
+                    B, static_cast<const uint8_t*>(ptr(pin)), &out.c, static_cast<int32_t*>(ptr(n_free)), flags_of(*K, false), ptr(ws),
+                    (size_t)ws->numel(), reinterpret_cast<void*>(integer(v[12])));
+  });
+}
+
+// (K, V, idx, sumsq, pages, len, keep, max_len, policy, pin, pages_out, len_out, workspace, stream)
+PyObject* page_compact(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
+  return guarded([&]() -> PyObject* {
+    check_count(n_args, 14);
+    const at::Tensor *K = tensor(v[0], "K_c"), *V = tensor(v[1], "V_c", true), *idx = tensor(v[2], "idx", true),
+                     *key = tensor(v[3], "sumsq_c", true), *len = tensor(v[5], "cur_len_dev"), *keep = tensor(v[6], "keep_dev"),
+                     *pin = tensor(v[9], "pin", true), *len_out = tensor(v[11], "len_out_dev"), *ws = tensor(v[12], "workspace");
+    Tables in, out;
+    const l2kv_layout a = layout(*K, 0, v[4], &in);
+    out.get(v[10]);
+    one_device(*K, V, idx, key, len, keep, pin, len_out, ws, in.t, in.r, out.t, out.r);
+    same_geometry(*K, V);
+    if (out.t->size(0) != a.batch || out.t->size(1) != a.layers) throw Bad{"tables differ in sequences or layers"};
+    entries(idx, pool_rows(a), "idx");
+    entries(key, pool_rows(a), "sumsq_c", at::kFloat);
+    for (const at::Tensor* t : {len, keep, len_out}) entries(t, n_lengths(a, false), "cur_len_dev, keep_dev and len_out_dev");
+    entries(pin, in.c.n_pages, "pin", at::kByte);
+    entries(ws, -1, "workspace", at::kByte);
+    return unlocked(fn_page_compact, ptr(K), ptr(V), static_cast<int32_t*>(ptr(idx)), static_cast<float*>(ptr(key)), &a, &in.c,
+                    static_cast<const int32_t*>(ptr(len)), static_cast<const int32_t*>(ptr(keep)), integer32(v[7], "max_len"),
+                    integer32(v[8], "policy"), static_cast<const uint8_t*>(ptr(pin)), &out.c, static_cast<int32_t*>(ptr(len_out)),
+                    flags_of(*K, false), ptr(ws), (size_t)ws->numel(), reinterpret_cast<void*>(integer(v[13])));
+  });
+}
+
+// (K_c, pages, batch_out, max_len) -> bytes, or a negative status
+PyObject* page_workspace_bytes(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
+  return guarded([&]() -> PyObject* {
+    check_count(n_args, 4);
+    Tables in;
+    const l2kv_layout a = layout(*tensor(v[0], "K_c"), 0, v[1], &in);
+    size_t bytes = 0;
+    const int rc = fn_page_workspace_bytes(&a, &in.c, v[2] == Py_None ? a.batch : integer32(v[2], "batch_out"), integer32(v[3], "max_len"), &bytes);
+    return PyLong_FromLongLong(rc == L2KV_OK ? (long long)bytes : rc);
   });
 }
 
@@ -238,26 +375,32 @@ PyObject* tree_commit(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
 
 PyObject* attention(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
   return guarded([&]() -> PyObject* {
-    check_count(n_args, 14);
+    check_count(n_args, 15);
     const at::Tensor *q = tensor(v[0], "q"), *off = tensor(v[1], "tok_off"), *mask = tensor(v[2], "tree_mask", true),
                      *K = tensor(v[3], "K_c"), *V = tensor(v[4], "V_c", true), *cur = tensor(v[5], "cur_len_dev"),
                      *out = tensor(v[7], "out"), *lse = tensor(v[8], "lse_out", true), *ws = tensor(v[10], "workspace", true);
     const bool per_head = truth(v[12]);
     Ranges held;
-    const l2kv_layout a = layout(*K, heads_of(*q), v[11], &held);
+    Tables tables;
+    const bool paged = v[13] != Py_None;
+    const l2kv_layout a = paged ? layout(*K, heads_of(*q), v[13], &tables) : layout(*K, heads_of(*q), v[11], &held);
     const int32_t n = narrow(q->size(-3), "the number of tokens");
-    one_device(*K, q, off, mask, V, cur, out, lse, ws);
+    one_device(*K, q, off, mask, V, cur, out, lse, ws, tables.t, tables.r);
     same_geometry(*K, V);
     entries(off, (int64_t)a.batch + 1, "tok_off");
     entries(cur, n_lengths(a, per_head), "cur_len_dev");
     entries(lse, (int64_t)a.layers * n * a.q_heads, "lse_out", at::kFloat);
     entries(ws, -1, "workspace", at::kByte);
     const l2kv_tokens tq = tokens(*q, a, n, a.q_heads), to = tokens(*out, a, n, a.q_heads);
-    void* stream = reinterpret_cast<void*>(integer(v[13]));
+    void* stream = reinterpret_cast<void*>(integer(v[14]));
     const int32_t max_len = integer32(v[6], "max_len");
     const float scale = (float)real(v[9]);
     const uint32_t flags = flags_of(*K, per_head);
     const size_t ws_bytes = ws ? (size_t)ws->numel() : 0;
+    if (paged)
+      return unlocked(fn_paged_attention,
+          &tq, static_cast<const int32_t*>(ptr(off)), n, ptr(K), ptr(V), &a, &tables.c, static_cast<const int32_t*>(ptr(cur)),
+          max_len, scale, flags, &to, static_cast<float*>(ptr(lse)), ptr(ws), ws_bytes, stream);
     if (!mask)
       return unlocked(fn_prompt_attention,
           &tq, static_cast<const int32_t*>(ptr(off)), n, ptr(K), ptr(V), &a, static_cast<const int32_t*>(ptr(cur)),
@@ -272,15 +415,18 @@ PyObject* attention(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
   });
 }
 
-// (K_c, q, max_len, rows) -> bytes, or a negative status
+// (K_c, q, max_len, rows, pages) -> bytes, or a negative status
 PyObject* workspace_bytes(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
   return guarded([&]() -> PyObject* {
-    check_count(n_args, 4);
+    check_count(n_args, 5);
     const at::Tensor *K = tensor(v[0], "K_c"), *q = tensor(v[1], "q");
     Ranges held;
-    const l2kv_layout a = layout(*K, heads_of(*q), v[3], &held);
+    Tables tables;
+    const bool paged = v[4] != Py_None;
+    const l2kv_layout a = paged ? layout(*K, heads_of(*q), v[4], &tables) : layout(*K, heads_of(*q), v[3], &held);
+    const int32_t n = narrow(q->size(-3), "the number of tokens"), max_len = integer32(v[2], "max_len");
     size_t bytes = 0;
-    const int rc = fn_workspace_bytes(&a, narrow(q->size(-3), "the number of tokens"), integer32(v[2], "max_len"), &bytes);
+    const int rc = paged ? fn_paged_workspace_bytes(&a, &tables.c, n, max_len, &bytes) : fn_workspace_bytes(&a, n, max_len, &bytes);
     return PyLong_FromLongLong(rc == L2KV_OK ? (long long)bytes : rc);
   });
 }
@@ -298,6 +444,20 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     Py_RETURN_NONE;
   });
 }
+// The same of the calls on caches in pages.
+PyObject* bind_pages(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
+  return guarded([&]() -> PyObject* {
+    check_count(n_args, 6);
+    auto at = [&](int i) { return reinterpret_cast<void*>(integer(v[i])); };
+    fn_norm_rotary_write = reinterpret_cast<decltype(fn_norm_rotary_write)>(at(0));
+    fn_paged_attention = reinterpret_cast<decltype(fn_paged_attention)>(at(1));
+    fn_paged_workspace_bytes = reinterpret_cast<decltype(fn_paged_workspace_bytes)>(at(2));
+    fn_page_update = reinterpret_cast<decltype(fn_page_update)>(at(3));
+    fn_page_compact = reinterpret_cast<decltype(fn_page_compact)>(at(4));
+    fn_page_workspace_bytes = reinterpret_cast<decltype(fn_page_workspace_bytes)>(at(5));
+    Py_RETURN_NONE;
+  });
+}
 
 PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, nullptr},
@@ -305,6 +465,11 @@ PyMethodDef methods[] = {
     {"tree_commit", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(tree_commit)), METH_FASTCALL, nullptr},
     {"attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attention)), METH_FASTCALL, nullptr},
     {"workspace_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(workspace_bytes)), METH_FASTCALL, nullptr},
+    {"bind_pages", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind_pages)), METH_FASTCALL, nullptr},
+    {"norm_rotary_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm_rotary_write)), METH_FASTCALL, nullptr},
+    {"page_update", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(page_update)), METH_FASTCALL, nullptr},
+    {"page_compact", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(page_compact)), METH_FASTCALL, nullptr},
+    {"page_workspace_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(page_workspace_bytes)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_token_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

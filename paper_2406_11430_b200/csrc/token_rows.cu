@@ -47,14 +47,6 @@ __device__ __forceinline__ uint4 pack_piece<__nv_bfloat16>(const float (&y)[8]) 
   return make_uint4(two(y[0], y[1]), two(y[2], y[3]), two(y[4], y[5]), two(y[6], y[7]));
 }
 
-// A 16-byte load that leaves no line in L1.  (Not through the read-only path: q_out may be q.)
-__device__ __forceinline__ uint4 ld_once(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
-  return v;
-}
-
 // Cosine and sine of the angle a in fp64, to about 1e-15: their fp32 roundings are those of the exact values
 // but for one in some 10^7.  a / 2 pi is formed as a sum of two doubles and the nearest quarter turn taken off it,
 // which leaves the rest exact for any position; at most an eighth of a turn is left, where the Taylor series
@@ -85,15 +77,21 @@ __device__ __forceinline__ void cos_sin(double a, double* c, double* s) {
   *s = q & 2 ? -v : v;
 }
 
-// WPT: warps that share a token.  PAIRS: interleaved pairs.
-template <typename T, int D, int WPT, bool PAIRS>
+struct NormRotaryArgs : RotaryArgs { NormArgs norm; };
+
+// WPT: warps that share a token.  PAIRS: interleaved pairs.  NORM: norms of queries and keys before the rotation, and
+// caches in pages.  A row's norm is one factor r = 1 / sqrt(mean x^2 + eps), a sum over the lanes that hold the row, so the
+// rotation of r w x is r times that of w x: the weights go into the cosines and sines a lane keeps (one set for the
+// queries, one for the keys), r comes last, and the row is rounded once.
+template <typename T, int D, int WPT, bool PAIRS, bool NORM = false>
 __global__ void __launch_bounds__(kRotaryThreads, 3)
-rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* K, T* V) {
+rotary_write_kernel(const __grid_constant__ std::conditional_t<NORM, NormRotaryArgs, RotaryArgs> args, T* K, T* V) {
   constexpr int EPV = Elem<T>::kPerVec, LPR = D / EPV, RPW = 32 / LPR;
   constexpr int U = WPT == 1 ? 8 : 4;                    // pieces per lane in flight
   constexpr int TPB = kRotaryWarps / WPT;                // tokens per block
   constexpr int STEP = WPT * RPW;                        // rows that a token's warps take at once
   __shared__ float2 s_turn[kRotaryWarps][D / 2];
+  const RotaryArgs& a = args;
   const Geom& g = a.g;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane % LPR;
   next_may_start();
@@ -106,7 +104,10 @@ rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* K, T* V) {
     if (u >= units) return;
     const long long bl = a.per_head ? u / g.H : u;
     const int n = tokens_of(a.tok_off, (int)(bl / g.L), a.n_tokens).n;
-    a.cur_len[u] = (int)min((long long)g.cap(bl), (long long)max(0, a.start[u]) + n);
+    int cap = g.cap(bl);
+    if constexpr (NORM)
+      if (args.norm.pages.table && args.norm.pages.room) cap = max(0, min(cap, args.norm.pages.room[bl]));
+    a.cur_len[u] = (int)min((long long)cap, (long long)max(0, a.start[u]) + n);
     return;
   }
   const unsigned il = blockIdx.x * TPB + warp / WPT;     // token * layers + layer
@@ -140,12 +141,33 @@ rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* K, T* V) {
   const bool turns = piece < rot_pieces, upper = piece >= hp;
   const int partner = PAIRS || !turns ? lane : upper ? lane - hp : lane + hp;   // lane with the pairs' other elements
   float cs[EPV], sn[EPV];                                // y = x * cs + other * sn
+  auto turn = [&]() {
 #pragma unroll
-  for (int e = 0; e < EPV; ++e) {
-    const int p = PAIRS ? (piece * EPV + e) / 2 : (upper ? piece - hp : piece) * EPV + e;
-    const float2 t = s_turn[warp][turns ? p : 0];
-    cs[e] = t.x;
-    sn[e] = (PAIRS ? (e & 1) != 0 : upper) ? t.y : -t.y;
+    for (int e = 0; e < EPV; ++e) {
+      const int p = PAIRS ? (piece * EPV + e) / 2 : (upper ? piece - hp : piece) * EPV + e;
+      const float2 t = s_turn[warp][turns ? p : 0];
+      cs[e] = t.x;
+      sn[e] = (PAIRS ? (e & 1) != 0 : upper) ? t.y : -t.y;
+      if (NORM && !turns) { cs[e] = 1.f; sn[e] = 0.f; }
+    }
+  };
+  turn();
+  [[maybe_unused]] bool norms = false;
+  // Cosines and sines times the weights of this piece and of its partner's.
+  [[maybe_unused]] auto weigh = [&](const void* weight, float offset) {
+    if (!weight) return;
+    float mine[EPV], other[EPV];
+    Elem<T>::unpack(static_cast<const uint4*>(weight)[piece], mine);
+    Elem<T>::unpack(static_cast<const uint4*>(weight)[partner % LPR], other);
+#pragma unroll
+    for (int e = 0; e < EPV; ++e) {
+      cs[e] *= mine[e] + offset;
+      sn[e] *= (PAIRS ? mine[e ^ 1] : other[e]) + offset;
+    }
+  };
+  if constexpr (NORM) {
+    norms = args.norm.norm_q;
+    if (norms) weigh(args.norm.q_weight, args.norm.offset);
   }
   auto rotated = [&](const uint4& v) {                   // whole warps
     float f[EPV], o[EPV], y[EPV];
@@ -163,6 +185,14 @@ rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* K, T* V) {
     // Two products and a sum, each rounded: the arithmetic of the formula as it is written, so that a stored bf16
     // key, and with it the ordering key, is the one any plain fp32 form of it stores
     for (int e = 0; e < EPV; ++e) y[e] = __fadd_rn(__fmul_rn(f[e], cs[e]), __fmul_rn(o[e], sn[e]));
+    if constexpr (NORM) {
+      if (norms) {
+        const float r = __frcp_rn(__fsqrt_rn(piece_sumsq_reduce<T, LPR>(v) * (1.f / D) + args.norm.eps));
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) y[e] = (turns ? y[e] : f[e] * cs[e]) * r;
+        return pack_piece<T>(y);
+      }
+    }
     const uint4 r = pack_piece<T>(y);
     return turns ? r : v;                                // (dimensions from rot_dim on are copied)
   };
@@ -180,13 +210,28 @@ rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* K, T* V) {
 
   // keys and values side by side, half a batch of each
   const long long bl = (long long)b * g.L + l;
-  const int cap = g.cap(bl);
+  int cap = g.cap(bl);
   const long long slot_all = a.per_head ? 0 : (long long)max(0, a.start[bl]) + at;
+  [[maybe_unused]] const int32_t* table = nullptr;
+  [[maybe_unused]] int page_all = -1;                    // (per_head: each head's own)
+  if constexpr (NORM) {
+    if (args.norm.pages.table) {
+      const PageView& pages = args.norm.pages;
+      table = pages.of(b, l);
+      if (pages.room) cap = max(0, min(cap, pages.room[bl]));
+      if (!a.per_head && slot_all < cap) page_all = table[slot_all >> pages.shift];
+    }
+    turn();
+    norms = args.norm.norm_k;
+    if (norms) weigh(args.norm.k_weight, args.norm.offset);
+  }
   const char* const k_from = reinterpret_cast<const char*>(a.k.row<T>(l, i, 0)) + piece * 16;
   const char* const v_from = reinterpret_cast<const char*>(a.v.row<T>(l, i, 0)) + piece * 16;
   const long long k_stride = a.k.sh * (long long)sizeof(T), v_stride = a.v.sh * (long long)sizeof(T);
-  const long long cache0 = g.base(b, l, 0) + piece * EPV, meta0 = g.meta(bl * g.H);
-  const long long meta_h = g.row_off ? g.total_rows : (long long)g.t_cap;
+  bool in_pages = false;
+  if constexpr (NORM) in_pages = table != nullptr;
+  const long long cache0 = (in_pages ? 0 : g.base(b, l, 0)) + piece * EPV, meta0 = in_pages ? 0 : g.meta(bl * g.H);
+  const long long meta_h = g.row_off || in_pages ? g.total_rows : (long long)g.t_cap;
   for (int r0 = row0; r0 - row0 + group < g.H; r0 += U / 2 * STEP) {
 #pragma unroll
     for (int u = 0; u < U / 2; ++u) {
@@ -200,12 +245,23 @@ rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* K, T* V) {
       const uint4 y = rotated(x[2 * u]);
       const float key = piece_sumsq_reduce<T, LPR>(y);   // of the row as it is stored
       if (h >= g.H) continue;
-      const long long slot = a.per_head ? (long long)max(0, a.start[bl * g.H + h]) + at : slot_all;
+      long long slot = a.per_head ? (long long)max(0, a.start[bl * g.H + h]) + at : slot_all;
       if (slot >= cap) {
         if (piece == 0) atomicExch(a.status, (int)L2KV_ERR_DEVICE_OVERFLOW);
         continue;
       }
       if (!L2KV_BOUNDS(g.holds(bl, slot), a.status)) continue;
+      if constexpr (NORM) {
+        if (in_pages) {
+          const PageView& pages = args.norm.pages;
+          const int page = a.per_head ? table[slot >> pages.shift] : page_all;
+          if (!pages.valid(page)) {
+            if (piece == 0) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
+            continue;
+          }
+          slot = ((long long)page << pages.shift) | (slot & (pages.rows() - 1));
+        }
+      }
       const long long to = cache0 + h * g.sh + slot * g.st;
       *reinterpret_cast<uint4*>(K + to) = y;
       *reinterpret_cast<uint4*>(V + to) = x[2 * u + 1];
@@ -218,22 +274,27 @@ rotary_write_kernel(const __grid_constant__ RotaryArgs a, T* K, T* V) {
   }
 }
 
-template <typename T, int D, int WPT, bool PAIRS>
-static int launch_rw(const RotaryArgs& a, void* K, void* V, cudaStream_t s) {
+template <typename T, int D, int WPT, bool PAIRS, typename A>
+static int launch_rw(const A& a, void* K, void* V, cudaStream_t s) {
   constexpr int TPB = kRotaryWarps / WPT;
   const long long units = (long long)a.g.B * a.g.L * (a.per_head ? a.g.H : 1);
   const long long blocks = ((long long)a.n_tokens * a.g.L + TPB - 1) / TPB + (units + kRotaryThreads - 1) / kRotaryThreads;
   if (blocks * TPB > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
-  return launch_early(rotary_write_kernel<T, D, WPT, PAIRS>, dim3((unsigned)blocks), kRotaryThreads, 0, s, a,
-                      static_cast<T*>(K), static_cast<T*>(V));
+  return launch_early(rotary_write_kernel<T, D, WPT, PAIRS, std::is_same_v<A, NormRotaryArgs>>, dim3((unsigned)blocks),
+                      kRotaryThreads, 0, s, a, static_cast<T*>(K), static_cast<T*>(V));
 }
 // One warp per token where that gives every SM a block of them (148 of 8), else a block per token.  (32 + 8 heads of 128,
 // warp / block in us: 300 tokens 7.0 / 5.3, 600 8.9 / 8.2, 1200 12.3 / 12.7, 2400 13.8 / 22.5, 9600 42.6 / 89.4.)
-template <typename T, int D>
-static int launch_rw_t(const RotaryArgs& a, void* K, void* V, cudaStream_t s) {
+template <typename T, int D, typename A>
+static int launch_rw_t(const A& a, void* K, void* V, cudaStream_t s) {
   const bool many = (long long)a.n_tokens * a.g.L >= 148 * kRotaryWarps;
   if (a.interleaved) return many ? launch_rw<T, D, 1, true>(a, K, V, s) : launch_rw<T, D, kRotaryWarps, true>(a, K, V, s);
   return many ? launch_rw<T, D, 1, false>(a, K, V, s) : launch_rw<T, D, kRotaryWarps, false>(a, K, V, s);
+}
+template <typename A>
+static int launch_rw_of(const A& a, void* K, void* V, int dtype, cudaStream_t s) {
+  if (dtype == L2KV_BF16) return a.g.D == 128 ? launch_rw_t<__nv_bfloat16, 128>(a, K, V, s) : launch_rw_t<__nv_bfloat16, 64>(a, K, V, s);
+  return a.g.D == 128 ? launch_rw_t<float, 128>(a, K, V, s) : launch_rw_t<float, 64>(a, K, V, s);
 }
 
 int launch_rotary_write(const TokView& q, const TokView& k, const TokView& v, const TokView& q_out,
@@ -243,8 +304,17 @@ int launch_rotary_write(const TokView& q, const TokView& k, const TokView& v, co
                         int per_head, int32_t* status, cudaStream_t s) {
   const RotaryArgs a{q, k, v, q_out, g, tok_off, pos, freq, start, cur_len, idx, sumsq, status,
                      n_tokens, rot_dim, interleaved, per_head, scale};
-  if (dtype == L2KV_BF16) return g.D == 128 ? launch_rw_t<__nv_bfloat16, 128>(a, K, V, s) : launch_rw_t<__nv_bfloat16, 64>(a, K, V, s);
-  return g.D == 128 ? launch_rw_t<float, 128>(a, K, V, s) : launch_rw_t<float, 64>(a, K, V, s);
+  return launch_rw_of(a, K, V, dtype, s);
+}
+
+int launch_norm_rotary_write(const TokView& q, const TokView& k, const TokView& v, const TokView& q_out,
+                             const int32_t* tok_off, int n_tokens, const int32_t* pos, const double* freq,
+                             int rot_dim, double scale, int interleaved, const NormArgs& norm, void* K, void* V,
+                             int32_t* idx, float* sumsq, const Geom& g, int dtype, const int32_t* start,
+                             int32_t* cur_len, int per_head, int32_t* status, cudaStream_t s) {
+  const NormRotaryArgs a{{q, k, v, q_out, g, tok_off, pos, freq, start, cur_len, idx, sumsq, status,
+                          n_tokens, rot_dim, interleaved, per_head, scale}, norm};
+  return launch_rw_of(a, K, V, dtype, s);
 }
 
 // ---- the accepted path of a tree -----------------------------------------------------------------

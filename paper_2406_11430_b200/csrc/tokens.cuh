@@ -1,7 +1,7 @@
 // The packed list of new tokens: which sequence a token belongs to, and where its rows lie.
 #pragma once
 
-#include "common.cuh"
+#include "pages.cuh"
 
 namespace l2kv {
 
@@ -68,11 +68,33 @@ inline int launch_early(void (*kern)(P...), dim3 grid, unsigned threads, size_t 
   return cudaLaunchKernelEx(&cfg, kern, static_cast<A&&>(args)...) == cudaSuccess ? L2KV_OK : L2KV_ERR_CUDA;
 }
 
+// A 16-byte load that leaves no line in L1.  (Not through the read-only path: q_out may be q, and
+// other calls write the rows.)
+__device__ __forceinline__ uint4 ld_once(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+
 int launch_rotary_write(const TokView& q, const TokView& k, const TokView& v, const TokView& q_out,
                         const int32_t* tok_off, int n_tokens, const int32_t* pos, const double* freq,
                         int rot_dim, double scale, int interleaved, void* K, void* V, int32_t* idx,
                         float* sumsq, const Geom& g, int dtype, const int32_t* start, int32_t* cur_len,
                         int per_head, int32_t* status, cudaStream_t s);
+// The same with norms of queries and keys before the rotation, into pages or rows.
+struct NormArgs {
+  PageView pages;                                        // table == nullptr: the cache has rows of its own
+  const void* q_weight;                                  // [head_dim] in the cache's dtype, or null: ones
+  const void* k_weight;
+  int norm_q, norm_k;
+  float eps, offset;                                     // offset: what is added to the weights
+};
+int launch_norm_rotary_write(const TokView& q, const TokView& k, const TokView& v, const TokView& q_out,
+                             const int32_t* tok_off, int n_tokens, const int32_t* pos, const double* freq,
+                             int rot_dim, double scale, int interleaved, const NormArgs& norm, void* K, void* V,
+                             int32_t* idx, float* sumsq, const Geom& g, int dtype, const int32_t* start,
+                             int32_t* cur_len, int per_head, int32_t* status, cudaStream_t s);
 int launch_tree_commit(void* K, void* V, int32_t* idx, float* sumsq, const Geom& g, int dtype,
                        const int32_t* start, const int32_t* cur, const int32_t* path, int path_cap,
                        const int32_t* n_path, int32_t* len_out, int per_head, int32_t* status, cudaStream_t s);
@@ -90,6 +112,7 @@ struct TokenAttention {
   const uint32_t* mask;                                  // [n_tokens, 2 * mask_words] 32-bit halves
   int mask_words;
   int32_t* status;                                       // may be null
+  PageView pages;                                        // table == nullptr: the cache has rows of its own
 };
 size_t token_attention_scratch(const Geom& g, int dtype, int n_tokens, int max_len);
 int launch_token_attention(const TokenAttention& a, const void* K, const void* V, int dtype, char* scratch,
