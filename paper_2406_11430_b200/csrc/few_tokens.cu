@@ -1,0 +1,575 @@
+// Attention of few new tokens per sequence (decode steps) over bf16 caches in pages.
+//
+// An item is up to eight query rows, the (token, head-of-the-group) pairs of 8 / G tokens of one sequence that share a KV
+// head; with so few the work is the stream of the cached rows, and the tile of 128 rows that the tensor-memory kernel
+// takes would be empty but for one in 16 or 32.  Here a warp multiplies 16 cached rows by the eight query rows with one instruction
+// (mma.sync m16n8k16), both ways:
+//   S^T[row, query] = K Q^T,   P = 2^(s - m) against a running maximum,   O^T[dim, query] += V^T P^T,
+// the weights turned from the one's result to the other's operand by movmatrix.  They go in as two bf16 terms (16 significant
+// bits): the second product is free here, and what is left is the rounding of the result.
+//
+// Roles: one warp works out the items and fetches blocks of 16 KB (K and V of 32 rows; of 64 for 64-wide heads), a TMA box per page, half
+// row and tensor, through a ring of 12; four warps take the blocks by turns, each with sums of its own, and join them
+// when the item ends.  A fixed grid of CTAs takes equal shares of all blocks; items that a share's end cuts leave
+// partial results that a second kernel joins.  Every wait is bounded; one that gives up ends the CTA and marks the workspace.
+#include <algorithm>
+#include <climits>
+#include <cstring>
+
+#include "token_maps.cuh"
+#include "umma.cuh"
+
+namespace l2kv {
+
+constexpr int kFtWarps = 4;                     // warps that multiply
+constexpr int kFtThreads = 32 * (kFtWarps + 1);
+constexpr int kFtGrid = 148;
+constexpr int kFtCols = 8;                      // query rows of an item
+constexpr int kFtSlots = 12;                    // a multiple of kFtWarps: a slot is always the same warp's
+constexpr int kFtSlot = 16384;                  // bytes of a block
+constexpr int kFtDescs = 4;                     // items whose queries are on their way
+constexpr int kFtPolls = 18;                    // log2 of the polls a wait may take
+constexpr int kFtItemCost = 2;                  // what an item costs beyond its blocks, in blocks
+constexpr int kFtMinShare = 4;                  // no shorter shares: a block for each warp
+constexpr int kFtWholeLen = 512;                // caches up to this length are never cut
+constexpr float kFtRescaleGap = 8.f;            // log2 units a maximum may drift before sums are rescaled
+template <int D> constexpr int kFtRows = 4096 / D;               // cached rows of a block
+template <int D> constexpr int kFtHalf = kFtRows<D> * 128;       // bytes of 64 elements of them
+template <int D> constexpr int kFtPitch = D + 4;                 // floats between query rows in shared memory (no bank twice)
+template <int D> constexpr int kFtPart = kFtWarps * kFtCols * kFtPitch<D> * 4;
+constexpr int kFtCtrl = 1024;
+template <int D> constexpr int kFtSmem = 1024 + kFtSlots * kFtSlot + kFtDescs * 2048 + kFtPart<D> + kFtCtrl;
+
+struct FtSpot {
+  long long at;          // cost of everything before the item
+  int e, item, off;      // entry (b, l), number of the item within it (tokens by tokens, head by head), block within the item
+  int pad;
+};
+struct FtArgs {
+  TokenAttention a;
+  int G, TG;             // query heads per KV head, tokens per item
+  FtSpot* plan;          // [kFtGrid] where each CTA's share begins; null: items stay whole
+  float* part;           // [2 kFtGrid][8][D] rows, then [2 kFtGrid][8] log2-sum-exps
+  float* part_lse;
+};
+struct FtEntry { int n, cur; };
+// An entry as the shares see it: with a length per head, the longest head's.
+__device__ __forceinline__ FtEntry ft_entry(const TokenAttention& a, int e) {
+  const int n = tokens_of(a.tok_off, e / a.g.L, a.n_tokens).n;
+  if (n == 0) return {0, 0};
+  int cur = a.lens.at(e, 0, a.g.H);
+  if (a.lens.per_head)
+    for (int h = 1; h < a.g.H; ++h) cur = max(cur, a.lens.at(e, h, a.g.H));
+  return {n, max(0, min(cur, min(a.max_len, a.g.t_cap)))};
+}
+template <int D> __device__ __forceinline__ int ft_blocks(int rows) { return (rows + kFtRows<D> - 1) / kFtRows<D>; }
+__device__ __forceinline__ int ft_items(const FtArgs& A, const FtEntry& e) { return (e.n + A.TG - 1) / A.TG * A.a.g.H; }
+template <int D> __device__ __forceinline__ int ft_each(const FtEntry& e) { return ft_blocks<D>(e.cur) + kFtItemCost; }
+
+struct FtItem {
+  int l, h, tok0, nq;    // first token in the list, tokens
+  int first, cur, end;   // rows its first token sees; rows there are; rows that some token sees
+  int row0, n;           // first row of the piece, its blocks
+  uint32_t at;           // running number of its first block
+  int slot;              // where a partial result goes; -1: the result itself
+  int stop;
+};
+template <int D>
+__device__ __forceinline__ FtItem ft_item(const FtArgs& A, int e, int item, int from, int to, int slot) {
+  const TokenAttention& a = A.a;
+  const int b = e / a.g.L, p = item / a.g.H;
+  const TokRange r = tokens_of(a.tok_off, b, a.n_tokens);
+  FtItem it;
+  it.l = e % a.g.L;
+  it.h = item % a.g.H;
+  it.tok0 = r.first + p * A.TG;
+  it.nq = min(A.TG, r.n - p * A.TG);
+  it.cur = max(0, min(a.lens.at(e, it.h, a.g.H), min(a.max_len, a.g.t_cap)));
+  it.first = it.cur - r.n + p * A.TG + 1;
+  it.end = max(0, min(it.cur, it.first + it.nq - 1));
+  it.row0 = from * kFtRows<D>;
+  it.n = max(0, min(to, ft_blocks<D>(it.end)) - from);
+  it.slot = slot;
+  it.stop = 0;
+  return it;
+}
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_trans(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// An 8 x 8 matrix of 16-bit elements, two per lane, turned about its diagonal.
+__device__ __forceinline__ uint32_t turned(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kFtThreads, 1)
+few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUtensorMap map_q,
+                  const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  constexpr int ROWS = kFtRows<D>, HALF = kFtHalf<D>, PITCH = kFtPitch<D>, MT = ROWS / 16, KS = D / 16;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzled tiles
+  const TokenAttention& a = A.a;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t s_ring = smem_u32(smem), s_q = s_ring + kFtSlots * kFtSlot;
+  float* const s_part = reinterpret_cast<float*>(smem + kFtSlots * kFtSlot + kFtDescs * 2048);
+  unsigned char* const ctrl = smem + kFtSlots * kFtSlot + kFtDescs * 2048 + kFtPart<D>;
+  const uint32_t bars = smem_u32(ctrl);
+  FtItem* const items = reinterpret_cast<FtItem*>(ctrl + 384);           // [kFtDescs]
+  float2* const s_stat = reinterpret_cast<float2*>(ctrl + 640);          // [kFtWarps][8]: maximum, sum
+  __shared__ FtSpot s_spot[2];
+  __shared__ long long s_sum[kFtThreads / 32];
+  __shared__ int s_fail_word, s_marked;
+  volatile int* const s_fail = &s_fail_word;
+  auto full = [&](uint32_t at) { return bars + 8u * (at % kFtSlots); };
+  auto empty = [&](uint32_t at) { return bars + 96u + 8u * (at % kFtSlots); };
+  auto desc_full = [&](uint32_t i) { return bars + 192u + 8u * (i % kFtDescs); };
+  auto desc_free = [&](uint32_t i) { return bars + 224u + 8u * (i % kFtDescs); };
+  const uint32_t part_full = bars + 256u, part_free = bars + 264u;
+  if (tid == 0) {
+    for (int i = 0; i < kFtSlots; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
+    for (int i = 0; i < kFtDescs; ++i) { mbar_init(desc_full(i), 1); mbar_init(desc_free(i), kFtWarps); }
+    mbar_init(part_full, kFtWarps);
+    mbar_init(part_free, kFtWarps);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    *s_fail = 0;
+  }
+  if (warp == kFtWarps && lane < 3) {
+    const CUtensorMap* const map = lane == 0 ? &map_q : lane == 1 ? &map_k : &map_v;
+    asm volatile("prefetch.tensormap [%0];" :: "l"(map) : "memory");
+  }
+  wait_for_previous();
+  // A wait that gave up in an earlier call marks the workspace; nothing runs until it is cleared.
+  if (tid == 0) s_marked = a.status ? *reinterpret_cast<volatile int32_t*>(a.status + 2) : 0;
+
+  // ---- this CTA's share: [c, c + 1) of equal stretches of all items' cost, each thread with a run of entries -----------
+  const int entries = a.g.B * a.g.L, run = (entries + kFtThreads - 1) / kFtThreads, e0 = min(entries, tid * run), e1 = min(entries, e0 + run);
+  long long mine = 0;
+  FtEntry only{0, 0};
+  for (int e = e0; e < e1; ++e) {
+    only = ft_entry(a, e);
+    mine += (long long)ft_items(A, only) * ft_each<D>(only);
+  }
+  long long incl = mine;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const long long o = __shfl_up_sync(0xffffffffu, incl, off);
+    if (lane >= off) incl += o;
+  }
+  if (lane == 31) s_sum[warp] = incl;
+  __syncthreads();
+  long long total = 0, before = incl - mine;
+  for (int w = 0; w < kFtThreads / 32; ++w) {
+    if (w < warp) before += s_sum[w];
+    total += s_sum[w];
+  }
+  const long long share = A.plan ? max((total + gridDim.x - 1) / gridDim.x, (long long)kFtMinShare) : (total + gridDim.x - 1) / gridDim.x;
+  for (int k = 0; k < 2; ++k) {
+    const long long x = (blockIdx.x + k) * share;
+    if (tid == 0 && x >= total) s_spot[k] = FtSpot{total, entries, 0, 0, 0};
+    if (x < before || x >= before + mine) continue;
+    long long at = before;
+    int e = e0;
+    FtEntry y = e1 - e0 == 1 ? only : ft_entry(a, e);
+    while (true) {
+      const long long here = (long long)ft_items(A, y) * ft_each<D>(y);
+      if (x < at + here) break;
+      at += here;
+      y = ft_entry(a, ++e);
+    }
+    const int each = ft_each<D>(y), n = each - kFtItemCost;
+    FtSpot s{0, e, (int)((x - at) / each), 0, 0};
+    s.at = at + (long long)s.item * each;
+    s.off = max(0, (int)(x - s.at) - kFtItemCost);
+    if (s.off < 2) s.off = 0;                            // (no slivers)
+    if (s.off > 0 && (!A.plan || n - s.off < 2)) {       // the next item
+      s.at += each;
+      s.off = 0;
+      if (++s.item == ft_items(A, y)) {
+        s.item = 0;
+        do ++s.e; while (s.e < entries && tokens_of(a.tok_off, s.e / a.g.L, a.n_tokens).n == 0);
+      }
+    }
+    s_spot[k] = s;
+  }
+  __syncthreads();
+  next_may_start();
+  if (s_marked) return;
+  if (A.plan && tid == 0) A.plan[blockIdx.x] = s_spot[0];
+  // A wait that another role's failure ends too.
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    if (mbar_test(bar, parity)) return true;
+    return *s_fail == 0 && mbar_wait<kFtPolls>(bar, parity);
+  };
+
+  if (warp == kFtWarps) {
+    // ---- items and blocks ------------------------------------------------------------------------------
+    const PageView& pages = a.pages;
+    const int box = min(ROWS, pages.rows()), n_boxes = ROWS / box, per_tensor = D / 64 * n_boxes;
+    const bool is_v = lane >= per_tensor;
+    const int of_half = lane % per_tensor / n_boxes, of_box = lane % n_boxes;
+    FtSpot spot = s_spot[0];
+    const FtSpot end = s_spot[1];
+    uint32_t at = 0, n_desc = 0;
+    bool ok = true;
+    int entry = -1, items_of = 0, each = 1;
+    while (ok) {
+      FtItem it;
+      it.stop = 1;
+      it.n = 0;
+      if (spot.at < end.at || (spot.at == end.at && spot.off < end.off)) {
+        if (spot.e != entry) {
+          const FtEntry y = ft_entry(a, spot.e);
+          entry = spot.e;
+          items_of = ft_items(A, y);
+          each = ft_each<D>(y);
+        }
+        const int n = each - kFtItemCost, to = spot.at == end.at ? end.off : n;
+        // a piece that does not begin its item goes to this CTA's first slot, one that does to its second
+        it = ft_item<D>(A, spot.e, spot.item, spot.off, to, spot.off > 0 ? 2 * (int)blockIdx.x : to < n ? 2 * (int)blockIdx.x + 1 : -1);
+        spot.at += each;
+        spot.off = 0;
+        if (++spot.item == items_of) {
+          spot.item = 0;
+          do ++spot.e; while (spot.e < entries && tokens_of(a.tok_off, spot.e / a.g.L, a.n_tokens).n == 0);
+        }
+      }
+      if (n_desc >= kFtDescs) ok = __all_sync(0xffffffffu, wait(desc_free(n_desc), (n_desc / kFtDescs - 1) & 1u));
+      if (!ok) break;
+      it.at = at;
+      if (lane == 0) {
+        items[n_desc % kFtDescs] = it;
+        if (it.n == 0) {
+          mbar_arrive(desc_full(n_desc));
+        } else {
+          mbar_expect_tx(desc_full(n_desc), D / 64 * 1024);
+          for (int c = 0; c < D / 64; ++c)
+            tma_load_4d(s_q + n_desc % kFtDescs * 2048 + c * 1024, &map_q, desc_full(n_desc), c * 64, it.h * A.G, it.tok0, it.l);
+        }
+      }
+      __syncwarp();
+      ++n_desc;
+      if (it.stop) break;
+      if (it.n == 0) continue;
+      // lane i holds entry i of 32 of the table's, and the one 32 further on is on its way
+      const int32_t* const table = pages.of(entry / a.g.L, entry % a.g.L);
+      const int n_ids = (it.end + pages.rows() - 1) >> pages.shift;
+      auto ids = [&](int chunk) {
+        const int p = chunk * 32 + lane;
+        const int id = p < n_ids ? table[p] : -1;
+        const bool bad = p < n_ids && !pages.valid(id);
+        if (bad && a.status) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
+        return bad ? -1 : id;
+      };
+      int chunk = it.row0 >> pages.shift >> 5, now = ids(chunk), later = ids(chunk + 1);
+      for (int g = 0; g < it.n; ++g, ++at) {
+        const int t = it.row0 + g * ROWS, page = t >> pages.shift;
+        if (page >> 5 != chunk) { ++chunk; now = later; later = ids(chunk + 1); }
+        const int id = __shfl_sync(0xffffffffu, now, (page + of_box) & 31);
+        if (at >= kFtSlots) ok = __all_sync(0xffffffffu, wait(empty(at), (at / kFtSlots - 1) & 1u));
+        if (!ok) break;
+        if (lane == 0) mbar_expect_tx(full(at), kFtSlot);
+        __syncwarp();
+        if (lane < 2 * per_tensor) {
+          const int row = id < 0 ? pages.n << pages.shift : (id << pages.shift) + (t & (pages.rows() - 1));
+          tma_load_5d(s_ring + at % kFtSlots * kFtSlot + (is_v ? kFtSlot / 2 : 0) + of_half * HALF + of_box * box * 128,
+                      is_v ? &map_v : &map_k, full(at), of_half * 64, row, it.h, 0, 0);
+        }
+      }
+    }
+    if (!ok) {                                           // copies that may still be in flight
+      *s_fail = 1;
+      for (uint32_t parity = 0; parity < 2; ++parity) {
+        for (int i = 0; i < kFtSlots; ++i) mbar_wait<12>(full(i), parity);
+        for (int i = 0; i < kFtDescs; ++i) mbar_wait<12>(desc_full(i), parity);
+      }
+    }
+  } else {
+    // ---- products ----------------------------------------------------------------------------------------
+    const int fr = lane >> 2, fc = lane & 3;             // row and pair of columns of a fragment
+    const float sc = a.scale_log2e;
+    bool ok = true;
+    uint32_t n_desc = 0;
+    while (true) {
+      ok = __all_sync(0xffffffffu, wait(desc_full(n_desc), (n_desc / kFtDescs) & 1u));
+      if (!ok) break;
+      const FtItem it = items[n_desc % kFtDescs];
+      if (it.stop) break;
+      uint32_t qb[KS][2];
+      if (it.n > 0) {
+#pragma unroll
+        for (int j = 0; j < KS / 2; ++j) {
+          uint32_t r[4];
+          const int ch = 4 * j + (lane >> 3);
+          ldsm4(r, s_q + n_desc % kFtDescs * 2048 + (ch >> 3) * 1024 + (lane & 7) * 128 + (((ch & 7) ^ (lane & 7)) << 4));
+          qb[2 * j][0] = r[0]; qb[2 * j][1] = r[1]; qb[2 * j + 1][0] = r[2]; qb[2 * j + 1][1] = r[3];
+        }
+      }
+      // columns 2 fc and 2 fc + 1: rows that they see (columns that are nobody's: anything)
+      const int q0 = 2 * fc / A.G, q1 = (2 * fc + 1) / A.G;
+      const int lim0 = q0 < it.nq ? min(it.cur, it.first + q0) : INT_MAX, lim1 = q1 < it.nq ? min(it.cur, it.first + q1) : INT_MAX;
+      float o[KS][4], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+#pragma unroll
+      for (int d = 0; d < KS; ++d) o[d][0] = o[d][1] = o[d][2] = o[d][3] = 0.f;
+      const uint32_t first = (uint32_t)((warp - (int)(it.at % kFtWarps) + kFtWarps) % kFtWarps);
+      for (int u = (int)first; u < it.n; u += kFtWarps) {
+        const uint32_t at = it.at + u, slot = s_ring + at % kFtSlots * kFtSlot;
+        ok = __all_sync(0xffffffffu, wait(full(at), (at / kFtSlots) & 1u));
+        if (!ok) break;
+        const int r0 = it.row0 + u * ROWS;
+        float c[MT][4];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = 0.f;
+        const int krow = (lane & 7) + ((lane >> 3) & 1) * 8;
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+          const uint32_t k_at = slot + (j >> 2) * HALF + krow * 128 + (((2 * (j & 3) + (lane >> 4)) ^ (lane & 7)) << 4);
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            uint32_t x[4];
+            ldsm4(x, k_at + t * 2048);
+            mma16816(c[t], x, qb[j][0], qb[j][1]);
+          }
+        }
+        if (r0 + ROWS > it.first) {                      // (the first token sees least)
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            const int row = r0 + t * 16 + fr;
+            if (row >= lim0) c[t][0] = -INFINITY;
+            if (row >= lim1) c[t][1] = -INFINITY;
+            if (row + 8 >= lim0) c[t][2] = -INFINITY;
+            if (row + 8 >= lim1) c[t][3] = -INFINITY;
+          }
+        }
+        if (r0 + ROWS > it.end) {
+          // Rows that no token sees can hold anything; clear them, so that a zero weight times Inf or NaN cannot reach O.
+          for (int e = lane; e < (r0 + ROWS - it.end) * (D / 8); e += 32) {
+            const int row = it.end - r0 + e / (D / 8), ch = e % (D / 8);
+            st_shared16(slot + kFtSlot / 2 + (ch >> 3) * HALF + row * 128 + ((ch & 7) << 4), 0, 0, 0, 0);
+          }
+          __syncwarp();
+          proxy_fence();
+        }
+        float t0 = fmaxf(c[0][0], c[0][2]), t1 = fmaxf(c[0][1], c[0][3]);
+#pragma unroll
+        for (int t = 1; t < MT; ++t) {
+          t0 = fmaxf(t0, fmaxf(c[t][0], c[t][2]));
+          t1 = fmaxf(t1, fmaxf(c[t][1], c[t][3]));
+        }
+        if (__any_sync(0xffffffffu, t0 * sc > m0 + kFtRescaleGap || t1 * sc > m1 + kFtRescaleGap)) {
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) {
+            t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, off));
+            t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, off));
+          }
+          const float n0 = fmaxf(m0, t0 * sc), n1 = fmaxf(m1, t1 * sc);
+          const float f0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - n0), f1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - n1);
+          m0 = n0; m1 = n1;
+          l0 *= f0; l1 *= f1;
+#pragma unroll
+          for (int d = 0; d < KS; ++d) { o[d][0] *= f0; o[d][1] *= f1; o[d][2] *= f0; o[d][3] *= f1; }
+        }
+        const float s0 = m0 == -INFINITY ? 0.f : -m0, s1 = m1 == -INFINITY ? 0.f : -m1;   // (nothing seen yet)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          const float w0 = fast_exp2(fmaf(c[t][0], sc, s0)), w1 = fast_exp2(fmaf(c[t][1], sc, s1));
+          const float w2 = fast_exp2(fmaf(c[t][2], sc, s0)), w3 = fast_exp2(fmaf(c[t][3], sc, s1));
+          l0 += w0 + w2;
+          l1 += w1 + w3;
+          const uint32_t ha = pack_bf16(w0, w1), hb = pack_bf16(w2, w3);
+          const uint32_t la = turned(pack_bf16_rest(w0, w1, ha)), lb = turned(pack_bf16_rest(w2, w3, hb));
+          const uint32_t pa = turned(ha), pb = turned(hb);
+          const uint32_t v_at = slot + kFtSlot / 2 + t * 2048 + ((lane & 7) + (lane >> 4) * 8) * 128;
+#pragma unroll
+          for (int d = 0; d < KS; ++d) {
+            uint32_t x[4];
+            ldsm4_trans(x, v_at + (d >> 2) * HALF + (((2 * (d & 3) + ((lane >> 3) & 1)) ^ (lane & 7)) << 4));
+            mma16816(o[d], x, pa, pb);
+            mma16816(o[d], x, la, lb);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(at));
+      }
+      if (!ok) break;
+      // ---- the item's four parts are joined, and go out --------------------------------------------------
+#pragma unroll
+      for (int off = 4; off < 32; off <<= 1) {
+        l0 += __shfl_xor_sync(0xffffffffu, l0, off);
+        l1 += __shfl_xor_sync(0xffffffffu, l1, off);
+      }
+      if (n_desc > 0) ok = __all_sync(0xffffffffu, wait(part_free, (n_desc - 1) & 1u));
+      if (!ok) break;
+      float* const part = s_part + warp * kFtCols * PITCH;
+#pragma unroll
+      for (int d = 0; d < KS; ++d) {
+        part[2 * fc * PITCH + 16 * d + fr] = o[d][0];
+        part[(2 * fc + 1) * PITCH + 16 * d + fr] = o[d][1];
+        part[2 * fc * PITCH + 16 * d + fr + 8] = o[d][2];
+        part[(2 * fc + 1) * PITCH + 16 * d + fr + 8] = o[d][3];
+      }
+      if (fr == 0) {
+        s_stat[warp * kFtCols + 2 * fc] = make_float2(m0, l0);
+        s_stat[warp * kFtCols + 2 * fc + 1] = make_float2(m1, l1);
+      }
+      __syncwarp();
+      if (lane == 0) { mbar_arrive(desc_free(n_desc)); mbar_arrive(part_full); }
+      ok = __all_sync(0xffffffffu, wait(part_full, n_desc & 1u));
+      if (!ok) break;
+      const int col = tid >> 4, piece = tid & 15, tok = it.tok0 + col / A.G, head = it.h * A.G + col % A.G;
+      if (col < it.nq * A.G && L2KV_BOUNDS(tok >= 0 && tok < a.n_tokens && head < a.g.Hq && it.slot < 2 * kFtGrid, a.status)) {
+        float m = -INFINITY, sum = 0.f, f[kFtWarps];
+#pragma unroll
+        for (int w = 0; w < kFtWarps; ++w) m = fmaxf(m, s_stat[w * kFtCols + col].x);
+#pragma unroll
+        for (int w = 0; w < kFtWarps; ++w) {
+          const float2 st = s_stat[w * kFtCols + col];
+          f[w] = st.x == -INFINITY ? 0.f : fast_exp2(st.x - m);
+          sum = fmaf(st.y, f[w], sum);
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          const int d = 4 * piece + 64 * i;
+          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int w = 0; w < kFtWarps; ++w) {
+            const float4 y = *reinterpret_cast<const float4*>(s_part + (w * kFtCols + col) * PITCH + d);
+            x.x = fmaf(y.x, f[w], x.x); x.y = fmaf(y.y, f[w], x.y); x.z = fmaf(y.z, f[w], x.z); x.w = fmaf(y.w, f[w], x.w);
+          }
+          x.x *= inv; x.y *= inv; x.z *= inv; x.w *= inv;
+          if (it.slot >= 0)
+            *reinterpret_cast<float4*>(A.part + ((long long)it.slot * kFtCols + col) * D + d) = x;
+          else
+            *reinterpret_cast<uint2*>(a.out.row<__nv_bfloat16>(it.l, tok, head) + d) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+        }
+        if (piece == 0) {
+          const float lse2 = sum == 0.f ? -INFINITY : m + log2f(sum);
+          if (it.slot >= 0) A.part_lse[it.slot * kFtCols + col] = lse2;
+          else if (a.lse) a.lse[((long long)it.l * a.n_tokens + tok) * a.g.Hq + head] = lse2 * 0.6931471805599453f;
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(part_free);
+      ++n_desc;
+    }
+    if (!ok) *s_fail = 1;
+  }
+  __syncthreads();
+  if (*s_fail && tid == 0) record_timeout(a.status);
+}
+
+// Joins the pieces of items that were cut: out = sum_c w_c O_c / sum_c w_c, w_c = 2^(lse_c - max lse), piece by piece in
+// order.  A block per share that begins inside an item (the first of them where there are several), a warp per query row.
+template <int D>
+__global__ void __launch_bounds__(32 * kFtCols)
+few_tokens_join_kernel(const __grid_constant__ FtArgs A) {
+  constexpr int V = D / 32;
+  __shared__ FtSpot plan[kFtGrid];
+  const TokenAttention& a = A.a;
+  const int lane = threadIdx.x & 31, col = threadIdx.x >> 5;
+  next_may_start();
+  wait_for_previous();
+  if (a.status && a.status[2] != 0) return;              // a wait gave up: no output
+  for (int i = threadIdx.x; i < kFtGrid; i += 32 * kFtCols) plan[i] = A.plan[i];
+  __syncthreads();
+  const int c0 = (int)blockIdx.x + 1;
+  const FtSpot s = plan[c0];
+  if (s.off == 0 || (plan[c0 - 1].at == s.at && plan[c0 - 1].off > 0)) return;
+  int nc = 2;                                            // the piece before c0's, and c0's
+  while (c0 + nc - 1 < kFtGrid && plan[c0 + nc - 1].at == s.at && plan[c0 + nc - 1].off > 0) ++nc;
+  if (!L2KV_BOUNDS(s.e >= 0 && s.e < a.g.B * a.g.L && s.item >= 0, a.status)) return;
+  const FtItem it = ft_item<D>(A, s.e, s.item, 0, INT_MAX, 0);
+  if (col >= it.nq * A.G) return;
+  auto row = [&](int c) { return (long long)(c == 0 ? 2 * c0 - 1 : 2 * (c0 + c - 1)) * kFtCols + col; };
+  float top = -INFINITY;
+  for (int c = lane; c < nc; c += 32) top = fmaxf(top, A.part_lse[row(c)]);
+#pragma unroll
+  for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+  float den = 0.f, num[V] = {};
+  for (int b = 0; b < nc; b += 32) {
+    const float lse2 = b + lane < nc ? A.part_lse[row(b + lane)] : -INFINITY;
+    const float mine = lse2 == -INFINITY ? 0.f : exp2f(lse2 - top);
+#pragma unroll 8
+    for (int c = 0; c < min(32, nc - b); ++c) {
+      const float w = __shfl_sync(0xffffffffu, mine, c);
+      const float* const from = A.part + row(b + c) * D + lane * V;
+      float x[V];
+      if constexpr (V == 4) {
+        const float4 y = *reinterpret_cast<const float4*>(from);
+        x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w;
+      } else {
+        const float2 y = *reinterpret_cast<const float2*>(from);
+        x[0] = y.x; x[1] = y.y;
+      }
+      den += w;
+#pragma unroll
+      for (int i = 0; i < V; ++i) num[i] = fmaf(w, x[i], num[i]);       // (rows of a piece that sees nothing are zeros)
+    }
+  }
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  const int tok = it.tok0 + col / A.G, head = it.h * A.G + col % A.G;
+  __nv_bfloat16* const to = a.out.row<__nv_bfloat16>(it.l, tok, head) + lane * V;
+  if constexpr (V == 4)
+    *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16(num[0] * inv, num[1] * inv), pack_bf16(num[2] * inv, num[3] * inv));
+  else
+    *reinterpret_cast<uint32_t*>(to) = pack_bf16(num[0] * inv, num[1] * inv);
+  if (a.lse && lane == 0)
+    a.lse[((long long)it.l * a.n_tokens + tok) * a.g.Hq + head] = den == 0.f ? -INFINITY : (top + log2f(den)) * 0.6931471805599453f;
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+
+constexpr size_t kFtPlanBytes = (kFtGrid * sizeof(FtSpot) + 255) / 256 * 256;
+
+// One new token per sequence on average, or fewer: with more of them a tile's rows fill.
+bool few_tokens(const TokenAttention& a, int dtype) { return dtype == L2KV_BF16 && a.pages.table && a.n_tokens <= a.g.B; }
+
+size_t few_tokens_scratch(const Geom& g, int max_len) {
+  return max_len > kFtWholeLen ? kFtPlanBytes + (size_t)2 * kFtGrid * kFtCols * (g.D + 1) * sizeof(float) : 0;
+}
+
+template <int D>
+static int launch_ft(const FtArgs& A, const void* K, const void* V, cudaStream_t s) {
+  const TokenAttention& a = A.a;
+  alignas(64) CUtensorMap map_q, map_k, map_v;
+  std::memset(&map_q, 0, sizeof map_q);
+  std::memset(&map_k, 0, sizeof map_k);
+  std::memset(&map_v, 0, sizeof map_v);
+  const int box = std::min(kFtRows<D>, 1 << a.pages.shift);
+  if (!make_query_map(&map_q, a, A.TG) || !make_cache_map(&map_k, K, a.g, box, true) || !make_cache_map(&map_v, V, a.g, box, true))
+    return L2KV_ERR_UNSUPPORTED;
+  auto kern = few_tokens_kernel<D>;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kFtSmem<D>) != cudaSuccess) return L2KV_ERR_CUDA;
+  const int rc = launch_chained(kern, kFtGrid, 1, kFtThreads, kFtSmem<D>, s, A, map_q, map_k, map_v);
+  if (rc != L2KV_OK || !A.plan) return rc;
+  return launch_chained(few_tokens_join_kernel<D>, kFtGrid - 1, 1, 32 * kFtCols, 0, s, A);
+}
+
+int launch_few_tokens(const TokenAttention& a, const void* K, const void* V, char* scratch, size_t scratch_bytes, cudaStream_t s) {
+  FtArgs A{};
+  A.a = a;
+  A.G = a.g.Hq / a.g.H;
+  A.TG = kFtCols / A.G;
+  const size_t need = few_tokens_scratch(a.g, a.max_len);
+  if (need > 0 && scratch && scratch_bytes >= need) {
+    A.plan = reinterpret_cast<FtSpot*>(scratch);
+    A.part = reinterpret_cast<float*>(scratch + kFtPlanBytes);
+    A.part_lse = A.part + (size_t)2 * kFtGrid * kFtCols * a.g.D;
+  }
+  return a.g.D == 128 ? launch_ft<128>(A, K, V, s) : launch_ft<64>(A, K, V, s);
+}
+
+}  // namespace l2kv

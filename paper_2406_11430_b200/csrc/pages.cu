@@ -24,12 +24,6 @@ constexpr int kPageGroup = 256;                          // pages per count of h
 constexpr int kCopyHeads = 8;                            // heads whose rows one block copies
 constexpr uint32_t kPinned = 0xffffffffu;
 
-// Launched as the other calls on new tokens are: set up while the kernel before them runs.
-template <typename... P, typename... A>
-static int launch_chained(void (*kern)(P...), long long blocks, unsigned y, unsigned threads, cudaStream_t s, A&&... args) {
-  return launch_early(kern, dim3((unsigned)blocks, y), threads, 0, s, static_cast<A&&>(args)...);
-}
-
 // One (b, l) of a call.
 struct PageAsk {
   int have, more;        // pages of the rows that it keeps, and with those it asks for
@@ -423,17 +417,17 @@ static PageScratch scratch_of(const PagePlan& p, char* base, long long entries) 
 }
 static int groups_of(int n_pages) { return std::max(1, (n_pages + kPageGroup - 1) / kPageGroup); }
 static int begin_pages(const PageScratch& w, const uint8_t* pin, int n_pages, cudaStream_t s) {
-  return launch_chained(page_begin_kernel, groups_of(n_pages), 1, kPageThreads, s, w, pin, n_pages);
+  return launch_chained(page_begin_kernel, groups_of(n_pages), 1, kPageThreads, 0, s, w, pin, n_pages);
 }
 template <typename A>
 static int deal_pages(const A& a, const PageScratch& w, int n_pages, int32_t* n_free, cudaStream_t s) {
-  return launch_chained(page_deal_kernel<A>, (n_pages + kPageBlock - 1) / kPageBlock + 1, 1, kDealThreads, s, a, w, n_pages,
+  return launch_chained(page_deal_kernel<A>, (n_pages + kPageBlock - 1) / kPageBlock + 1, 1, kDealThreads, 0, s, a, w, n_pages,
                         (n_pages + kPageGroup - 1) / kPageGroup, n_free);
 }
 
 template <typename T, int D>
 static int launch_pu(const PageUpdate& a, const PageScratch& w, void* K, void* V, int32_t* idx, float* sumsq, const Geom& g, cudaStream_t s) {
-  return launch_chained(page_update_kernel<T, D>, w.entries, (unsigned)((g.H + kCopyHeads - 1) / kCopyHeads), kPageThreads, s, a, w,
+  return launch_chained(page_update_kernel<T, D>, w.entries, (unsigned)((g.H + kCopyHeads - 1) / kCopyHeads), kPageThreads, 0, s, a, w,
                         static_cast<T*>(K), static_cast<T*>(V), idx, sumsq, g);
 }
 
@@ -444,7 +438,7 @@ int launch_page_update(const PageUpdate& a, void* K, void* V, int32_t* idx, floa
   int rc = begin_pages(w, a.pin, a.in.n, s);
   if (rc != L2KV_OK) return rc;
   constexpr int kWarps = kPageThreads / 32;
-  rc = launch_chained(page_mark_kernel, (entries + kWarps - 1) / kWarps, 1, kPageThreads, s, a, w);
+  rc = launch_chained(page_mark_kernel, (entries + kWarps - 1) / kWarps, 1, kPageThreads, 0, s, a, w);
   if (rc != L2KV_OK) return rc;
   rc = deal_pages(a, w, a.in.n, a.n_free, s);
   if (rc != L2KV_OK) return rc;
@@ -455,7 +449,7 @@ int launch_page_update(const PageUpdate& a, void* K, void* V, int32_t* idx, floa
 template <typename T, int D>
 static int launch_pc(const PageCompact& a, const PageScratch& w, const CompactSelect& c, void* K, void* V, int32_t* idx, float* sumsq,
                      const Geom& g, cudaStream_t s) {
-  return launch_chained(page_compact_kernel<T, D>, (long long)w.entries * a.H * c.n_chunks + w.entries, 1, kPageThreads, s, a, w, c,
+  return launch_chained(page_compact_kernel<T, D>, (long long)w.entries * a.H * c.n_chunks + w.entries, 1, kPageThreads, 0, s, a, w, c,
                         static_cast<T*>(K), static_cast<T*>(V), idx, sumsq, g);
 }
 
@@ -470,7 +464,7 @@ int launch_page_compact(const PageCompact& a, void* K, void* V, int32_t* idx, fl
   int rc = begin_pages(w, a.pin, a.in.n, s);
   if (rc != L2KV_OK) return rc;
   constexpr int kWarps = kPageThreads / 32;
-  rc = launch_chained(page_mark_select_kernel, units + (entries + kWarps - 1) / kWarps, 1, kPageThreads, s, a, w, c);
+  rc = launch_chained(page_mark_select_kernel, units + (entries + kWarps - 1) / kWarps, 1, kPageThreads, 0, s, a, w, c);
   if (rc != L2KV_OK) return rc;
   rc = deal_pages(a, w, a.in.n, nullptr, s);
   if (rc != L2KV_OK) return rc;

@@ -37,7 +37,7 @@
 #include <climits>
 #include <cstring>
 
-#include "tokens.cuh"
+#include "token_maps.cuh"
 #include "umma.cuh"
 
 namespace l2kv {
@@ -302,13 +302,6 @@ __device__ __forceinline__ TaItem ta_item(const TaArgs& A, int b, int l, int p, 
 // other at its end).
 __device__ __forceinline__ int ta_places(int n, bool pair) { return pair ? n : (n + 1) & ~1; }
 
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1,
-                                            int c2, int c3) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-               "[%0], [%1, {%3, %4, %5, %6}], [%2];"
-               :: "r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
-               : "memory");
-}
 // The lowest x bits.
 __device__ __forceinline__ uint32_t low_bits(int x) { return x >= 32 ? 0xffffffffu : x <= 0 ? 0u : (1u << x) - 1u; }
 
@@ -1038,19 +1031,7 @@ static TaRoom ta_room(const Geom& g, int n_tokens, int max_len) {
 }
 
 size_t token_attention_scratch(const Geom& g, int dtype, int n_tokens, int max_len) {
-  return dtype == L2KV_BF16 ? ta_room(g, n_tokens, max_len).bytes : 0;
-}
-
-// Rank-4 map of the queries (head_dim, head, token, layer); a box is one half row of a tile's rows.
-static bool make_query_map(CUtensorMap* map, const TokenAttention& a) {
-  const Geom& g = a.g;
-  const int G = g.Hq / g.H;
-  const long long tight = g.D;
-  const cuuint64_t dims[4] = {(cuuint64_t)g.D, (cuuint64_t)g.Hq, (cuuint64_t)a.n_tokens, (cuuint64_t)g.L};
-  const cuuint64_t strides[3] = {(cuuint64_t)(g.Hq > 1 ? a.q.sh : tight) * 2, (cuuint64_t)(a.n_tokens > 1 ? a.q.st : tight) * 2,
-                                 (cuuint64_t)(g.L > 1 ? a.q.sl : tight) * 2};
-  const cuuint32_t box[4] = {64, (cuuint32_t)G, (cuuint32_t)(kTaRows / G), 1};
-  return encode_bf16_map(map, 4, a.q.p, dims, strides, box);
+  return dtype == L2KV_BF16 ? std::max(ta_room(g, n_tokens, max_len).bytes, few_tokens_scratch(g, max_len)) : 0;
 }
 
 template <int D, bool TREE, bool PAGED = false>
@@ -1061,7 +1042,7 @@ static int launch_ta(const TaArgs& A, const void* K, const void* V, long long it
   std::memset(&map_k, 0, sizeof map_k);
   std::memset(&map_v, 0, sizeof map_v);
   const int box = PAGED ? std::min(kTaSub, 1 << a.pages.shift) : kTaSub;
-  if (!make_query_map(&map_q, a) || !make_cache_map(&map_k, K, a.g, box, PAGED) || !make_cache_map(&map_v, V, a.g, box, PAGED))
+  if (!make_query_map(&map_q, a, kTaRows / A.G) || !make_cache_map(&map_k, K, a.g, box, PAGED) || !make_cache_map(&map_v, V, a.g, box, PAGED))
     return L2KV_ERR_UNSUPPORTED;
   auto kern = token_attention_kernel<D, TREE, PAGED>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTaSmem<D>) != cudaSuccess)
@@ -1076,6 +1057,7 @@ static int launch_ta(const TaArgs& A, const void* K, const void* V, long long it
 int launch_token_attention(const TokenAttention& a, const void* K, const void* V, int dtype, char* scratch,
                            size_t scratch_bytes, cudaStream_t s) {
   if (dtype != L2KV_BF16) return launch_token_attention_fp32(a, K, V, s);
+  if (few_tokens(a, dtype)) return launch_few_tokens(a, K, V, scratch, scratch_bytes, s);
   const TaRoom room = ta_room(a.g, a.n_tokens, a.max_len);
   if (room.items > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
   TaArgs A{};

@@ -77,6 +77,11 @@ __device__ __forceinline__ uint4 ld_once(const void* p) {
   return v;
 }
 
+template <typename... P, typename... A>
+inline int launch_chained(void (*kern)(P...), long long blocks, unsigned y, unsigned threads, size_t smem, cudaStream_t s, A&&... args) {
+  return launch_early(kern, dim3((unsigned)blocks, y), threads, smem, s, static_cast<A&&>(args)...);
+}
+
 int launch_rotary_write(const TokView& q, const TokView& k, const TokView& v, const TokView& q_out,
                         const int32_t* tok_off, int n_tokens, const int32_t* pos, const double* freq,
                         int rot_dim, double scale, int interleaved, void* K, void* V, int32_t* idx,
@@ -117,6 +122,10 @@ struct TokenAttention {
 size_t token_attention_scratch(const Geom& g, int dtype, int n_tokens, int max_len);
 int launch_token_attention(const TokenAttention& a, const void* K, const void* V, int dtype, char* scratch,
                            size_t scratch_bytes, cudaStream_t s);
+// The form for few tokens per sequence of a bf16 cache in pages, where that is the faster one.
+bool few_tokens(const TokenAttention& a, int dtype);
+size_t few_tokens_scratch(const Geom& g, int max_len);
+int launch_few_tokens(const TokenAttention& a, const void* K, const void* V, char* scratch, size_t scratch_bytes, cudaStream_t s);
 int launch_token_attention_fp32(const TokenAttention& a, const void* K, const void* V, cudaStream_t s);
 
 }  // namespace l2kv

@@ -75,6 +75,32 @@ def test_single_tokens_of_many_sequences(l2, G, L):
     check(l2, Paged(l2, [1] * 40, r.randint(0, 1500, (40, L)), L, 2, G, 128, 16, seed=G))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+@pytest.mark.parametrize("D", [64, 128])
+def test_few_tokens_in_uneven_numbers(l2, D, G, dtype):
+    """No more tokens than sequences, but several of one sequence: more than one item for some, none for others."""
+    check(l2, Paged(l2, [0, 5, 0, 0, 1, 0, 0, 12, 0, 2] + [0] * 12, [[i * 37 % 200] for i in range(22)], 1, 2, G, D, 32, dtype, seed=G, pad=2))
+    check(l2, Paged(l2, [17] + [0] * 17, [[2500]] + [[0]] * 17, 1, 2, G, D, 16, dtype, seed=G))
+
+
+@pytest.mark.parametrize("workspace", ["full", "status"])
+@pytest.mark.parametrize("P", [16, 32, 64, 512])
+@pytest.mark.parametrize("D", [64, 128])
+def test_single_tokens_over_lengths_around_blocks(l2, D, P, workspace):
+    """From a cache of the token alone to long ones, around blocks of 32 and 64 rows, pages, and shares of the work."""
+    ctx = [0, 1, 14, 15, 16, 30, 31, 32, 62, 63, 64, 127, 128, 500, 511, 512, 513, 1000, 5000, 9001]
+    check(l2, Paged(l2, [1] * 20, [[x] for x in ctx], 1, 3, 4, D, P, seed=D), workspace=workspace)
+    for x in (0, 40, 600, 3000):
+        check(l2, Paged(l2, [1], [[x]], 1, 1, 1, D, P, seed=x), workspace=workspace)
+
+
+def test_single_tokens_of_hundreds_of_sequences(l2):
+    """More sequences than threads work out the shares."""
+    r = np.random.RandomState(6)
+    check(l2, Paged(l2, [int(x) for x in r.choice([0, 1, 1, 1], 700)], r.randint(0, 90, (700, 1)), 1, 1, 4, 64, 16, seed=6))
+
+
 @pytest.mark.parametrize("P", [16, 64])
 def test_chunks_and_single_tokens_mixed(l2, P):
     r = np.random.RandomState(3)
@@ -91,8 +117,12 @@ def test_lengths_per_head_layers_padding_and_scale(l2, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_tokens_that_see_nothing(l2, dtype):
     """Fewer rows than new tokens: the first tokens see none and give zeros and -inf."""
-    c = Paged(l2, [5, 1, 80], [[0], [0], [0]], 1, 2, 4, 128, 16, dtype, seed=2)
-    out, lse = call(l2, c, cur=i32([[2], [0], [33]]))
+    for more in (0, 100):                                    # (empty sequences: few tokens per sequence)
+        see_nothing(l2, Paged(l2, [5, 1, 80] + [0] * more, [[0]] * (3 + more), 1, 2, 4, 128, 16, dtype, seed=2), dtype, more)
+
+
+def see_nothing(l2, c, dtype, more):
+    out, lse = call(l2, c, cur=i32([[2], [0], [33]] + [[0]] * more))
     for b, (n, cur) in enumerate(zip(c.n, (2, 0, 33))):
         for s in range(n):
             seen, i = max(0, cur - n + s + 1), int(c.off[b]) + s
@@ -121,7 +151,11 @@ def test_a_table_is_read_below_the_length_only(l2):
 @pytest.mark.parametrize("P", [16, 64])
 def test_pages_that_the_pool_does_not_have(l2, P, dtype):
     """They are told, and read as rows of zeros."""
-    c = Paged(l2, [2, 90], [[300], [40]], 1, 2, 4, 128, P, dtype, seed=6)
+    no_such_pages(l2, Paged(l2, [2, 90], [[300], [40]], 1, 2, 4, 128, P, dtype, seed=6), P)
+    no_such_pages(l2, Paged(l2, [1, 1], [[300], [140]], 1, 2, 4, 128, P, dtype, seed=6), P)
+
+
+def no_such_pages(l2, c, P):
     t = c.pages.table.clone()
     bad = [(0, 0, c.n_pages), (0, 2, -1), (1, 1, 2 ** 31 - 1), (1, 0, -2 ** 31)]
     for b, j, page in bad:

@@ -153,19 +153,20 @@ def test_pools_beyond_32_bits_are_refused():
         l2.page_workspace_bytes(K, pages)
 
 
-def _kernels():
-    """Signature and body of every kernel of pages.cu."""
-    path = os.path.join(os.path.dirname(l2.__file__), "csrc", "pages.cu")
+def _kernels(name):
+    """Signature and body of every kernel of a source file."""
+    path = os.path.join(os.path.dirname(l2.__file__), "csrc", name)
     with open(path) as f:
         code = re.sub(r"//[^\n]*|/\*.*?\*/", "", f.read(), flags=re.S)
     return [part.split("{", 1) for part in code.split("__global__")[1:]]
 
 
-def test_the_early_kernels_wait_and_promise_nothing():
+@pytest.mark.parametrize("name,count", [("pages.cu", 6), ("few_tokens.cu", 2)])
+def test_the_early_kernels_wait_and_promise_nothing(name, count):
     """All of them are set up while the kernel before them runs: they wait before they read what that one writes, and no
     __restrict__ parameter lets the compiler read earlier."""
-    kernels = _kernels()
-    assert len(kernels) == 6
+    kernels = _kernels(name)
+    assert len(kernels) == count
     for signature, body in kernels:
         assert "__restrict__" not in signature
         assert "wait_for_previous();" in body
