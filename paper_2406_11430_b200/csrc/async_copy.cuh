@@ -63,13 +63,12 @@ inline bool encode_bf16_map(CUtensorMap* map, int rank, const void* base, const 
 }
 
 // The rank-5 tensor map (head_dim, token, kv head, layer, batch) of a bf16 cache with a box of 64
-// elements x box_rows tokens; `pool`: of the rows of all pages of a paged cache, which are laid out as a packed
-// cache's.  Returns false as above (callers then use another path).
-inline bool make_cache_map(CUtensorMap* map, const void* base, const Geom& g, int box_rows, bool pool = false) {
+// elements x box_rows tokens.  Returns false as above (callers then use another path).
+inline bool make_cache_map(CUtensorMap* map, const void* base, const Geom& g, int box_rows) {
   cuuint64_t dims[5] = {(cuuint64_t)g.D, (cuuint64_t)g.t_cap, (cuuint64_t)g.H, (cuuint64_t)g.L, (cuuint64_t)g.B};
   cuuint64_t strides[4] = {(cuuint64_t)g.st * 2, (cuuint64_t)g.sh * 2, (cuuint64_t)g.sl * 2,
                            (cuuint64_t)g.sb * 2};
-  if (g.row_off || pool) {
+  if (g.row_off) {
     // packed cache: one [H, total_rows, 128] plane; the two outer dimensions have extent 1
     if (g.st <= 0 || g.sh <= 0 || g.total_rows <= 0 || g.total_rows > 0x7fffffffLL) return false;
     dims[1] = (cuuint64_t)g.total_rows; dims[3] = 1; dims[4] = 1;
@@ -78,6 +77,19 @@ inline bool make_cache_map(CUtensorMap* map, const void* base, const Geom& g, in
     return false;                                                       // broadcast views
   }
   const cuuint32_t box[5] = {64, (cuuint32_t)box_rows, 1, 1, 1};
+  return encode_bf16_map(map, 5, base, dims, strides, box);
+}
+
+// The map of a paged cache's pool, [H, total_rows, D]: dimensions 64 elements, row of a group of 8, half of the head, group,
+// head.  One box takes box_rows whole rows (a multiple of 8), and in shared memory its groups of 8 rows follow one another with
+// their halves side by side: [group][half][8][64], so that pages one after the other have the same distance from group to
+// group as rows within a page.  The copy engine takes about 120 cycles per box of 2 KB, and of 4 KB, so a page of 16 rows of 128 is
+// one box and not a box per half.
+inline bool make_pool_map(CUtensorMap* map, const void* base, const Geom& g, int box_rows) {
+  if (g.st <= 0 || g.total_rows <= 0 || g.total_rows > 0x7fffffffLL || (g.H > 1 && g.sh <= 0)) return false;
+  const cuuint64_t dims[5] = {64, 8, (cuuint64_t)(g.D / 64), (cuuint64_t)(g.total_rows / 8), (cuuint64_t)g.H};
+  const cuuint64_t strides[4] = {(cuuint64_t)g.st * 2, 128, (cuuint64_t)g.st * 16, (cuuint64_t)(g.H > 1 ? g.sh : g.st * g.total_rows) * 2};
+  const cuuint32_t box[5] = {64, 8, (cuuint32_t)(g.D / 64), (cuuint32_t)(box_rows / 8), 1};
   return encode_bf16_map(map, 5, base, dims, strides, box);
 }
 

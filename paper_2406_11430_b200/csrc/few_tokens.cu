@@ -8,8 +8,8 @@
 // the weights turned from the one's result to the other's operand by movmatrix.  They go in as two bf16 terms (16 significant
 // bits): the second product is free here, and what is left is the rounding of the result.
 //
-// Roles: one warp works out the items and fetches blocks of 16 KB (K and V of 32 rows; of 64 for 64-wide heads), a TMA box per page, half
-// row and tensor, through a ring of 12; four warps take the blocks by turns, each with sums of its own, and join them
+// Roles: one warp works out the items and fetches blocks of 16 KB (K and V of 32 rows; of 64 for 64-wide heads), a TMA box per page and
+// tensor, through a ring of 12; four warps take the blocks by turns, each with sums of its own, and join them
 // when the item ends.  A fixed grid of CTAs takes equal shares of all blocks; items that a share's end cuts leave
 // partial results that a second kernel joins.  Every wait is bounded; one that gives up ends the CTA and marks the workspace.
 #include <algorithm>
@@ -22,7 +22,8 @@
 namespace l2kv {
 
 constexpr int kFtWarps = 4;                     // warps that multiply
-constexpr int kFtThreads = 32 * (kFtWarps + 1);
+constexpr int kFtFetch = 4;                     // and warps that fetch: keys and values of every second block
+constexpr int kFtThreads = 32 * (kFtWarps + kFtFetch);
 constexpr int kFtGrid = 148;
 constexpr int kFtCols = 8;                      // query rows of an item
 constexpr int kFtSlots = 12;                    // a multiple of kFtWarps: a slot is always the same warp's
@@ -34,7 +35,7 @@ constexpr int kFtMinShare = 4;                  // no shorter shares: a block fo
 constexpr int kFtWholeLen = 512;                // caches up to this length are never cut
 constexpr float kFtRescaleGap = 8.f;            // log2 units a maximum may drift before sums are rescaled
 template <int D> constexpr int kFtRows = 4096 / D;               // cached rows of a block
-template <int D> constexpr int kFtHalf = kFtRows<D> * 128;       // bytes of 64 elements of them
+template <int D> constexpr int kFtGroup = D * 16;                // bytes of 8 of them: their halves of 1 KB
 template <int D> constexpr int kFtPitch = D + 4;                 // floats between query rows in shared memory (no bank twice)
 template <int D> constexpr int kFtPart = kFtWarps * kFtCols * kFtPitch<D> * 4;
 constexpr int kFtCtrl = 1024;
@@ -118,7 +119,7 @@ template <int D>
 __global__ void __launch_bounds__(kFtThreads, 1)
 few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUtensorMap map_q,
                   const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
-  constexpr int ROWS = kFtRows<D>, HALF = kFtHalf<D>, PITCH = kFtPitch<D>, MT = ROWS / 16, KS = D / 16;
+  constexpr int ROWS = kFtRows<D>, GROUP = kFtGroup<D>, PITCH = kFtPitch<D>, MT = ROWS / 16, KS = D / 16;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);   // swizzled tiles
   const TokenAttention& a = A.a;
@@ -139,7 +140,7 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
   auto desc_free = [&](uint32_t i) { return bars + 224u + 8u * (i % kFtDescs); };
   const uint32_t part_full = bars + 256u, part_free = bars + 264u;
   if (tid == 0) {
-    for (int i = 0; i < kFtSlots; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
+    for (int i = 0; i < kFtSlots; ++i) { mbar_init(full(i), 2); mbar_init(empty(i), 1); }
     for (int i = 0; i < kFtDescs; ++i) { mbar_init(desc_full(i), 1); mbar_init(desc_free(i), kFtWarps); }
     mbar_init(part_full, kFtWarps);
     mbar_init(part_free, kFtWarps);
@@ -214,12 +215,12 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
     return *s_fail == 0 && mbar_wait<kFtPolls>(bar, parity);
   };
 
-  if (warp == kFtWarps) {
+  if (warp >= kFtWarps) {
     // ---- items and blocks ------------------------------------------------------------------------------
     const PageView& pages = a.pages;
-    const int box = min(ROWS, pages.rows()), n_boxes = ROWS / box, per_tensor = D / 64 * n_boxes;
-    const bool is_v = lane >= per_tensor;
-    const int of_half = lane % per_tensor / n_boxes, of_box = lane % n_boxes;
+    const int box = min(ROWS, pages.rows()), n_boxes = ROWS / box, of_box = lane % n_boxes;
+    const int me = warp - kFtWarps;
+    const bool is_v = me & 1, leads = me == 0;
     FtSpot spot = s_spot[0];
     const FtSpot end = s_spot[1];
     uint32_t at = 0, n_desc = 0;
@@ -246,10 +247,10 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
           do ++spot.e; while (spot.e < entries && tokens_of(a.tok_off, spot.e / a.g.L, a.n_tokens).n == 0);
         }
       }
-      if (n_desc >= kFtDescs) ok = __all_sync(0xffffffffu, wait(desc_free(n_desc), (n_desc / kFtDescs - 1) & 1u));
-      if (!ok) break;
       it.at = at;
-      if (lane == 0) {
+      if (leads && n_desc >= kFtDescs) ok = __all_sync(0xffffffffu, wait(desc_free(n_desc), (n_desc / kFtDescs - 1) & 1u));
+      if (!ok) break;
+      if (leads && lane == 0) {
         items[n_desc % kFtDescs] = it;
         if (it.n == 0) {
           mbar_arrive(desc_full(n_desc));
@@ -277,15 +278,18 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
       for (int g = 0; g < it.n; ++g, ++at) {
         const int t = it.row0 + g * ROWS, page = t >> pages.shift;
         if (page >> 5 != chunk) { ++chunk; now = later; later = ids(chunk + 1); }
+        if ((at & 1) != (uint32_t)(me >> 1)) continue;
         const int id = __shfl_sync(0xffffffffu, now, (page + of_box) & 31);
+        const int row = id < 0 ? pages.n << pages.shift : (id << pages.shift) + (t & (pages.rows() - 1));
         if (at >= kFtSlots) ok = __all_sync(0xffffffffu, wait(empty(at), (at / kFtSlots - 1) & 1u));
         if (!ok) break;
-        if (lane == 0) mbar_expect_tx(full(at), kFtSlot);
+        const uint32_t to = s_ring + at % kFtSlots * kFtSlot + (is_v ? kFtSlot / 2 : 0);
+        if (elect_one()) mbar_expect_tx(full(at), kFtSlot / 2);
         __syncwarp();
-        if (lane < 2 * per_tensor) {
-          const int row = id < 0 ? pages.n << pages.shift : (id << pages.shift) + (t & (pages.rows() - 1));
-          tma_load_5d(s_ring + at % kFtSlots * kFtSlot + (is_v ? kFtSlot / 2 : 0) + of_half * HALF + of_box * box * 128,
-                      is_v ? &map_v : &map_k, full(at), of_half * 64, row, it.h, 0, 0);
+        if (n_boxes == 1) {
+          if (elect_one()) tma_load_5d(to, is_v ? &map_v : &map_k, full(at), 0, 0, 0, row >> 3, it.h);
+        } else if (lane < n_boxes) {
+          tma_load_5d(to + of_box * box * D * 2, is_v ? &map_v : &map_k, full(at), 0, 0, 0, row >> 3, it.h);
         }
       }
     }
@@ -332,14 +336,13 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
         float c[MT][4];
 #pragma unroll
         for (int t = 0; t < MT; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = 0.f;
-        const int krow = (lane & 7) + ((lane >> 3) & 1) * 8;
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
-          const uint32_t k_at = slot + (j >> 2) * HALF + krow * 128 + (((2 * (j & 3) + (lane >> 4)) ^ (lane & 7)) << 4);
+          const uint32_t k_at = slot + (j >> 2) * 1024 + ((lane >> 3) & 1) * GROUP + (lane & 7) * 128 + (((2 * (j & 3) + (lane >> 4)) ^ (lane & 7)) << 4);
 #pragma unroll
           for (int t = 0; t < MT; ++t) {
             uint32_t x[4];
-            ldsm4(x, k_at + t * 2048);
+            ldsm4(x, k_at + t * 2 * GROUP);
             mma16816(c[t], x, qb[j][0], qb[j][1]);
           }
         }
@@ -357,7 +360,7 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
           // Rows that no token sees can hold anything; clear them, so that a zero weight times Inf or NaN cannot reach O.
           for (int e = lane; e < (r0 + ROWS - it.end) * (D / 8); e += 32) {
             const int row = it.end - r0 + e / (D / 8), ch = e % (D / 8);
-            st_shared16(slot + kFtSlot / 2 + (ch >> 3) * HALF + row * 128 + ((ch & 7) << 4), 0, 0, 0, 0);
+            st_shared16(slot + kFtSlot / 2 + (ch >> 3) * 1024 + (row >> 3) * GROUP + (row & 7) * 128 + ((ch & 7) << 4), 0, 0, 0, 0);
           }
           __syncwarp();
           proxy_fence();
@@ -391,11 +394,11 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
           const uint32_t ha = pack_bf16(w0, w1), hb = pack_bf16(w2, w3);
           const uint32_t la = turned(pack_bf16_rest(w0, w1, ha)), lb = turned(pack_bf16_rest(w2, w3, hb));
           const uint32_t pa = turned(ha), pb = turned(hb);
-          const uint32_t v_at = slot + kFtSlot / 2 + t * 2048 + ((lane & 7) + (lane >> 4) * 8) * 128;
+          const uint32_t v_at = slot + kFtSlot / 2 + t * 2 * GROUP + (lane >> 4) * GROUP + (lane & 7) * 128;
 #pragma unroll
           for (int d = 0; d < KS; ++d) {
             uint32_t x[4];
-            ldsm4_trans(x, v_at + (d >> 2) * HALF + (((2 * (d & 3) + ((lane >> 3) & 1)) ^ (lane & 7)) << 4));
+            ldsm4_trans(x, v_at + (d >> 2) * 1024 + (((2 * (d & 3) + ((lane >> 3) & 1)) ^ (lane & 7)) << 4));
             mma16816(o[d], x, pa, pb);
             mma16816(o[d], x, la, lb);
           }
@@ -549,7 +552,7 @@ static int launch_ft(const FtArgs& A, const void* K, const void* V, cudaStream_t
   std::memset(&map_k, 0, sizeof map_k);
   std::memset(&map_v, 0, sizeof map_v);
   const int box = std::min(kFtRows<D>, 1 << a.pages.shift);
-  if (!make_query_map(&map_q, a, A.TG) || !make_cache_map(&map_k, K, a.g, box, true) || !make_cache_map(&map_v, V, a.g, box, true))
+  if (!make_query_map(&map_q, a, A.TG) || !make_pool_map(&map_k, K, a.g, box) || !make_pool_map(&map_v, V, a.g, box))
     return L2KV_ERR_UNSUPPORTED;
   auto kern = few_tokens_kernel<D>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kFtSmem<D>) != cudaSuccess) return L2KV_ERR_CUDA;

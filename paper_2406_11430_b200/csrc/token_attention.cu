@@ -354,6 +354,8 @@ __global__ void __launch_bounds__(kTaThreads, 1)
 token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__ CUtensorMap map_q,
                        const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   constexpr int QTILE = kTaQTile<D>, TILE = kTaTile<D>, SLOTS = kTaSlots<D>;
+  // between the halves of a tile of cached rows, and between its groups of 8 rows (pages: see make_pool_map)
+  constexpr int HALF = PAGED ? 1024 : kTaSubHalf, GROUP = PAGED ? D * 16 : 1024;
   extern __shared__ __align__(1024) unsigned char smem[];
   const TokenAttention& a = A.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -483,15 +485,14 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
   };
   // The same over pages, by the whole warp: lane i holds entry i of 32 of the table's, for K and, behind it, for V,
   // and asked for the 32 after them when it got these, so that no copy waits for an entry.  A tile is one box or, of pages
-  // shorter than it, several, a lane's each; what lies behind the item's rows, or in a page that is none, is filled with zeros
+  // shorter than it, one for each, a lane's each; what lies behind the item's rows, or in a page that is none, is filled with zeros
   // (a box outside the pool), and such pages are told.
   [[maybe_unused]] auto fetch_pages = [&](const TaItem& it) {
     const PageView& pages = a.pages;
     const int32_t* const table = pages.of(it.b, it.l);
     const int places = ta_places(it.n, it.pair), ahead = it.pair ? 2 : 4;
-    const int box = min(kTaSub, pages.rows()), n_boxes = kTaSub / box;          // boxes of a tile's half row
+    const int box = min(kTaSub, pages.rows()), n_boxes = kTaSub / box;
     const int n_ids = (it.end + pages.rows() - 1) >> pages.shift;              // pages with rows that a token sees
-    const int of_half = lane / n_boxes, of_box = lane % n_boxes;
     auto ids = [&](int chunk) {
       const int p = chunk * 32 + lane;
       const int id = p < n_ids ? table[p] : -1;
@@ -526,12 +527,11 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
         if (!it.pair) mbar_arrive(empty);                // for the chain that does not use it
         mbar_expect_tx(full, TILE);
       }
-      const int id = __shfl_sync(0xffffffffu, is_k ? k_ids : v_ids, (page + of_box) & 31);
+      const int id = __shfl_sync(0xffffffffu, is_k ? k_ids : v_ids, (page + lane) & 31);
       __syncwarp();
-      if (of_half < D / 64) {
+      if (lane < n_boxes) {
         const int row = id < 0 ? pages.n << pages.shift : (id << pages.shift) + (t & (pages.rows() - 1));
-        tma_load_5d((is_k ? s_k : s_v) + (at % SLOTS) * TILE + of_half * kTaSubHalf + of_box * box * 128, is_k ? &map_k : &map_v, full,
-                    of_half * 64, row, it.h, 0, 0);
+        tma_load_5d((is_k ? s_k : s_v) + (at % SLOTS) * TILE + lane * box * D * 2, is_k ? &map_k : &map_v, full, 0, 0, 0, row >> 3, it.h);
       }
     };
     for (int g = 0; ok && g < places + ahead; ++g) {
@@ -631,11 +631,11 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
       auto place = [&](int u) { return pos + (pair ? u : 2 * u + c); };
       const uint64_t dq = umma_desc(s_q + (pair ? c * QTILE : 0), 16, 1024);
       auto qk = [&](uint32_t at) {                       // S[n_s & 1] = Q K^T; elected lane only
-        const uint64_t dk = umma_desc(s_k + (at % SLOTS) * TILE, 16, 1024);
+        const uint64_t dk = umma_desc(s_k + (at % SLOTS) * TILE, 16, GROUP);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)                 // (the address fields count 16 bytes)
           umma_ss(t_c + (n_s & 1) * 64, dq + (((k >> 2) * kTaHalf + (k & 3) * 32) >> 4),
-                  dk + (((k >> 2) * kTaSubHalf + (k & 3) * 32) >> 4), kTaIdescQK, k > 0);
+                  dk + (((k >> 2) * HALF + (k & 3) * 32) >> 4), kTaIdescQK, k > 0);
         umma_commit(s_full(c, n_s));
         umma_commit(k_empty(at));
       };
@@ -658,11 +658,11 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
         ok = wait(p_full(c, n_p), (n_p >> 1) & 1u) && ok;
         if (!__all_sync(0xffffffffu, ok)) break;
         tc_fence_after();
-        const uint64_t dv = umma_desc(s_v + (v % SLOTS) * TILE, kTaSubHalf, 1024);
+        const uint64_t dv = umma_desc(s_v + (v % SLOTS) * TILE, HALF, GROUP);
         if (elect_one()) {                               // O += P V(u)
 #pragma unroll
           for (int k = 0; k < kTaSub / 16; ++k)
-            umma_ts(t_c + 128, t_c + (n_p & 1) * 64 + k * 8, dv + (k * 2048 >> 4), kTaIdescPV<D>, u > 0 || k > 0);
+            umma_ts(t_c + 128, t_c + (n_p & 1) * 64 + k * 8, dv + (k * 2 * GROUP >> 4), kTaIdescPV<D>, u > 0 || k > 0);
           umma_commit(v_empty(v));
           // The score columns that P V(u) reads its weights from take scores u + 2: both products come
           // from one thread and run on one tensor core, which takes them in the order of issue.
@@ -749,7 +749,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
           if (row < kTaSub && row >= it.end - r0) {
 #pragma unroll
             for (int c = 0; c < D / 8; ++c)
-              st_shared16(s_v + (v % SLOTS) * TILE + (c >> 3) * kTaSubHalf + row * 128 + ((c & 7) << 4), 0, 0, 0, 0);
+              st_shared16(s_v + (v % SLOTS) * TILE + (c >> 3) * HALF + (row >> 3) * GROUP + (row & 7) * 128 + ((c & 7) << 4), 0, 0, 0, 0);
           }
           proxy_fence();
         }
@@ -1042,7 +1042,8 @@ static int launch_ta(const TaArgs& A, const void* K, const void* V, long long it
   std::memset(&map_k, 0, sizeof map_k);
   std::memset(&map_v, 0, sizeof map_v);
   const int box = PAGED ? std::min(kTaSub, 1 << a.pages.shift) : kTaSub;
-  if (!make_query_map(&map_q, a, kTaRows / A.G) || !make_cache_map(&map_k, K, a.g, box, PAGED) || !make_cache_map(&map_v, V, a.g, box, PAGED))
+  if (!make_query_map(&map_q, a, kTaRows / A.G) || !(PAGED ? make_pool_map(&map_k, K, a.g, box) : make_cache_map(&map_k, K, a.g, box)) ||
+      !(PAGED ? make_pool_map(&map_v, V, a.g, box) : make_cache_map(&map_v, V, a.g, box)))
     return L2KV_ERR_UNSUPPORTED;
   auto kern = token_attention_kernel<D, TREE, PAGED>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTaSmem<D>) != cudaSuccess)
