@@ -8,10 +8,13 @@
 // the weights turned from the one's result to the other's operand by movmatrix.  They go in as two bf16 terms (16 significant
 // bits): the second product is free here, and what is left is the rounding of the result.
 //
-// Roles: one warp works out the items and fetches blocks of 16 KB (K and V of 32 rows; of 64 for 64-wide heads), a TMA box per page and
-// tensor, through a ring of 12; four warps take the blocks by turns, each with sums of its own, and join them
-// when the item ends.  A fixed grid of CTAs takes equal shares of all blocks; items that a share's end cuts leave
-// partial results that a second kernel joins.  Every wait is bounded; one that gives up ends the CTA and marks the workspace.
+// Roles: four warps fetch blocks of 16 KB (K and V of 32 rows; of 64 for 64-wide heads), a TMA box per page and tensor,
+// through a ring of 12 (a warp takes 100 to 150 cycles per box, so that one could not feed pages of 16 rows); the first of
+// them also works out the items.  Four warps take the blocks by turns, each with sums of its own, and join them when the item
+// ends.  The blocks of all items are dealt out in stretches of equal cost, chunks: a large one to each CTA, the last part in
+// small ones to whoever is done first (with equal shares the CTAs of a stream of 1.4 GB ended between 167 and 228 us: the
+// memory does not serve all SMs alike).  Items that a chunk's end cuts leave partial results that a second kernel joins.
+// Every wait is bounded; one that gives up ends the CTA and marks the workspace.
 #include <algorithm>
 #include <climits>
 #include <cstring>
@@ -31,7 +34,10 @@ constexpr int kFtSlot = 16384;                  // bytes of a block
 constexpr int kFtDescs = 4;                     // items whose queries are on their way
 constexpr int kFtPolls = 18;                    // log2 of the polls a wait may take
 constexpr int kFtItemCost = 2;                  // what an item costs beyond its blocks, in blocks
-constexpr int kFtMinShare = 4;                  // no shorter shares: a block for each warp
+constexpr int kFtMinShare = 4;                  // no shorter chunks: a block for each warp
+constexpr int kFtDealFrom = 64;                 // equal shares up to this many blocks
+constexpr int kFtChunks = kFtGrid * 6;          // at most: one to each CTA, and a quarter of the cost in sixteenths of a share
+constexpr int kFtTicket = 8;                    // word of the status block that counts the chunks taken (rests at zero)
 constexpr int kFtWholeLen = 512;                // caches up to this length are never cut
 constexpr float kFtRescaleGap = 8.f;            // log2 units a maximum may drift before sums are rescaled
 template <int D> constexpr int kFtRows = 4096 / D;               // cached rows of a block
@@ -39,36 +45,36 @@ template <int D> constexpr int kFtGroup = D * 16;                // bytes of 8 o
 template <int D> constexpr int kFtPitch = D + 4;                 // floats between query rows in shared memory (no bank twice)
 template <int D> constexpr int kFtPart = kFtWarps * kFtCols * kFtPitch<D> * 4;
 constexpr int kFtCtrl = 1024;
-template <int D> constexpr int kFtSmem = 1024 + kFtSlots * kFtSlot + kFtDescs * 2048 + kFtPart<D> + kFtCtrl;
+template <int D> constexpr int kFtSmem = 1024 + kFtSlots * kFtSlot + kFtDescs * 2048 + kFtPart<D> + kFtCtrl + kFtThreads * 24;
 
+// Where a chunk begins.
 struct FtSpot {
   long long at;          // cost of everything before the item
   int e, item, off;      // entry (b, l), number of the item within it (tokens by tokens, head by head), block within the item
-  int pad;
+  int tok0, nq, chunks;  // the item's first token in the list, its tokens; chunks of the call
 };
 struct FtArgs {
   TokenAttention a;
   int G, TG;             // query heads per KV head, tokens per item
-  FtSpot* plan;          // [kFtGrid] where each CTA's share begins; null: items stay whole
-  float* part;           // [2 kFtGrid][8][D] rows, then [2 kFtGrid][8] log2-sum-exps
+  FtSpot* plan;          // [kFtChunks] where each chunk begins; null: items stay whole
+  float* part;           // [2 kFtChunks][8][D] rows, then [2 kFtChunks][8] log2-sum-exps
   float* part_lse;
 };
-struct FtEntry { int n, cur; };
-// An entry as the shares see it: with a length per head, the longest head's.
+// An entry as the chunks see it: with a length per head, the longest head's.
+struct FtEntry { int n, cur, first; };
 __device__ __forceinline__ FtEntry ft_entry(const TokenAttention& a, int e) {
-  const int n = tokens_of(a.tok_off, e / a.g.L, a.n_tokens).n;
-  if (n == 0) return {0, 0};
   int cur = a.lens.at(e, 0, a.g.H);
   if (a.lens.per_head)
     for (int h = 1; h < a.g.H; ++h) cur = max(cur, a.lens.at(e, h, a.g.H));
-  return {n, max(0, min(cur, min(a.max_len, a.g.t_cap)))};
+  const TokRange r = tokens_of(a.tok_off, e / a.g.L, a.n_tokens);
+  return {r.n, max(0, min(cur, min(a.max_len, a.g.t_cap))), r.first};
 }
 template <int D> __device__ __forceinline__ int ft_blocks(int rows) { return (rows + kFtRows<D> - 1) / kFtRows<D>; }
 __device__ __forceinline__ int ft_items(const FtArgs& A, const FtEntry& e) { return (e.n + A.TG - 1) / A.TG * A.a.g.H; }
 template <int D> __device__ __forceinline__ int ft_each(const FtEntry& e) { return ft_blocks<D>(e.cur) + kFtItemCost; }
 
 struct FtItem {
-  int l, h, tok0, nq;    // first token in the list, tokens
+  int b, l, h, tok0, nq; // first token in the list, tokens
   int first, cur, end;   // rows its first token sees; rows there are; rows that some token sees
   int row0, n;           // first row of the piece, its blocks
   uint32_t at;           // running number of its first block
@@ -76,17 +82,17 @@ struct FtItem {
   int stop;
 };
 template <int D>
-__device__ __forceinline__ FtItem ft_item(const FtArgs& A, int e, int item, int from, int to, int slot) {
+__device__ __forceinline__ FtItem ft_item(const FtArgs& A, int e, const FtEntry& y, int item, int from, int to, int slot) {
   const TokenAttention& a = A.a;
-  const int b = e / a.g.L, p = item / a.g.H;
-  const TokRange r = tokens_of(a.tok_off, b, a.n_tokens);
+  const int p = item / a.g.H;
   FtItem it;
+  it.b = e / a.g.L;
   it.l = e % a.g.L;
   it.h = item % a.g.H;
-  it.tok0 = r.first + p * A.TG;
-  it.nq = min(A.TG, r.n - p * A.TG);
-  it.cur = max(0, min(a.lens.at(e, it.h, a.g.H), min(a.max_len, a.g.t_cap)));
-  it.first = it.cur - r.n + p * A.TG + 1;
+  it.tok0 = y.first + p * A.TG;
+  it.nq = min(A.TG, y.n - p * A.TG);
+  it.cur = a.lens.per_head ? max(0, min(a.lens.at(e, it.h, a.g.H), min(a.max_len, a.g.t_cap))) : y.cur;
+  it.first = it.cur - y.n + p * A.TG + 1;
   it.end = max(0, min(it.cur, it.first + it.nq - 1));
   it.row0 = from * kFtRows<D>;
   it.n = max(0, min(to, ft_blocks<D>(it.end)) - from);
@@ -130,7 +136,8 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
   const uint32_t bars = smem_u32(ctrl);
   FtItem* const items = reinterpret_cast<FtItem*>(ctrl + 384);           // [kFtDescs]
   float2* const s_stat = reinterpret_cast<float2*>(ctrl + 640);          // [kFtWarps][8]: maximum, sum
-  __shared__ FtSpot s_spot[2];
+  long long* const s_before = reinterpret_cast<long long*>(ctrl + kFtCtrl);         // [kFtThreads]: cost before a thread's entries
+  FtEntry* const s_entry = reinterpret_cast<FtEntry*>(s_before + kFtThreads);       // [kFtThreads]: its first entry
   __shared__ long long s_sum[kFtThreads / 32];
   __shared__ int s_fail_word, s_marked;
   volatile int* const s_fail = &s_fail_word;
@@ -138,10 +145,15 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
   auto empty = [&](uint32_t at) { return bars + 96u + 8u * (at % kFtSlots); };
   auto desc_full = [&](uint32_t i) { return bars + 192u + 8u * (i % kFtDescs); };
   auto desc_free = [&](uint32_t i) { return bars + 224u + 8u * (i % kFtDescs); };
-  const uint32_t part_full = bars + 256u, part_free = bars + 264u;
+  auto item_full = [&](uint32_t i) { return bars + 256u + 8u * (i % kFtDescs); };
+  const uint32_t part_full = bars + 288u, part_free = bars + 296u;
   if (tid == 0) {
     for (int i = 0; i < kFtSlots; ++i) { mbar_init(full(i), 2); mbar_init(empty(i), 1); }
-    for (int i = 0; i < kFtDescs; ++i) { mbar_init(desc_full(i), 1); mbar_init(desc_free(i), kFtWarps); }
+    for (int i = 0; i < kFtDescs; ++i) {
+      mbar_init(desc_full(i), 1);
+      mbar_init(desc_free(i), kFtWarps + kFtFetch - 1);
+      mbar_init(item_full(i), 1);
+    }
     mbar_init(part_full, kFtWarps);
     mbar_init(part_free, kFtWarps);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -155,13 +167,13 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
   // A wait that gave up in an earlier call marks the workspace; nothing runs until it is cleared.
   if (tid == 0) s_marked = a.status ? *reinterpret_cast<volatile int32_t*>(a.status + 2) : 0;
 
-  // ---- this CTA's share: [c, c + 1) of equal stretches of all items' cost, each thread with a run of entries -----------
+  // ---- the cost of everything, each thread with a run of entries ---------------------------------------
   const int entries = a.g.B * a.g.L, run = (entries + kFtThreads - 1) / kFtThreads, e0 = min(entries, tid * run), e1 = min(entries, e0 + run);
   long long mine = 0;
-  FtEntry only{0, 0};
-  for (int e = e0; e < e1; ++e) {
-    only = ft_entry(a, e);
-    mine += (long long)ft_items(A, only) * ft_each<D>(only);
+  for (int e = e1 - 1; e >= e0; --e) {
+    const FtEntry y = ft_entry(a, e);
+    mine += (long long)ft_items(A, y) * ft_each<D>(y);
+    if (e == e0) s_entry[tid] = y;
   }
   long long incl = mine;
 #pragma unroll
@@ -172,43 +184,15 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
   if (lane == 31) s_sum[warp] = incl;
   __syncthreads();
   long long total = 0, before = incl - mine;
+#pragma unroll
   for (int w = 0; w < kFtThreads / 32; ++w) {
     if (w < warp) before += s_sum[w];
     total += s_sum[w];
   }
-  const long long share = A.plan ? max((total + gridDim.x - 1) / gridDim.x, (long long)kFtMinShare) : (total + gridDim.x - 1) / gridDim.x;
-  for (int k = 0; k < 2; ++k) {
-    const long long x = (blockIdx.x + k) * share;
-    if (tid == 0 && x >= total) s_spot[k] = FtSpot{total, entries, 0, 0, 0};
-    if (x < before || x >= before + mine) continue;
-    long long at = before;
-    int e = e0;
-    FtEntry y = e1 - e0 == 1 ? only : ft_entry(a, e);
-    while (true) {
-      const long long here = (long long)ft_items(A, y) * ft_each<D>(y);
-      if (x < at + here) break;
-      at += here;
-      y = ft_entry(a, ++e);
-    }
-    const int each = ft_each<D>(y), n = each - kFtItemCost;
-    FtSpot s{0, e, (int)((x - at) / each), 0, 0};
-    s.at = at + (long long)s.item * each;
-    s.off = max(0, (int)(x - s.at) - kFtItemCost);
-    if (s.off < 2) s.off = 0;                            // (no slivers)
-    if (s.off > 0 && (!A.plan || n - s.off < 2)) {       // the next item
-      s.at += each;
-      s.off = 0;
-      if (++s.item == ft_items(A, y)) {
-        s.item = 0;
-        do ++s.e; while (s.e < entries && tokens_of(a.tok_off, s.e / a.g.L, a.n_tokens).n == 0);
-      }
-    }
-    s_spot[k] = s;
-  }
+  s_before[tid] = before;
   __syncthreads();
   next_may_start();
   if (s_marked) return;
-  if (A.plan && tid == 0) A.plan[blockIdx.x] = s_spot[0];
   // A wait that another role's failure ends too.
   auto wait = [&](uint32_t bar, uint32_t parity) {
     if (mbar_test(bar, parity)) return true;
@@ -221,63 +205,134 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
     const int box = min(ROWS, pages.rows()), n_boxes = ROWS / box, of_box = lane % n_boxes;
     const int me = warp - kFtWarps;
     const bool is_v = me & 1, leads = me == 0;
-    FtSpot spot = s_spot[0];
-    const FtSpot end = s_spot[1];
     uint32_t at = 0, n_desc = 0;
     bool ok = true;
-    int entry = -1, items_of = 0, each = 1;
+
+    // The chunks: of `large` to each CTA, then of `small` (where there is enough to deal out).
+    const long long fair = total < INT_MAX ? ((int)total + kFtGrid - 1) / kFtGrid : (total + kFtGrid - 1) / kFtGrid;
+    const bool deals = A.plan && fair > kFtDealFrom;
+    const long long large = !A.plan ? fair : deals ? fair * 3 / 4 : max(fair, (long long)kFtMinShare), small = (fair + 15) / 16;
+    const int chunks = !deals ? kFtGrid : kFtGrid + (int)((total - kFtGrid * large + small - 1) / small);
+    auto begins = [&](int c) { return c <= kFtGrid ? c * large : kFtGrid * large + (c - kFtGrid) * small; };
+    // The place in the list where x of the cost is behind; `y`: its entry.  A place close to an item's start or end is moved
+    // there, so that no sliver is cut off.
+    auto find = [&](long long x, FtEntry& y) {
+      FtSpot s{total, entries, 0, 0, 0, 0, chunks};
+      y = FtEntry{0, 0, 0};
+      if (x >= total) return s;
+      int t = 8 * (__popc(__ballot_sync(0xffffffffu, s_before[kFtThreads / 32 * lane] <= x)) - 1);   // the last run that begins by x
+      t += __popc(__ballot_sync(0xffffffffu, lane < kFtThreads / 32 && s_before[t + (lane & 7)] <= x)) - 1;
+      s.e = t * run;
+      s.at = s_before[t];
+      y = s_entry[t];
+      int items = ft_items(A, y), each = ft_each<D>(y);
+      while (x >= s.at + (long long)items * each) {
+        s.at += (long long)items * each;
+        y = ft_entry(a, ++s.e);
+        items = ft_items(A, y);
+        each = ft_each<D>(y);
+      }
+      const long long in = x - s.at;
+      s.item = in < INT_MAX ? (int)in / each : (int)(in / each);
+      s.at += (long long)s.item * each;
+      s.off = max(0, (int)(x - s.at) - kFtItemCost);
+      const int n = each - kFtItemCost;
+      if (s.off < 2) s.off = 0;
+      if (s.off > 0 && (!A.plan || n - s.off < 2)) {     // the next item
+        s.at += each;
+        s.off = 0;
+        if (++s.item == items) {
+          s.item = 0;
+          do y = ++s.e < entries ? (run == 1 ? s_entry[s.e] : ft_entry(a, s.e)) : FtEntry{0, 0, 0};
+          while (s.e < entries && y.n == 0);
+        }
+      }
+      s.tok0 = y.first + s.item / a.g.H * A.TG;
+      s.nq = min(A.TG, y.n - s.item / a.g.H * A.TG);
+      return s;
+    };
+
+    int chunk = (int)blockIdx.x;
+    FtSpot spot{}, end{};
+    FtEntry y{};
+    bool more = leads;                                   // chunks to come
+    if (leads) {
+      FtEntry z;
+      spot = find(begins(chunk), y);
+      end = find(begins(chunk + 1), z);
+      if (A.plan && lane == 0) A.plan[chunk] = spot;
+    }
     while (ok) {
       FtItem it;
-      it.stop = 1;
-      it.n = 0;
-      if (spot.at < end.at || (spot.at == end.at && spot.off < end.off)) {
-        if (spot.e != entry) {
-          const FtEntry y = ft_entry(a, spot.e);
-          entry = spot.e;
-          items_of = ft_items(A, y);
-          each = ft_each<D>(y);
+      if (leads) {
+        while (more && !(spot.at < end.at || (spot.at == end.at && spot.off < end.off))) {
+          more = false;
+          if (deals) {
+            int ticket = 0;
+            if (lane == 0) ticket = atomicAdd(a.status + kFtTicket, 1);
+            chunk = kFtGrid + __shfl_sync(0xffffffffu, ticket, 0);
+            if (chunk < chunks) {
+              FtEntry z;
+              more = true;
+              spot = find(begins(chunk), y);
+              end = find(begins(chunk + 1), z);
+              if (lane == 0) A.plan[chunk] = spot;
+            }
+          }
         }
-        const int n = each - kFtItemCost, to = spot.at == end.at ? end.off : n;
-        // a piece that does not begin its item goes to this CTA's first slot, one that does to its second
-        it = ft_item<D>(A, spot.e, spot.item, spot.off, to, spot.off > 0 ? 2 * (int)blockIdx.x : to < n ? 2 * (int)blockIdx.x + 1 : -1);
-        spot.at += each;
-        spot.off = 0;
-        if (++spot.item == items_of) {
-          spot.item = 0;
-          do ++spot.e; while (spot.e < entries && tokens_of(a.tok_off, spot.e / a.g.L, a.n_tokens).n == 0);
+        it = FtItem{};
+        it.stop = 1;
+        if (more) {
+          const int each = ft_each<D>(y), n = each - kFtItemCost, to = spot.at == end.at ? end.off : n;
+          // a piece that does not begin its item goes to this chunk's first slot, one that does to its second
+          it = ft_item<D>(A, spot.e, y, spot.item, spot.off, to, spot.off > 0 ? 2 * chunk : to < n ? 2 * chunk + 1 : -1);
+          spot.at += each;
+          spot.off = 0;
+          if (++spot.item == ft_items(A, y)) {
+            spot.item = 0;
+            do y = ++spot.e < entries ? (run == 1 ? s_entry[spot.e] : ft_entry(a, spot.e)) : FtEntry{0, 0, 0};
+            while (spot.e < entries && y.n == 0);
+          }
         }
+        it.at = at;
+        if (n_desc >= kFtDescs) ok = __all_sync(0xffffffffu, wait(desc_free(n_desc), (n_desc / kFtDescs - 1) & 1u));
+        if (!ok) break;
+        if (lane == 0) {
+          items[n_desc % kFtDescs] = it;
+          mbar_arrive(item_full(n_desc));
+          if (it.n == 0) {
+            mbar_arrive(desc_full(n_desc));
+          } else {
+            mbar_expect_tx(desc_full(n_desc), D / 64 * 1024);
+            for (int c = 0; c < D / 64; ++c)
+              tma_load_4d(s_q + n_desc % kFtDescs * 2048 + c * 1024, &map_q, desc_full(n_desc), c * 64, it.h * A.G, it.tok0, it.l);
+          }
+        }
+        __syncwarp();
+      } else {
+        ok = __all_sync(0xffffffffu, wait(item_full(n_desc), (n_desc / kFtDescs) & 1u));
+        if (!ok) break;
+        it = items[n_desc % kFtDescs];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(desc_free(n_desc));
       }
-      it.at = at;
-      if (leads && n_desc >= kFtDescs) ok = __all_sync(0xffffffffu, wait(desc_free(n_desc), (n_desc / kFtDescs - 1) & 1u));
-      if (!ok) break;
-      if (leads && lane == 0) {
-        items[n_desc % kFtDescs] = it;
-        if (it.n == 0) {
-          mbar_arrive(desc_full(n_desc));
-        } else {
-          mbar_expect_tx(desc_full(n_desc), D / 64 * 1024);
-          for (int c = 0; c < D / 64; ++c)
-            tma_load_4d(s_q + n_desc % kFtDescs * 2048 + c * 1024, &map_q, desc_full(n_desc), c * 64, it.h * A.G, it.tok0, it.l);
-        }
-      }
-      __syncwarp();
       ++n_desc;
       if (it.stop) break;
       if (it.n == 0) continue;
       // lane i holds entry i of 32 of the table's, and the one 32 further on is on its way
-      const int32_t* const table = pages.of(entry / a.g.L, entry % a.g.L);
+      const int32_t* const table = pages.of(it.b, it.l);
       const int n_ids = (it.end + pages.rows() - 1) >> pages.shift;
-      auto ids = [&](int chunk) {
-        const int p = chunk * 32 + lane;
+      auto ids = [&](int from) {
+        const int p = from * 32 + lane;
         const int id = p < n_ids ? table[p] : -1;
         const bool bad = p < n_ids && !pages.valid(id);
         if (bad && a.status) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
         return bad ? -1 : id;
       };
-      int chunk = it.row0 >> pages.shift >> 5, now = ids(chunk), later = ids(chunk + 1);
+      int held = it.row0 >> pages.shift >> 5, now = ids(held), later = ids(held + 1);
       for (int g = 0; g < it.n; ++g, ++at) {
         const int t = it.row0 + g * ROWS, page = t >> pages.shift;
-        if (page >> 5 != chunk) { ++chunk; now = later; later = ids(chunk + 1); }
+        if (page >> 5 != held) { ++held; now = later; later = ids(held + 1); }
         if ((at & 1) != (uint32_t)(me >> 1)) continue;
         const int id = __shfl_sync(0xffffffffu, now, (page + of_box) & 31);
         const int row = id < 0 ? pages.n << pages.shift : (id << pages.shift) + (t & (pages.rows() - 1));
@@ -432,7 +487,7 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
       ok = __all_sync(0xffffffffu, wait(part_full, n_desc & 1u));
       if (!ok) break;
       const int col = tid >> 4, piece = tid & 15, tok = it.tok0 + col / A.G, head = it.h * A.G + col % A.G;
-      if (col < it.nq * A.G && L2KV_BOUNDS(tok >= 0 && tok < a.n_tokens && head < a.g.Hq && it.slot < 2 * kFtGrid, a.status)) {
+      if (col < it.nq * A.G && L2KV_BOUNDS(tok >= 0 && tok < a.n_tokens && head < a.g.Hq && it.slot < 2 * kFtChunks, a.status)) {
         float m = -INFINITY, sum = 0.f, f[kFtWarps];
 #pragma unroll
         for (int w = 0; w < kFtWarps; ++w) m = fmaxf(m, s_stat[w * kFtCols + col].x);
@@ -475,28 +530,43 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
 }
 
 // Joins the pieces of items that were cut: out = sum_c w_c O_c / sum_c w_c, w_c = 2^(lse_c - max lse), piece by piece in
-// order.  A block per share that begins inside an item (the first of them where there are several), a warp per query row.
+// order.  A block per chunk that begins inside an item (the first of them where there are several), a warp per query row.
+// What it takes is a chain of loads, so up to kJoinAhead pieces are asked for before anything is known of them.
+constexpr int kJoinAhead = 8;
 template <int D>
 __global__ void __launch_bounds__(32 * kFtCols)
 few_tokens_join_kernel(const __grid_constant__ FtArgs A) {
   constexpr int V = D / 32;
-  __shared__ FtSpot plan[kFtGrid];
   const TokenAttention& a = A.a;
-  const int lane = threadIdx.x & 31, col = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, col = threadIdx.x >> 5, c0 = (int)blockIdx.x + 1;
   next_may_start();
   wait_for_previous();
-  if (a.status && a.status[2] != 0) return;              // a wait gave up: no output
-  for (int i = threadIdx.x; i < kFtGrid; i += 32 * kFtCols) plan[i] = A.plan[i];
-  __syncthreads();
-  const int c0 = (int)blockIdx.x + 1;
-  const FtSpot s = plan[c0];
-  if (s.off == 0 || (plan[c0 - 1].at == s.at && plan[c0 - 1].off > 0)) return;
-  int nc = 2;                                            // the piece before c0's, and c0's
-  while (c0 + nc - 1 < kFtGrid && plan[c0 + nc - 1].at == s.at && plan[c0 + nc - 1].off > 0) ++nc;
-  if (!L2KV_BOUNDS(s.e >= 0 && s.e < a.g.B * a.g.L && s.item >= 0, a.status)) return;
-  const FtItem it = ft_item<D>(A, s.e, s.item, 0, INT_MAX, 0);
-  if (col >= it.nq * A.G) return;
+  const int marked = a.status[2], chunks = A.plan[0].chunks;
+  const FtSpot prior = A.plan[c0 - 1], s = A.plan[c0];   // (behind the last chunk: whatever the workspace holds)
+  if (c0 == 1 && threadIdx.x == 0) a.status[kFtTicket] = 0;
+  if (marked || c0 >= chunks) return;                    // (marked: a wait gave up, no output)
+  if (s.off == 0 || (prior.at == s.at && prior.off > 0) || col >= s.nq * A.G) return;
   auto row = [&](int c) { return (long long)(c == 0 ? 2 * c0 - 1 : 2 * (c0 + c - 1)) * kFtCols + col; };
+  auto piece = [&](int c, float (&x)[V]) {
+    const float* const from = A.part + row(c) * D + lane * V;
+    if constexpr (V == 4) {
+      const float4 y = *reinterpret_cast<const float4*>(from);
+      x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w;
+    } else {
+      const float2 y = *reinterpret_cast<const float2*>(from);
+      x[0] = y.x; x[1] = y.y;
+    }
+  };
+  // the piece before c0's, c0's, and those of the chunks behind it that begin in the same item
+  int nc = 2;
+  while (true) {
+    const int c = c0 + nc - 1 + lane;
+    const bool in = c < chunks && A.plan[min(c, kFtChunks - 1)].at == s.at && A.plan[min(c, kFtChunks - 1)].off > 0;
+    const unsigned more = __ballot_sync(0xffffffffu, in);
+    nc += more == 0xffffffffu ? 32 : __ffs(~more) - 1;
+    if (more != 0xffffffffu) break;
+  }
+  if (!L2KV_BOUNDS(s.e >= 0 && s.e < a.g.B * a.g.L && s.item >= 0 && c0 + nc - 2 < kFtChunks, a.status)) return;
   float top = -INFINITY;
   for (int c = lane; c < nc; c += 32) top = fmaxf(top, A.part_lse[row(c)]);
 #pragma unroll
@@ -505,43 +575,40 @@ few_tokens_join_kernel(const __grid_constant__ FtArgs A) {
   for (int b = 0; b < nc; b += 32) {
     const float lse2 = b + lane < nc ? A.part_lse[row(b + lane)] : -INFINITY;
     const float mine = lse2 == -INFINITY ? 0.f : exp2f(lse2 - top);
-#pragma unroll 8
-    for (int c = 0; c < min(32, nc - b); ++c) {
-      const float w = __shfl_sync(0xffffffffu, mine, c);
-      const float* const from = A.part + row(b + c) * D + lane * V;
-      float x[V];
-      if constexpr (V == 4) {
-        const float4 y = *reinterpret_cast<const float4*>(from);
-        x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w;
-      } else {
-        const float2 y = *reinterpret_cast<const float2*>(from);
-        x[0] = y.x; x[1] = y.y;
-      }
-      den += w;
+    for (int c = 0; c < min(32, nc - b); c += kJoinAhead) {
+      float x[kJoinAhead][V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) num[i] = fmaf(w, x[i], num[i]);       // (rows of a piece that sees nothing are zeros)
+      for (int i = 0; i < kJoinAhead; ++i) piece(min(b + c + i, nc - 1), x[i]);
+#pragma unroll
+      for (int i = 0; i < kJoinAhead; ++i) {             // (behind the last piece the weight is zero)
+        const float w = __shfl_sync(0xffffffffu, mine, c + i);
+        den += w;
+#pragma unroll
+        for (int k = 0; k < V; ++k) num[k] = fmaf(w, x[i][k], num[k]);       // (rows of a piece that sees nothing are zeros)
+      }
     }
   }
   const float inv = den == 0.f ? 0.f : 1.f / den;
-  const int tok = it.tok0 + col / A.G, head = it.h * A.G + col % A.G;
-  __nv_bfloat16* const to = a.out.row<__nv_bfloat16>(it.l, tok, head) + lane * V;
+  const int tok = s.tok0 + col / A.G, head = s.item % a.g.H * A.G + col % A.G, l = s.e % a.g.L;
+  if (!L2KV_BOUNDS(tok >= 0 && tok < a.n_tokens && head < a.g.Hq, a.status)) return;
+  __nv_bfloat16* const to = a.out.row<__nv_bfloat16>(l, tok, head) + lane * V;
   if constexpr (V == 4)
     *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16(num[0] * inv, num[1] * inv), pack_bf16(num[2] * inv, num[3] * inv));
   else
     *reinterpret_cast<uint32_t*>(to) = pack_bf16(num[0] * inv, num[1] * inv);
   if (a.lse && lane == 0)
-    a.lse[((long long)it.l * a.n_tokens + tok) * a.g.Hq + head] = den == 0.f ? -INFINITY : (top + log2f(den)) * 0.6931471805599453f;
+    a.lse[((long long)l * a.n_tokens + tok) * a.g.Hq + head] = den == 0.f ? -INFINITY : (top + log2f(den)) * 0.6931471805599453f;
 }
 
 // ---- host ------------------------------------------------------------------------------------------
 
-constexpr size_t kFtPlanBytes = (kFtGrid * sizeof(FtSpot) + 255) / 256 * 256;
+constexpr size_t kFtPlanBytes = (kFtChunks * sizeof(FtSpot) + 255) / 256 * 256;
 
 // One new token per sequence on average, or fewer: with more of them a tile's rows fill.
 bool few_tokens(const TokenAttention& a, int dtype) { return dtype == L2KV_BF16 && a.pages.table && a.n_tokens <= a.g.B; }
 
 size_t few_tokens_scratch(const Geom& g, int max_len) {
-  return max_len > kFtWholeLen ? kFtPlanBytes + (size_t)2 * kFtGrid * kFtCols * (g.D + 1) * sizeof(float) : 0;
+  return max_len > kFtWholeLen ? kFtPlanBytes + (size_t)2 * kFtChunks * kFtCols * (g.D + 1) * sizeof(float) : 0;
 }
 
 template <int D>
@@ -558,7 +625,7 @@ static int launch_ft(const FtArgs& A, const void* K, const void* V, cudaStream_t
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kFtSmem<D>) != cudaSuccess) return L2KV_ERR_CUDA;
   const int rc = launch_chained(kern, kFtGrid, 1, kFtThreads, kFtSmem<D>, s, A, map_q, map_k, map_v);
   if (rc != L2KV_OK || !A.plan) return rc;
-  return launch_chained(few_tokens_join_kernel<D>, kFtGrid - 1, 1, 32 * kFtCols, 0, s, A);
+  return launch_chained(few_tokens_join_kernel<D>, kFtChunks - 1, 1, 32 * kFtCols, 0, s, A);
 }
 
 int launch_few_tokens(const TokenAttention& a, const void* K, const void* V, char* scratch, size_t scratch_bytes, cudaStream_t s) {
@@ -570,7 +637,7 @@ int launch_few_tokens(const TokenAttention& a, const void* K, const void* V, cha
   if (need > 0 && scratch && scratch_bytes >= need) {
     A.plan = reinterpret_cast<FtSpot*>(scratch);
     A.part = reinterpret_cast<float*>(scratch + kFtPlanBytes);
-    A.part_lse = A.part + (size_t)2 * kFtGrid * kFtCols * a.g.D;
+    A.part_lse = A.part + (size_t)2 * kFtChunks * kFtCols * a.g.D;
   }
   return a.g.D == 128 ? launch_ft<128>(A, K, V, s) : launch_ft<64>(A, K, V, s);
 }
