@@ -11,8 +11,8 @@
 // Roles: four warps fetch blocks of 16 KB (K and V of 32 rows; of 64 for 64-wide heads), a TMA box per page and tensor,
 // through a ring of 12 (a warp takes 100 to 150 cycles per box, so that one could not feed pages of 16 rows); the first of
 // them also works out the items.  Four warps take the blocks by turns, each with sums of its own, and join them when the item
-// ends.  The blocks of all items are dealt out in stretches of equal cost, chunks: a large one to each CTA, the last part in
-// small ones to whoever is done first (with equal shares the CTAs of a stream of 1.4 GB ended between 167 and 228 us: the
+// ends.  The blocks of all items are dealt out in shares of equal cost: three quarters of a share to its CTA, the rest of
+// all shares in sixteenths to whoever is done first (with equal shares the CTAs of a stream of 1.4 GB ended between 167 and 228 us: the
 // memory does not serve all SMs alike).  Items that a chunk's end cuts leave partial results that a second kernel joins.
 // Every wait is bounded; one that gives up ends the CTA and marks the workspace.
 #include <algorithm>
@@ -29,14 +29,15 @@ constexpr int kFtFetch = 4;                     // and warps that fetch: keys an
 constexpr int kFtThreads = 32 * (kFtWarps + kFtFetch);
 constexpr int kFtGrid = 148;
 constexpr int kFtCols = 8;                      // query rows of an item
-constexpr int kFtSlots = 12;                    // a multiple of kFtWarps: a slot is always the same warp's
+constexpr int kFtSlots = 12;                    // a multiple of kFtWarps: within an item a slot is always the same warp's
 constexpr int kFtSlot = 16384;                  // bytes of a block
 constexpr int kFtDescs = 4;                     // items whose queries are on their way
 constexpr int kFtPolls = 18;                    // log2 of the polls a wait may take
 constexpr int kFtItemCost = 2;                  // what an item costs beyond its blocks, in blocks
 constexpr int kFtMinShare = 4;                  // no shorter chunks: a block for each warp
-constexpr int kFtDealFrom = 64;                 // equal shares up to this many blocks
-constexpr int kFtChunks = kFtGrid * 6;          // at most: one to each CTA, and a quarter of the cost in sixteenths of a share
+constexpr int kFtDealFrom = 64;                 // equal shares, whole, up to this many blocks
+constexpr int kFtParts = 5;                     // chunks of a share: three quarters of it, and four sixteenths
+constexpr int kFtChunks = kFtGrid * kFtParts;
 constexpr int kFtTicket = 8;                    // word of the status block that counts the chunks taken (rests at zero)
 constexpr int kFtWholeLen = 512;                // caches up to this length are never cut
 constexpr float kFtRescaleGap = 8.f;            // log2 units a maximum may drift before sums are rescaled
@@ -51,26 +52,35 @@ template <int D> constexpr int kFtSmem = 1024 + kFtSlots * kFtSlot + kFtDescs * 
 struct FtSpot {
   long long at;          // cost of everything before the item
   int e, item, off;      // entry (b, l), number of the item within it (tokens by tokens, head by head), block within the item
-  int tok0, nq, chunks;  // the item's first token in the list, its tokens; chunks of the call
+  int tok0, nq, parts;   // the item's first token in the list, its tokens; chunks of a share in this call
 };
 struct FtArgs {
   TokenAttention a;
-  int G, TG;             // query heads per KV head, tokens per item
+  int G, TG, tg_shift;   // query heads per KV head, tokens per item, log2 of those
   FtSpot* plan;          // [kFtChunks] where each chunk begins; null: items stay whole
   float* part;           // [2 kFtChunks][8][D] rows, then [2 kFtChunks][8] log2-sum-exps
   float* part_lse;
 };
+// a / b for a >= 0, b > 0; quotients of small numbers through fp32 (a division of integers is a chain of about 150 cycles, and
+// working out where a CTA begins is a chain of them).
+__device__ __forceinline__ int ft_div(int a, int b) {
+  if (b == 1) return a;
+  if (a >= 1 << 22) return a / b;
+  const int q = (int)(__int2float_rn(a) * __frcp_rn(__int2float_rn(b)));     // off by one at most
+  const int r = a - q * b;
+  return q + (r >= b) - (r < 0);
+}
 // An entry as the chunks see it: with a length per head, the longest head's.
 struct FtEntry { int n, cur, first; };
 __device__ __forceinline__ FtEntry ft_entry(const TokenAttention& a, int e) {
   int cur = a.lens.at(e, 0, a.g.H);
   if (a.lens.per_head)
     for (int h = 1; h < a.g.H; ++h) cur = max(cur, a.lens.at(e, h, a.g.H));
-  const TokRange r = tokens_of(a.tok_off, e / a.g.L, a.n_tokens);
+  const TokRange r = tokens_of(a.tok_off, ft_div(e, a.g.L), a.n_tokens);
   return {r.n, max(0, min(cur, min(a.max_len, a.g.t_cap))), r.first};
 }
 template <int D> __device__ __forceinline__ int ft_blocks(int rows) { return (rows + kFtRows<D> - 1) / kFtRows<D>; }
-__device__ __forceinline__ int ft_items(const FtArgs& A, const FtEntry& e) { return (e.n + A.TG - 1) / A.TG * A.a.g.H; }
+__device__ __forceinline__ int ft_items(const FtArgs& A, const FtEntry& e) { return ((e.n + A.TG - 1) >> A.tg_shift) * A.a.g.H; }
 template <int D> __device__ __forceinline__ int ft_each(const FtEntry& e) { return ft_blocks<D>(e.cur) + kFtItemCost; }
 
 struct FtItem {
@@ -84,11 +94,11 @@ struct FtItem {
 template <int D>
 __device__ __forceinline__ FtItem ft_item(const FtArgs& A, int e, const FtEntry& y, int item, int from, int to, int slot) {
   const TokenAttention& a = A.a;
-  const int p = item / a.g.H;
+  const int p = ft_div(item, a.g.H);
   FtItem it;
-  it.b = e / a.g.L;
-  it.l = e % a.g.L;
-  it.h = item % a.g.H;
+  it.b = ft_div(e, a.g.L);
+  it.l = e - it.b * a.g.L;
+  it.h = item - p * a.g.H;
   it.tok0 = y.first + p * A.TG;
   it.nq = min(A.TG, y.n - p * A.TG);
   it.cur = a.lens.per_head ? max(0, min(a.lens.at(e, it.h, a.g.H), min(a.max_len, a.g.t_cap))) : y.cur;
@@ -139,6 +149,7 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
   long long* const s_before = reinterpret_cast<long long*>(ctrl + kFtCtrl);         // [kFtThreads]: cost before a thread's entries
   FtEntry* const s_entry = reinterpret_cast<FtEntry*>(s_before + kFtThreads);       // [kFtThreads]: its first entry
   __shared__ long long s_sum[kFtThreads / 32];
+  __shared__ FtSpot s_end;
   __shared__ int s_fail_word, s_marked;
   volatile int* const s_fail = &s_fail_word;
   auto full = [&](uint32_t at) { return bars + 8u * (at % kFtSlots); };
@@ -208,16 +219,19 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
     uint32_t at = 0, n_desc = 0;
     bool ok = true;
 
-    // The chunks: of `large` to each CTA, then of `small` (where there is enough to deal out).
+    // The shares, and, where there is enough to deal out, their chunks.
     const long long fair = total < INT_MAX ? ((int)total + kFtGrid - 1) / kFtGrid : (total + kFtGrid - 1) / kFtGrid;
     const bool deals = A.plan && fair > kFtDealFrom;
-    const long long large = !A.plan ? fair : deals ? fair * 3 / 4 : max(fair, (long long)kFtMinShare), small = (fair + 15) / 16;
-    const int chunks = !deals ? kFtGrid : kFtGrid + (int)((total - kFtGrid * large + small - 1) / small);
-    auto begins = [&](int c) { return c <= kFtGrid ? c * large : kFtGrid * large + (c - kFtGrid) * small; };
+    const int parts = deals ? kFtParts : 1;
+    const long long share = A.plan ? max(fair, (long long)kFtMinShare) : fair;
+    auto begins = [&](int c) {                           // chunk c: part c % parts of a share
+      const int of = c / kFtParts, part = c - of * kFtParts;
+      return !deals ? c * share : of * share + (part ? share * (11 + part) >> 4 : 0);
+    };
     // The place in the list where x of the cost is behind; `y`: its entry.  A place close to an item's start or end is moved
     // there, so that no sliver is cut off.
     auto find = [&](long long x, FtEntry& y) {
-      FtSpot s{total, entries, 0, 0, 0, 0, chunks};
+      FtSpot s{total, entries, 0, 0, 0, 0, parts};
       y = FtEntry{0, 0, 0};
       if (x >= total) return s;
       int t = 8 * (__popc(__ballot_sync(0xffffffffu, s_before[kFtThreads / 32 * lane] <= x)) - 1);   // the last run that begins by x
@@ -233,7 +247,7 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
         each = ft_each<D>(y);
       }
       const long long in = x - s.at;
-      s.item = in < INT_MAX ? (int)in / each : (int)(in / each);
+      s.item = in < INT_MAX ? ft_div((int)in, each) : (int)(in / each);
       s.at += (long long)s.item * each;
       s.off = max(0, (int)(x - s.at) - kFtItemCost);
       const int n = each - kFtItemCost;
@@ -247,20 +261,22 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
           while (s.e < entries && y.n == 0);
         }
       }
-      s.tok0 = y.first + s.item / a.g.H * A.TG;
-      s.nq = min(A.TG, y.n - s.item / a.g.H * A.TG);
+      const int p = ft_div(s.item, a.g.H) << A.tg_shift;
+      s.tok0 = y.first + p;
+      s.nq = min(A.TG, y.n - p);
       return s;
     };
 
-    int chunk = (int)blockIdx.x;
+    int chunk = (int)blockIdx.x * parts;
     FtSpot spot{}, end{};
     FtEntry y{};
     bool more = leads;                                   // chunks to come
-    if (leads) {
-      FtEntry z;
-      spot = find(begins(chunk), y);
-      end = find(begins(chunk + 1), z);
-      if (A.plan && lane == 0) A.plan[chunk] = spot;
+    if (me < 2) {                                        // the first chunk's begin and end, a warp each
+      spot = find(begins(chunk + me), y);
+      if (me == 1 && lane == 0) s_end = spot;
+      asm volatile("bar.sync 1, 64;" ::: "memory");
+      end = s_end;
+      if (leads && A.plan && lane == 0) A.plan[chunk] = spot;
     }
     while (ok) {
       FtItem it;
@@ -270,8 +286,10 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
           if (deals) {
             int ticket = 0;
             if (lane == 0) ticket = atomicAdd(a.status + kFtTicket, 1);
-            chunk = kFtGrid + __shfl_sync(0xffffffffu, ticket, 0);
-            if (chunk < chunks) {
+            ticket = __shfl_sync(0xffffffffu, ticket, 0);
+            const int part = ticket / kFtGrid;           // the first of the sixteenths of all shares, then the second
+            chunk = (ticket - part * kFtGrid) * kFtParts + part + 1;
+            if (part < kFtParts - 1) {
               FtEntry z;
               more = true;
               spot = find(begins(chunk), y);
@@ -382,8 +400,11 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
       float o[KS][4], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
 #pragma unroll
       for (int d = 0; d < KS; ++d) o[d][0] = o[d][1] = o[d][2] = o[d][3] = 0.f;
-      const uint32_t first = (uint32_t)((warp - (int)(it.at % kFtWarps) + kFtWarps) % kFtWarps);
-      for (int u = (int)first; u < it.n; u += kFtWarps) {
+      // Block u is warp u % 4's, wherever the item's blocks lie in the ring, so that a result does not depend on what the
+      // CTA did before.  (A wait tells a phase from its neighbours only, so whoever waits for a block has to know that the one
+      // before it in the same slot has landed: within the item that was a block of the same warp, 12 before, and all blocks of
+      // the items before have been used when an item begins.)
+      for (int u = warp; u < it.n; u += kFtWarps) {
         const uint32_t at = it.at + u, slot = s_ring + at % kFtSlots * kFtSlot;
         ok = __all_sync(0xffffffffu, wait(full(at), (at / kFtSlots) & 1u));
         if (!ok) break;
@@ -529,24 +550,32 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
   if (*s_fail && tid == 0) record_timeout(a.status);
 }
 
-// Joins the pieces of items that were cut: out = sum_c w_c O_c / sum_c w_c, w_c = 2^(lse_c - max lse), piece by piece in
-// order.  A block per chunk that begins inside an item (the first of them where there are several), a warp per query row.
-// What it takes is a chain of loads, so up to kJoinAhead pieces are asked for before anything is known of them.
-constexpr int kJoinAhead = 8;
+// Joins the pieces of items that were cut: out = sum_c w_c O_c / sum_c w_c, w_c = 2^(lse_c - max lse).  A block per chunk
+// that begins inside an item (the first of them where there are several); its warps share the item's query rows and, of each,
+// take every 8th, 4th, .. piece, in a fixed order, so that a result is always the same.  What it takes is a chain of
+// loads, so each warp asks for its first pieces before it knows how many there are (behind the last one: whatever the workspace
+// holds, with no weight).
+constexpr int kJoinWarps = 8;
+constexpr int kJoinAhead = 6;
 template <int D>
-__global__ void __launch_bounds__(32 * kFtCols)
+__global__ void __launch_bounds__(32 * kJoinWarps)
 few_tokens_join_kernel(const __grid_constant__ FtArgs A) {
   constexpr int V = D / 32;
+  __shared__ float s_num[kJoinWarps][D], s_top[kJoinWarps], s_den[kJoinWarps];
   const TokenAttention& a = A.a;
-  const int lane = threadIdx.x & 31, col = threadIdx.x >> 5, c0 = (int)blockIdx.x + 1;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = (int)blockIdx.x + 1;
   next_may_start();
   wait_for_previous();
-  const int marked = a.status[2], chunks = A.plan[0].chunks;
-  const FtSpot prior = A.plan[c0 - 1], s = A.plan[c0];   // (behind the last chunk: whatever the workspace holds)
+  const int marked = a.status[2];
+  const FtSpot prior = A.plan[c0 - 1], s = A.plan[c0];
+  const int chunks = A.plan[0].parts * kFtGrid;
   if (c0 == 1 && threadIdx.x == 0) a.status[kFtTicket] = 0;
   if (marked || c0 >= chunks) return;                    // (marked: a wait gave up, no output)
-  if (s.off == 0 || (prior.at == s.at && prior.off > 0) || col >= s.nq * A.G) return;
-  auto row = [&](int c) { return (long long)(c == 0 ? 2 * c0 - 1 : 2 * (c0 + c - 1)) * kFtCols + col; };
+  if (s.off == 0 || (prior.at == s.at && prior.off > 0)) return;
+  const int cols = s.nq * A.G, log_cols = cols <= 1 ? 0 : cols <= 2 ? 1 : cols <= 4 ? 2 : 3;
+  const int col = warp & ((1 << log_cols) - 1), share = warp >> log_cols, shares = kJoinWarps >> log_cols;
+  // piece 0 is the chunk before c0's, piece c >= 1 chunk c0 + c - 1's; no further than the scratch
+  auto row = [&](int c) { return (long long)(c == 0 ? 2 * c0 - 1 : 2 * min(c0 + c - 1, kFtChunks - 1)) * kFtCols + col; };
   auto piece = [&](int c, float (&x)[V]) {
     const float* const from = A.part + row(c) * D + lane * V;
     if constexpr (V == 4) {
@@ -557,47 +586,72 @@ few_tokens_join_kernel(const __grid_constant__ FtArgs A) {
       x[0] = y.x; x[1] = y.y;
     }
   };
-  // the piece before c0's, c0's, and those of the chunks behind it that begin in the same item
-  int nc = 2;
+  float x[kJoinAhead][V], z[kJoinAhead];
+  auto ask = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < kJoinAhead; ++i) {
+      piece(c + i * shares, x[i]);
+      z[i] = A.part_lse[row(c + i * shares)];
+    }
+  };
+  ask(share);
+  int nc = 2;                                            // c0's piece is the second; then those of chunks that begin in the same item
   while (true) {
     const int c = c0 + nc - 1 + lane;
-    const bool in = c < chunks && A.plan[min(c, kFtChunks - 1)].at == s.at && A.plan[min(c, kFtChunks - 1)].off > 0;
-    const unsigned more = __ballot_sync(0xffffffffu, in);
+    const FtSpot& p = A.plan[min(c, kFtChunks - 1)];
+    const unsigned more = __ballot_sync(0xffffffffu, c < chunks && p.at == s.at && p.off > 0);
     nc += more == 0xffffffffu ? 32 : __ffs(~more) - 1;
     if (more != 0xffffffffu) break;
   }
   if (!L2KV_BOUNDS(s.e >= 0 && s.e < a.g.B * a.g.L && s.item >= 0 && c0 + nc - 2 < kFtChunks, a.status)) return;
-  float top = -INFINITY;
-  for (int c = lane; c < nc; c += 32) top = fmaxf(top, A.part_lse[row(c)]);
+  float top = -INFINITY, den = 0.f, num[V] = {};
+  for (int c = share; c < nc; c += kJoinAhead * shares) {
+    if (c != share) ask(c);
+    float t = top;
 #pragma unroll
-  for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-  float den = 0.f, num[V] = {};
-  for (int b = 0; b < nc; b += 32) {
-    const float lse2 = b + lane < nc ? A.part_lse[row(b + lane)] : -INFINITY;
-    const float mine = lse2 == -INFINITY ? 0.f : exp2f(lse2 - top);
-    for (int c = 0; c < min(32, nc - b); c += kJoinAhead) {
-      float x[kJoinAhead][V];
+    for (int i = 0; i < kJoinAhead; ++i) {
+      if (c + i * shares >= nc) z[i] = -INFINITY;
+      t = fmaxf(t, z[i]);
+    }
+    if (t == -INFINITY) continue;                        // (pieces that see nothing)
+    const float f = exp2f(top - t);
+    top = t;
+    den *= f;
 #pragma unroll
-      for (int i = 0; i < kJoinAhead; ++i) piece(min(b + c + i, nc - 1), x[i]);
+    for (int k = 0; k < V; ++k) num[k] *= f;
 #pragma unroll
-      for (int i = 0; i < kJoinAhead; ++i) {             // (behind the last piece the weight is zero)
-        const float w = __shfl_sync(0xffffffffu, mine, c + i);
-        den += w;
+    for (int i = 0; i < kJoinAhead; ++i) {
+      const float w = exp2f(z[i] - t);
+      den += w;
 #pragma unroll
-        for (int k = 0; k < V; ++k) num[k] = fmaf(w, x[i][k], num[k]);       // (rows of a piece that sees nothing are zeros)
-      }
+      for (int k = 0; k < V; ++k)
+        if (w > 0.f) num[k] = fmaf(w, x[i][k], num[k]);
     }
   }
-  const float inv = den == 0.f ? 0.f : 1.f / den;
+#pragma unroll
+  for (int k = 0; k < V; ++k) s_num[warp][lane * V + k] = num[k];
+  if (lane == 0) { s_top[warp] = top; s_den[warp] = den; }
+  __syncthreads();
+  if (share != 0 || col >= cols) return;                 // a warp per row joins what its shares have
+  float all_top = -INFINITY, all_den = 0.f, sum[V] = {};
+  for (int w = 0; w < shares; ++w) all_top = fmaxf(all_top, s_top[col + (w << log_cols)]);
+  for (int w = 0; w < shares; ++w) {
+    const int from = col + (w << log_cols);
+    const float f = s_top[from] == -INFINITY ? 0.f : exp2f(s_top[from] - all_top);
+    all_den = fmaf(s_den[from], f, all_den);
+#pragma unroll
+    for (int k = 0; k < V; ++k) sum[k] = fmaf(s_num[from][lane * V + k], f, sum[k]);
+  }
+  const float inv = all_den == 0.f ? 0.f : 1.f / all_den;
   const int tok = s.tok0 + col / A.G, head = s.item % a.g.H * A.G + col % A.G, l = s.e % a.g.L;
   if (!L2KV_BOUNDS(tok >= 0 && tok < a.n_tokens && head < a.g.Hq, a.status)) return;
   __nv_bfloat16* const to = a.out.row<__nv_bfloat16>(l, tok, head) + lane * V;
   if constexpr (V == 4)
-    *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16(num[0] * inv, num[1] * inv), pack_bf16(num[2] * inv, num[3] * inv));
+    *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv));
   else
-    *reinterpret_cast<uint32_t*>(to) = pack_bf16(num[0] * inv, num[1] * inv);
+    *reinterpret_cast<uint32_t*>(to) = pack_bf16(sum[0] * inv, sum[1] * inv);
   if (a.lse && lane == 0)
-    a.lse[((long long)l * a.n_tokens + tok) * a.g.Hq + head] = den == 0.f ? -INFINITY : (top + log2f(den)) * 0.6931471805599453f;
+    a.lse[((long long)l * a.n_tokens + tok) * a.g.Hq + head] = all_den == 0.f ? -INFINITY : (all_top + log2f(all_den)) * 0.6931471805599453f;
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -625,7 +679,9 @@ static int launch_ft(const FtArgs& A, const void* K, const void* V, cudaStream_t
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kFtSmem<D>) != cudaSuccess) return L2KV_ERR_CUDA;
   const int rc = launch_chained(kern, kFtGrid, 1, kFtThreads, kFtSmem<D>, s, A, map_q, map_k, map_v);
   if (rc != L2KV_OK || !A.plan) return rc;
-  return launch_chained(few_tokens_join_kernel<D>, kFtChunks - 1, 1, 32 * kFtCols, 0, s, A);
+  // (a share is dealt out in parts only where it can be long enough: the most that this call can cost)
+  const long long most = ((long long)a.n_tokens / A.TG + std::min(a.g.B, a.n_tokens)) * a.g.H * a.g.L * ((a.max_len + kFtRows<D> - 1) / kFtRows<D> + kFtItemCost);
+  return launch_chained(few_tokens_join_kernel<D>, most > kFtGrid * kFtDealFrom ? kFtChunks - 1 : kFtGrid - 1, 1, 32 * kJoinWarps, 0, s, A);
 }
 
 int launch_few_tokens(const TokenAttention& a, const void* K, const void* V, char* scratch, size_t scratch_bytes, cudaStream_t s) {
@@ -633,6 +689,7 @@ int launch_few_tokens(const TokenAttention& a, const void* K, const void* V, cha
   A.a = a;
   A.G = a.g.Hq / a.g.H;
   A.TG = kFtCols / A.G;
+  while ((1 << A.tg_shift) < A.TG) ++A.tg_shift;
   const size_t need = few_tokens_scratch(a.g, a.max_len);
   if (need > 0 && scratch && scratch_bytes >= need) {
     A.plan = reinterpret_cast<FtSpot*>(scratch);
