@@ -35,10 +35,11 @@ constexpr int kFtDescs = 4;                     // items whose queries are on th
 constexpr int kFtPolls = 18;                    // log2 of the polls a wait may take
 constexpr int kFtItemCost = 2;                  // what an item costs beyond its blocks, in blocks
 constexpr int kFtMinShare = 4;                  // no shorter chunks: a block for each warp
-constexpr int kFtDealFrom = 64;                 // equal shares, whole, up to this many blocks
+constexpr int kFtDealFrom = 256;                // equal shares, whole, up to this many blocks: a sixteenth has to be worth starting
 constexpr int kFtParts = 5;                     // chunks of a share: three quarters of it, and four sixteenths
 constexpr int kFtChunks = kFtGrid * kFtParts;
-constexpr int kFtTicket = 8;                    // word of the status block that counts the chunks taken (rests at zero)
+// words of the status block (they rest at zero): chunks taken, items to be joined, blocks that are done joining
+constexpr int kFtTicket = 8, kFtCut = 9, kFtDone = 10;
 constexpr int kFtWholeLen = 512;                // caches up to this length are never cut
 constexpr float kFtRescaleGap = 8.f;            // log2 units a maximum may drift before sums are rescaled
 template <int D> constexpr int kFtRows = 4096 / D;               // cached rows of a block
@@ -52,12 +53,18 @@ template <int D> constexpr int kFtSmem = 1024 + kFtSlots * kFtSlot + kFtDescs * 
 struct FtSpot {
   long long at;          // cost of everything before the item
   int e, item, off;      // entry (b, l), number of the item within it (tokens by tokens, head by head), block within the item
-  int tok0, nq, parts;   // the item's first token in the list, its tokens; chunks of a share in this call
+  int pad;
+};
+// An item that is cut, and the chunk that holds its first piece.
+struct FtCut {
+  long long at;
+  int tok0, nq, l, h, chunk, chunks;
 };
 struct FtArgs {
   TokenAttention a;
   int G, TG, tg_shift;   // query heads per KV head, tokens per item, log2 of those
   FtSpot* plan;          // [kFtChunks] where each chunk begins; null: items stay whole
+  FtCut* cuts;           // [kFtChunks] in any order
   float* part;           // [2 kFtChunks][8][D] rows, then [2 kFtChunks][8] log2-sum-exps
   float* part_lse;
 };
@@ -231,7 +238,7 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
     // The place in the list where x of the cost is behind; `y`: its entry.  A place close to an item's start or end is moved
     // there, so that no sliver is cut off.
     auto find = [&](long long x, FtEntry& y) {
-      FtSpot s{total, entries, 0, 0, 0, 0, parts};
+      FtSpot s{total, entries, 0, 0, 0};
       y = FtEntry{0, 0, 0};
       if (x >= total) return s;
       int t = 8 * (__popc(__ballot_sync(0xffffffffu, s_before[kFtThreads / 32 * lane] <= x)) - 1);   // the last run that begins by x
@@ -261,9 +268,6 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
           while (s.e < entries && y.n == 0);
         }
       }
-      const int p = ft_div(s.item, a.g.H) << A.tg_shift;
-      s.tok0 = y.first + p;
-      s.nq = min(A.TG, y.n - p);
       return s;
     };
 
@@ -278,9 +282,11 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
       end = s_end;
       if (leads && A.plan && lane == 0) A.plan[chunk] = spot;
     }
-    while (ok) {
-      FtItem it;
+    // The next item: worked out and handed on by the leading warp, taken over by the others.
+    uint32_t next_at = 0;
+    auto next_item = [&](FtItem& it) {
       if (leads) {
+        long long it_at = 0;
         while (more && !(spot.at < end.at || (spot.at == end.at && spot.off < end.off))) {
           more = false;
           if (deals) {
@@ -304,6 +310,7 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
           const int each = ft_each<D>(y), n = each - kFtItemCost, to = spot.at == end.at ? end.off : n;
           // a piece that does not begin its item goes to this chunk's first slot, one that does to its second
           it = ft_item<D>(A, spot.e, y, spot.item, spot.off, to, spot.off > 0 ? 2 * chunk : to < n ? 2 * chunk + 1 : -1);
+          it_at = spot.at;
           spot.at += each;
           spot.off = 0;
           if (++spot.item == ft_items(A, y)) {
@@ -312,9 +319,10 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
             while (spot.e < entries && y.n == 0);
           }
         }
-        it.at = at;
+        it.at = next_at;
+        next_at += it.n;
         if (n_desc >= kFtDescs) ok = __all_sync(0xffffffffu, wait(desc_free(n_desc), (n_desc / kFtDescs - 1) & 1u));
-        if (!ok) break;
+        if (!ok) return;
         if (lane == 0) {
           items[n_desc % kFtDescs] = it;
           mbar_arrive(item_full(n_desc));
@@ -325,46 +333,71 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
             for (int c = 0; c < D / 64; ++c)
               tma_load_4d(s_q + n_desc % kFtDescs * 2048 + c * 1024, &map_q, desc_full(n_desc), c * 64, it.h * A.G, it.tok0, it.l);
           }
+          if (!it.stop && it.slot >= 0 && (it.slot & 1))
+            A.cuts[atomicAdd(a.status + kFtCut, 1)] = FtCut{it_at, it.tok0, it.nq, it.l, it.h, chunk, parts * kFtGrid};
         }
         __syncwarp();
       } else {
         ok = __all_sync(0xffffffffu, wait(item_full(n_desc), (n_desc / kFtDescs) & 1u));
-        if (!ok) break;
+        if (!ok) return;
         it = items[n_desc % kFtDescs];
         __syncwarp();
         if (lane == 0) mbar_arrive(desc_free(n_desc));
       }
       ++n_desc;
-      if (it.stop) break;
-      if (it.n == 0) continue;
-      // lane i holds entry i of 32 of the table's, and the one 32 further on is on its way
-      const int32_t* const table = pages.of(it.b, it.l);
-      const int n_ids = (it.end + pages.rows() - 1) >> pages.shift;
-      auto ids = [&](int from) {
-        const int p = from * 32 + lane;
-        const int id = p < n_ids ? table[p] : -1;
-        const bool bad = p < n_ids && !pages.valid(id);
-        if (bad && a.status) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
-        return bad ? -1 : id;
-      };
-      int held = it.row0 >> pages.shift >> 5, now = ids(held), later = ids(held + 1);
+    };
+    // Lane i holds entry i of 32 of the table's, and the one 32 further on is on its way.
+    auto ids = [&](const FtItem& it, int from) {
+      const int p = from * 32 + lane, n_ids = (it.end + pages.rows() - 1) >> pages.shift;
+      const int id = p < n_ids ? pages.of(it.b, it.l)[p] : -1;
+      const bool bad = p < n_ids && !pages.valid(id);
+      if (bad && a.status) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
+      return bad ? -1 : id;
+    };
+    FtItem it, next;
+    int now = 0, later = 0, next_now = 0, next_later = 0;
+    auto ask = [&](const FtItem& of) {
+      const int first = of.row0 >> pages.shift >> 5;
+      next_now = ids(of, first);
+      next_later = ids(of, first + 1);
+    };
+    next_item(it);
+    if (ok && it.n > 0) ask(it);
+    while (ok && !it.stop) {
+      now = next_now;
+      later = next_later;
+      int here = it.row0 >> pages.shift >> 5;
+      // The next item is worked out while there is still enough on its way: about 3 us, ten blocks, before this one's last, but
+      // behind a CTA's first blocks, where nothing keeps them waiting.
+      const int prepare = it.n > 10 ? it.n - 10 : at >= kFtSlots ? 0 : it.n - 1;
       for (int g = 0; g < it.n; ++g, ++at) {
         const int t = it.row0 + g * ROWS, page = t >> pages.shift;
-        if (page >> 5 != held) { ++held; now = later; later = ids(held + 1); }
-        if ((at & 1) != (uint32_t)(me >> 1)) continue;
-        const int id = __shfl_sync(0xffffffffu, now, (page + of_box) & 31);
-        const int row = id < 0 ? pages.n << pages.shift : (id << pages.shift) + (t & (pages.rows() - 1));
-        if (at >= kFtSlots) ok = __all_sync(0xffffffffu, wait(empty(at), (at / kFtSlots - 1) & 1u));
-        if (!ok) break;
-        const uint32_t to = s_ring + at % kFtSlots * kFtSlot + (is_v ? kFtSlot / 2 : 0);
-        if (elect_one()) mbar_expect_tx(full(at), kFtSlot / 2);
-        __syncwarp();
-        if (n_boxes == 1) {
-          if (elect_one()) tma_load_5d(to, is_v ? &map_v : &map_k, full(at), 0, 0, 0, row >> 3, it.h);
-        } else if (lane < n_boxes) {
-          tma_load_5d(to + of_box * box * D * 2, is_v ? &map_v : &map_k, full(at), 0, 0, 0, row >> 3, it.h);
+        if (page >> 5 != here) { ++here; now = later; later = ids(it, here + 1); }
+        if ((at & 1) == (uint32_t)(me >> 1)) {
+          const int id = __shfl_sync(0xffffffffu, now, (page + of_box) & 31);
+          const int row = id < 0 ? pages.n << pages.shift : (id << pages.shift) + (t & (pages.rows() - 1));
+          if (at >= kFtSlots) ok = __all_sync(0xffffffffu, wait(empty(at), (at / kFtSlots - 1) & 1u));
+          if (!ok) break;
+          const uint32_t to = s_ring + at % kFtSlots * kFtSlot + (is_v ? kFtSlot / 2 : 0);
+          if (elect_one()) mbar_expect_tx(full(at), kFtSlot / 2);
+          __syncwarp();
+          if (n_boxes == 1) {
+            if (elect_one()) tma_load_5d(to, is_v ? &map_v : &map_k, full(at), 0, 0, 0, row >> 3, it.h);
+          } else if (lane < n_boxes) {
+            tma_load_5d(to + of_box * box * D * 2, is_v ? &map_v : &map_k, full(at), 0, 0, 0, row >> 3, it.h);
+          }
+        }
+        if (g == prepare) {
+          next_item(next);
+          if (!ok) break;
+          if (next.n > 0) ask(next);
         }
       }
+      if (ok && it.n == 0) {
+        next_item(next);
+        if (ok && next.n > 0) ask(next);
+      }
+      it = next;
     }
     if (!ok) {                                           // copies that may still be in flight
       *s_fail = 1;
@@ -550,113 +583,112 @@ few_tokens_kernel(const __grid_constant__ FtArgs A, const __grid_constant__ CUte
   if (*s_fail && tid == 0) record_timeout(a.status);
 }
 
-// Joins the pieces of items that were cut: out = sum_c w_c O_c / sum_c w_c, w_c = 2^(lse_c - max lse).  A block per chunk
-// that begins inside an item (the first of them where there are several); its warps share the item's query rows and, of each,
-// take every 8th, 4th, .. piece, in a fixed order, so that a result is always the same.  What it takes is a chain of
-// loads, so each warp asks for its first pieces before it knows how many there are (behind the last one: whatever the workspace
-// holds, with no weight).
-constexpr int kJoinWarps = 8;
-constexpr int kJoinAhead = 6;
+// Joins the pieces of items that were cut: out = sum_c w_c O_c / sum_c w_c, w_c = 2^(lse_c - max lse).  A block per item; its
+// warps share the item's query rows and, of each, take every 16th, 8th, .. piece, in a fixed order, so that a result is always
+// the same.  What it takes is a chain of loads of about a microsecond each (what other SMs have just written), so all that can be
+// is asked for at once: the counts and an item, then its pieces together with the places that say how many there are (behind
+// the last one: whatever the workspace holds, with no weight).
+constexpr int kJoinWarps = 16;
+constexpr int kJoinGrid = 2 * kFtGrid;
 template <int D>
-__global__ void __launch_bounds__(32 * kJoinWarps)
+__global__ void __launch_bounds__(32 * kJoinWarps, 2)
 few_tokens_join_kernel(const __grid_constant__ FtArgs A) {
-  constexpr int V = D / 32;
+  constexpr int V = D / 32, AHEAD = D == 128 ? 5 : 8;
+  using Vec = std::conditional_t<V == 4, float4, float2>;
   __shared__ float s_num[kJoinWarps][D], s_top[kJoinWarps], s_den[kJoinWarps];
   const TokenAttention& a = A.a;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = (int)blockIdx.x + 1;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   next_may_start();
   wait_for_previous();
-  const int marked = a.status[2];
-  const FtSpot prior = A.plan[c0 - 1], s = A.plan[c0];
-  const int chunks = A.plan[0].parts * kFtGrid;
-  if (c0 == 1 && threadIdx.x == 0) a.status[kFtTicket] = 0;
-  if (marked || c0 >= chunks) return;                    // (marked: a wait gave up, no output)
-  if (s.off == 0 || (prior.at == s.at && prior.off > 0)) return;
-  const int cols = s.nq * A.G, log_cols = cols <= 1 ? 0 : cols <= 2 ? 1 : cols <= 4 ? 2 : 3;
-  const int col = warp & ((1 << log_cols) - 1), share = warp >> log_cols, shares = kJoinWarps >> log_cols;
-  // piece 0 is the chunk before c0's, piece c >= 1 chunk c0 + c - 1's; no further than the scratch
-  auto row = [&](int c) { return (long long)(c == 0 ? 2 * c0 - 1 : 2 * min(c0 + c - 1, kFtChunks - 1)) * kFtCols + col; };
-  auto piece = [&](int c, float (&x)[V]) {
-    const float* const from = A.part + row(c) * D + lane * V;
-    if constexpr (V == 4) {
-      const float4 y = *reinterpret_cast<const float4*>(from);
-      x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w;
-    } else {
-      const float2 y = *reinterpret_cast<const float2*>(from);
-      x[0] = y.x; x[1] = y.y;
-    }
-  };
-  float x[kJoinAhead][V], z[kJoinAhead];
-  auto ask = [&](int c) {
+  const int marked = a.status[2], counted = a.status[kFtCut];
+  FtCut it = A.cuts[blockIdx.x];                         // (behind the last: whatever the workspace holds)
+  const int cut = marked ? 0 : counted;                  // (a wait that gave up: no output)
+  for (int i = (int)blockIdx.x; i < cut; i += kJoinGrid) {
+    if (i != (int)blockIdx.x) it = A.cuts[i];
+    const int cols = it.nq * A.G, log_cols = cols <= 1 ? 0 : cols <= 2 ? 1 : cols <= 4 ? 2 : 3;
+    const int col = warp & ((1 << log_cols) - 1), share = warp >> log_cols, shares = kJoinWarps >> log_cols;
+    // piece 0 is the second of its chunk's, pieces c >= 1 the first of the chunks behind it; no further than the scratch
+    auto row = [&](int c) { return (c == 0 ? 2 * it.chunk + 1 : 2 * min(it.chunk + c, kFtChunks - 1)) * kFtCols + col; };
+    Vec x[AHEAD];
+    float z[AHEAD];
+    auto ask = [&](int c) {
 #pragma unroll
-    for (int i = 0; i < kJoinAhead; ++i) {
-      piece(c + i * shares, x[i]);
-      z[i] = A.part_lse[row(c + i * shares)];
+      for (int k = 0; k < AHEAD; ++k) {
+        const int r = row(c + k * shares);
+        x[k] = reinterpret_cast<const Vec*>(A.part + (long long)r * D)[lane];
+        z[k] = A.part_lse[r];
+      }
+    };
+    ask(share);
+    int nc = 1;                                          // and a piece of every chunk that begins inside the item
+    while (true) {
+      const int c = it.chunk + nc + lane;
+      const FtSpot& p = A.plan[min(c, kFtChunks - 1)];
+      const unsigned more = __ballot_sync(0xffffffffu, c < it.chunks && p.at == it.at && p.off > 0);
+      nc += more == 0xffffffffu ? 32 : __ffs(~more) - 1;
+      if (more != 0xffffffffu) break;
     }
-  };
-  ask(share);
-  int nc = 2;                                            // c0's piece is the second; then those of chunks that begin in the same item
-  while (true) {
-    const int c = c0 + nc - 1 + lane;
-    const FtSpot& p = A.plan[min(c, kFtChunks - 1)];
-    const unsigned more = __ballot_sync(0xffffffffu, c < chunks && p.at == s.at && p.off > 0);
-    nc += more == 0xffffffffu ? 32 : __ffs(~more) - 1;
-    if (more != 0xffffffffu) break;
+    float top = -INFINITY, den = 0.f, num[V] = {};
+    for (int c = share; c < nc; c += AHEAD * shares) {
+      if (c != share) ask(c);
+      float t = top;
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        if (c + k * shares >= nc) z[k] = -INFINITY;
+        t = fmaxf(t, z[k]);
+      }
+      const float low = t == -INFINITY ? 0.f : t, f = fast_exp2(top - low);
+      top = t;
+      den *= f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) num[v] *= f;
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const float w = fast_exp2(z[k] - low);
+        if (w == 0.f) continue;                          // (rows behind the last piece can hold anything)
+        den += w;
+        num[0] = fmaf(w, x[k].x, num[0]);
+        num[1] = fmaf(w, x[k].y, num[1]);
+        if constexpr (V == 4) {
+          num[2] = fmaf(w, x[k].z, num[2]);
+          num[3] = fmaf(w, x[k].w, num[3]);
+        }
+      }
+    }
+    __syncthreads();                                     // the item before has been read
+#pragma unroll
+    for (int v = 0; v < V; ++v) s_num[warp][lane * V + v] = num[v];
+    if (lane == 0) { s_top[warp] = top; s_den[warp] = den; }
+    __syncthreads();
+    if (share != 0 || col >= cols) continue;             // a warp per row joins what its shares have
+    float all_top = -INFINITY, all_den = 0.f, sum[V] = {};
+    for (int w = col; w < kJoinWarps; w += 1 << log_cols) all_top = fmaxf(all_top, s_top[w]);
+    const float low = all_top == -INFINITY ? 0.f : all_top;
+    for (int w = col; w < kJoinWarps; w += 1 << log_cols) {
+      const float f = fast_exp2(s_top[w] - low);
+      all_den = fmaf(s_den[w], f, all_den);
+#pragma unroll
+      for (int v = 0; v < V; ++v) sum[v] = fmaf(s_num[w][lane * V + v], f, sum[v]);
+    }
+    const float inv = all_den == 0.f ? 0.f : 1.f / all_den;
+    const int tok = it.tok0 + col / A.G, head = it.h * A.G + col % A.G;
+    if (!L2KV_BOUNDS(tok >= 0 && tok < a.n_tokens && head < a.g.Hq && it.l < a.g.L && it.chunk + nc <= kFtChunks, a.status)) continue;
+    uint32_t* const to = reinterpret_cast<uint32_t*>(a.out.row<__nv_bfloat16>(it.l, tok, head) + lane * V);
+#pragma unroll
+    for (int v = 0; v < V; v += 2) to[v / 2] = pack_bf16(sum[v] * inv, sum[v + 1] * inv);
+    if (a.lse && lane == 0)
+      a.lse[((long long)it.l * a.n_tokens + tok) * a.g.Hq + head] = all_den == 0.f ? -INFINITY : (all_top + log2f(all_den)) * 0.6931471805599453f;
   }
-  if (!L2KV_BOUNDS(s.e >= 0 && s.e < a.g.B * a.g.L && s.item >= 0 && c0 + nc - 2 < kFtChunks, a.status)) return;
-  float top = -INFINITY, den = 0.f, num[V] = {};
-  for (int c = share; c < nc; c += kJoinAhead * shares) {
-    if (c != share) ask(c);
-    float t = top;
-#pragma unroll
-    for (int i = 0; i < kJoinAhead; ++i) {
-      if (c + i * shares >= nc) z[i] = -INFINITY;
-      t = fmaxf(t, z[i]);
-    }
-    if (t == -INFINITY) continue;                        // (pieces that see nothing)
-    const float f = exp2f(top - t);
-    top = t;
-    den *= f;
-#pragma unroll
-    for (int k = 0; k < V; ++k) num[k] *= f;
-#pragma unroll
-    for (int i = 0; i < kJoinAhead; ++i) {
-      const float w = exp2f(z[i] - t);
-      den += w;
-#pragma unroll
-      for (int k = 0; k < V; ++k)
-        if (w > 0.f) num[k] = fmaf(w, x[i][k], num[k]);
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < V; ++k) s_num[warp][lane * V + k] = num[k];
-  if (lane == 0) { s_top[warp] = top; s_den[warp] = den; }
   __syncthreads();
-  if (share != 0 || col >= cols) return;                 // a warp per row joins what its shares have
-  float all_top = -INFINITY, all_den = 0.f, sum[V] = {};
-  for (int w = 0; w < shares; ++w) all_top = fmaxf(all_top, s_top[col + (w << log_cols)]);
-  for (int w = 0; w < shares; ++w) {
-    const int from = col + (w << log_cols);
-    const float f = s_top[from] == -INFINITY ? 0.f : exp2f(s_top[from] - all_top);
-    all_den = fmaf(s_den[from], f, all_den);
-#pragma unroll
-    for (int k = 0; k < V; ++k) sum[k] = fmaf(s_num[from][lane * V + k], f, sum[k]);
-  }
-  const float inv = all_den == 0.f ? 0.f : 1.f / all_den;
-  const int tok = s.tok0 + col / A.G, head = s.item % a.g.H * A.G + col % A.G, l = s.e % a.g.L;
-  if (!L2KV_BOUNDS(tok >= 0 && tok < a.n_tokens && head < a.g.Hq, a.status)) return;
-  __nv_bfloat16* const to = a.out.row<__nv_bfloat16>(l, tok, head) + lane * V;
-  if constexpr (V == 4)
-    *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv));
-  else
-    *reinterpret_cast<uint32_t*>(to) = pack_bf16(sum[0] * inv, sum[1] * inv);
-  if (a.lse && lane == 0)
-    a.lse[((long long)l * a.n_tokens + tok) * a.g.Hq + head] = all_den == 0.f ? -INFINITY : (all_top + log2f(all_den)) * 0.6931471805599453f;
+  // the last block puts the counts back
+  if (threadIdx.x == 0 && atomicInc(reinterpret_cast<unsigned*>(a.status + kFtDone), kJoinGrid - 1) == kJoinGrid - 1)
+    a.status[kFtTicket] = a.status[kFtCut] = 0;
 }
 
 // ---- host ------------------------------------------------------------------------------------------
 
-constexpr size_t kFtPlanBytes = (kFtChunks * sizeof(FtSpot) + 255) / 256 * 256;
+constexpr size_t kFtPlanBytes = (kFtChunks * (sizeof(FtSpot) + sizeof(FtCut)) + 255) / 256 * 256;
+static_assert(kJoinGrid <= kFtChunks, "a block of the joining kernel reads its first entry before it knows how many there are");
 
 // One new token per sequence on average, or fewer: with more of them a tile's rows fill.
 bool few_tokens(const TokenAttention& a, int dtype) { return dtype == L2KV_BF16 && a.pages.table && a.n_tokens <= a.g.B; }
@@ -679,9 +711,7 @@ static int launch_ft(const FtArgs& A, const void* K, const void* V, cudaStream_t
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kFtSmem<D>) != cudaSuccess) return L2KV_ERR_CUDA;
   const int rc = launch_chained(kern, kFtGrid, 1, kFtThreads, kFtSmem<D>, s, A, map_q, map_k, map_v);
   if (rc != L2KV_OK || !A.plan) return rc;
-  // (a share is dealt out in parts only where it can be long enough: the most that this call can cost)
-  const long long most = ((long long)a.n_tokens / A.TG + std::min(a.g.B, a.n_tokens)) * a.g.H * a.g.L * ((a.max_len + kFtRows<D> - 1) / kFtRows<D> + kFtItemCost);
-  return launch_chained(few_tokens_join_kernel<D>, most > kFtGrid * kFtDealFrom ? kFtChunks - 1 : kFtGrid - 1, 1, 32 * kJoinWarps, 0, s, A);
+  return launch_chained(few_tokens_join_kernel<D>, kJoinGrid, 1, 32 * kJoinWarps, 0, s, A);
 }
 
 int launch_few_tokens(const TokenAttention& a, const void* K, const void* V, char* scratch, size_t scratch_bytes, cudaStream_t s) {
@@ -693,6 +723,7 @@ int launch_few_tokens(const TokenAttention& a, const void* K, const void* V, cha
   const size_t need = few_tokens_scratch(a.g, a.max_len);
   if (need > 0 && scratch && scratch_bytes >= need) {
     A.plan = reinterpret_cast<FtSpot*>(scratch);
+    A.cuts = reinterpret_cast<FtCut*>(A.plan + kFtChunks);
     A.part = reinterpret_cast<float*>(scratch + kFtPlanBytes);
     A.part_lse = A.part + (size_t)2 * kFtChunks * kFtCols * a.g.D;
   }
