@@ -161,7 +161,7 @@ def _kernels(name):
     return [part.split("{", 1) for part in code.split("__global__")[1:]]
 
 
-@pytest.mark.parametrize("name,count", [("pages.cu", 6), ("few_tokens.cu", 2)])
+@pytest.mark.parametrize("name,count", [("pages.cu", 7), ("few_tokens.cu", 2)])
 def test_the_early_kernels_wait_and_promise_nothing(name, count):
     """All of them are set up while the kernel before them runs: they wait before they read what that one writes, and no
     __restrict__ parameter lets the compiler read earlier."""
