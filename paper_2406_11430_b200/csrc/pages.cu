@@ -4,12 +4,15 @@
 // Nothing can leak, and a call has the same result however often it is repeated.
 //
 //   page_begin_kernel   marks: nothing but the pinned pages is held
-//   page_mark_kernel    every entry in use claims its page (atomicMax of rows used, then of the lower (b, l)); for a
-//                       compaction, besides, a block per (b, l, h) takes its keys through the table and selects
-//   page_deal_kernel    the free pages in ascending order, from counts per kPageGroup pages that the first claims have kept;
-//                       one block: what each (b, l) asks for, and where its pages begin in that order
+//   page_mark_kernel    every entry in use claims its page (the maximum of rows used, then of the lower (b, l)), and every (b, l)
+//                       notes what it asks for; page_mark_select_kernel, for a compaction: besides, a block per (b, l, h) takes
+//                       its keys through the table and selects
+//   page_deal_kernel    a block per stretch of pages lists its free ones in ascending order; a block per 4096 (b, l) adds up
+//                       what they ask for.  Nobody waits for anybody: whoever needs the k-th free page finds its stretch
+//                       by the stretches' counts (at most 512), and whoever needs to know where a (b, l) begins adds the sums
 //   page_update_kernel  the new tables, and the rows of the pages that are copied
 //   page_compact_kernel the new tables, and the kept rows, gathered as select_compact gathers them
+// Calls with few entries and pages do all of an update in one block (page_update_small_kernel).
 #include <algorithm>
 #include <climits>
 
@@ -20,89 +23,89 @@ namespace l2kv {
 
 constexpr int kPageThreads = 256;
 constexpr int kDealThreads = 1024;
-constexpr int kPageGroup = 256;                          // pages per count of held ones
+constexpr int kAsks = 4;                                 // (b, l) per thread of a block that adds up what they ask for
+constexpr int kAskBlock = kAsks * kDealThreads;
+constexpr int kMaxAskBlocks = (1 << kClaimBits) / kAskBlock;
 constexpr int kCopyHeads = 4;                            // heads whose rows one block copies
 constexpr uint32_t kPinned = 0xffffffffu;
 
-// One (b, l) of a call.
-struct PageAsk {
-  int have, more;        // pages of the rows that it keeps, and with those it asks for
-  int part;              // rows in the last kept page, where that is not full
-  bool grows;
-};
 __device__ __forceinline__ int pages_of(long long rows, const PageView& v) { return (int)((rows + v.rows() - 1) >> v.shift); }
 // The sequence that (b, l) goes on from; -1: none.
 __device__ __forceinline__ int parent_of(const PageUpdate& a, int b) {
   const int p = a.parent[b];
   return p >= 0 && p < a.B_in ? p : -1;
 }
-__device__ __forceinline__ int kept_rows(const PageUpdate& a, int b, int l) {
-  return parent_of(a, b) < 0 ? 0 : max(0, min(a.keep[(long long)b * a.L + l], a.in.cap << a.in.shift));
-}
-__device__ __forceinline__ PageAsk ask_of(const PageUpdate& a, int b, int l) {
-  const int keep = kept_rows(a, b, l), grow = max(0, a.grow[b]);
-  return {pages_of(keep, a.in), pages_of((long long)keep + grow, a.in), keep & (a.in.rows() - 1), grow > 0};
+__device__ __forceinline__ int kept_rows(const PageUpdate& a, int b, int l, int parent) {
+  return parent < 0 ? 0 : max(0, min(a.keep[(long long)b * a.L + l], a.in.cap << a.in.shift));
 }
 __device__ __forceinline__ int cached_rows(const PageCompact& a, long long u) { return max(0, min(a.len[u], min(a.max_len, a.in.cap << a.in.shift))); }
 
-struct PageScratch {
-  uint32_t* mark;
-  int32_t* used;
-  int32_t* order;
-  int2* deal;            // per (b, l): where its pages begin in the order (-1: it gets none); update: whether its last
-                         // page is copied, compaction: its length
-  int entries;
+// What a (b, l) asks for.
+struct PageAsk {
+  int need;              // pages; -1: it does not ask
+  int page;              // its last kept page, where that is not full and the (b, l) grows; else -1
+  uint32_t claim;        // its claim on that page
+  int rows;              // rows that it keeps (update), that it has (compaction)
 };
+struct PageScratch {
+  uint32_t* mark;        // [n_pages] highest claim on a page; 0: free
+  int32_t* order;        // [n_pages] the free pages of each stretch, in ascending order, from the stretch's first entry on
+  int32_t* count;        // [stretches] how many
+  PageAsk* ask;          // [entries]
+  int2* deal;            // [entries] pages asked for before it in its block of kAskBlock; its own, and kCopies
+  long long* asked;      // [ask blocks] pages asked for
+  int entries, n_pages, stretch_shift;
+  __host__ __device__ int stretches() const { return (int)(((long long)n_pages + (1ll << stretch_shift) - 1) >> stretch_shift); }
+  __host__ __device__ int ask_blocks() const { return (entries + kAskBlock - 1) / kAskBlock; }
+};
+constexpr int kCopies = 1 << 30, kAsksNot = 1 << 31;     // flags beside the pages of a (b, l), which are fewer than 2^28
 
-// need[u] of a compaction: a page that is none among its entries
-constexpr int kBadPage = -2;
-
-__global__ void __launch_bounds__(kPageThreads)
-page_begin_kernel(PageScratch w, const uint8_t* pin, int n_pages) {
-  next_may_start();
-  wait_for_previous();
-  const int p = blockIdx.x * kPageGroup + threadIdx.x;
-  const bool pinned = p < n_pages && pin && pin[p];
-  if (p < n_pages) w.mark[p] = pinned ? kPinned : 0u;
-  const int held = __syncthreads_count(pinned);
-  if (threadIdx.x == 0) w.used[blockIdx.x] = held;
-  for (long long u = (long long)blockIdx.x * kPageThreads + threadIdx.x; u < w.entries; u += (long long)gridDim.x * kPageThreads)
-    w.deal[u] = make_int2(-1, 0);
+// Marks [p0, p1), by threads `thread` of `threads`.
+__device__ __forceinline__ void begin_pages(uint32_t* mark, const uint8_t* pin, int p0, int p1, int thread, int threads) {
+  for (int p = p0 + thread; p < p1; p += threads) mark[p] = pin && pin[p] ? kPinned : 0u;
 }
 
-// Claims of the entries [0, n) of one table row, by a warp, four to a lane at a time.  COUNT: the first claim on a page adds to
-// its group's count of held ones.
-template <bool COUNT>
-__device__ __forceinline__ void claim_pages(const PageScratch& w, const PageView& in, const int32_t* row, int n, long long u, int rows,
-                                            int32_t* status, bool* bad) {
+constexpr int kBeginPages = 2048;                        // pages per block
+__global__ void __launch_bounds__(kPageThreads)
+page_begin_kernel(PageScratch w, const uint8_t* pin) {
+  next_may_start();
+  wait_for_previous();
+  const long long p0 = (long long)blockIdx.x * kBeginPages;
+  begin_pages(w.mark, pin, (int)p0, (int)min((long long)w.n_pages, p0 + kBeginPages), threadIdx.x, kPageThreads);
+}
+
+// Claims of the entries [0, n) of one table row, by a warp, four to a lane at a time; whether one of them is no page.
+__device__ __forceinline__ bool claim_pages(uint32_t* mark, const PageView& in, const int32_t* row, int n, long long u, int rows) {
   const uint32_t who = (1u << kClaimBits) - 1u - (uint32_t)u;
+  bool bad = false;
   for (int j0 = threadIdx.x & 31; j0 < n; j0 += 128) {
     int page[4];
-    uint32_t was[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      page[i] = j0 + 32 * i < n ? row[j0 + 32 * i] : INT_MAX;
-      was[i] = 1;
-    }
+    for (int i = 0; i < 4; ++i) page[i] = j0 + 32 * i < n ? row[j0 + 32 * i] : INT_MAX;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int j = j0 + 32 * i;
-      if (in.valid(page[i])) {
-        const uint32_t claim = (uint32_t)min(in.rows(), rows - (j << in.shift)) << kClaimBits | who;
-        if (COUNT) was[i] = atomicMax(w.mark + page[i], claim);
-        else atomicMax(w.mark + page[i], claim);
-      } else if (j < n) {
-        *bad = true;
-      }
-    }
-    if (COUNT) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (was[i] == 0) atomicAdd(w.used + page[i] / kPageGroup, 1);
+      if (in.valid(page[i])) atomicMax(mark + page[i], (uint32_t)min(in.rows(), rows - (j << in.shift)) << kClaimBits | who);
+      else bad = bad || j < n;
     }
   }
-  *bad = __any_sync(0xffffffffu, *bad);
-  if (*bad && (threadIdx.x & 31) == 0) atomicExch(status, (int)L2KV_ERR_OUT_OF_RANGE);
+  return __any_sync(0xffffffffu, bad);
+}
+
+// The claims of (b, l) = u of the next step, and what it asks for, by a warp.  A page that several hold stays with the one that
+// has most rows in it, the first of several: it writes behind them; the others copy.
+__device__ __forceinline__ void mark_entry(const PageUpdate& a, const PageScratch& w, uint32_t* mark, long long u) {
+  const int b = (int)(u / a.L), l = (int)(u % a.L), given = a.parent[b], parent = given >= 0 && given < a.B_in ? given : -1;
+  const int grow = max(0, a.grow[b]), keep = kept_rows(a, b, l, parent), have = pages_of(keep, a.in), part = keep & (a.in.rows() - 1);
+  const int32_t* const row = a.in.of(max(0, parent), l);
+  const bool fits = pages_of((long long)keep + grow, a.in) <= a.in.cap, grows = grow > 0 && fits;
+  const int last = grows && part ? row[have - 1] : -1;   // (asked for before the claims)
+  const bool bad = claim_pages(mark, a.in, row, have, u, keep) || given >= a.B_in;   // (told, and taken as none)
+  if (threadIdx.x & 31) return;
+  if (bad) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
+  if (!fits && grow > 0) atomicExch(a.status, (int)L2KV_ERR_DEVICE_OVERFLOW);
+  w.ask[u] = PageAsk{grows ? pages_of((long long)keep + grow, a.in) - have : -1, a.in.valid(last) ? last : -1,
+                     (uint32_t)part << kClaimBits | ((1u << kClaimBits) - 1u - (uint32_t)u), keep};
 }
 
 __global__ void __launch_bounds__(kPageThreads)
@@ -110,11 +113,7 @@ page_mark_kernel(const __grid_constant__ PageUpdate a, PageScratch w) {
   next_may_start();
   wait_for_previous();
   const long long u = (long long)blockIdx.x * (kPageThreads / 32) + (threadIdx.x >> 5);
-  if (u >= w.entries) return;
-  const int b = (int)(u / a.L), l = (int)(u % a.L);
-  bool bad = a.parent[b] >= a.B_in;                      // (told, and taken as none)
-  const int keep = kept_rows(a, b, l);
-  claim_pages<true>(w, a.in, a.in.of(max(0, parent_of(a, b)), l), pages_of(keep, a.in), u, keep, a.status, &bad);
+  if (u < w.entries) mark_entry(a, w, w.mark, u);
 }
 
 // A (b, l)'s keys in row order, and the selection, a block per head; further blocks claim.
@@ -136,10 +135,11 @@ page_mark_select_kernel(const __grid_constant__ PageCompact a, PageScratch w, Co
   if (blockIdx.x >= units) {
     const long long u = (blockIdx.x - units) * (NT / 32) + (threadIdx.x >> 5);
     if (u >= w.entries) return;
-    const int rows = cached_rows(a, u);
-    bool bad = false;
-    claim_pages<true>(w, a.in, a.in.of((int)(u / a.L), (int)(u % a.L)), pages_of(rows, a.in), u, rows, a.status, &bad);
-    if (bad && (threadIdx.x & 31) == 0) w.deal[u].x = kBadPage;
+    const int rows = cached_rows(a, u), keep = max(0, a.keep[u]);
+    const bool bad = claim_pages(w.mark, a.in, a.in.of((int)(u / a.L), (int)(u % a.L)), pages_of(rows, a.in), u, rows);
+    if (threadIdx.x & 31) return;
+    if (bad) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
+    w.ask[u] = PageAsk{keep < rows && !bad ? pages_of(keep, a.in) : -1, -1, 0, rows};
     return;
   }
   const long long unit = blockIdx.x, u = unit / a.H;
@@ -196,101 +196,123 @@ __device__ __forceinline__ N block_sum(N x, N* s_warp, N* total) {
   return incl + (warp ? before : 0);
 }
 
-// What (b, l) = u asks for: pages, and whether its last kept page is copied.  A page that several hold stays with the one that
-// has most rows in it, the first of several: it writes behind them; the others copy.
-__device__ __forceinline__ int2 need_of(const PageUpdate& a, const PageScratch& w, long long u) {
-  const int b = (int)(u / a.L), l = (int)(u % a.L);
-  const PageAsk q = ask_of(a, b, l);
-  if (!q.grows) return make_int2(0, 0);
-  if (q.more > a.in.cap) {
-    atomicExch(a.status, (int)L2KV_ERR_DEVICE_OVERFLOW);
-    return make_int2(0, 0);
-  }
-  int copy = 0;
-  if (q.part) {
-    const int page = a.in.of(parent_of(a, b), l)[q.have - 1];
-    const uint32_t claim = (uint32_t)q.part << kClaimBits | ((1u << kClaimBits) - 1u - (uint32_t)u);
-    copy = a.in.valid(page) && w.mark[page] != claim;
-  }
-  return make_int2(q.more - q.have + copy, copy);
-}
-__device__ __forceinline__ int2 need_of(const PageCompact& a, const PageScratch& w, long long u) {
-  const int len = cached_rows(a, u), keep = max(0, a.keep[u]);
-  return make_int2(keep >= len || w.deal[u].x == kBadPage ? 0 : pages_of(keep, a.in), len);   // (len_out may be len)
-}
-__device__ __forceinline__ bool asks(const PageUpdate& a, const PageScratch&, long long u) {
-  const PageAsk q = ask_of(a, (int)(u / a.L), (int)(u % a.L));
-  return q.grows && q.more <= a.in.cap;
-}
-__device__ __forceinline__ bool asks(const PageCompact& a, const PageScratch& w, long long u) {
-  return w.deal[u].x != kBadPage && max(0, a.keep[u]) < cached_rows(a, u);
-}
-
-// By a block of kDealThreads: what every (b, l) gets of the n_all free pages, into w.deal; the pages given in all are returned.
-// Four (b, l) to a thread: what it takes is a chain of loads (the request, the last page, the claim on it) and sums.
-constexpr int kAsks = 4;
-template <typename A>
-__device__ __forceinline__ long long deal_out(const A& a, const PageScratch& w, int n_all, int32_t* n_free) {
-  __shared__ long long s_sums[32];
-  long long before = 0, given = 0, all;
-  for (int u0 = 0; u0 < w.entries; u0 += kAsks * kDealThreads) {
-    int2 need[kAsks];
-    bool wants[kAsks];
-    long long mine = 0;
-#pragma unroll
-    for (int i = 0; i < kAsks; ++i) {
-      const int u = u0 + (int)threadIdx.x * kAsks + i;
-      need[i] = make_int2(0, 0);
-      wants[i] = u < w.entries && asks(a, w, u);
-      if (u < w.entries) need[i] = need_of(a, w, u);
-      mine += need[i].x;
-    }
-    long long upto = before + block_sum<long long>(mine, s_sums, &all) - mine;
-#pragma unroll
-    for (int i = 0; i < kAsks; ++i) {
-      const int u = u0 + (int)threadIdx.x * kAsks + i;
-      upto += need[i].x;
-      const bool gets = wants[i] && (need[i].x == 0 || upto <= n_all);
-      if (wants[i] && !gets) atomicExch(a.status, (int)L2KV_ERR_DEVICE_OVERFLOW);
-      if (u < w.entries) w.deal[u] = make_int2(!gets ? -1 : need[i].x ? (int)(upto - need[i].x) : 0, need[i].y);
-      if (gets) given += need[i].x;
-    }
-    before += all;
-  }
-  block_sum(given, s_sums, &all);
-  if (n_free && threadIdx.x == 0) *n_free = n_all - (int)all;
-  return all;
-}
-
-template <typename A>
-__global__ void __launch_bounds__(kDealThreads)
-page_deal_kernel(const __grid_constant__ A a, PageScratch w, int n_pages, int n_groups, int32_t* n_free) {
-  __shared__ int s_warp[32];
-  next_may_start();
-  wait_for_previous();
-  // free pages before the block's own; in the last block, all
-  const bool deals = blockIdx.x == gridDim.x - 1;
-  const int first_group = deals ? n_groups : (int)blockIdx.x * (kPageBlock / kPageGroup);
-  int x = 0, held;
-  for (int i = threadIdx.x; i < first_group; i += kDealThreads) x += w.used[i];
-  block_sum(x, s_warp, &held);
-  if (!deals) {
-    constexpr int kEach = kPageBlock / kDealThreads;
-    const int p0 = (int)blockIdx.x * kPageBlock + (int)threadIdx.x * kEach;
+// The free pages among [p0, p1), listed from order[p0] on, by a block of kDealThreads; how many.
+__device__ __forceinline__ int list_free(const uint32_t* mark, int32_t* order, int p0, int p1, int* s_warp) {
+  constexpr int kEach = 4;
+  int listed = 0;
+  for (int q0 = p0; q0 < p1; q0 += kEach * kDealThreads) {
+    const int p = q0 + (int)threadIdx.x * kEach;
     bool is_free[kEach];
     int n = 0, all;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      is_free[i] = p0 + i < n_pages && w.mark[p0 + i] == 0;
+      is_free[i] = p + i < p1 && mark[p + i] == 0;
       n += is_free[i];
     }
-    int at = first_group * kPageGroup - held + block_sum(n, s_warp, &all) - n;
+    int at = p0 + listed + block_sum(n, s_warp, &all) - n;
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
-      if (is_free[i]) w.order[at++] = p0 + i;
+      if (is_free[i]) order[at++] = p + i;
+    listed += all;
+  }
+  return listed;
+}
+
+// What the (b, l) of block `block` ask for, added up, by a block of kDealThreads; the sum.
+__device__ __forceinline__ long long add_up(const PageScratch& w, const uint32_t* mark, int block, long long* s_sums) {
+  int need[kAsks];
+  long long mine = 0, all;
+  const int u0 = block * kAskBlock + (int)threadIdx.x * kAsks;
+#pragma unroll
+  for (int i = 0; i < kAsks; ++i) {
+    PageAsk q{-1, -1, 0, 0};
+    if (u0 + i < w.entries) q = w.ask[u0 + i];
+    const int copies = q.page >= 0 && mark[q.page] != q.claim;
+    need[i] = q.need < 0 ? kAsksNot : (q.need + copies) | (copies ? kCopies : 0);
+    mine += max(0, q.need) + copies;
+  }
+  long long upto = block_sum(mine, s_sums, &all) - mine;
+#pragma unroll
+  for (int i = 0; i < kAsks; ++i) {
+    if (u0 + i < w.entries) w.deal[u0 + i] = make_int2((int)min(upto, (long long)INT_MAX), need[i]);
+    upto += need[i] & (kCopies - 1) & ~kAsksNot;
+  }
+  return all;
+}
+
+__global__ void __launch_bounds__(kDealThreads)
+page_deal_kernel(PageScratch w) {
+  __shared__ long long s_sums[32];
+  __shared__ int s_warp[32];
+  next_may_start();
+  wait_for_previous();
+  const int stretch = (int)blockIdx.x - w.ask_blocks();
+  if (stretch < 0) {
+    const long long all = add_up(w, w.mark, (int)blockIdx.x, s_sums);
+    if (threadIdx.x == 0) w.asked[blockIdx.x] = all;
     return;
   }
-  deal_out(a, w, n_pages - held, n_free);
+  const long long p0 = (long long)stretch << w.stretch_shift;
+  const int n = list_free(w.mark, w.order, (int)p0, (int)min((long long)w.n_pages, p0 + (1ll << w.stretch_shift)), s_warp);
+  if (threadIdx.x == 0) w.count[stretch] = n;
+}
+
+// ---- what comes of it: read by every block of the kernels behind ----------------------------------------
+
+struct PageSums {
+  int free_before[kMaxStretches];                        // free pages in the stretches before
+  long long asked_before[kMaxAskBlocks];
+  int n_free;
+};
+// By a whole block of two warps or more.
+__device__ __forceinline__ void load_sums(const PageScratch& w, PageSums& s) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (warp < 2) {
+    const int n = warp == 0 ? w.stretches() : w.ask_blocks();
+    long long before = 0;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+      const int i = i0 + lane;
+      const long long x = i >= n ? 0 : warp == 0 ? w.count[i] : w.asked[i];
+      long long incl = x;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const long long o = __shfl_up_sync(0xffffffffu, incl, off);
+        if (lane >= off) incl += o;
+      }
+      if (i < n) {
+        if (warp == 0) s.free_before[i] = (int)(before + incl - x);
+        else s.asked_before[i] = before + incl - x;
+      }
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (warp == 0 && lane == 0) s.n_free = (int)before;
+  }
+  __syncthreads();
+}
+// The k-th free page.
+__device__ __forceinline__ int free_page(const PageScratch& w, const PageSums& s, int k) {
+  int lo = 0, n = w.stretches();
+  while (n > 1) {                                        // the last stretch with no more than k before it
+    const int half = n / 2;
+    if (s.free_before[lo + half] <= k) lo += half;
+    n -= half;
+  }
+  return w.order[((long long)lo << w.stretch_shift) + k - s.free_before[lo]];
+}
+struct PageDeal {
+  int begin, need;       // its pages are the free ones [begin, begin + need)
+  bool asks, gets, copies;
+};
+__device__ __forceinline__ PageDeal deal_of(const PageScratch& w, const PageSums& s, long long u) {
+  const int2 d = w.deal[u];
+  PageDeal r;
+  r.asks = d.y >= 0;
+  r.need = r.asks ? d.y & (kCopies - 1) : 0;
+  const long long begin = s.asked_before[u / kAskBlock] + d.x;
+  r.gets = r.asks && (r.need == 0 || begin + r.need <= s.n_free);
+  r.copies = r.gets && (d.y & kCopies);
+  r.begin = r.gets && r.need ? (int)begin : 0;
+  return r;
 }
 
 // Rows of one page to another, for heads [h0, h1): kCopyAhead pieces of K and of V per thread in flight.
@@ -326,90 +348,104 @@ __device__ __forceinline__ void copy_rows(T* K, T* V, int32_t* idx, float* sumsq
   }
 }
 
-// The new table of (b, l) = u, by `threads` threads; returns the page its last one is copied from, and through `to` and
-// `rows` where; -1: none is.
-__device__ __forceinline__ int write_table(const PageUpdate& a, const PageScratch& w, long long u, int thread, int threads, bool writes,
-                                           int* to_page, int* rows) {
-  const int b = (int)(u / a.L), l = (int)(u % a.L);
-  const int2 deal = w.deal[u];
-  const bool gets = deal.x >= 0, copies = gets && deal.y;
-  const PageAsk q = ask_of(a, b, l);
-  const int32_t* const old = a.in.of(max(0, parent_of(a, b)), l);
-  if (writes) {
-    int32_t* const to = a.out_table + b * a.out.sb + l * a.out.sl;
-    const int begin = q.have - (copies ? 1 : 0), more = gets ? q.more : q.have;
-#pragma unroll 4
-    for (int j = thread; j < a.out.cap; j += threads)
-      to[j] = j < begin ? old[j] : j >= more ? -1 : gets ? w.order[deal.x + j - begin] : old[j];
-    if (a.out_room && thread == 0) a.out_room[u] = gets ? q.more << a.in.shift : kept_rows(a, b, l);
+// The new table of (b, l) = u, by a warp.
+__device__ __forceinline__ void write_table(const PageUpdate& a, const PageScratch& w, const PageSums& s, const PageDeal& d, long long u) {
+  const int b = (int)(u / a.L), l = (int)(u % a.L), lane = threadIdx.x & 31, parent = parent_of(a, b);
+  const int keep = w.ask[u].rows, have = pages_of(keep, a.in), begin = have - (d.copies ? 1 : 0), more = begin + d.need;
+  const int32_t* const old = a.in.of(max(0, parent), l);
+  int32_t* const to = a.out_table + b * a.out.sb + l * a.out.sl;
+  for (int j0 = lane; j0 < a.out.cap; j0 += 128) {
+    int page[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) page[i] = j0 + 32 * i < begin || (j0 + 32 * i < have && !d.copies) ? old[j0 + 32 * i] : -1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = j0 + 32 * i;
+      if (d.gets && j >= begin && j < more) page[i] = free_page(w, s, d.begin + j - begin);
+      if (j < a.out.cap) to[j] = page[i];
+    }
   }
-  if (!copies) return -1;
-  *to_page = w.order[deal.x];
-  *rows = q.part;
-  return old[q.have - 1];
+  if (lane == 0) {
+    if (a.out_room) a.out_room[u] = d.gets ? more << a.in.shift : keep;
+    if (d.asks && !d.gets) atomicExch(a.status, (int)L2KV_ERR_DEVICE_OVERFLOW);
+  }
+}
+// Rows of the page that (b, l) = u gets in the place of its last one, for heads [h0, h1).
+template <typename T, int D>
+__device__ __forceinline__ void copy_page(const PageUpdate& a, const PageScratch& w, const PageSums& s, const PageDeal& d, long long u, T* K,
+                                          T* V, int32_t* idx, float* sumsq, const Geom& g, int h0, int h1, int thread, int threads) {
+  const PageAsk q = w.ask[u];
+  copy_rows<T, D>(K, V, idx, sumsq, g, (long long)q.page << a.in.shift, (long long)free_page(w, s, d.begin) << a.in.shift,
+                  q.rows & (a.in.rows() - 1), h0, h1, thread, threads);
+}
+// Pages that are left, by a block of NT.
+template <int NT>
+__device__ __forceinline__ void count_left(const PageUpdate& a, const PageScratch& w, const PageSums& s, long long* s_sums) {
+  long long given = 0, all;
+  for (int u = threadIdx.x; u < w.entries; u += NT) {
+    const PageDeal d = deal_of(w, s, u);
+    if (d.gets) given += d.need;
+  }
+  block_sum(given, s_sums, &all);
+  if (threadIdx.x == 0) *a.n_free = s.n_free - (int)all;
 }
 
-// Blocks [0, table_blocks): the tables, a warp per (b, l).  The others, where copies are possible: a block per (b, l) and kCopyHeads heads.
+// Block 0: the pages left.  Blocks [1, 1 + table_blocks): the tables, a warp per (b, l).  The others: a block per (b, l) and
+// kCopyHeads heads copies, where that is one to copy.
 template <typename T, int D>
 __global__ void __launch_bounds__(kPageThreads)
 page_update_kernel(const __grid_constant__ PageUpdate a, PageScratch w, T* K, T* V, int32_t* idx, float* sumsq, Geom g, int table_blocks,
                    int copy_groups) {
+  __shared__ PageSums sums;
+  __shared__ long long s_sums[32];
   next_may_start();
   wait_for_previous();
-  int to, rows;
-  if ((int)blockIdx.x < table_blocks) {
-    const long long u = (long long)blockIdx.x * (kPageThreads / 32) + (threadIdx.x >> 5);
-    if (u < w.entries) write_table(a, w, u, threadIdx.x & 31, 32, true, &to, &rows);
-    return;
+  const int i = (int)blockIdx.x - 1 - table_blocks;
+  if (i >= 0 && !(w.deal[i / copy_groups].y >= 0 && w.deal[i / copy_groups].y & kCopies)) return;
+  load_sums(w, sums);
+  if (blockIdx.x == 0) {
+    if (a.n_free) count_left<kPageThreads>(a, w, sums, s_sums);
+  } else if (i < 0) {
+    const long long u = (long long)(blockIdx.x - 1) * (kPageThreads / 32) + (threadIdx.x >> 5);
+    if (u < w.entries) write_table(a, w, sums, deal_of(w, sums, u), u);
+  } else {
+    const PageDeal d = deal_of(w, sums, i / copy_groups);
+    const int h0 = i % copy_groups * kCopyHeads;
+    if (d.copies) copy_page<T, D>(a, w, sums, d, i / copy_groups, K, V, idx, sumsq, g, h0, min(g.H, h0 + kCopyHeads), threadIdx.x, kPageThreads);
   }
-  const int i = (int)blockIdx.x - table_blocks;
-  const long long u = i / copy_groups;
-  const int2 deal = w.deal[u];
-  if (deal.x < 0 || !deal.y) return;
-  const int from = write_table(a, w, u, 0, 1, false, &to, &rows), h0 = i % copy_groups * kCopyHeads;
-  copy_rows<T, D>(K, V, idx, sumsq, g, (long long)from << a.in.shift, (long long)to << a.in.shift, rows, h0, min(g.H, h0 + kCopyHeads),
-                  threadIdx.x, kPageThreads);
 }
 
-// Pools of up to kSmallPool pages: the claims in one block's shared memory, and with them the free pages and what
-// everyone gets.  ALL: the tables and copies too, where they are few.
-constexpr int kSmallPool = 49152, kSmallEntries = 65536, kSmallAsks = 4096;
-constexpr long long kSmallCopy = 128 << 10;              // bytes that one block copies as fast as another kernel starts
-template <typename T, int D, bool ALL>
+// All of an update by one block, with the claims in its shared memory.
+constexpr int kSmallPool = 40960, kSmallEntries = 64;
+constexpr long long kSmallCopy = 128 << 10;              // bytes that one block copies as fast as more kernels start
+template <typename T, int D>
 __global__ void __launch_bounds__(kDealThreads)
 page_update_small_kernel(const __grid_constant__ PageUpdate a, PageScratch w, T* K, T* V, int32_t* idx, float* sumsq, Geom g) {
   extern __shared__ uint32_t s_mark[];
+  __shared__ PageSums sums;
+  __shared__ long long s_sums[32];
   __shared__ int s_warp[32];
-  const int tid = threadIdx.x, warp = tid >> 5, n_pages = a.in.n;
+  const int tid = threadIdx.x, warp = tid >> 5;
   next_may_start();
   wait_for_previous();
-  PageScratch mine = w;
-  mine.mark = s_mark;
-  for (int p = tid; p < n_pages; p += kDealThreads) s_mark[p] = a.pin && a.pin[p] ? kPinned : 0u;
+  begin_pages(s_mark, a.pin, 0, w.n_pages, tid, kDealThreads);
   __syncthreads();
-  for (int u = warp; u < w.entries; u += kDealThreads / 32) {
-    const int b = u / a.L, l = u % a.L;
-    bool bad = a.parent[b] >= a.B_in;
-    const int keep = kept_rows(a, b, l);
-    claim_pages<false>(mine, a.in, a.in.of(max(0, parent_of(a, b)), l), pages_of(keep, a.in), u, keep, a.status, &bad);
+  for (int u = warp; u < w.entries; u += kDealThreads / 32) mark_entry(a, w, s_mark, u);
+  __syncthreads();
+  const int n = list_free(s_mark, w.order, 0, w.n_pages, s_warp);
+  add_up(w, s_mark, 0, s_sums);
+  if (tid == 0) {
+    sums.free_before[0] = 0;
+    sums.asked_before[0] = 0;
+    sums.n_free = n;
   }
   __syncthreads();
-  // a run of pages to each thread, of odd length: no two threads of a warp in one bank
-  const int run = (n_pages + kDealThreads - 1) / kDealThreads | 1, p0 = min(n_pages, tid * run), p1 = min(n_pages, p0 + run);
-  int n = 0, all;
-  for (int p = p0; p < p1; ++p) n += s_mark[p] == 0;
-  int at = block_sum(n, s_warp, &all) - n;
-  const long long given = deal_out(a, mine, all, a.n_free);
-  for (int p = p0; p < p1 && at < given; ++p)
-    if (s_mark[p] == 0) w.order[at++] = p;
-  if (!ALL) return;
-  __syncthreads();
   for (int u = warp; u < w.entries; u += kDealThreads / 32) {
-    int to, rows;
-    const int from = write_table(a, w, u, tid & 31, 32, true, &to, &rows);
-    if (from >= 0)
-      copy_rows<T, D>(K, V, idx, sumsq, g, (long long)from << a.in.shift, (long long)to << a.in.shift, rows, 0, g.H, tid & 31, 32);
+    const PageDeal d = deal_of(w, sums, u);
+    write_table(a, w, sums, d, u);
+    if (d.copies) copy_page<T, D>(a, w, sums, d, u, K, V, idx, sumsq, g, 0, g.H, tid & 31, 32);
   }
+  if (a.n_free) count_left<kDealThreads>(a, w, sums, s_sums);
 }
 
 // ---- the kept rows of a compaction ------------------------------------------------------------------
@@ -424,27 +460,32 @@ page_compact_kernel(const __grid_constant__ PageCompact a, PageScratch w, Compac
   constexpr int LPR = D / Elem<T>::kPerVec, RPS = kPageThreads / LPR, TPT = kGatherChunk / kPageThreads;
   __shared__ int s_from[kGatherChunk], s_to[kGatherChunk];   // pool rows that the kept rows move from and to
   __shared__ int s_warp[32];
+  __shared__ PageSums sums;
   next_may_start();
   wait_for_previous();
   const long long chunks = (long long)w.entries * a.H * c.n_chunks;
   if (blockIdx.x >= chunks * parts) {                    // the tables and lengths: a block per (b, l)
     const long long u = blockIdx.x - chunks * parts;
-    const int b = (int)(u / a.L), l = (int)(u % a.L), len = w.deal[u].y, at = w.deal[u].x;
-    const int rows = at >= 0 ? max(0, a.keep[u]) : len, n = pages_of(rows, a.in);
+    load_sums(w, sums);
+    const PageDeal d = deal_of(w, sums, u);
+    const int b = (int)(u / a.L), l = (int)(u % a.L), rows = d.gets ? max(0, a.keep[u]) : w.ask[u].rows, n = pages_of(rows, a.in);
     const int32_t* const old = a.in.of(b, l);
     int32_t* const to = a.out_table + b * a.out.sb + l * a.out.sl;
-    for (int j = threadIdx.x; j < a.out.cap; j += kPageThreads) to[j] = j >= n ? -1 : at >= 0 ? w.order[at + j] : old[j];
+    for (int j = threadIdx.x; j < a.out.cap; j += kPageThreads) to[j] = j >= n ? -1 : d.gets ? free_page(w, sums, d.begin + j) : old[j];
     if (threadIdx.x == 0) {
       a.len_out[u] = rows;
       if (a.out_room) a.out_room[u] = rows;
+      if (d.asks && !d.gets) atomicExch(a.status, (int)L2KV_ERR_DEVICE_OVERFLOW);
     }
     return;
   }
   const long long unit = blockIdx.x / parts / c.n_chunks, u = unit / a.H;
   const int part = (int)(blockIdx.x % parts), chunk = (int)(blockIdx.x / parts % c.n_chunks), h = (int)(unit % a.H), tid = threadIdx.x;
-  const int2 deal = w.deal[u];
-  const int len = deal.y, t0 = chunk * kGatherChunk, at = deal.x;
-  if (t0 >= len || at < 0 || a.keep[u] <= 0) return;
+  const int len = w.ask[u].rows, t0 = chunk * kGatherChunk;
+  if (t0 >= len || w.ask[u].need <= 0) return;           // (nothing asked for, or nothing kept)
+  load_sums(w, sums);
+  const PageDeal d = deal_of(w, sums, u);
+  if (!d.gets) return;
   const UnitRec rec = c.units[unit];
   const int2 cr = c.chunks[unit * c.n_chunks + chunk];   // slot of the chunk's first kept row, ties before it
   const float* const key = c.keys + unit * c.ld;
@@ -472,7 +513,7 @@ page_compact_kernel(const __grid_constant__ PageCompact a, PageScratch w, Compac
       const bool ok = L2KV_BOUNDS(j >= 0 && j < kGatherChunk && slot >= 0 && slot < rec.n_keep, a.status);
       if (ok) {
         s_from[j] = (page[i] << a.in.shift) | (t & (a.in.rows() - 1));
-        s_to[j] = (w.order[at + (slot >> a.in.shift)] << a.in.shift) | (slot & (a.in.rows() - 1));
+        s_to[j] = (free_page(w, sums, d.begin + (slot >> a.in.shift)) << a.in.shift) | (slot & (a.in.rows() - 1));
       }
     }
     before += less ? 0x10000 : tie;
@@ -526,9 +567,11 @@ PagePlan plan_pages(long long entries, long long units, int n_pages, int max_len
   p.ld = round_up_ll(max_len > 0 ? max_len : 1, 64);
   p.n_chunks = std::max(1, (max_len + kGatherChunk - 1) / kGatherChunk);
   p.mark_off = take(4ll * n_pages);
-  p.used_off = take(4ll * std::max(1, (n_pages + kPageGroup - 1) / kPageGroup));
   p.order_off = take(4ll * n_pages);
-  p.need_off = take(8 * entries);
+  p.count_off = take(4ll * kMaxStretches);
+  p.ask_off = take((long long)sizeof(PageAsk) * entries);
+  p.deal_off = take(8 * entries);
+  p.asked_off = take(8ll * kMaxAskBlocks);
   p.key_off = take(4 * units * p.ld);
   p.unit_off = take(16 * units);
   p.chunk_off = take(8 * units * p.n_chunks);
@@ -536,56 +579,44 @@ PagePlan plan_pages(long long entries, long long units, int n_pages, int max_len
   return p;
 }
 
-static PageScratch scratch_of(const PagePlan& p, char* base, long long entries) {
-  return PageScratch{reinterpret_cast<uint32_t*>(base + p.mark_off), reinterpret_cast<int32_t*>(base + p.used_off),
-                     reinterpret_cast<int32_t*>(base + p.order_off), reinterpret_cast<int2*>(base + p.need_off), (int)entries};
+static PageScratch scratch_of(const PagePlan& p, char* base, long long entries, int n_pages) {
+  PageScratch w{reinterpret_cast<uint32_t*>(base + p.mark_off), reinterpret_cast<int32_t*>(base + p.order_off),
+                reinterpret_cast<int32_t*>(base + p.count_off), reinterpret_cast<PageAsk*>(base + p.ask_off),
+                reinterpret_cast<int2*>(base + p.deal_off), reinterpret_cast<long long*>(base + p.asked_off), (int)entries, n_pages, 12};
+  while (w.stretches() > kMaxStretches) ++w.stretch_shift;
+  return w;
 }
-static int groups_of(int n_pages) { return std::max(1, (n_pages + kPageGroup - 1) / kPageGroup); }
-static int begin_pages(const PageScratch& w, const uint8_t* pin, int n_pages, cudaStream_t s) {
-  return launch_chained(page_begin_kernel, groups_of(n_pages), 1, kPageThreads, 0, s, w, pin, n_pages);
+static int launch_begin(const PageScratch& w, const uint8_t* pin, cudaStream_t s) {
+  return launch_chained(page_begin_kernel, std::max(1, (int)(((long long)w.n_pages + kBeginPages - 1) / kBeginPages)), 1, kPageThreads, 0, s, w, pin);
 }
-template <typename A>
-static int deal_pages(const A& a, const PageScratch& w, int n_pages, int32_t* n_free, cudaStream_t s) {
-  return launch_chained(page_deal_kernel<A>, (n_pages + kPageBlock - 1) / kPageBlock + 1, 1, kDealThreads, 0, s, a, w, n_pages,
-                        (n_pages + kPageGroup - 1) / kPageGroup, n_free);
-}
-
-template <typename T, int D, bool ALL>
-static int launch_ps(const PageUpdate& a, const PageScratch& w, void* K, void* V, int32_t* idx, float* sumsq, const Geom& g, cudaStream_t s) {
-  auto kern = page_update_small_kernel<T, D, ALL>;
-  const size_t smem = ((size_t)a.in.n * 4 + 15) / 16 * 16;
-  if (smem > 40 << 10 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallPool * 4) != cudaSuccess)
-    return L2KV_ERR_CUDA;
-  return launch_chained(kern, 1, 1, kDealThreads, smem, s, a, w, static_cast<T*>(K), static_cast<T*>(V), idx, sumsq, g);
+static int launch_deal(const PageScratch& w, cudaStream_t s) {
+  return launch_chained(page_deal_kernel, w.ask_blocks() + w.stretches(), 1, kDealThreads, 0, s, w);
 }
 
 template <typename T, int D>
 static int launch_pu(const PageUpdate& a, const PageScratch& w, void* K, void* V, int32_t* idx, float* sumsq, const Geom& g, cudaStream_t s) {
-  int rc;
-  if (a.in.n <= kSmallPool && w.entries <= kSmallAsks && (long long)w.entries * a.in.cap <= kSmallEntries) {
-    // (what all of them together can have to copy)
-    const bool all = w.entries <= 32 && (long long)w.entries * g.H * (2 * (D * sizeof(T) + 4) << a.in.shift) <= kSmallCopy;
-    if (all) return launch_ps<T, D, true>(a, w, K, V, idx, sumsq, g, s);
-    rc = launch_ps<T, D, false>(a, w, K, V, idx, sumsq, g, s);
-  } else {
-    rc = begin_pages(w, a.pin, a.in.n, s);
-    if (rc != L2KV_OK) return rc;
-    constexpr int kWarps = kPageThreads / 32;
-    rc = launch_chained(page_mark_kernel, (w.entries + kWarps - 1) / kWarps, 1, kPageThreads, 0, s, a, w);
-    if (rc != L2KV_OK) return rc;
-    rc = deal_pages(a, w, a.in.n, a.n_free, s);
+  // (what all of them together can have to copy)
+  if (w.n_pages <= kSmallPool && w.entries <= kSmallEntries && (long long)w.entries * g.H * (2 * (D * sizeof(T) + 4) << a.in.shift) <= kSmallCopy) {
+    auto kern = page_update_small_kernel<T, D>;
+    const size_t smem = ((size_t)w.n_pages * 4 + 15) / 16 * 16;
+    if (smem > 32 << 10 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallPool * 4) != cudaSuccess)
+      return L2KV_ERR_CUDA;
+    return launch_chained(kern, 1, 1, kDealThreads, smem, s, a, w, static_cast<T*>(K), static_cast<T*>(V), idx, sumsq, g);
   }
-  if (rc != L2KV_OK) return rc;
   const long long table_blocks = (w.entries + kPageThreads / 32 - 1) / (kPageThreads / 32), groups = (g.H + kCopyHeads - 1) / kCopyHeads;
-  if (table_blocks + w.entries * groups > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
-  return launch_chained(page_update_kernel<T, D>, table_blocks + w.entries * groups, 1, kPageThreads, 0, s, a, w, static_cast<T*>(K),
+  if (1 + table_blocks + w.entries * groups > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
+  int rc = launch_begin(w, a.pin, s);
+  if (rc == L2KV_OK) rc = launch_chained(page_mark_kernel, table_blocks, 1, kPageThreads, 0, s, a, w);
+  if (rc == L2KV_OK) rc = launch_deal(w, s);
+  if (rc != L2KV_OK) return rc;
+  return launch_chained(page_update_kernel<T, D>, 1 + table_blocks + w.entries * groups, 1, kPageThreads, 0, s, a, w, static_cast<T*>(K),
                         static_cast<T*>(V), idx, sumsq, g, (int)table_blocks, (int)groups);
 }
 
 int launch_page_update(const PageUpdate& a, void* K, void* V, int32_t* idx, float* sumsq, const Geom& g, int dtype,
                        char* scratch, cudaStream_t s) {
   const long long entries = (long long)a.B * a.L;
-  const PageScratch w = scratch_of(plan_pages(entries, 0, a.in.n, 0), scratch, entries);
+  const PageScratch w = scratch_of(plan_pages(entries, 0, a.in.n, 0), scratch, entries, a.in.n);
   if (dtype == L2KV_BF16) return g.D == 128 ? launch_pu<__nv_bfloat16, 128>(a, w, K, V, idx, sumsq, g, s) : launch_pu<__nv_bfloat16, 64>(a, w, K, V, idx, sumsq, g, s);
   return g.D == 128 ? launch_pu<float, 128>(a, w, K, V, idx, sumsq, g, s) : launch_pu<float, 64>(a, w, K, V, idx, sumsq, g, s);
 }
@@ -609,15 +640,15 @@ int launch_page_compact(const PageCompact& a, void* K, void* V, int32_t* idx, fl
   const long long entries = (long long)a.B * a.L, units = entries * a.H;
   const PagePlan p = plan_pages(entries, units, a.in.n, a.max_len);
   if (p.n_chunks > kMaxChunks || units * p.n_chunks + entries > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
-  const PageScratch w = scratch_of(p, scratch, entries);
+  const PageScratch w = scratch_of(p, scratch, entries, a.in.n);
   const CompactSelect c{sumsq, reinterpret_cast<float*>(scratch + p.key_off), reinterpret_cast<UnitRec*>(scratch + p.unit_off),
                         reinterpret_cast<int2*>(scratch + p.chunk_off), p.ld, g.total_rows, p.n_chunks};
-  int rc = begin_pages(w, a.pin, a.in.n, s);
+  int rc = launch_begin(w, a.pin, s);
   if (rc != L2KV_OK) return rc;
   // a block per unit: as many threads as the SMs have room for at once
   rc = units <= 148 ? launch_select<1024>(a, w, c, units, s) : launch_select<512>(a, w, c, units, s);
   if (rc != L2KV_OK) return rc;
-  rc = deal_pages(a, w, a.in.n, nullptr, s);
+  rc = launch_deal(w, s);
   if (rc != L2KV_OK) return rc;
   if (dtype == L2KV_BF16) return g.D == 128 ? launch_pc<__nv_bfloat16, 128>(a, w, c, K, V, idx, sumsq, g, s) : launch_pc<__nv_bfloat16, 64>(a, w, c, K, V, idx, sumsq, g, s);
   return g.D == 128 ? launch_pc<float, 128>(a, w, c, K, V, idx, sumsq, g, s) : launch_pc<float, 64>(a, w, c, K, V, idx, sumsq, g, s);

@@ -26,12 +26,10 @@ inline PageView make_pages(const l2kv_pages& p) {
   return PageView{p.table_dev, p.stride_b, p.stride_l, p.table_cap, shift, p.n_pages, p.room_dev};
 }
 
-// What page_update and page_compact share: which pages are held, and which free ones each (b, l) gets.
+// The scratch that page_update and page_compact share: which pages are held, and which free ones each (b, l) gets.
+constexpr int kMaxStretches = 512;                       // stretches of the pool whose free pages are listed
 struct PagePlan {
-  size_t mark_off;       // uint32 [n_pages]            highest claim on a page; 0: free
-  size_t used_off;       // int32  [groups]             pages held, per group of pages
-  size_t order_off;      // int32  [n_pages]            the free pages in ascending order
-  size_t need_off;       // int2   [entries]            what (b, l) gets: where its pages begin in that order, or -1; a number more
+  size_t mark_off, order_off, count_off, ask_off, deal_off, asked_off;   // as in pages.cu
   size_t key_off;        // float  [units][ld]          page_compact: keys in row order
   size_t unit_off;       // UnitRec [units]
   size_t chunk_off;      // int2   [units][n_chunks]
@@ -39,7 +37,6 @@ struct PagePlan {
   long long ld;
   int n_chunks;
 };
-constexpr int kPageBlock = 4096;                         // pages per block of the scan
 PagePlan plan_pages(long long entries, long long units, int n_pages, int max_len);
 
 struct PageUpdate {
