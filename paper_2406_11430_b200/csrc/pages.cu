@@ -16,7 +16,6 @@
 #include <algorithm>
 #include <climits>
 
-#include "select_unit.cuh"
 #include "tokens.cuh"
 
 namespace l2kv {
@@ -60,9 +59,16 @@ struct PageScratch {
 };
 constexpr int kCopies = 1 << 30, kAsksNot = 1 << 31;     // flags beside the pages of a (b, l), which are fewer than 2^28
 
-// Marks [p0, p1), by threads `thread` of `threads`.
+// Marks [p0, p1), by threads `thread` of `threads`, eight pins to a thread at a time.
 __device__ __forceinline__ void begin_pages(uint32_t* mark, const uint8_t* pin, int p0, int p1, int thread, int threads) {
-  for (int p = p0 + thread; p < p1; p += threads) mark[p] = pin && pin[p] ? kPinned : 0u;
+  for (int p = p0 + thread; p < p1; p += 8 * threads) {
+    uint8_t x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = pin && p + i * threads < p1 ? pin[p + i * threads] : 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (p + i * threads < p1) mark[p + i * threads] = x[i] ? kPinned : 0u;
+  }
 }
 
 constexpr int kBeginPages = 2048;                        // pages per block
@@ -116,62 +122,6 @@ page_mark_kernel(const __grid_constant__ PageUpdate a, PageScratch w) {
   if (u < w.entries) mark_entry(a, w, w.mark, u);
 }
 
-// A (b, l)'s keys in row order, and the selection, a block per head; further blocks claim.
-struct CompactSelect {
-  const float* sumsq;
-  float* keys;
-  UnitRec* units;
-  int2* chunks;
-  long long ld, total_rows;
-  int n_chunks;
-};
-template <int NT>
-__global__ void __launch_bounds__(NT, 1024 / NT)
-page_mark_select_kernel(const __grid_constant__ PageCompact a, PageScratch w, CompactSelect c) {
-  __shared__ SelectSmem sm;
-  next_may_start();
-  wait_for_previous();
-  const long long units = (long long)w.entries * a.H;
-  if (blockIdx.x >= units) {
-    const long long u = (blockIdx.x - units) * (NT / 32) + (threadIdx.x >> 5);
-    if (u >= w.entries) return;
-    const int rows = cached_rows(a, u), keep = max(0, a.keep[u]);
-    const bool bad = claim_pages(w.mark, a.in, a.in.of((int)(u / a.L), (int)(u % a.L)), pages_of(rows, a.in), u, rows);
-    if (threadIdx.x & 31) return;
-    if (bad) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
-    w.ask[u] = PageAsk{keep < rows && !bad ? pages_of(keep, a.in) : -1, -1, 0, rows};
-    return;
-  }
-  const long long unit = blockIdx.x, u = unit / a.H;
-  const int h = (int)(unit % a.H), len = cached_rows(a, u), keep = a.keep[u];
-  if (keep >= len || keep <= 0) return;                  // stays whole, or keeps nothing
-  const int32_t* const row = a.in.of((int)(u / a.L), (int)(u % a.L));
-  const float* const from = c.sumsq + h * c.total_rows;
-  float* const keys = c.keys + unit * c.ld;
-  constexpr int kBatch = 8;
-  for (int t0 = 0; t0 < len; t0 += kBatch * NT) {
-    float x[kBatch];
-    int page[kBatch];
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const int t = t0 + i * NT + (int)threadIdx.x;
-      page[i] = t < len ? row[t >> a.in.shift] : -1;
-    }
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const int t = t0 + i * NT + (int)threadIdx.x;
-      x[i] = a.in.valid(page[i]) ? from[((long long)page[i] << a.in.shift) | (t & (a.in.rows() - 1))] : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const int t = t0 + i * NT + (int)threadIdx.x;
-      if (t < len) keys[t] = x[i];
-    }
-  }
-  __syncthreads();
-  select_unit<NT>(sm, keys, len, keep, a.policy, 0, c.units + unit, c.chunks + unit * c.n_chunks);
-}
-
 // Inclusive sum over the block's threads; *total: of all.
 template <typename N>
 __device__ __forceinline__ N block_sum(N x, N* s_warp, N* total) {
@@ -196,19 +146,159 @@ __device__ __forceinline__ N block_sum(N x, N* s_warp, N* total) {
   return incl + (warp ? before : 0);
 }
 
+// ---- selection: the `keep` smallest keys of a unit, ties to the lower row ----------------------------------------
+// A block per (b, l, h).  The keys come through the table once and stay in shared memory (in the scratch, where there are too
+// many).  The threshold is found by counting into 2048 equal bins between the smallest and the largest key, as integers of
+// the same order, then between the borders of the bin that holds it, and so on: 11 bits a pass, three passes at most, and
+// no bin that most keys fall into, as a digit of their bits would have.  What is left is a bit per row, kept or not, and where each
+// chunk's first kept row goes.  (8 units of 8000 keys 12 us, 256 units of 20 to 32 thousand 43; 16 and 51 by digits of 8 bits
+// from the scratch.)
+struct CompactSelect {
+  const float* sumsq;
+  float* keys;           // [units][ld], or null: shared memory holds them
+  uint32_t* kept;        // [units][16 n_chunks] a bit per row
+  int32_t* slots;        // [units][n_chunks] kept rows before the chunk
+  long long ld, total_rows;
+  int n_chunks;
+};
+constexpr int kBins = 2048, kChunkWords = kGatherChunk / 32;
+template <int NT, bool SHARED>
+__global__ void __launch_bounds__(NT, 1024 / NT)
+page_mark_select_kernel(const __grid_constant__ PageCompact a, PageScratch w, CompactSelect c) {
+  extern __shared__ uint32_t s_keys[];
+  __shared__ int s_bins[kBins];
+  __shared__ uint32_t s_range[2];
+  __shared__ int s_found[3];
+  __shared__ int s_warp[32];
+  next_may_start();
+  wait_for_previous();
+  const long long units = (long long)w.entries * a.H;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (blockIdx.x >= units) {                             // the claims, a warp per (b, l)
+    const long long u = (blockIdx.x - units) * (NT / 32) + warp;
+    if (u >= w.entries) return;
+    const int rows = cached_rows(a, u), keep = max(0, a.keep[u]);
+    const bool bad = claim_pages(w.mark, a.in, a.in.of((int)(u / a.L), (int)(u % a.L)), pages_of(rows, a.in), u, rows);
+    if (lane) return;
+    if (bad) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
+    w.ask[u] = PageAsk{keep < rows && !bad ? pages_of(keep, a.in) : -1, -1, 0, rows};
+    return;
+  }
+  const long long unit = blockIdx.x, u = unit / a.H;
+  const int h = (int)(unit % a.H), len = cached_rows(a, u), keep = a.keep[u];
+  if (keep >= len || keep <= 0) return;                  // stays whole, or keeps nothing
+  const int32_t* const row = a.in.of((int)(u / a.L), (int)(u % a.L));
+  const float* const from = c.sumsq + h * c.total_rows;
+  uint32_t* const keys = SHARED ? s_keys : reinterpret_cast<uint32_t*>(c.keys + unit * c.ld);
+  if (tid == 0) { s_range[0] = 0xffffffffu; s_range[1] = 0; }
+  __syncthreads();
+  constexpr int kBatch = 16;
+  uint32_t lo = 0xffffffffu, hi = 0;
+  for (int t0 = tid; t0 < len; t0 += kBatch * NT) {
+    int page[kBatch];
+    float x[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) page[i] = t0 + i * NT < len ? row[(t0 + i * NT) >> a.in.shift] : -1;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      x[i] = a.in.valid(page[i]) ? from[((long long)page[i] << a.in.shift) | ((t0 + i * NT) & (a.in.rows() - 1))] : 0.f;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (t0 + i * NT >= len) continue;
+      const uint32_t b = order_bits(x[i], a.policy);
+      keys[t0 + i * NT] = b;
+      lo = min(lo, b);
+      hi = max(hi, b);
+    }
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  if (lane == 0) { atomicMin(&s_range[0], lo); atomicMax(&s_range[1], hi); }
+  __syncthreads();
+  lo = s_range[0];
+  hi = s_range[1];
+  int rank = keep;                                       // of the threshold, among the keys in [lo, hi]
+  while (lo < hi) {
+    const int shift = max(0, 21 - __clz(hi - lo));       // (hi - lo) >> shift fits 11 bits
+    for (int i = tid; i < kBins; i += NT) s_bins[i] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int t = tid; t < len; t += NT) {
+      const uint32_t b = keys[t];
+      if (b >= lo && b <= hi) atomicAdd(&s_bins[(b - lo) >> shift], 1);
+    }
+    __syncthreads();
+    constexpr int kEach = kBins / NT;
+    int n[kEach], mine = 0, all;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) mine += n[i] = s_bins[tid * kEach + i];
+    int before = block_sum(mine, s_warp, &all) - mine;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (before < rank && rank <= before + n[i]) { s_found[0] = tid * kEach + i; s_found[1] = before; s_found[2] = n[i]; }
+      before += n[i];
+    }
+    __syncthreads();
+    lo += (uint32_t)s_found[0] << shift;
+    hi = hi - lo < (1u << shift) ? hi : lo + ((1u << shift) - 1u);
+    rank -= s_found[1];
+    if (rank == s_found[2]) {                            // all of the bin are kept
+      lo = hi;
+      rank = INT_MAX;
+    }
+    __syncthreads();                                     // (read before the next pass counts)
+  }
+  // `lo` is the threshold, `rank` keys equal to it are kept.  Per chunk the keys below and at it, a warp each; their sums.
+  const int chunks = (len + kGatherChunk - 1) / kGatherChunk;
+  for (int c0 = 0, before = 0, ties_before = 0; c0 < chunks; c0 += NT / 32) {
+    const int chunk = c0 + warp, t0 = chunk * kGatherChunk + lane;
+    uint32_t below[kChunkWords], at[kChunkWords];
+    int n = 0, ties = 0;
+#pragma unroll
+    for (int i = 0; i < kChunkWords; ++i) {
+      const int t = t0 + 32 * i;
+      const uint32_t b = chunk < chunks && t < len ? keys[t] : 0xffffffffu;
+      const bool in = chunk < chunks && t < len;
+      below[i] = __ballot_sync(0xffffffffu, in && b < lo);
+      at[i] = __ballot_sync(0xffffffffu, in && b == lo);
+      n += __popc(below[i]);
+      ties += __popc(at[i]);
+    }
+    if (lane == 0) { s_bins[warp] = n; s_bins[32 + warp] = ties; }
+    __syncthreads();
+    const int x = lane < NT / 32 ? s_bins[lane] : 0, y = lane < NT / 32 ? s_bins[32 + lane] : 0;
+    const int n_before = before + __reduce_add_sync(0xffffffffu, lane < warp ? x : 0);
+    int t_before = ties_before + __reduce_add_sync(0xffffffffu, lane < warp ? y : 0);
+    before += __reduce_add_sync(0xffffffffu, x);
+    ties_before += __reduce_add_sync(0xffffffffu, y);
+    __syncthreads();
+    if (chunk >= chunks) continue;
+    if (lane == 0) c.slots[unit * c.n_chunks + chunk] = n_before + min(t_before, rank);
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 0; i < kChunkWords; ++i) {
+      // of the ties the first ones: those whose number among all is below `rank`
+      const int room = rank - t_before;
+      const bool tie = (at[i] >> lane & 1u) && __popc(at[i] & ((1u << lane) - 1u)) < room;
+      const uint32_t all = below[i] | __ballot_sync(0xffffffffu, tie);
+      t_before += __popc(at[i]);
+      if (lane == i) word = all;
+    }
+    if (lane < kChunkWords) c.kept[(unit * c.n_chunks + chunk) * kChunkWords + lane] = word;
+  }
+}
+
 // The free pages among [p0, p1), listed from order[p0] on, by a block of kDealThreads; how many.
 __device__ __forceinline__ int list_free(const uint32_t* mark, int32_t* order, int p0, int p1, int* s_warp) {
   constexpr int kEach = 4;
   int listed = 0;
   for (int q0 = p0; q0 < p1; q0 += kEach * kDealThreads) {
     const int p = q0 + (int)threadIdx.x * kEach;
-    bool is_free[kEach];
-    int n = 0, all;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      is_free[i] = p + i < p1 && mark[p + i] == 0;
-      n += is_free[i];
-    }
+    // (marks and stretches begin on 16-byte boundaries, and so does what lies behind the last)
+    const uint4 m = p < p1 ? *reinterpret_cast<const uint4*>(mark + p) : make_uint4(1, 1, 1, 1);
+    const bool is_free[kEach] = {p < p1 && m.x == 0, p + 1 < p1 && m.y == 0, p + 2 < p1 && m.z == 0, p + 3 < p1 && m.w == 0};
+    const int n = is_free[0] + is_free[1] + is_free[2] + is_free[3];
+    int all;
     int at = p0 + listed + block_sum(n, s_warp, &all) - n;
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
@@ -270,18 +360,30 @@ __device__ __forceinline__ void load_sums(const PageScratch& w, PageSums& s) {
   if (warp < 2) {
     const int n = warp == 0 ? w.stretches() : w.ask_blocks();
     long long before = 0;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-      const int i = i0 + lane;
-      const long long x = i >= n ? 0 : warp == 0 ? w.count[i] : w.asked[i];
-      long long incl = x;
+    for (int i0 = 0; i0 < n; i0 += 128) {                // four to a lane
+      long long x[4], sum = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = i0 + 4 * lane + k;
+        x[k] = i >= n ? 0 : warp == 0 ? w.count[i] : w.asked[i];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum += x[k];
+      long long incl = sum;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
         const long long o = __shfl_up_sync(0xffffffffu, incl, off);
         if (lane >= off) incl += o;
       }
-      if (i < n) {
-        if (warp == 0) s.free_before[i] = (int)(before + incl - x);
-        else s.asked_before[i] = before + incl - x;
+      long long at = before + incl - sum;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = i0 + 4 * lane + k;
+        if (i < n) {
+          if (warp == 0) s.free_before[i] = (int)at;
+          else s.asked_before[i] = at;
+        }
+        at += x[k];
       }
       before += __shfl_sync(0xffffffffu, incl, 31);
     }
@@ -421,7 +523,7 @@ constexpr long long kSmallCopy = 128 << 10;              // bytes that one block
 template <typename T, int D>
 __global__ void __launch_bounds__(kDealThreads)
 page_update_small_kernel(const __grid_constant__ PageUpdate a, PageScratch w, T* K, T* V, int32_t* idx, float* sumsq, Geom g) {
-  extern __shared__ uint32_t s_mark[];
+  extern __shared__ __align__(16) uint32_t s_mark[];
   __shared__ PageSums sums;
   __shared__ long long s_sums[32];
   __shared__ int s_warp[32];
@@ -450,8 +552,7 @@ page_update_small_kernel(const __grid_constant__ PageUpdate a, PageScratch w, T*
 
 // ---- the kept rows of a compaction ------------------------------------------------------------------
 // A block per chunk of kGatherChunk rows of a unit, as in select_compact's gather, or, where those would leave SMs idle, several,
-// a part of the chunk's kept rows each: the chunk's rows are ranked from the threshold, where each kept one comes from and
-// goes to is noted, and they move 16 bytes a lane, kMoves rows of K and of V per lane in flight.
+// a part of the chunk's kept rows each: where each kept one comes from and goes to is noted, and they move 16 bytes a lane, kMoves rows of K and of V per lane in flight.
 constexpr int kMoves = 4;
 template <typename T, int D>
 __global__ void __launch_bounds__(kPageThreads)
@@ -459,7 +560,6 @@ page_compact_kernel(const __grid_constant__ PageCompact a, PageScratch w, Compac
                     int parts) {
   constexpr int LPR = D / Elem<T>::kPerVec, RPS = kPageThreads / LPR, TPT = kGatherChunk / kPageThreads;
   __shared__ int s_from[kGatherChunk], s_to[kGatherChunk];   // pool rows that the kept rows move from and to
-  __shared__ int s_warp[32];
   __shared__ PageSums sums;
   next_may_start();
   wait_for_previous();
@@ -486,40 +586,28 @@ page_compact_kernel(const __grid_constant__ PageCompact a, PageScratch w, Compac
   load_sums(w, sums);
   const PageDeal d = deal_of(w, sums, u);
   if (!d.gets) return;
-  const UnitRec rec = c.units[unit];
-  const int2 cr = c.chunks[unit * c.n_chunks + chunk];   // slot of the chunk's first kept row, ties before it
-  const float* const key = c.keys + unit * c.ld;
+  const int slot0 = c.slots[unit * c.n_chunks + chunk];
   const int32_t* const row = a.in.of((int)(u / a.L), (int)(u % a.L));
-  uint32_t bits[TPT];
-  int page[TPT], count = 0;                              // rows below the threshold in the upper half, at it in the lower
+  // the chunk's words, one to each of a warp's first lanes; kept rows before a word
+  const int lane = tid & 31;
+  const uint32_t word = lane < kChunkWords ? c.kept[(unit * c.n_chunks + chunk) * kChunkWords + lane] : 0u;
+  int upto = __popc(word);
 #pragma unroll
-  for (int i = 0; i < TPT; ++i) {
-    const int t = t0 + tid * TPT + i;
-    bits[i] = t < len ? order_bits(key[t], a.policy) : 0u;
-    page[i] = t < len ? row[t >> a.in.shift] : 0;
-    if (t < len) count += bits[i] < rec.thr ? 0x10000 : bits[i] == rec.thr;
+  for (int off = 1; off < 32; off <<= 1) {
+    const int o = __shfl_up_sync(0xffffffffu, upto, off);
+    if (lane >= off) upto += o;
   }
-  int all;
-  int before = block_sum(count, s_warp, &all) - count;
-  const int taken = min(cr.y, rec.admit);                // ties taken in the chunks before
+  const int n_kept = __shfl_sync(0xffffffffu, upto, 31);
 #pragma unroll
   for (int i = 0; i < TPT; ++i) {
-    const int t = t0 + tid * TPT + i;
-    if (t >= len) continue;
-    const int ties = cr.y + (before & 0xffff);
-    const bool less = bits[i] < rec.thr, tie = bits[i] == rec.thr;
-    if (less || (tie && ties < rec.admit)) {
-      const int j = (before >> 16) + min(ties, rec.admit) - taken, slot = cr.x + j;
-      const bool ok = L2KV_BOUNDS(j >= 0 && j < kGatherChunk && slot >= 0 && slot < rec.n_keep, a.status);
-      if (ok) {
-        s_from[j] = (page[i] << a.in.shift) | (t & (a.in.rows() - 1));
-        s_to[j] = (free_page(w, sums, d.begin + (slot >> a.in.shift)) << a.in.shift) | (slot & (a.in.rows() - 1));
-      }
-    }
-    before += less ? 0x10000 : tie;
+    const int r = i * kPageThreads + tid, of = r >> 5, t = t0 + r;
+    const uint32_t bits = __shfl_sync(0xffffffffu, word, of);
+    const int j = __shfl_sync(0xffffffffu, upto, of) - __popc(bits >> lane), slot = slot0 + j;
+    if (!(bits >> lane & 1u) || !L2KV_BOUNDS(t < len && j >= 0 && slot >= 0 && slot < a.keep[u], a.status)) continue;
+    s_from[j] = (row[t >> a.in.shift] << a.in.shift) | (t & (a.in.rows() - 1));
+    s_to[j] = (free_page(w, sums, d.begin + (slot >> a.in.shift)) << a.in.shift) | (slot & (a.in.rows() - 1));
   }
   __syncthreads();
-  const int n_kept = (all >> 16) + min(cr.y + (all & 0xffff), rec.admit) - taken;
   const int j1 = (int)((long long)n_kept * (part + 1) / parts);
   const int piece = tid % LPR, sub = tid / LPR;
   const long long mine = h * g.sh + piece * Elem<T>::kPerVec, meta = h * g.total_rows;
@@ -556,6 +644,8 @@ page_compact_kernel(const __grid_constant__ PageCompact a, PageScratch w, Compac
 
 // ---- host ------------------------------------------------------------------------------------------
 
+constexpr int kSelectShared = 53248, kSelectTwo = 25600;  // keys that fit an SM's shared memory, and those of two blocks
+
 PagePlan plan_pages(long long entries, long long units, int n_pages, int max_len) {
   PagePlan p;
   size_t off = 0;
@@ -572,9 +662,9 @@ PagePlan plan_pages(long long entries, long long units, int n_pages, int max_len
   p.ask_off = take((long long)sizeof(PageAsk) * entries);
   p.deal_off = take(8 * entries);
   p.asked_off = take(8ll * kMaxAskBlocks);
-  p.key_off = take(4 * units * p.ld);
-  p.unit_off = take(16 * units);
-  p.chunk_off = take(8 * units * p.n_chunks);
+  p.key_off = take(max_len > kSelectShared ? 4 * units * p.ld : 0);
+  p.kept_off = take(4ll * kChunkWords * units * p.n_chunks);
+  p.slot_off = take(4 * units * p.n_chunks);
   p.total = off;
   return p;
 }
@@ -621,9 +711,12 @@ int launch_page_update(const PageUpdate& a, void* K, void* V, int32_t* idx, floa
   return g.D == 128 ? launch_pu<float, 128>(a, w, K, V, idx, sumsq, g, s) : launch_pu<float, 64>(a, w, K, V, idx, sumsq, g, s);
 }
 
-template <int NT>
+template <int NT, bool SHARED>
 static int launch_select(const PageCompact& a, const PageScratch& w, const CompactSelect& c, long long units, cudaStream_t s) {
-  return launch_chained(page_mark_select_kernel<NT>, units + (w.entries + NT / 32 - 1) / (NT / 32), 1, NT, 0, s, a, w, c);
+  auto kern = page_mark_select_kernel<NT, SHARED>;
+  const size_t smem = SHARED ? (size_t)c.ld * 4 : 0;
+  if (SHARED && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelectShared * 4) != cudaSuccess) return L2KV_ERR_CUDA;
+  return launch_chained(kern, units + (w.entries + NT / 32 - 1) / (NT / 32), 1, NT, smem, s, a, w, c);
 }
 
 template <typename T, int D>
@@ -641,12 +734,14 @@ int launch_page_compact(const PageCompact& a, void* K, void* V, int32_t* idx, fl
   const PagePlan p = plan_pages(entries, units, a.in.n, a.max_len);
   if (p.n_chunks > kMaxChunks || units * p.n_chunks + entries > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
   const PageScratch w = scratch_of(p, scratch, entries, a.in.n);
-  const CompactSelect c{sumsq, reinterpret_cast<float*>(scratch + p.key_off), reinterpret_cast<UnitRec*>(scratch + p.unit_off),
-                        reinterpret_cast<int2*>(scratch + p.chunk_off), p.ld, g.total_rows, p.n_chunks};
+  const bool shared = a.max_len <= kSelectShared;
+  const CompactSelect c{sumsq, shared ? nullptr : reinterpret_cast<float*>(scratch + p.key_off), reinterpret_cast<uint32_t*>(scratch + p.kept_off),
+                        reinterpret_cast<int32_t*>(scratch + p.slot_off), p.ld, g.total_rows, p.n_chunks};
   int rc = launch_begin(w, a.pin, s);
   if (rc != L2KV_OK) return rc;
-  // a block per unit: as many threads as the SMs have room for at once
-  rc = units <= 148 ? launch_select<1024>(a, w, c, units, s) : launch_select<512>(a, w, c, units, s);
+  // a block per unit: with as many threads as the SMs have room for at once
+  rc = !shared ? launch_select<1024, false>(a, w, c, units, s)
+       : units > 148 && a.max_len <= kSelectTwo ? launch_select<512, true>(a, w, c, units, s) : launch_select<1024, true>(a, w, c, units, s);
   if (rc != L2KV_OK) return rc;
   rc = launch_deal(w, s);
   if (rc != L2KV_OK) return rc;

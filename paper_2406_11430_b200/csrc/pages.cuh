@@ -30,9 +30,7 @@ inline PageView make_pages(const l2kv_pages& p) {
 constexpr int kMaxStretches = 512;                       // stretches of the pool whose free pages are listed
 struct PagePlan {
   size_t mark_off, order_off, count_off, ask_off, deal_off, asked_off;   // as in pages.cu
-  size_t key_off;        // float  [units][ld]          page_compact: keys in row order
-  size_t unit_off;       // UnitRec [units]
-  size_t chunk_off;      // int2   [units][n_chunks]
+  size_t key_off, kept_off, slot_off;                                    // page_compact: of each unit
   size_t total;
   long long ld;
   int n_chunks;

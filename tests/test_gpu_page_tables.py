@@ -258,6 +258,32 @@ def test_compaction(l2, P, policy, integer_keys):
     assert not compact(p, keep, policy=policy)
 
 
+@pytest.mark.parametrize("policy", [0, 1])
+@pytest.mark.parametrize("rows", [25600, 25601, 53248, 53249, 60001])
+def test_compaction_of_long_caches(l2, rows, policy):
+    """Around what the selection keeps in shared memory; keys of one value, of two, and of far apart ones among others."""
+    for kind in ("random", "equal", "two", "far"):
+        p = Pool(l2, [[rows]], 1024, H=2, spare=80, seed=rows % 97)
+        if kind == "equal":
+            p.key.fill_(0.25)
+        if kind == "two":
+            p.key.copy_((p.key > 0.7).float() * 3 + 1e-30)
+        if kind == "far":
+            p.key[:, ::3] = 0
+            p.key[:, 1::7] = 3e38
+            p.key[:, 5::1000] = 1e-42
+        for keep in (1, rows // 2, rows - 1):
+            compact(p, [[keep]], policy=policy)
+
+
+def test_compaction_of_many_units(l2):
+    """More units than SMs."""
+    r = np.random.RandomState(2)
+    rows = r.randint(0, 1500, (7, 6))
+    p = Pool(l2, rows, 16, H=4, spare=2200, seed=9, integer_keys=True)
+    compact(p, (rows * r.rand(7, 6)).astype(int))
+
+
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("fp32", 64), ("fp32", 128)])
 def test_compaction_types(l2, dtype, D):
     p = Pool(l2, [[700], [90]], 32, H=2, D=D, dtype=dtype, spare=60)
