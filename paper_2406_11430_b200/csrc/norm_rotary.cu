@@ -1,0 +1,256 @@
+// Norms, rotary positions and cache write of new tokens, where a pair is an element of the head's lower half and the one
+// as far into the upper half, and all of the head turns.
+//
+// As in rotary_write_kernel a token's rows are one warp's (or, of few tokens, several warps'), and a row belongs to LPR adjacent
+// lanes, a 16-byte piece each.  There every lane fetched its partner's piece to compute its own half of the pairs, and a warp
+// spent 114 instructions on two rows, which bound the kernel (65 % of the issue slots; 10 k tokens of 32 + 16 rows of 256 bytes
+// 43 us).  Here two rows that a lane has pieces of are dealt out anew: the lanes of the lower half hand over the second row's piece and get
+// the first row's upper one, those of the upper half the other way round.  A lane then has both halves of one row's pairs,
+// so every product is formed once, and sums over a row cross half as many lanes; results go out from where they are.  The
+// norm's factor r = 1 / sqrt(mean x^2 + eps) comes last, the weights go into cosines and sines, and a row is rounded once.  The
+// ordering key keeps its order of summation: a piece with the one LPR / 2 further on first.
+#include <climits>
+
+#include "rotary.cuh"
+
+namespace l2kv {
+
+template <typename T>
+__device__ __forceinline__ void unpack_pairs(const uint4& v, float2 (&x)[Elem<T>::kPerVec / 2]) {
+  float f[Elem<T>::kPerVec];
+  Elem<T>::unpack(v, f);
+#pragma unroll
+  for (int i = 0; i < Elem<T>::kPerVec / 2; ++i) x[i] = make_float2(f[2 * i], f[2 * i + 1]);
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack_pairs(const float2 (&x)[Elem<T>::kPerVec / 2]) {
+  float f[Elem<T>::kPerVec];
+#pragma unroll
+  for (int i = 0; i < Elem<T>::kPerVec / 2; ++i) { f[2 * i] = x[i].x; f[2 * i + 1] = x[i].y; }
+  return pack_piece<T>(f);
+}
+__device__ __forceinline__ uint4 pick(bool first, const uint4& a, const uint4& b) {
+  return make_uint4(first ? a.x : b.x, first ? a.y : b.y, first ? a.z : b.z, first ? a.w : b.w);
+}
+
+// WPT: warps that share a token.
+template <typename T, int D, int WPT>
+__global__ void __launch_bounds__(kRotaryThreads, 2)
+norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
+  constexpr int EPV = Elem<T>::kPerVec, LPR = D / EPV, RPW = 32 / LPR, HALF = LPR / 2, NP = EPV / 2;
+  constexpr int U = WPT == 1 ? 8 : 4;                    // pieces per lane in flight
+  constexpr int TPB = kRotaryWarps / WPT, STEP = WPT * RPW;
+  __shared__ float2 s_turn[kRotaryWarps][D / 2];
+  const Geom& g = a.g;
+  const PageView& pages = a.norm.pages;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane % LPR, pair = piece % HALF;
+  const bool lower = piece < HALF;
+  next_may_start();
+  wait_for_previous();
+  const unsigned n_rows = (unsigned)a.n_tokens * (unsigned)g.L, token_blocks = (n_rows + TPB - 1) / TPB;
+  if (blockIdx.x >= token_blocks) {
+    // trailing blocks: the new lengths (sequences without new tokens have one too)
+    const long long u = (long long)(blockIdx.x - token_blocks) * kRotaryThreads + threadIdx.x;
+    const long long units = (long long)g.B * g.L * (a.per_head ? g.H : 1);
+    if (u >= units) return;
+    const long long bl = a.per_head ? u / g.H : u;
+    const int n = tokens_of(a.tok_off, (int)(bl / g.L), a.n_tokens).n;
+    int cap = g.cap(bl);
+    if (pages.table && pages.room) cap = max(0, min(cap, pages.room[bl]));
+    a.cur_len[u] = (int)min((long long)cap, (long long)max(0, a.start[u]) + n);
+    return;
+  }
+  const unsigned il = blockIdx.x * TPB + warp / WPT;     // token * layers + layer
+  if (il >= n_rows) return;
+  const int i = (int)(il / (unsigned)g.L), l = (int)(il % (unsigned)g.L);
+  const int group = (warp % WPT) * RPW, row0 = group + lane / LPR;           // this lane's first row of each kind
+
+  auto load = [&](uint4 (&x)[U], const char* from, long long stride, int r0, int n) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      x[u] = r0 + u * STEP < n ? ld_once(from + (r0 + u * STEP) * stride) : make_uint4(0, 0, 0, 0);
+  };
+  const char* const q_from = reinterpret_cast<const char*>(a.q.row<T>(l, i, 0)) + piece * 16;
+  const long long q_stride = a.q.sh * (long long)sizeof(T);
+  uint4 x[U];
+  load(x, q_from, q_stride, row0, g.Hq);
+
+  const int pos = a.pos[i];
+#pragma unroll
+  for (int p = lane; p < D / 2; p += 32) {
+    double c, s;
+    cos_sin((double)pos * a.freq[p], &c, &s);
+    s_turn[warp][p] = make_float2((float)(c * a.scale), (float)(s * a.scale));
+  }
+  const int b = sequence_of(a.tok_off, g.B, a.n_tokens, i);
+  if (b < 0) return;                                     // a token of no sequence (the whole warp)
+  const int at = i - tokens_of(a.tok_off, b, a.n_tokens).first;
+  const long long bl = (long long)b * g.L + l;
+  int cap = g.cap(bl);
+  const long long slot_all = a.per_head ? 0 : (long long)max(0, a.start[bl]) + at;
+  const int32_t* const table = pages.table ? pages.of(b, l) : nullptr;
+  if (table && pages.room) cap = max(0, min(cap, pages.room[bl]));
+  const int page_all = table && !a.per_head && slot_all < cap ? table[slot_all >> pages.shift] : -1;
+  __syncwarp();
+
+  // y_lower = lower * cl + upper * su, y_upper = upper * cu + lower * sl, weights included
+  float2 cl[NP], cu[NP], sl[NP], su[NP];
+  auto turn = [&](const void* weight) {
+    float2 wl[NP], wu[NP];
+    if (weight) {
+      unpack_pairs<T>(static_cast<const uint4*>(weight)[pair], wl);
+      unpack_pairs<T>(static_cast<const uint4*>(weight)[pair + HALF], wu);
+    }
+#pragma unroll
+    for (int e = 0; e < NP; ++e) {
+      const float2 t0 = s_turn[warp][pair * EPV + 2 * e], t1 = s_turn[warp][pair * EPV + 2 * e + 1];
+      cl[e] = cu[e] = make_float2(t0.x, t1.x);
+      sl[e] = make_float2(t0.y, t1.y);
+      su[e] = make_float2(-t0.y, -t1.y);
+      if (weight) {
+        const float2 off = make_float2(a.norm.offset, a.norm.offset), l2 = add_pair(wl[e], off), u2 = add_pair(wu[e], off);
+        cl[e] = mul_pair(cl[e], l2);
+        su[e] = mul_pair(su[e], u2);
+        cu[e] = mul_pair(cu[e], u2);
+        sl[e] = mul_pair(sl[e], l2);
+      }
+    }
+  };
+  // The two halves of one of the rows x0 (lanes of the lower half) and x1 (the others), turned; whole warps.
+  auto rotated = [&](const uint4& x0, const uint4& x1, bool norms, uint4& lo, uint4& hi) {
+    const uint4 mine = pick(lower, x0, x1), send = pick(lower, x1, x0);
+    uint4 got;
+    got.x = __shfl_xor_sync(0xffffffffu, send.x, HALF); got.y = __shfl_xor_sync(0xffffffffu, send.y, HALF);
+    got.z = __shfl_xor_sync(0xffffffffu, send.z, HALF); got.w = __shfl_xor_sync(0xffffffffu, send.w, HALF);
+    float2 f[NP], o[NP], y[NP], z[NP];
+    unpack_pairs<T>(pick(lower, mine, got), f);
+    unpack_pairs<T>(pick(lower, got, mine), o);
+    if (norms) {
+      float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int e = 0; e < NP; ++e) sum = fma_pair(o[e], o[e], fma_pair(f[e], f[e], sum));
+      float ss = sum.x + sum.y;
+#pragma unroll
+      for (int off = HALF / 2; off >= 1; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+      const float r = __frcp_rn(__fsqrt_rn(ss * (1.f / D) + a.norm.eps));
+      const float2 r2 = make_float2(r, r);
+#pragma unroll
+      for (int e = 0; e < NP; ++e) {
+        y[e] = mul_pair(fma_pair(o[e], su[e], mul_pair(f[e], cl[e])), r2);
+        z[e] = mul_pair(fma_pair(f[e], sl[e], mul_pair(o[e], cu[e])), r2);
+      }
+    } else {
+      // two products and a sum, each rounded, as rotary_write_kernel forms them
+#pragma unroll
+      for (int e = 0; e < NP; ++e) {
+        y[e] = add_pair(mul_pair(f[e], cl[e]), mul_pair(o[e], su[e]));
+        z[e] = add_pair(mul_pair(o[e], cu[e]), mul_pair(f[e], sl[e]));
+      }
+    }
+    lo = pack_pairs<T>(y);
+    hi = pack_pairs<T>(z);
+  };
+
+  turn(a.norm.norm_q ? a.norm.q_weight : nullptr);
+  char* const q_to = reinterpret_cast<char*>(a.q_out.row<T>(l, i, 0)) + pair * 16;
+  const long long q_to_stride = a.q_out.sh * (long long)sizeof(T);
+  for (int r0 = row0; r0 - row0 + group < g.Hq; r0 += U * STEP) {
+    if (r0 != row0) load(x, q_from, q_stride, r0, g.Hq);
+#pragma unroll
+    for (int u = 0; u < U; u += 2) {
+      uint4 lo, hi;
+      rotated(x[u], x[u + 1], a.norm.norm_q, lo, hi);
+      const int r = r0 + (lower ? u : u + 1) * STEP;
+      if (r >= g.Hq) continue;
+      st_stream(q_to + r * q_to_stride, lo);
+      st_stream(q_to + r * q_to_stride + HALF * 16, hi);
+    }
+  }
+
+  // keys and values side by side, half a batch of each
+  turn(a.norm.norm_k ? a.norm.k_weight : nullptr);
+  const char* const k_from = reinterpret_cast<const char*>(a.k.row<T>(l, i, 0)) + piece * 16;
+  const char* const v_from = reinterpret_cast<const char*>(a.v.row<T>(l, i, 0)) + piece * 16;
+  const long long k_stride = a.k.sh * (long long)sizeof(T), v_stride = a.v.sh * (long long)sizeof(T);
+  const long long cache0 = table ? 0 : g.base(b, l, 0), meta0 = table ? 0 : g.meta(bl * g.H);
+  const long long meta_h = g.row_off || table ? g.total_rows : (long long)g.t_cap;
+  // Where head h's row goes; -1: nowhere (`tells`: the lane that says why).
+  auto slot_of = [&](int h, bool tells) -> long long {
+    const long long slot = a.per_head ? (long long)max(0, a.start[bl * g.H + h]) + at : slot_all;
+    if (slot >= cap) {
+      if (tells) atomicExch(a.status, (int)L2KV_ERR_DEVICE_OVERFLOW);
+      return -1;
+    }
+    if (!L2KV_BOUNDS(g.holds(bl, slot), a.status)) return -1;
+    if (!table) return slot;
+    const int page = a.per_head ? table[slot >> pages.shift] : page_all;
+    if (!pages.valid(page)) {
+      if (tells) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
+      return -1;
+    }
+    return ((long long)page << pages.shift) | (slot & (pages.rows() - 1));
+  };
+  for (int r0 = row0; r0 - row0 + group < g.H; r0 += U / 2 * STEP) {
+#pragma unroll
+    for (int u = 0; u < U / 2; ++u) {
+      const int h = r0 + u * STEP;
+      x[2 * u] = h < g.H ? ld_once(k_from + h * k_stride) : make_uint4(0, 0, 0, 0);
+      x[2 * u + 1] = h < g.H ? ld_once(v_from + h * v_stride) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < U / 2; u += 2) {
+      uint4 lo, hi;
+      rotated(x[2 * u], x[2 * u + 2], a.norm.norm_k, lo, hi);
+      // the key of the row as it is stored
+      float f[EPV], low = 0.f, high = 0.f;
+      Elem<T>::unpack(lo, f);
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) low = __fmaf_rn(f[e], f[e], low);
+      Elem<T>::unpack(hi, f);
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) high = __fmaf_rn(f[e], f[e], high);
+      float key = low + high;
+#pragma unroll
+      for (int off = HALF / 2; off >= 1; off >>= 1) key = key + __shfl_xor_sync(0xffffffffu, key, off);
+      const int h = r0 + (lower ? u : u + 1) * STEP;
+      const long long slot = h < g.H ? slot_of(h, pair == 0) : -1;
+      if (slot >= 0) {
+        T* const to = K + cache0 + h * g.sh + slot * g.st + pair * EPV;
+        *reinterpret_cast<uint4*>(to) = lo;
+        *reinterpret_cast<uint4*>(to + D / 2) = hi;
+        if (pair == 0) {
+          const long long m = meta0 + h * meta_h + slot;
+          if (a.idx) a.idx[m] = pos;
+          if (a.sumsq) a.sumsq[m] = key;
+        }
+      }
+      // the values as they were loaded: of both rows
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int hv = r0 + (u + k) * STEP;
+        const long long sv = hv < g.H ? slot_of(hv, false) : -1;
+        if (sv >= 0) *reinterpret_cast<uint4*>(V + cache0 + hv * g.sh + sv * g.st + piece * EPV) = x[2 * (u + k) + 1];
+      }
+    }
+  }
+}
+
+template <typename T, int D, int WPT>
+static int launch_nr(const NormRotaryArgs& a, void* K, void* V, cudaStream_t s) {
+  constexpr int TPB = kRotaryWarps / WPT;
+  const long long units = (long long)a.g.B * a.g.L * (a.per_head ? a.g.H : 1);
+  const long long blocks = ((long long)a.n_tokens * a.g.L + TPB - 1) / TPB + (units + kRotaryThreads - 1) / kRotaryThreads;
+  if (blocks * TPB > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
+  return launch_chained(norm_rotary_kernel<T, D, WPT>, blocks, 1, kRotaryThreads, 0, s, a, static_cast<T*>(K), static_cast<T*>(V));
+}
+// One warp per token where that gives every SM a block of them, else a block per token, as for rotary_write_kernel.
+template <typename T, int D>
+static int launch_nr_t(const NormRotaryArgs& a, void* K, void* V, cudaStream_t s) {
+  return (long long)a.n_tokens * a.g.L >= 148 * kRotaryWarps ? launch_nr<T, D, 1>(a, K, V, s) : launch_nr<T, D, kRotaryWarps>(a, K, V, s);
+}
+int launch_norm_rotary_halves(const NormRotaryArgs& a, void* K, void* V, int dtype, cudaStream_t s) {
+  if (dtype == L2KV_BF16) return a.g.D == 128 ? launch_nr_t<__nv_bfloat16, 128>(a, K, V, s) : launch_nr_t<__nv_bfloat16, 64>(a, K, V, s);
+  return a.g.D == 128 ? launch_nr_t<float, 128>(a, K, V, s) : launch_nr_t<float, 64>(a, K, V, s);
+}
+
+}  // namespace l2kv

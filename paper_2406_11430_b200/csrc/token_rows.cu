@@ -4,7 +4,7 @@
 // tokens, the chain of dependent loads before the first row can go out.
 #include <climits>
 
-#include "tokens.cuh"
+#include "rotary.cuh"
 
 namespace l2kv {
 
@@ -15,70 +15,6 @@ namespace l2kv {
 // same piece.  A lane meets the same piece of every row, so it keeps that piece's cosines and sines in
 // registers.  Rows are read kRotaryBatch pieces per lane at a time, the first batch before
 // anything is known of the token; angle, sequence and cache row are worked out under those loads.
-constexpr int kRotaryThreads = 256;
-constexpr int kRotaryWarps = kRotaryThreads / 32;
-struct RotaryArgs {
-  TokView q, k, v, q_out;
-  Geom g;
-  const int32_t* tok_off;
-  const int32_t* pos;
-  const double* freq;
-  const int32_t* start;
-  int32_t* cur_len;
-  int32_t* idx;
-  float* sumsq;
-  int32_t* status;
-  int n_tokens, rot_dim, interleaved, per_head;
-  double scale;
-};
-
-template <typename T>
-__device__ __forceinline__ uint4 pack_piece(const float (&y)[Elem<T>::kPerVec]);
-template <>
-__device__ __forceinline__ uint4 pack_piece<float>(const float (&y)[4]) {
-  return make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
-}
-template <>
-__device__ __forceinline__ uint4 pack_piece<__nv_bfloat16>(const float (&y)[8]) {
-  auto two = [](float a, float b) {
-    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&p);
-  };
-  return make_uint4(two(y[0], y[1]), two(y[2], y[3]), two(y[4], y[5]), two(y[6], y[7]));
-}
-
-// Cosine and sine of the angle a in fp64, to about 1e-15: their fp32 roundings are those of the exact values
-// but for one in some 10^7.  a / 2 pi is formed as a sum of two doubles and the nearest quarter turn taken off it,
-// which leaves the rest exact for any position; at most an eighth of a turn is left, where the Taylor series
-// are short (the first terms left out: x^17 / 17! < 4.7e-17, x^16 / 16! < 1.01e-15).
-__device__ __forceinline__ void cos_sin(double a, double* c, double* s) {
-  constexpr double kHi = 0.15915494309189535, kLo = -9.839338337591243e-18;   // 1 / 2 pi
-  const double t = a * kHi;
-  const double rest = __fma_rn(a, kLo, __fma_rn(a, kHi, -t));
-  const double quarters = rint(4.0 * t);
-  const double x = (__fma_rn(-0.25, quarters, t) + rest) * 6.283185307179586, z = x * x;
-  double sx = __fma_rn(z, -1.0 / 1307674368000.0, 1.0 / 6227020800.0);
-  double cx = __fma_rn(z, -1.0 / 87178291200.0, 1.0 / 479001600.0);
-  sx = __fma_rn(z, sx, -1.0 / 39916800.0);
-  cx = __fma_rn(z, cx, -1.0 / 3628800.0);
-  sx = __fma_rn(z, sx, 1.0 / 362880.0);
-  cx = __fma_rn(z, cx, 1.0 / 40320.0);
-  sx = __fma_rn(z, sx, -1.0 / 5040.0);
-  cx = __fma_rn(z, cx, -1.0 / 720.0);
-  sx = __fma_rn(z, sx, 1.0 / 120.0);
-  cx = __fma_rn(z, cx, 1.0 / 24.0);
-  sx = __fma_rn(z, sx, -1.0 / 6.0);
-  cx = __fma_rn(z, cx, -0.5);
-  sx = __fma_rn(x * z, sx, x);
-  cx = __fma_rn(z, cx, 1.0);
-  const int q = (int)(long long)quarters;                // only its last two bits count
-  const double u = q & 1 ? sx : cx, v = q & 1 ? cx : sx;
-  *c = (q + 1) & 2 ? -u : u;
-  *s = q & 2 ? -v : v;
-}
-
-struct NormRotaryArgs : RotaryArgs { NormArgs norm; };
-
 // WPT: warps that share a token.  PAIRS: interleaved pairs.  NORM: norms of queries and keys before the rotation, and
 // caches in pages.  A row's norm is one factor r = 1 / sqrt(mean x^2 + eps), a sum over the lanes that hold the row, so the
 // rotation of r w x is r times that of w x: the weights go into the cosines and sines a lane keeps (one set for the
@@ -314,6 +250,7 @@ int launch_norm_rotary_write(const TokView& q, const TokView& k, const TokView& 
                              int32_t* cur_len, int per_head, int32_t* status, cudaStream_t s) {
   const NormRotaryArgs a{{q, k, v, q_out, g, tok_off, pos, freq, start, cur_len, idx, sumsq, status,
                           n_tokens, rot_dim, interleaved, per_head, scale}, norm};
+  if (!interleaved && rot_dim == g.D) return launch_norm_rotary_halves(a, K, V, dtype, s);
   return launch_rw_of(a, K, V, dtype, s);
 }
 
