@@ -38,7 +38,7 @@ template <typename T, int D, int WPT>
 __global__ void __launch_bounds__(kRotaryThreads, 2)
 norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
   constexpr int EPV = Elem<T>::kPerVec, LPR = D / EPV, RPW = 32 / LPR, HALF = LPR / 2, NP = EPV / 2;
-  constexpr int U = WPT == 1 ? 8 : 4;                    // pieces per lane in flight
+  constexpr int U = 4;                                   // pieces per lane and batch; two batches are in flight
   constexpr int TPB = kRotaryWarps / WPT, STEP = WPT * RPW;
   __shared__ float2 s_turn[kRotaryWarps][D / 2];
   const Geom& g = a.g;
@@ -65,31 +65,45 @@ norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
   const int i = (int)(il / (unsigned)g.L), l = (int)(il % (unsigned)g.L);
   const int group = (warp % WPT) * RPW, row0 = group + lane / LPR;           // this lane's first row of each kind
 
-  auto load = [&](uint4 (&x)[U], const char* from, long long stride, int r0, int n) {
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      x[u] = r0 + u * STEP < n ? ld_once(from + (r0 + u * STEP) * stride) : make_uint4(0, 0, 0, 0);
-  };
+  // Batches: U rows of q per lane, then U / 2 of k and of v (side by side).
   const char* const q_from = reinterpret_cast<const char*>(a.q.row<T>(l, i, 0)) + piece * 16;
-  const long long q_stride = a.q.sh * (long long)sizeof(T);
-  uint4 x[U];
-  load(x, q_from, q_stride, row0, g.Hq);
+  const char* const k_from = reinterpret_cast<const char*>(a.k.row<T>(l, i, 0)) + piece * 16;
+  const char* const v_from = reinterpret_cast<const char*>(a.v.row<T>(l, i, 0)) + piece * 16;
+  const long long q_stride = a.q.sh * (long long)sizeof(T), k_stride = a.k.sh * (long long)sizeof(T), v_stride = a.v.sh * (long long)sizeof(T);
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  auto load_q = [&](uint4 (&x)[U], int r0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = r0 + u * STEP < g.Hq ? ld_once(q_from + (r0 + u * STEP) * q_stride) : zero;
+  };
+  auto load_kv = [&](uint4 (&x)[U], int r0) {
+#pragma unroll
+    for (int u = 0; u < U / 2; ++u) {
+      const int h = r0 + u * STEP;
+      x[2 * u] = h < g.H ? ld_once(k_from + h * k_stride) : zero;
+      x[2 * u + 1] = h < g.H ? ld_once(v_from + h * v_stride) : zero;
+    }
+  };
+  uint4 x[U], ahead[U];
+  if (g.Hq > 0) load_q(x, row0);
+  else load_kv(x, row0);
 
+  // (in this order: the angles are worked out while the sequence's start is on its way)
   const int pos = a.pos[i];
+  const int b = sequence_of(a.tok_off, g.B, a.n_tokens, i);
+  if (b < 0) return;                                     // a token of no sequence (the whole warp)
+  const int at = i - tokens_of(a.tok_off, b, a.n_tokens).first;
+  const long long bl = (long long)b * g.L + l;
+  int cap = g.cap(bl);
+  if (pages.table && pages.room) cap = max(0, min(cap, pages.room[bl]));
+  const int start = a.per_head ? 0 : a.start[bl];
 #pragma unroll
   for (int p = lane; p < D / 2; p += 32) {
     double c, s;
     cos_sin((double)pos * a.freq[p], &c, &s);
     s_turn[warp][p] = make_float2((float)(c * a.scale), (float)(s * a.scale));
   }
-  const int b = sequence_of(a.tok_off, g.B, a.n_tokens, i);
-  if (b < 0) return;                                     // a token of no sequence (the whole warp)
-  const int at = i - tokens_of(a.tok_off, b, a.n_tokens).first;
-  const long long bl = (long long)b * g.L + l;
-  int cap = g.cap(bl);
-  const long long slot_all = a.per_head ? 0 : (long long)max(0, a.start[bl]) + at;
+  const long long slot_all = a.per_head ? 0 : (long long)max(0, start) + at;
   const int32_t* const table = pages.table ? pages.of(b, l) : nullptr;
-  if (table && pages.room) cap = max(0, min(cap, pages.room[bl]));
   const int page_all = table && !a.per_head && slot_all < cap ? table[slot_all >> pages.shift] : -1;
   __syncwarp();
 
@@ -155,7 +169,9 @@ norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
   char* const q_to = reinterpret_cast<char*>(a.q_out.row<T>(l, i, 0)) + pair * 16;
   const long long q_to_stride = a.q_out.sh * (long long)sizeof(T);
   for (int r0 = row0; r0 - row0 + group < g.Hq; r0 += U * STEP) {
-    if (r0 != row0) load(x, q_from, q_stride, r0, g.Hq);
+    const int next = r0 + U * STEP;
+    if (next - row0 + group < g.Hq) load_q(ahead, next);
+    else load_kv(ahead, row0);
 #pragma unroll
     for (int u = 0; u < U; u += 2) {
       uint4 lo, hi;
@@ -165,13 +181,12 @@ norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
       st_stream(q_to + r * q_to_stride, lo);
       st_stream(q_to + r * q_to_stride + HALF * 16, hi);
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = ahead[u];
   }
+  if (group >= g.Hq && g.Hq > 0) load_kv(x, row0);       // (a warp without a row of q)
 
-  // keys and values side by side, half a batch of each
   turn(a.norm.norm_k ? a.norm.k_weight : nullptr);
-  const char* const k_from = reinterpret_cast<const char*>(a.k.row<T>(l, i, 0)) + piece * 16;
-  const char* const v_from = reinterpret_cast<const char*>(a.v.row<T>(l, i, 0)) + piece * 16;
-  const long long k_stride = a.k.sh * (long long)sizeof(T), v_stride = a.v.sh * (long long)sizeof(T);
   const long long cache0 = table ? 0 : g.base(b, l, 0), meta0 = table ? 0 : g.meta(bl * g.H);
   const long long meta_h = g.row_off || table ? g.total_rows : (long long)g.t_cap;
   // Where head h's row goes; -1: nowhere (`tells`: the lane that says why).
@@ -191,12 +206,8 @@ norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
     return ((long long)page << pages.shift) | (slot & (pages.rows() - 1));
   };
   for (int r0 = row0; r0 - row0 + group < g.H; r0 += U / 2 * STEP) {
-#pragma unroll
-    for (int u = 0; u < U / 2; ++u) {
-      const int h = r0 + u * STEP;
-      x[2 * u] = h < g.H ? ld_once(k_from + h * k_stride) : make_uint4(0, 0, 0, 0);
-      x[2 * u + 1] = h < g.H ? ld_once(v_from + h * v_stride) : make_uint4(0, 0, 0, 0);
-    }
+    const int next = r0 + U / 2 * STEP;
+    if (next - row0 + group < g.H) load_kv(ahead, next);
 #pragma unroll
     for (int u = 0; u < U / 2; u += 2) {
       uint4 lo, hi;
@@ -232,6 +243,8 @@ norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
         if (sv >= 0) *reinterpret_cast<uint4*>(V + cache0 + hv * g.sh + sv * g.st + piece * EPV) = x[2 * (u + k) + 1];
       }
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = ahead[u];
   }
 }
 
@@ -243,10 +256,16 @@ static int launch_nr(const NormRotaryArgs& a, void* K, void* V, cudaStream_t s) 
   if (blocks * TPB > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
   return launch_chained(norm_rotary_kernel<T, D, WPT>, blocks, 1, kRotaryThreads, 0, s, a, static_cast<T*>(K), static_cast<T*>(V));
 }
-// One warp per token where that gives every SM a block of them, else a block per token, as for rotary_write_kernel.
+// As many warps to a token as leave all blocks on the SMs at once (two on each), one from there on.  (32 + 16 heads of 128, 8 / 4 / 2 /
+// 1 warps in us: 100 tokens 5.4 / 5.4 / 6.4 / 8.3, 300 9.1 / 6.6 / 7.4 / 9.9, 1000 18.4 / 11.6 / 8.1 / 10.7, 2400 39 / 24 / 17.9 /
+// 17.6, 10000 149 / 86 / 58 / 52.)
 template <typename T, int D>
 static int launch_nr_t(const NormRotaryArgs& a, void* K, void* V, cudaStream_t s) {
-  return (long long)a.n_tokens * a.g.L >= 148 * kRotaryWarps ? launch_nr<T, D, 1>(a, K, V, s) : launch_nr<T, D, kRotaryWarps>(a, K, V, s);
+  const long long rows = (long long)a.n_tokens * a.g.L, blocks = 2 * 148;
+  if (rows <= blocks) return launch_nr<T, D, 8>(a, K, V, s);
+  if (rows <= 2 * blocks) return launch_nr<T, D, 4>(a, K, V, s);
+  if (rows <= 4 * blocks) return launch_nr<T, D, 2>(a, K, V, s);
+  return launch_nr<T, D, 1>(a, K, V, s);
 }
 int launch_norm_rotary_halves(const NormRotaryArgs& a, void* K, void* V, int dtype, cudaStream_t s) {
   if (dtype == L2KV_BF16) return a.g.D == 128 ? launch_nr_t<__nv_bfloat16, 128>(a, K, V, s) : launch_nr_t<__nv_bfloat16, 64>(a, K, V, s);
