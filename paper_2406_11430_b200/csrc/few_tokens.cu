@@ -40,7 +40,7 @@ constexpr int kFtParts = 5;                     // chunks of a share: three quar
 constexpr int kFtChunks = kFtGrid * kFtParts;
 // words of the status block (they rest at zero): chunks taken, items to be joined, blocks that are done joining
 constexpr int kFtTicket = 8, kFtCut = 9, kFtDone = 10;
-constexpr int kFtWholeLen = 512;                // caches up to this length are never cut
+constexpr int kFtWholeLen = 704;                // caches up to this length are never cut
 constexpr float kFtRescaleGap = 8.f;            // log2 units a maximum may drift before sums are rescaled
 template <int D> constexpr int kFtRows = 4096 / D;               // cached rows of a block
 template <int D> constexpr int kFtGroup = D * 16;                // bytes of 8 of them: their halves of 1 KB
@@ -690,8 +690,17 @@ few_tokens_join_kernel(const __grid_constant__ FtArgs A) {
 constexpr size_t kFtPlanBytes = (kFtChunks * (sizeof(FtSpot) + sizeof(FtCut)) + 255) / 256 * 256;
 static_assert(kJoinGrid <= kFtChunks, "a block of the joining kernel reads its first entry before it knows how many there are");
 
-// One new token per sequence on average, or fewer: with more of them a tile's rows fill.
-bool few_tokens(const TokenAttention& a, int dtype) { return dtype == L2KV_BF16 && a.pages.table && a.n_tokens <= a.g.B; }
+// Where the rows of all sequences' tokens fit an item each on average, the stream of cached rows decides, and this form is
+// the faster one (48 sequences of 8k rows, 8 heads in groups of 4, this / tiles of 128 rows in us: 1 token 225 / 265, 2 tokens 226 / 277, 3 tokens,
+// which take two items, 432 / 271).  With more rows it reads caches several times over, which still pays while that
+// is little work, as it starts sooner: up to four items per sequence and 96 blocks per SM (one sequence of 3k rows: 3 tokens
+// 13.5 / 25.2, 8 tokens 17 / 25; of 30k rows: 8 tokens 68 / 49).
+bool few_tokens(const TokenAttention& a, int dtype) {
+  if (dtype != L2KV_BF16 || !a.pages.table) return false;
+  const long long rows = (long long)a.n_tokens * (a.g.Hq / a.g.H), items = (rows + kFtCols - 1) / kFtCols;
+  if (items <= a.g.B) return true;
+  return items <= 4ll * a.g.B && items * a.g.H * a.g.L * (a.max_len * (long long)a.g.D / 4096 + 1) <= 96 * kFtGrid;
+}
 
 size_t few_tokens_scratch(const Geom& g, int max_len) {
   return max_len > kFtWholeLen ? kFtPlanBytes + (size_t)2 * kFtChunks * kFtCols * (g.D + 1) * sizeof(float) : 0;
