@@ -114,6 +114,15 @@ __device__ __forceinline__ void mark_entry(const PageUpdate& a, const PageScratc
                      (uint32_t)part << kClaimBits | ((1u << kClaimBits) - 1u - (uint32_t)u), keep};
 }
 
+// The same of a compaction.
+__device__ __forceinline__ void mark_entry(const PageCompact& a, const PageScratch& w, uint32_t* mark, long long u) {
+  const int rows = cached_rows(a, u), keep = max(0, a.keep[u]);
+  const bool bad = claim_pages(mark, a.in, a.in.of((int)(u / a.L), (int)(u % a.L)), pages_of(rows, a.in), u, rows);
+  if (threadIdx.x & 31) return;
+  if (bad) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
+  w.ask[u] = PageAsk{keep < rows && !bad ? pages_of(keep, a.in) : -1, -1, 0, rows};
+}
+
 __global__ void __launch_bounds__(kPageThreads)
 page_mark_kernel(const __grid_constant__ PageUpdate a, PageScratch w) {
   next_may_start();
@@ -146,6 +155,80 @@ __device__ __forceinline__ N block_sum(N x, N* s_warp, N* total) {
   return incl + (warp ? before : 0);
 }
 
+// The free pages among [p0, p1), listed from order[p0] on, by a block of kDealThreads; how many.
+__device__ __forceinline__ int list_free(const uint32_t* mark, int32_t* order, int p0, int p1, int* s_warp) {
+  constexpr int kEach = 4;
+  int listed = 0;
+  for (int q0 = p0; q0 < p1; q0 += kEach * kDealThreads) {
+    const int p = q0 + (int)threadIdx.x * kEach;
+    // (marks and stretches begin on 16-byte boundaries, and so does what lies behind the last)
+    const uint4 m = p < p1 ? *reinterpret_cast<const uint4*>(mark + p) : make_uint4(1, 1, 1, 1);
+    const bool is_free[kEach] = {p < p1 && m.x == 0, p + 1 < p1 && m.y == 0, p + 2 < p1 && m.z == 0, p + 3 < p1 && m.w == 0};
+    const int n = is_free[0] + is_free[1] + is_free[2] + is_free[3];
+    int all;
+    int at = p0 + listed + block_sum(n, s_warp, &all) - n;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (is_free[i]) order[at++] = p + i;
+    listed += all;
+  }
+  return listed;
+}
+
+// What the (b, l) of block `block` ask for, added up, by a block of kDealThreads; the sum.
+__device__ __forceinline__ long long add_up(const PageScratch& w, const uint32_t* mark, int block, long long* s_sums) {
+  int need[kAsks];
+  long long mine = 0, all;
+  const int u0 = block * kAskBlock + (int)threadIdx.x * kAsks;
+#pragma unroll
+  for (int i = 0; i < kAsks; ++i) {
+    PageAsk q{-1, -1, 0, 0};
+    if (u0 + i < w.entries) q = w.ask[u0 + i];
+    const int copies = q.page >= 0 && mark[q.page] != q.claim;
+    need[i] = q.need < 0 ? kAsksNot : (q.need + copies) | (copies ? kCopies : 0);
+    mine += max(0, q.need) + copies;
+  }
+  long long upto = block_sum(mine, s_sums, &all) - mine;
+#pragma unroll
+  for (int i = 0; i < kAsks; ++i) {
+    if (u0 + i < w.entries) w.deal[u0 + i] = make_int2((int)min(upto, (long long)INT_MAX), need[i]);
+    upto += need[i] & (kCopies - 1) & ~kAsksNot;
+  }
+  return all;
+}
+
+__global__ void __launch_bounds__(kDealThreads)
+page_deal_kernel(PageScratch w) {
+  __shared__ long long s_sums[32];
+  __shared__ int s_warp[32];
+  next_may_start();
+  wait_for_previous();
+  const int stretch = (int)blockIdx.x - w.ask_blocks();
+  if (stretch < 0) {
+    const long long all = add_up(w, w.mark, (int)blockIdx.x, s_sums);
+    if (threadIdx.x == 0) w.asked[blockIdx.x] = all;
+    return;
+  }
+  const long long p0 = (long long)stretch << w.stretch_shift;
+  const int n = list_free(w.mark, w.order, (int)p0, (int)min((long long)w.n_pages, p0 + (1ll << w.stretch_shift)), s_warp);
+  if (threadIdx.x == 0) w.count[stretch] = n;
+}
+
+// All of the above by one block of kDealThreads, with the marks in its shared memory, for small pools; free pages.
+constexpr int kSmallPool = 40960, kSmallEntries = 64;
+__host__ __device__ inline bool is_small(const PageScratch& w) { return w.n_pages <= kSmallPool && w.entries <= kSmallEntries; }
+template <typename A>
+__device__ __forceinline__ int plan_small(const A& a, const uint8_t* pin, PageScratch w, uint32_t* mark, int* s_warp, long long* s_sums) {
+  begin_pages(mark, pin, 0, w.n_pages, threadIdx.x, kDealThreads);
+  __syncthreads();
+  for (int u = threadIdx.x >> 5; u < w.entries; u += kDealThreads / 32) mark_entry(a, w, mark, u);
+  __syncthreads();
+  const long long all = add_up(w, mark, 0, s_sums);
+  if (threadIdx.x == 0) w.asked[0] = all;
+  const int n = list_free(mark, w.order, 0, w.n_pages, s_warp);
+  return n;
+}
+
 // ---- selection: the `keep` smallest keys of a unit, ties to the lower row ----------------------------------------
 // A block per (b, l, h).  The keys come through the table once and stay in shared memory (in the scratch, where there are too
 // many).  The threshold is found by counting into 2048 equal bins between the smallest and the largest key, as integers of
@@ -164,24 +247,27 @@ struct CompactSelect {
 constexpr int kBins = 2048, kChunkWords = kGatherChunk / 32;
 template <int NT, bool SHARED>
 __global__ void __launch_bounds__(NT, 1024 / NT)
-page_mark_select_kernel(const __grid_constant__ PageCompact a, PageScratch w, CompactSelect c) {
-  extern __shared__ uint32_t s_keys[];
+page_mark_select_kernel(const __grid_constant__ PageCompact a, PageScratch w, CompactSelect c, bool small) {
+  extern __shared__ __align__(16) uint32_t s_keys[];
   __shared__ int s_bins[kBins];
   __shared__ uint32_t s_range[2];
   __shared__ int s_found[3];
   __shared__ int s_warp[32];
+  __shared__ long long s_sums[32];
   next_may_start();
   wait_for_previous();
   const long long units = (long long)w.entries * a.H;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (blockIdx.x >= units && small) {                    // claims, free pages and requests, all by one block
+    if constexpr (NT == kDealThreads && SHARED) {
+      const int n = plan_small(a, a.pin, w, s_keys, s_warp, s_sums);
+      if (tid == 0) w.count[0] = n;
+    }
+    return;
+  }
   if (blockIdx.x >= units) {                             // the claims, a warp per (b, l)
     const long long u = (blockIdx.x - units) * (NT / 32) + warp;
-    if (u >= w.entries) return;
-    const int rows = cached_rows(a, u), keep = max(0, a.keep[u]);
-    const bool bad = claim_pages(w.mark, a.in, a.in.of((int)(u / a.L), (int)(u % a.L)), pages_of(rows, a.in), u, rows);
-    if (lane) return;
-    if (bad) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
-    w.ask[u] = PageAsk{keep < rows && !bad ? pages_of(keep, a.in) : -1, -1, 0, rows};
+    if (u < w.entries) mark_entry(a, w, w.mark, u);
     return;
   }
   const long long unit = blockIdx.x, u = unit / a.H;
@@ -288,65 +374,6 @@ page_mark_select_kernel(const __grid_constant__ PageCompact a, PageScratch w, Co
   }
 }
 
-// The free pages among [p0, p1), listed from order[p0] on, by a block of kDealThreads; how many.
-__device__ __forceinline__ int list_free(const uint32_t* mark, int32_t* order, int p0, int p1, int* s_warp) {
-  constexpr int kEach = 4;
-  int listed = 0;
-  for (int q0 = p0; q0 < p1; q0 += kEach * kDealThreads) {
-    const int p = q0 + (int)threadIdx.x * kEach;
-    // (marks and stretches begin on 16-byte boundaries, and so does what lies behind the last)
-    const uint4 m = p < p1 ? *reinterpret_cast<const uint4*>(mark + p) : make_uint4(1, 1, 1, 1);
-    const bool is_free[kEach] = {p < p1 && m.x == 0, p + 1 < p1 && m.y == 0, p + 2 < p1 && m.z == 0, p + 3 < p1 && m.w == 0};
-    const int n = is_free[0] + is_free[1] + is_free[2] + is_free[3];
-    int all;
-    int at = p0 + listed + block_sum(n, s_warp, &all) - n;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      if (is_free[i]) order[at++] = p + i;
-    listed += all;
-  }
-  return listed;
-}
-
-// What the (b, l) of block `block` ask for, added up, by a block of kDealThreads; the sum.
-__device__ __forceinline__ long long add_up(const PageScratch& w, const uint32_t* mark, int block, long long* s_sums) {
-  int need[kAsks];
-  long long mine = 0, all;
-  const int u0 = block * kAskBlock + (int)threadIdx.x * kAsks;
-#pragma unroll
-  for (int i = 0; i < kAsks; ++i) {
-    PageAsk q{-1, -1, 0, 0};
-    if (u0 + i < w.entries) q = w.ask[u0 + i];
-    const int copies = q.page >= 0 && mark[q.page] != q.claim;
-    need[i] = q.need < 0 ? kAsksNot : (q.need + copies) | (copies ? kCopies : 0);
-    mine += max(0, q.need) + copies;
-  }
-  long long upto = block_sum(mine, s_sums, &all) - mine;
-#pragma unroll
-  for (int i = 0; i < kAsks; ++i) {
-    if (u0 + i < w.entries) w.deal[u0 + i] = make_int2((int)min(upto, (long long)INT_MAX), need[i]);
-    upto += need[i] & (kCopies - 1) & ~kAsksNot;
-  }
-  return all;
-}
-
-__global__ void __launch_bounds__(kDealThreads)
-page_deal_kernel(PageScratch w) {
-  __shared__ long long s_sums[32];
-  __shared__ int s_warp[32];
-  next_may_start();
-  wait_for_previous();
-  const int stretch = (int)blockIdx.x - w.ask_blocks();
-  if (stretch < 0) {
-    const long long all = add_up(w, w.mark, (int)blockIdx.x, s_sums);
-    if (threadIdx.x == 0) w.asked[blockIdx.x] = all;
-    return;
-  }
-  const long long p0 = (long long)stretch << w.stretch_shift;
-  const int n = list_free(w.mark, w.order, (int)p0, (int)min((long long)w.n_pages, p0 + (1ll << w.stretch_shift)), s_warp);
-  if (threadIdx.x == 0) w.count[stretch] = n;
-}
-
 // ---- what comes of it: read by every block of the kernels behind ----------------------------------------
 
 struct PageSums {
@@ -405,8 +432,7 @@ struct PageDeal {
   int begin, need;       // its pages are the free ones [begin, begin + need)
   bool asks, gets, copies;
 };
-__device__ __forceinline__ PageDeal deal_of(const PageScratch& w, const PageSums& s, long long u) {
-  const int2 d = w.deal[u];
+__device__ __forceinline__ PageDeal deal_of(const PageSums& s, long long u, int2 d) {
   PageDeal r;
   r.asks = d.y >= 0;
   r.need = r.asks ? d.y & (kCopies - 1) : 0;
@@ -451,9 +477,9 @@ __device__ __forceinline__ void copy_rows(T* K, T* V, int32_t* idx, float* sumsq
 }
 
 // The new table of (b, l) = u, by a warp.
-__device__ __forceinline__ void write_table(const PageUpdate& a, const PageScratch& w, const PageSums& s, const PageDeal& d, long long u) {
-  const int b = (int)(u / a.L), l = (int)(u % a.L), lane = threadIdx.x & 31, parent = parent_of(a, b);
-  const int keep = w.ask[u].rows, have = pages_of(keep, a.in), begin = have - (d.copies ? 1 : 0), more = begin + d.need;
+__device__ __forceinline__ void write_table(const PageUpdate& a, const PageScratch& w, const PageSums& s, const PageDeal& d, long long u,
+                                            int parent, int keep) {
+  const int b = (int)(u / a.L), l = (int)(u % a.L), lane = threadIdx.x & 31, have = pages_of(keep, a.in), begin = have - (d.copies ? 1 : 0), more = begin + d.need;
   const int32_t* const old = a.in.of(max(0, parent), l);
   int32_t* const to = a.out_table + b * a.out.sb + l * a.out.sl;
   for (int j0 = lane; j0 < a.out.cap; j0 += 128) {
@@ -472,11 +498,10 @@ __device__ __forceinline__ void write_table(const PageUpdate& a, const PageScrat
     if (d.asks && !d.gets) atomicExch(a.status, (int)L2KV_ERR_DEVICE_OVERFLOW);
   }
 }
-// Rows of the page that (b, l) = u gets in the place of its last one, for heads [h0, h1).
+// Rows of the page that a (b, l) gets in the place of its last one, for heads [h0, h1).
 template <typename T, int D>
-__device__ __forceinline__ void copy_page(const PageUpdate& a, const PageScratch& w, const PageSums& s, const PageDeal& d, long long u, T* K,
+__device__ __forceinline__ void copy_page(const PageUpdate& a, const PageScratch& w, const PageSums& s, const PageDeal& d, const PageAsk& q, T* K,
                                           T* V, int32_t* idx, float* sumsq, const Geom& g, int h0, int h1, int thread, int threads) {
-  const PageAsk q = w.ask[u];
   copy_rows<T, D>(K, V, idx, sumsq, g, (long long)q.page << a.in.shift, (long long)free_page(w, s, d.begin) << a.in.shift,
                   q.rows & (a.in.rows() - 1), h0, h1, thread, threads);
 }
@@ -485,7 +510,7 @@ template <int NT>
 __device__ __forceinline__ void count_left(const PageUpdate& a, const PageScratch& w, const PageSums& s, long long* s_sums) {
   long long given = 0, all;
   for (int u = threadIdx.x; u < w.entries; u += NT) {
-    const PageDeal d = deal_of(w, s, u);
+    const PageDeal d = deal_of(s, u, w.deal[u]);
     if (d.gets) given += d.need;
   }
   block_sum(given, s_sums, &all);
@@ -495,30 +520,37 @@ __device__ __forceinline__ void count_left(const PageUpdate& a, const PageScratc
 // Block 0: the pages left.  Blocks [1, 1 + table_blocks): the tables, a warp per (b, l).  The others: a block per (b, l) and
 // kCopyHeads heads copies, where that is one to copy.
 template <typename T, int D>
-__global__ void __launch_bounds__(kPageThreads)
+__global__ void __launch_bounds__(kPageThreads, 4)
 page_update_kernel(const __grid_constant__ PageUpdate a, PageScratch w, T* K, T* V, int32_t* idx, float* sumsq, Geom g, int table_blocks,
                    int copy_groups) {
   __shared__ PageSums sums;
   __shared__ long long s_sums[32];
   next_may_start();
   wait_for_previous();
+  // (everything that does not depend on the sums is asked for before them)
   const int i = (int)blockIdx.x - 1 - table_blocks;
-  if (i >= 0 && !(w.deal[i / copy_groups].y >= 0 && w.deal[i / copy_groups].y & kCopies)) return;
+  const long long u = i >= 0 ? i / copy_groups : (long long)(blockIdx.x - 1) * (kPageThreads / 32) + (threadIdx.x >> 5);
+  const bool mine = blockIdx.x > 0 && u < w.entries;
+  const int2 deal = mine ? w.deal[u] : make_int2(0, kAsksNot);
+  if (i >= 0 && !(deal.y >= 0 && deal.y & kCopies)) return;
+  const PageAsk q = mine ? w.ask[u] : PageAsk{};
+  const int parent = mine ? parent_of(a, (int)(u / a.L)) : -1;
   load_sums(w, sums);
   if (blockIdx.x == 0) {
     if (a.n_free) count_left<kPageThreads>(a, w, sums, s_sums);
-  } else if (i < 0) {
-    const long long u = (long long)(blockIdx.x - 1) * (kPageThreads / 32) + (threadIdx.x >> 5);
-    if (u < w.entries) write_table(a, w, sums, deal_of(w, sums, u), u);
-  } else {
-    const PageDeal d = deal_of(w, sums, i / copy_groups);
+    return;
+  }
+  if (!mine) return;
+  const PageDeal d = deal_of(sums, u, deal);
+  if (i < 0) {
+    write_table(a, w, sums, d, u, parent, q.rows);
+  } else if (d.copies) {
     const int h0 = i % copy_groups * kCopyHeads;
-    if (d.copies) copy_page<T, D>(a, w, sums, d, i / copy_groups, K, V, idx, sumsq, g, h0, min(g.H, h0 + kCopyHeads), threadIdx.x, kPageThreads);
+    copy_page<T, D>(a, w, sums, d, q, K, V, idx, sumsq, g, h0, min(g.H, h0 + kCopyHeads), threadIdx.x, kPageThreads);
   }
 }
 
 // All of an update by one block, with the claims in its shared memory.
-constexpr int kSmallPool = 40960, kSmallEntries = 64;
 constexpr long long kSmallCopy = 128 << 10;              // bytes that one block copies as fast as more kernels start
 template <typename T, int D>
 __global__ void __launch_bounds__(kDealThreads)
@@ -530,12 +562,7 @@ page_update_small_kernel(const __grid_constant__ PageUpdate a, PageScratch w, T*
   const int tid = threadIdx.x, warp = tid >> 5;
   next_may_start();
   wait_for_previous();
-  begin_pages(s_mark, a.pin, 0, w.n_pages, tid, kDealThreads);
-  __syncthreads();
-  for (int u = warp; u < w.entries; u += kDealThreads / 32) mark_entry(a, w, s_mark, u);
-  __syncthreads();
-  const int n = list_free(s_mark, w.order, 0, w.n_pages, s_warp);
-  add_up(w, s_mark, 0, s_sums);
+  const int n = plan_small(a, a.pin, w, s_mark, s_warp, s_sums);
   if (tid == 0) {
     sums.free_before[0] = 0;
     sums.asked_before[0] = 0;
@@ -543,9 +570,10 @@ page_update_small_kernel(const __grid_constant__ PageUpdate a, PageScratch w, T*
   }
   __syncthreads();
   for (int u = warp; u < w.entries; u += kDealThreads / 32) {
-    const PageDeal d = deal_of(w, sums, u);
-    write_table(a, w, sums, d, u);
-    if (d.copies) copy_page<T, D>(a, w, sums, d, u, K, V, idx, sumsq, g, 0, g.H, tid & 31, 32);
+    const PageDeal d = deal_of(sums, u, w.deal[u]);
+    const PageAsk q = w.ask[u];
+    write_table(a, w, sums, d, u, parent_of(a, u / a.L), q.rows);
+    if (d.copies) copy_page<T, D>(a, w, sums, d, q, K, V, idx, sumsq, g, 0, g.H, tid & 31, 32);
   }
   if (a.n_free) count_left<kDealThreads>(a, w, sums, s_sums);
 }
@@ -566,9 +594,11 @@ page_compact_kernel(const __grid_constant__ PageCompact a, PageScratch w, Compac
   const long long chunks = (long long)w.entries * a.H * c.n_chunks;
   if (blockIdx.x >= chunks * parts) {                    // the tables and lengths: a block per (b, l)
     const long long u = blockIdx.x - chunks * parts;
+    const int2 deal = w.deal[u];
+    const int had = w.ask[u].rows, keep = max(0, a.keep[u]);
     load_sums(w, sums);
-    const PageDeal d = deal_of(w, sums, u);
-    const int b = (int)(u / a.L), l = (int)(u % a.L), rows = d.gets ? max(0, a.keep[u]) : w.ask[u].rows, n = pages_of(rows, a.in);
+    const PageDeal d = deal_of(sums, u, deal);
+    const int b = (int)(u / a.L), l = (int)(u % a.L), rows = d.gets ? keep : had, n = pages_of(rows, a.in);
     const int32_t* const old = a.in.of(b, l);
     int32_t* const to = a.out_table + b * a.out.sb + l * a.out.sl;
     for (int j = threadIdx.x; j < a.out.cap; j += kPageThreads) to[j] = j >= n ? -1 : d.gets ? free_page(w, sums, d.begin + j) : old[j];
@@ -581,16 +611,22 @@ page_compact_kernel(const __grid_constant__ PageCompact a, PageScratch w, Compac
   }
   const long long unit = blockIdx.x / parts / c.n_chunks, u = unit / a.H;
   const int part = (int)(blockIdx.x % parts), chunk = (int)(blockIdx.x / parts % c.n_chunks), h = (int)(unit % a.H), tid = threadIdx.x;
-  const int len = w.ask[u].rows, t0 = chunk * kGatherChunk;
-  if (t0 >= len || w.ask[u].need <= 0) return;           // (nothing asked for, or nothing kept)
-  load_sums(w, sums);
-  const PageDeal d = deal_of(w, sums, u);
-  if (!d.gets) return;
+  // (everything that does not depend on the sums is asked for before them; of a unit that keeps nothing or all: whatever is there)
+  const PageAsk ask = w.ask[u];
+  const int2 deal = w.deal[u];
+  const int len = ask.rows, t0 = chunk * kGatherChunk, lane = tid & 31;
+  [[maybe_unused]] const int keep = a.keep[u];
   const int slot0 = c.slots[unit * c.n_chunks + chunk];
-  const int32_t* const row = a.in.of((int)(u / a.L), (int)(u % a.L));
-  // the chunk's words, one to each of a warp's first lanes; kept rows before a word
-  const int lane = tid & 31;
+  // the chunk's words, one to each of a warp's first lanes
   const uint32_t word = lane < kChunkWords ? c.kept[(unit * c.n_chunks + chunk) * kChunkWords + lane] : 0u;
+  const int32_t* const row = a.in.of((int)(u / a.L), (int)(u % a.L));
+  int page[TPT];
+#pragma unroll
+  for (int i = 0; i < TPT; ++i) page[i] = t0 + i * kPageThreads + tid < len ? row[(t0 + i * kPageThreads + tid) >> a.in.shift] : 0;
+  if (t0 >= len || ask.need <= 0) return;                // (nothing asked for, or nothing kept)
+  load_sums(w, sums);
+  const PageDeal d = deal_of(sums, u, deal);
+  if (!d.gets) return;
   int upto = __popc(word);
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
@@ -603,8 +639,8 @@ page_compact_kernel(const __grid_constant__ PageCompact a, PageScratch w, Compac
     const int r = i * kPageThreads + tid, of = r >> 5, t = t0 + r;
     const uint32_t bits = __shfl_sync(0xffffffffu, word, of);
     const int j = __shfl_sync(0xffffffffu, upto, of) - __popc(bits >> lane), slot = slot0 + j;
-    if (!(bits >> lane & 1u) || !L2KV_BOUNDS(t < len && j >= 0 && slot >= 0 && slot < a.keep[u], a.status)) continue;
-    s_from[j] = (row[t >> a.in.shift] << a.in.shift) | (t & (a.in.rows() - 1));
+    if (!(bits >> lane & 1u) || !L2KV_BOUNDS(t < len && j >= 0 && slot >= 0 && slot < keep, a.status)) continue;
+    s_from[j] = (page[i] << a.in.shift) | (t & (a.in.rows() - 1));
     s_to[j] = (free_page(w, sums, d.begin + (slot >> a.in.shift)) << a.in.shift) | (slot & (a.in.rows() - 1));
   }
   __syncthreads();
@@ -676,6 +712,11 @@ static PageScratch scratch_of(const PagePlan& p, char* base, long long entries, 
   while (w.stretches() > kMaxStretches) ++w.stretch_shift;
   return w;
 }
+// Where one block lists all of the pool.
+static PageScratch in_one_stretch(PageScratch w) {
+  while (w.stretches() > 1) ++w.stretch_shift;
+  return w;
+}
 static int launch_begin(const PageScratch& w, const uint8_t* pin, cudaStream_t s) {
   return launch_chained(page_begin_kernel, std::max(1, (int)(((long long)w.n_pages + kBeginPages - 1) / kBeginPages)), 1, kPageThreads, 0, s, w, pin);
 }
@@ -686,12 +727,12 @@ static int launch_deal(const PageScratch& w, cudaStream_t s) {
 template <typename T, int D>
 static int launch_pu(const PageUpdate& a, const PageScratch& w, void* K, void* V, int32_t* idx, float* sumsq, const Geom& g, cudaStream_t s) {
   // (what all of them together can have to copy)
-  if (w.n_pages <= kSmallPool && w.entries <= kSmallEntries && (long long)w.entries * g.H * (2 * (D * sizeof(T) + 4) << a.in.shift) <= kSmallCopy) {
+  if (is_small(w) && (long long)w.entries * g.H * (2 * (D * sizeof(T) + 4) << a.in.shift) <= kSmallCopy) {
     auto kern = page_update_small_kernel<T, D>;
     const size_t smem = ((size_t)w.n_pages * 4 + 15) / 16 * 16;
     if (smem > 32 << 10 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallPool * 4) != cudaSuccess)
       return L2KV_ERR_CUDA;
-    return launch_chained(kern, 1, 1, kDealThreads, smem, s, a, w, static_cast<T*>(K), static_cast<T*>(V), idx, sumsq, g);
+    return launch_chained(kern, 1, 1, kDealThreads, smem, s, a, in_one_stretch(w), static_cast<T*>(K), static_cast<T*>(V), idx, sumsq, g);
   }
   const long long table_blocks = (w.entries + kPageThreads / 32 - 1) / (kPageThreads / 32), groups = (g.H + kCopyHeads - 1) / kCopyHeads;
   if (1 + table_blocks + w.entries * groups > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
@@ -712,11 +753,11 @@ int launch_page_update(const PageUpdate& a, void* K, void* V, int32_t* idx, floa
 }
 
 template <int NT, bool SHARED>
-static int launch_select(const PageCompact& a, const PageScratch& w, const CompactSelect& c, long long units, cudaStream_t s) {
+static int launch_select(const PageCompact& a, const PageScratch& w, const CompactSelect& c, long long units, bool small, cudaStream_t s) {
   auto kern = page_mark_select_kernel<NT, SHARED>;
-  const size_t smem = SHARED ? (size_t)c.ld * 4 : 0;
+  const size_t smem = SHARED ? (size_t)std::max<long long>(c.ld, small ? (w.n_pages + 3) / 4 * 4 : 0) * 4 : 0;
   if (SHARED && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelectShared * 4) != cudaSuccess) return L2KV_ERR_CUDA;
-  return launch_chained(kern, units + (w.entries + NT / 32 - 1) / (NT / 32), 1, NT, smem, s, a, w, c);
+  return launch_chained(kern, units + (small ? 1 : (w.entries + NT / 32 - 1) / (NT / 32)), 1, NT, smem, s, a, w, c, small);
 }
 
 template <typename T, int D>
@@ -733,17 +774,19 @@ int launch_page_compact(const PageCompact& a, void* K, void* V, int32_t* idx, fl
   const long long entries = (long long)a.B * a.L, units = entries * a.H;
   const PagePlan p = plan_pages(entries, units, a.in.n, a.max_len);
   if (p.n_chunks > kMaxChunks || units * p.n_chunks + entries > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
-  const PageScratch w = scratch_of(p, scratch, entries, a.in.n);
+  PageScratch w = scratch_of(p, scratch, entries, a.in.n);
   const bool shared = a.max_len <= kSelectShared;
   const CompactSelect c{sumsq, shared ? nullptr : reinterpret_cast<float*>(scratch + p.key_off), reinterpret_cast<uint32_t*>(scratch + p.kept_off),
                         reinterpret_cast<int32_t*>(scratch + p.slot_off), p.ld, g.total_rows, p.n_chunks};
-  int rc = launch_begin(w, a.pin, s);
+  // A block per unit selects, with as many threads as the SMs have room for at once; beside them the claims, or, of a small
+  // call, one block that does everything about the pages.
+  const bool two = units > 148 && a.max_len <= kSelectTwo, small = shared && !two && is_small(w);
+  if (small) w = in_one_stretch(w);
+  int rc = small ? L2KV_OK : launch_begin(w, a.pin, s);
   if (rc != L2KV_OK) return rc;
-  // a block per unit: with as many threads as the SMs have room for at once
-  rc = !shared ? launch_select<1024, false>(a, w, c, units, s)
-       : units > 148 && a.max_len <= kSelectTwo ? launch_select<512, true>(a, w, c, units, s) : launch_select<1024, true>(a, w, c, units, s);
-  if (rc != L2KV_OK) return rc;
-  rc = launch_deal(w, s);
+  rc = !shared ? launch_select<1024, false>(a, w, c, units, false, s)
+       : two ? launch_select<512, true>(a, w, c, units, false, s) : launch_select<1024, true>(a, w, c, units, small, s);
+  if (rc == L2KV_OK && !small) rc = launch_deal(w, s);
   if (rc != L2KV_OK) return rc;
   if (dtype == L2KV_BF16) return g.D == 128 ? launch_pc<__nv_bfloat16, 128>(a, w, c, K, V, idx, sumsq, g, s) : launch_pc<__nv_bfloat16, 64>(a, w, c, K, V, idx, sumsq, g, s);
   return g.D == 128 ? launch_pc<float, 128>(a, w, c, K, V, idx, sumsq, g, s) : launch_pc<float, 64>(a, w, c, K, V, idx, sumsq, g, s);
