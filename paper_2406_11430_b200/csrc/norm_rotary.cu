@@ -107,38 +107,40 @@ norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
   const int page_all = table && !a.per_head && slot_all < cap ? table[slot_all >> pages.shift] : -1;
   __syncwarp();
 
-  // y_lower = lower * cl + upper * su, y_upper = upper * cu + lower * sl, weights included
-  float2 cl[NP], cu[NP], sl[NP], su[NP];
+  // Of a row the lane has the piece of its own half and, exchanged, the one of the other: y_own = own * co + other * so,
+  // y_other = other * cx + own * sx, weights included.
+  float2 co[NP], cx[NP], so[NP], sx[NP];
   auto turn = [&](const void* weight) {
-    float2 wl[NP], wu[NP];
+    float2 wo[NP], wx[NP];
     if (weight) {
-      unpack_pairs<T>(static_cast<const uint4*>(weight)[pair], wl);
-      unpack_pairs<T>(static_cast<const uint4*>(weight)[pair + HALF], wu);
+      unpack_pairs<T>(static_cast<const uint4*>(weight)[piece], wo);
+      unpack_pairs<T>(static_cast<const uint4*>(weight)[piece ^ HALF], wx);
     }
 #pragma unroll
     for (int e = 0; e < NP; ++e) {
       const float2 t0 = s_turn[warp][pair * EPV + 2 * e], t1 = s_turn[warp][pair * EPV + 2 * e + 1];
-      cl[e] = cu[e] = make_float2(t0.x, t1.x);
-      sl[e] = make_float2(t0.y, t1.y);
-      su[e] = make_float2(-t0.y, -t1.y);
+      const float2 s = lower ? make_float2(-t0.y, -t1.y) : make_float2(t0.y, t1.y);
+      co[e] = cx[e] = make_float2(t0.x, t1.x);
+      so[e] = s;
+      sx[e] = make_float2(-s.x, -s.y);
       if (weight) {
-        const float2 off = make_float2(a.norm.offset, a.norm.offset), l2 = add_pair(wl[e], off), u2 = add_pair(wu[e], off);
-        cl[e] = mul_pair(cl[e], l2);
-        su[e] = mul_pair(su[e], u2);
-        cu[e] = mul_pair(cu[e], u2);
-        sl[e] = mul_pair(sl[e], l2);
+        const float2 off = make_float2(a.norm.offset, a.norm.offset), own = add_pair(wo[e], off), other = add_pair(wx[e], off);
+        co[e] = mul_pair(co[e], own);
+        so[e] = mul_pair(so[e], other);
+        cx[e] = mul_pair(cx[e], other);
+        sx[e] = mul_pair(sx[e], own);
       }
     }
   };
-  // The two halves of one of the rows x0 (lanes of the lower half) and x1 (the others), turned; whole warps.
-  auto rotated = [&](const uint4& x0, const uint4& x1, bool norms, uint4& lo, uint4& hi) {
+  // Both halves of one of the rows x0 (lanes of the lower half) and x1 (the others), turned; whole warps.
+  auto rotated = [&](const uint4& x0, const uint4& x1, bool norms, uint4& own, uint4& other) {
     const uint4 mine = pick(lower, x0, x1), send = pick(lower, x1, x0);
     uint4 got;
     got.x = __shfl_xor_sync(0xffffffffu, send.x, HALF); got.y = __shfl_xor_sync(0xffffffffu, send.y, HALF);
     got.z = __shfl_xor_sync(0xffffffffu, send.z, HALF); got.w = __shfl_xor_sync(0xffffffffu, send.w, HALF);
     float2 f[NP], o[NP], y[NP], z[NP];
-    unpack_pairs<T>(pick(lower, mine, got), f);
-    unpack_pairs<T>(pick(lower, got, mine), o);
+    unpack_pairs<T>(mine, f);
+    unpack_pairs<T>(got, o);
     if (norms) {
       float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
@@ -146,27 +148,29 @@ norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
       float ss = sum.x + sum.y;
 #pragma unroll
       for (int off = HALF / 2; off >= 1; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-      const float r = __frcp_rn(__fsqrt_rn(ss * (1.f / D) + a.norm.eps));
+      // 1 / sqrt(m) to about a rounding: one step of Newton's method behind the approximation; sums beyond fp32 give zeros
+      const float m = ss * (1.f / D) + a.norm.eps, r0 = rsqrtf(m);
+      const float r = m == INFINITY ? 0.f : fmaf(0.5f * r0, fmaf(-m * r0, r0, 1.f), r0);
       const float2 r2 = make_float2(r, r);
 #pragma unroll
       for (int e = 0; e < NP; ++e) {
-        y[e] = mul_pair(fma_pair(o[e], su[e], mul_pair(f[e], cl[e])), r2);
-        z[e] = mul_pair(fma_pair(f[e], sl[e], mul_pair(o[e], cu[e])), r2);
+        y[e] = mul_pair(fma_pair(o[e], so[e], mul_pair(f[e], co[e])), r2);
+        z[e] = mul_pair(fma_pair(f[e], sx[e], mul_pair(o[e], cx[e])), r2);
       }
     } else {
       // two products and a sum, each rounded, as rotary_write_kernel forms them
 #pragma unroll
       for (int e = 0; e < NP; ++e) {
-        y[e] = add_pair(mul_pair(f[e], cl[e]), mul_pair(o[e], su[e]));
-        z[e] = add_pair(mul_pair(o[e], cu[e]), mul_pair(f[e], sl[e]));
+        y[e] = add_pair(mul_pair(f[e], co[e]), mul_pair(o[e], so[e]));
+        z[e] = add_pair(mul_pair(o[e], cx[e]), mul_pair(f[e], sx[e]));
       }
     }
-    lo = pack_pairs<T>(y);
-    hi = pack_pairs<T>(z);
+    own = pack_pairs<T>(y);
+    other = pack_pairs<T>(z);
   };
 
   turn(a.norm.norm_q ? a.norm.q_weight : nullptr);
-  char* const q_to = reinterpret_cast<char*>(a.q_out.row<T>(l, i, 0)) + pair * 16;
+  char* const q_to = reinterpret_cast<char*>(a.q_out.row<T>(l, i, 0));
   const long long q_to_stride = a.q_out.sh * (long long)sizeof(T);
   for (int r0 = row0; r0 - row0 + group < g.Hq; r0 += U * STEP) {
     const int next = r0 + U * STEP;
@@ -174,12 +178,12 @@ norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
     else load_kv(ahead, row0);
 #pragma unroll
     for (int u = 0; u < U; u += 2) {
-      uint4 lo, hi;
-      rotated(x[u], x[u + 1], a.norm.norm_q, lo, hi);
+      uint4 own, other;
+      rotated(x[u], x[u + 1], a.norm.norm_q, own, other);
       const int r = r0 + (lower ? u : u + 1) * STEP;
       if (r >= g.Hq) continue;
-      st_stream(q_to + r * q_to_stride, lo);
-      st_stream(q_to + r * q_to_stride + HALF * 16, hi);
+      st_stream(q_to + r * q_to_stride + piece * 16, own);
+      st_stream(q_to + r * q_to_stride + (piece ^ HALF) * 16, other);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) x[u] = ahead[u];
@@ -210,25 +214,25 @@ norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
     if (next - row0 + group < g.H) load_kv(ahead, next);
 #pragma unroll
     for (int u = 0; u < U / 2; u += 2) {
-      uint4 lo, hi;
-      rotated(x[2 * u], x[2 * u + 2], a.norm.norm_k, lo, hi);
+      uint4 own, other;
+      rotated(x[2 * u], x[2 * u + 2], a.norm.norm_k, own, other);
       // the key of the row as it is stored
-      float f[EPV], low = 0.f, high = 0.f;
-      Elem<T>::unpack(lo, f);
+      float f[EPV], p = 0.f, p_other = 0.f;
+      Elem<T>::unpack(own, f);
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) low = __fmaf_rn(f[e], f[e], low);
-      Elem<T>::unpack(hi, f);
+      for (int e = 0; e < EPV; ++e) p = __fmaf_rn(f[e], f[e], p);
+      Elem<T>::unpack(other, f);
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) high = __fmaf_rn(f[e], f[e], high);
-      float key = low + high;
+      for (int e = 0; e < EPV; ++e) p_other = __fmaf_rn(f[e], f[e], p_other);
+      float key = p + p_other;
 #pragma unroll
       for (int off = HALF / 2; off >= 1; off >>= 1) key = key + __shfl_xor_sync(0xffffffffu, key, off);
       const int h = r0 + (lower ? u : u + 1) * STEP;
       const long long slot = h < g.H ? slot_of(h, pair == 0) : -1;
       if (slot >= 0) {
-        T* const to = K + cache0 + h * g.sh + slot * g.st + pair * EPV;
-        *reinterpret_cast<uint4*>(to) = lo;
-        *reinterpret_cast<uint4*>(to + D / 2) = hi;
+        T* const to = K + cache0 + h * g.sh + slot * g.st;
+        *reinterpret_cast<uint4*>(to + piece * EPV) = own;
+        *reinterpret_cast<uint4*>(to + (piece ^ HALF) * EPV) = other;
         if (pair == 0) {
           const long long m = meta0 + h * meta_h + slot;
           if (a.idx) a.idx[m] = pos;
