@@ -633,20 +633,25 @@ static int token_attention_impl(bool tree, const l2kv_pages* pages, const l2kv_t
                                 static_cast<cudaStream_t>(stream));
 }
 
-int l2kv_prompt_attention_workspace_bytes(const l2kv_layout* lay, int32_t n_tokens, int32_t max_len,
-                                          size_t* bytes) {
+static int attention_workspace(const l2kv_layout* lay, const l2kv_pages* pages, int32_t n_tokens, int32_t max_len, size_t* bytes) {
   if (!bytes) return L2KV_ERR_INVALID_ARG;
   int rc = check_layout(lay);
   if (rc != L2KV_OK) return rc;
   rc = check_groups(lay);
   if (rc != L2KV_OK) return rc;
+  if (pages && (rc = check_pages(lay, pages, lay->batch, false)) != L2KV_OK) return rc;
   if (n_tokens < 0 || max_len < 0) return L2KV_ERR_INVALID_ARG;
   if (max_len > lay->t_cap) return L2KV_ERR_OUT_OF_RANGE;
   *bytes = (size_t)kStatusBytes;
   if (empty(lay) || n_tokens == 0) return L2KV_OK;
-  const size_t scratch = token_attention_scratch(make_geom(*lay), lay->dtype, n_tokens, max_len);
+  const size_t scratch = token_attention_scratch(make_geom(*lay), lay->dtype, n_tokens, max_len, pages != nullptr);
   if (scratch) *bytes = plan_workspace(*lay, 0).sumsq_off + scratch;
   return L2KV_OK;
+}
+
+int l2kv_prompt_attention_workspace_bytes(const l2kv_layout* lay, int32_t n_tokens, int32_t max_len,
+                                          size_t* bytes) {
+  return attention_workspace(lay, nullptr, n_tokens, max_len, bytes);
 }
 
 int l2kv_prompt_attention(const l2kv_tokens* q, const int32_t* tok_off_dev, int32_t n_tokens,
@@ -671,8 +676,7 @@ int l2kv_tree_attention(const l2kv_tokens* q, const int32_t* tok_off_dev, int32_
 
 int l2kv_paged_attention_workspace_bytes(const l2kv_layout* lay, const l2kv_pages* pages, int32_t n_tokens, int32_t max_len,
                                          size_t* bytes) {
-  const int rc = l2kv_prompt_attention_workspace_bytes(lay, n_tokens, max_len, bytes);
-  return rc != L2KV_OK ? rc : check_pages(lay, pages, lay->batch, false);
+  return pages ? attention_workspace(lay, pages, n_tokens, max_len, bytes) : L2KV_ERR_INVALID_ARG;
 }
 
 int l2kv_paged_attention(const l2kv_tokens* q, const int32_t* tok_off_dev, int32_t n_tokens, const void* K_c,

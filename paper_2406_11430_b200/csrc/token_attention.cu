@@ -1030,8 +1030,8 @@ static TaRoom ta_room(const Geom& g, int n_tokens, int max_len) {
   return r;
 }
 
-size_t token_attention_scratch(const Geom& g, int dtype, int n_tokens, int max_len) {
-  return dtype == L2KV_BF16 ? std::max(ta_room(g, n_tokens, max_len).bytes, few_tokens_scratch(g, max_len)) : 0;
+size_t token_attention_scratch(const Geom& g, int dtype, int n_tokens, int max_len, bool pages) {
+  return dtype == L2KV_BF16 ? std::max(ta_room(g, n_tokens, max_len).bytes, pages ? few_tokens_scratch(g, max_len) : 0) : 0;
 }
 
 template <int D, bool TREE, bool PAGED = false>

@@ -119,7 +119,7 @@ struct TokenAttention {
   int32_t* status;                                       // may be null
   PageView pages;                                        // table == nullptr: the cache has rows of its own
 };
-size_t token_attention_scratch(const Geom& g, int dtype, int n_tokens, int max_len);
+size_t token_attention_scratch(const Geom& g, int dtype, int n_tokens, int max_len, bool pages);
 int launch_token_attention(const TokenAttention& a, const void* K, const void* V, int dtype, char* scratch,
                            size_t scratch_bytes, cudaStream_t s);
 // The form for few tokens per sequence of a bf16 cache in pages, where that is the faster one.
