@@ -155,8 +155,8 @@ __device__ __forceinline__ N block_sum(N x, N* s_warp, N* total) {
   return incl + (warp ? before : 0);
 }
 
-// The free pages among [p0, p1), listed from order[p0] on, by a block of kDealThreads; how many.
-__device__ __forceinline__ int list_free(const uint32_t* mark, int32_t* order, int p0, int p1, int* s_warp) {
+// The free pages among [p0, p1), listed from order[p0] on, the first `limit` of them, by a block of kDealThreads; how many there are.
+__device__ __forceinline__ int list_free(const uint32_t* mark, int32_t* order, int p0, int p1, int* s_warp, int limit = INT_MAX) {
   constexpr int kEach = 4;
   int listed = 0;
   for (int q0 = p0; q0 < p1; q0 += kEach * kDealThreads) {
@@ -169,7 +169,10 @@ __device__ __forceinline__ int list_free(const uint32_t* mark, int32_t* order, i
     int at = p0 + listed + block_sum(n, s_warp, &all) - n;
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
-      if (is_free[i]) order[at++] = p + i;
+      if (is_free[i]) {
+        if (at - p0 < limit) order[at] = p + i;
+        ++at;
+      }
     listed += all;
   }
   return listed;
@@ -214,19 +217,15 @@ page_deal_kernel(PageScratch w) {
   if (threadIdx.x == 0) w.count[stretch] = n;
 }
 
-// All of the above by one block of kDealThreads, with the marks in its shared memory, for small pools; free pages.
-constexpr int kSmallPool = 40960, kSmallEntries = 64;
+// The claims by one block of kDealThreads, with the marks in its shared memory, for small pools.
+constexpr int kSmallPool = 32768, kSmallEntries = 64;
 __host__ __device__ inline bool is_small(const PageScratch& w) { return w.n_pages <= kSmallPool && w.entries <= kSmallEntries; }
 template <typename A>
-__device__ __forceinline__ int plan_small(const A& a, const uint8_t* pin, PageScratch w, uint32_t* mark, int* s_warp, long long* s_sums) {
+__device__ __forceinline__ void mark_small(const A& a, const uint8_t* pin, const PageScratch& w, uint32_t* mark) {
   begin_pages(mark, pin, 0, w.n_pages, threadIdx.x, kDealThreads);
   __syncthreads();
   for (int u = threadIdx.x >> 5; u < w.entries; u += kDealThreads / 32) mark_entry(a, w, mark, u);
   __syncthreads();
-  const long long all = add_up(w, mark, 0, s_sums);
-  if (threadIdx.x == 0) w.asked[0] = all;
-  const int n = list_free(mark, w.order, 0, w.n_pages, s_warp);
-  return n;
 }
 
 // ---- selection: the `keep` smallest keys of a unit, ties to the lower row ----------------------------------------
@@ -260,8 +259,10 @@ page_mark_select_kernel(const __grid_constant__ PageCompact a, PageScratch w, Co
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (blockIdx.x >= units && small) {                    // claims, free pages and requests, all by one block
     if constexpr (NT == kDealThreads && SHARED) {
-      const int n = plan_small(a, a.pin, w, s_keys, s_warp, s_sums);
-      if (tid == 0) w.count[0] = n;
+      mark_small(a, a.pin, w, s_keys);
+      const long long all = add_up(w, s_keys, 0, s_sums);
+      const int n = list_free(s_keys, w.order, 0, w.n_pages, s_warp);
+      if (tid == 0) { w.asked[0] = all; w.count[0] = n; }
     }
     return;
   }
@@ -551,6 +552,7 @@ page_update_kernel(const __grid_constant__ PageUpdate a, PageScratch w, T* K, T*
 }
 
 // All of an update by one block, with the claims in its shared memory.
+constexpr int kSmallDealt = 1024;
 constexpr long long kSmallCopy = 128 << 10;              // bytes that one block copies as fast as more kernels start
 template <typename T, int D>
 __global__ void __launch_bounds__(kDealThreads)
@@ -562,7 +564,16 @@ page_update_small_kernel(const __grid_constant__ PageUpdate a, PageScratch w, T*
   const int tid = threadIdx.x, warp = tid >> 5;
   next_may_start();
   wait_for_previous();
-  const int n = plan_small(a, a.pin, w, s_mark, s_warp, s_sums);
+  // (what everyone asks for and gets, and the pages dealt out, stay in shared memory: each would be a trip to L2 and back)
+  __shared__ PageAsk s_ask[kSmallEntries];
+  __shared__ int2 s_deal[kSmallEntries];
+  __shared__ int32_t s_order[kSmallDealt];
+  w.ask = s_ask;
+  w.deal = s_deal;
+  mark_small(a, a.pin, w, s_mark);
+  const long long all = add_up(w, s_mark, 0, s_sums);
+  if (all <= kSmallDealt) w.order = s_order;
+  const int n = list_free(s_mark, w.order, 0, w.n_pages, s_warp, (int)min(all, (long long)INT_MAX));
   if (tid == 0) {
     sums.free_before[0] = 0;
     sums.asked_before[0] = 0;
