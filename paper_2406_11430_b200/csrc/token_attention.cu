@@ -132,6 +132,14 @@ __device__ __forceinline__ long long ta_cost(const TokenAttention& a, const TaEn
   return sum;
 }
 
+// The unit of cost.  Over pages it is an eighth of a sub-block of a pair: one of a single tile, which its two chains take by turns,
+// costs five of them (chunks of 1 to 256 tokens: CTAs of pairs ended 170 to 193 us after the start, those of single tiles at
+// 115).  The calls over rows count both alike; their shares, and with them the bits of their results, stay.
+template <bool PAGED> constexpr int kTaUnit = PAGED ? 8 : 1;
+template <bool PAGED> __device__ __forceinline__ int ta_weight(const TaArgs& A, int n, int p) {      // of a sub-block of tile pair p
+  return PAGED && n - p * 2 * A.QT <= A.QT ? 5 : kTaUnit<PAGED>;
+}
+
 // A place in the list of all items, (b, l) by (b, l), within it tile pair by tile pair, within that head by
 // head: an item, the cost of everything before it, and a number of its sub-blocks.
 struct TaSpot {
@@ -142,7 +150,9 @@ struct TaSpot {
 // The shares of the CTAs: stretches of the list that cost the same.  Where a share ends inside an item the item
 // is cut, unless there is no room for partial results or cutting would not pay: then the share ends with the
 // item.  One warp; the first 32 entries stay in registers.
+template <bool PAGED>
 struct TaShares {
+  static constexpr int U = kTaUnit<PAGED>;
   const TaArgs& A;
   TaEntry mine;                // entry number `lane`
   int entries, QP;
@@ -154,7 +164,11 @@ struct TaShares {
     return e < entries ? ta_plan_entry(A.a, e) : TaEntry{0, 0, 0};
   }
   // Cost of the first m items of an entry and one head.
-  __device__ __forceinline__ long long cost(const TaEntry& e, int m) const { return one_each ? m : ta_cost(A.a, e, QP, m); }
+  __device__ __forceinline__ long long cost(const TaEntry& e, int m) const {
+    if (one_each) return m;
+    const int pairs = (e.n + QP - 1) / QP;
+    return U * ta_cost(A.a, e, QP, m) - (m >= pairs ? (U - ta_weight<PAGED>(A, e.n, pairs - 1)) * ta_subs(e.cur) : 0);
+  }
   __device__ __forceinline__ long long cost_of(const TaEntry& e) const {
     return e.n > 0 ? cost(e, (e.n + QP - 1) / QP) * A.a.g.H : 0;
   }
@@ -170,7 +184,7 @@ struct TaShares {
       const TaEntry e = entry(e0);
       sum += cost_of(e);
       items += (e.n + QP - 1) / QP;
-      if (e.n > 0) longest = max(longest, ta_subs(e.cur) + kTaItemCost);
+      if (e.n > 0) longest = max(longest, U * (ta_subs(e.cur) + kTaItemCost));
     }
 #pragma unroll
     for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
@@ -188,9 +202,9 @@ struct TaShares {
       // 147 / 136.)  With more items shares end up to half an item late, or, at equal lengths, after a number of
       // items.  (24 trees behind 1.1k 40 / 36, 16k 319 / 258; a prompt of 2k tokens 65 / 52; 32 pieces of 128 tokens
       // behind 2k 159 / 160.)
-      const long long memory = fair * 27 / 20, least = max((long long)kTaMinShare, fair);
-      cut = items <= grid ? max((long long)longest, memory) > max(least, memory) + kTaJoinCost
-                          : max(longest / 2ll, (items + grid - 1) / grid * (sum / items) - fair) > kTaJoinCost * 3 / 4;
+      const long long memory = fair * 27 / 20, least = max((long long)kTaMinShare * U, fair);
+      cut = items <= grid ? max((long long)longest, memory) > max(least, memory) + kTaJoinCost * U
+                          : max(longest / 2ll, (items + grid - 1) / grid * (sum / items) - fair) > kTaJoinCost * U * 3 / 4;
       if (cut) share = least;
     }
     if (!cut && items <= grid) { one_each = true; share = 1; }
@@ -235,10 +249,11 @@ struct TaShares {
         }
         const long long first = cost(z, lo);
         const int each = (int)(cost(z, lo + 1) - first), inside = (int)(rest - first * H);
-        const int n = each - kTaItemCost, near = cut ? 4 + (int)min(share / 64, 64ll) : (n + 1) / 2 + 1;
+        const int w = ta_weight<PAGED>(A, z.n, lo), n = (each - kTaItemCost * U) / w;
+        const int near = cut ? 4 + (int)min(share / (64 * U), 64ll) : (n + 1) / 2 + 1;
         TaSpot s{start + first * H + (long long)(inside / each) * each, e0 + who, lo, inside / each, 0};
         if (one_each) return s;
-        s.off = max(0, inside % each - kTaItemCost);
+        s.off = max(0, inside % each - kTaItemCost * U) / w;
         if (s.off < near) s.off = 0;
         else if (n - s.off < near) next(s, each, z.n);
         return s;
@@ -428,7 +443,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
     TaSpot end;
     one_each = ta_small_call(A, spot, end);
     if (!one_each) {
-      const TaShares shares(A);
+      const TaShares<PAGED> shares(A);
       spot = end = shares.begin((int)blockIdx.x + (warp == 10));
       one_each = shares.one_each;
     }
@@ -566,7 +581,7 @@ token_attention_kernel(const __grid_constant__ TaArgs A, const __grid_constant__
         // a piece that does not begin its item goes to this CTA's first slot, one that does to its second
         const int slot = spot.off > 0 ? 2 * (int)blockIdx.x : to < n ? 2 * (int)blockIdx.x + 1 : -1;
         it = ta_item(A, spot.e / L, spot.e % L, spot.p, spot.h, spot.off, to, slot);
-        spot.at += one_each ? 1 : n + kTaItemCost;
+        spot.at += one_each ? 1 : n * ta_weight<PAGED>(A, e.n, spot.p) + kTaItemCost * kTaUnit<PAGED>;
         spot.off = 0;
         if (++spot.h == a.g.H) { spot.h = 0; ++spot.p; }
         if (spot.p * QP >= e.n) {
