@@ -66,26 +66,27 @@ norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
   const int group = (warp % WPT) * RPW, row0 = group + lane / LPR;           // this lane's first row of each kind
 
   // Batches: U rows of q per lane, then U / 2 of k and of v (side by side).
-  const char* const q_from = reinterpret_cast<const char*>(a.q.row<T>(l, i, 0)) + piece * 16;
-  const char* const k_from = reinterpret_cast<const char*>(a.k.row<T>(l, i, 0)) + piece * 16;
-  const char* const v_from = reinterpret_cast<const char*>(a.v.row<T>(l, i, 0)) + piece * 16;
-  const long long q_stride = a.q.sh * (long long)sizeof(T), k_stride = a.k.sh * (long long)sizeof(T), v_stride = a.v.sh * (long long)sizeof(T);
+  const char* q_from = reinterpret_cast<const char*>(a.q.row<T>(l, i, row0)) + piece * 16;
+  const char* k_from = reinterpret_cast<const char*>(a.k.row<T>(l, i, row0)) + piece * 16;
+  const char* v_from = reinterpret_cast<const char*>(a.v.row<T>(l, i, row0)) + piece * 16;
+  const long long q_step = a.q.sh * (long long)sizeof(T) * STEP, k_step = a.k.sh * (long long)sizeof(T) * STEP,
+                  v_step = a.v.sh * (long long)sizeof(T) * STEP;
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  auto load_q = [&](uint4 (&x)[U], int r0) {
+  // (`from`: the lane's row number r0)
+  auto load_q = [&](uint4 (&x)[U], const char* from, int r0) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = r0 + u * STEP < g.Hq ? ld_once(q_from + (r0 + u * STEP) * q_stride) : zero;
+    for (int u = 0; u < U; ++u, from += q_step) x[u] = r0 + u * STEP < g.Hq ? ld_once(from) : zero;
   };
-  auto load_kv = [&](uint4 (&x)[U], int r0) {
+  auto load_kv = [&](uint4 (&x)[U], const char* k, const char* v, int r0) {
 #pragma unroll
-    for (int u = 0; u < U / 2; ++u) {
-      const int h = r0 + u * STEP;
-      x[2 * u] = h < g.H ? ld_once(k_from + h * k_stride) : zero;
-      x[2 * u + 1] = h < g.H ? ld_once(v_from + h * v_stride) : zero;
+    for (int u = 0; u < U / 2; ++u, k += k_step, v += v_step) {
+      x[2 * u] = r0 + u * STEP < g.H ? ld_once(k) : zero;
+      x[2 * u + 1] = r0 + u * STEP < g.H ? ld_once(v) : zero;
     }
   };
   uint4 x[U], ahead[U];
-  if (g.Hq > 0) load_q(x, row0);
-  else load_kv(x, row0);
+  if (g.Hq > 0) load_q(x, q_from, row0);
+  else load_kv(x, k_from, v_from, row0);
 
   // (in this order: the angles are worked out while the sequence's start is on its way)
   const int pos = a.pos[i];
@@ -170,25 +171,26 @@ norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
   };
 
   turn(a.norm.norm_q ? a.norm.q_weight : nullptr);
-  char* const q_to = reinterpret_cast<char*>(a.q_out.row<T>(l, i, 0));
-  const long long q_to_stride = a.q_out.sh * (long long)sizeof(T);
+  // the lane's first row of the first two, and from each pair of rows to the next
+  char* q_to = reinterpret_cast<char*>(a.q_out.row<T>(l, i, row0 + (lower ? 0 : STEP)));
+  const long long q_to_step = a.q_out.sh * (long long)sizeof(T) * (2 * STEP);
   for (int r0 = row0; r0 - row0 + group < g.Hq; r0 += U * STEP) {
     const int next = r0 + U * STEP;
-    if (next - row0 + group < g.Hq) load_q(ahead, next);
-    else load_kv(ahead, row0);
+    q_from += U * q_step;
+    if (next - row0 + group < g.Hq) load_q(ahead, q_from, next);
+    else load_kv(ahead, k_from, v_from, row0);
 #pragma unroll
-    for (int u = 0; u < U; u += 2) {
+    for (int u = 0; u < U; u += 2, q_to += q_to_step) {
       uint4 own, other;
       rotated(x[u], x[u + 1], a.norm.norm_q, own, other);
-      const int r = r0 + (lower ? u : u + 1) * STEP;
-      if (r >= g.Hq) continue;
-      st_stream(q_to + r * q_to_stride + piece * 16, own);
-      st_stream(q_to + r * q_to_stride + (piece ^ HALF) * 16, other);
+      if (r0 + (lower ? u : u + 1) * STEP >= g.Hq) continue;
+      st_stream(q_to + piece * 16, own);
+      st_stream(q_to + (piece ^ HALF) * 16, other);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) x[u] = ahead[u];
   }
-  if (group >= g.Hq && g.Hq > 0) load_kv(x, row0);       // (a warp without a row of q)
+  if (group >= g.Hq && g.Hq > 0) load_kv(x, k_from, v_from, row0);       // (a warp without a row of q)
 
   turn(a.norm.norm_k ? a.norm.k_weight : nullptr);
   const long long cache0 = table ? 0 : g.base(b, l, 0), meta0 = table ? 0 : g.meta(bl * g.H);
@@ -211,7 +213,9 @@ norm_rotary_kernel(const __grid_constant__ NormRotaryArgs a, T* K, T* V) {
   };
   for (int r0 = row0; r0 - row0 + group < g.H; r0 += U / 2 * STEP) {
     const int next = r0 + U / 2 * STEP;
-    if (next - row0 + group < g.H) load_kv(ahead, next);
+    k_from += U / 2 * k_step;
+    v_from += U / 2 * v_step;
+    if (next - row0 + group < g.H) load_kv(ahead, k_from, v_from, next);
 #pragma unroll
     for (int u = 0; u < U / 2; u += 2) {
       uint4 own, other;
