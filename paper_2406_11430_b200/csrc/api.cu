@@ -538,8 +538,10 @@ static int rotary_write_impl(uint32_t known_flags, const NormArgs* norm, const l
     return launch_rotary_write(make_view(q), make_view(k), make_view(v), make_view(q_out), tok_off_dev, n_tokens, pos_dev,
                                freq_dev, rot_dim, rot_scale, interleaved, K_c, V_c, idx, sumsq_c, make_geom(*lay), lay->dtype,
                                start_dev, cur_len_dev, per_head, status, s);
+  NormArgs with_pages = *norm;
+  if (pages) with_pages.pages = make_pages(*pages);
   return launch_norm_rotary_write(make_view(q), make_view(k), make_view(v), make_view(q_out), tok_off_dev, n_tokens, pos_dev,
-                                  freq_dev, rot_dim, rot_scale, interleaved, *norm, K_c, V_c, idx, sumsq_c, make_geom(*lay),
+                                  freq_dev, rot_dim, rot_scale, interleaved, with_pages, K_c, V_c, idx, sumsq_c, make_geom(*lay),
                                   lay->dtype, start_dev, cur_len_dev, per_head, status, s);
 }
 
@@ -563,7 +565,6 @@ int l2kv_norm_rotary_write(const l2kv_tokens* q, const l2kv_tokens* k, const l2k
                            size_t workspace_bytes, void* stream) {
   const Range nvtx_range("l2kv_norm_rotary_write");
   NormArgs norm{};
-  if (pages) norm.pages = make_pages(*pages);
   norm.q_weight = q_weight;
   norm.k_weight = k_weight;
   norm.norm_q = (flags & L2KV_TOKENS_NORM_Q) != 0;

@@ -57,7 +57,7 @@ struct PageScratch {
   __host__ __device__ int stretches() const { return (int)(((long long)n_pages + (1ll << stretch_shift) - 1) >> stretch_shift); }
   __host__ __device__ int ask_blocks() const { return (entries + kAskBlock - 1) / kAskBlock; }
 };
-constexpr int kCopies = 1 << 30, kAsksNot = 1 << 31;     // flags beside the pages of a (b, l), which are fewer than 2^28
+constexpr int kCopies = 1 << 30, kAsksNot = INT_MIN;     // flags beside the pages of a (b, l), which are fewer than 2^28
 
 // Marks [p0, p1), by threads `thread` of `threads`, eight pins to a thread at a time.
 __device__ __forceinline__ void begin_pages(uint32_t* mark, const uint8_t* pin, int p0, int p1, int thread, int threads) {

@@ -20,6 +20,7 @@ struct PageView {
   __device__ __forceinline__ bool valid(int page) const { return page >= 0 && page < n; }
 };
 
+// (of tables that have been checked)
 inline PageView make_pages(const l2kv_pages& p) {
   int shift = 0;
   while ((1 << shift) < p.page_rows) ++shift;

@@ -121,6 +121,70 @@ def test_a_call_without_pages():
             l2.page_workspace_bytes(a["K"], pages)
 
 
+@pytest.mark.parametrize("page_rows", [0, -16, 24, 2048, 2 ** 30 + 1, 2 ** 31 - 1])
+def test_page_sizes_that_are_none(page_rows):
+    """Of an empty pool, so that nothing else is wrong with them."""
+    a = _inputs()
+    a.update(page_rows=page_rows, page_rows_out=page_rows, n_pages=0, table=I32(B, L, 0), table_out=I32(B, L, 0), idx=None, max_len=0)
+    for k in ("K", "V"):
+        a[k] = a[k][:, :0]
+    for call in CALLS:
+        a["key"] = torch.zeros((H, 0)) if call is _compact else None
+        with pytest.raises(l2.L2KVError) as e:
+            call(a)
+        assert e.value.status == -2
+
+
+def test_tables_live_as_long_as_the_call(tmp_path):
+    """Another thread runs while the library is at work, and takes the tables away from the objects that held them."""
+    import ctypes
+    import subprocess
+    import threading
+    import time
+    import weakref
+    from paper_2406_11430_b200 import binding
+    (tmp_path / "s.c").write_text("#include <unistd.h>\nvolatile int entered, go;\nint stand_in(void) { entered = 1; "
+                                  "for (int i = 0; i < 2000 && !go; ++i) usleep(1000); return go ? 0 : -1; }")
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-o", str(tmp_path / "s.so"), str(tmp_path / "s.c")], check=True)
+    lib = ctypes.CDLL(str(tmp_path / "s.so"))
+    entered, go = (ctypes.c_int.in_dll(lib, name) for name in ("entered", "go"))
+    names = ("l2kv_norm_rotary_write", "l2kv_paged_attention", "l2kv_paged_attention_workspace_bytes", "l2kv_page_update", "l2kv_page_compact",
+             "l2kv_page_workspace_bytes")
+    real = [ctypes.cast(getattr(l2.lib(), name), ctypes.c_void_p).value for name in names]
+    at, native = ctypes.cast(lib.stand_in, ctypes.c_void_p).value, binding._token_calls()
+    native.bind_pages(at, at, real[2], at, at, real[5])
+    try:
+        for call in CALLS:
+            entered.value = go.value = 0
+            a, alive = _inputs(), []
+            pages, out = l2.Pages(I32(B, L, CAP), P, PAGES, I32(B, L)), l2.Pages(I32(B, L, CAP), P, PAGES, I32(B, L))
+            held = [pages] + ([out] if call in (_update, _compact) else [])
+            refs = [weakref.ref(x) for p in held for x in (p.table, p.room)]
+
+            def take_away():
+                while not entered.value:
+                    time.sleep(1e-3)
+                for p in held:
+                    p.table = p.room = None
+                alive.extend(r() is not None for r in refs)
+                go.value = 1
+            thread = threading.Thread(target=take_away)
+            thread.start()
+            if call is _write:
+                l2.norm_rotary_write(a["q"], a["k"], a["v"], a["off"], a["pos"], a["freq"], a["out"], a["K"], a["V"], a["idx"], a["key"], a["start"],
+                                     a["cur"], a["ws"], pages=pages)
+            elif call is _attend:
+                l2.paged_attention(a["q"], a["off"], a["K"], a["V"], a["cur"], a["max_len"], a["out"], pages)
+            elif call is _update:
+                l2.page_update(a["K"], a["V"], None, None, pages, a["parent"], a["keep"], a["grow"], out, a["ws"])
+            else:
+                l2.page_compact(a["K"], a["V"], None, a["key"], pages, a["cur"], a["keep"], a["max_len"], out, a["len_out"], a["ws"])
+            thread.join()
+            assert alive == [True] * len(refs) and [r() for r in refs] == [None] * len(refs)
+    finally:
+        native.bind_pages(*real)
+
+
 def test_nothing_to_do():
     """No sequences, or no tokens: no error and no launch."""
     a = _inputs()
