@@ -380,6 +380,7 @@ page_mark_select_kernel(const __grid_constant__ PageCompact a, PageScratch w, Co
 struct PageSums {
   int free_before[kMaxStretches];                        // free pages in the stretches before
   long long asked_before[kMaxAskBlocks];
+  long long n_asked;
   int n_free;
 };
 // By a whole block of two warps or more.
@@ -415,7 +416,10 @@ __device__ __forceinline__ void load_sums(const PageScratch& w, PageSums& s) {
       }
       before += __shfl_sync(0xffffffffu, incl, 31);
     }
-    if (warp == 0 && lane == 0) s.n_free = (int)before;
+    if (lane == 0) {
+      if (warp == 0) s.n_free = (int)before;
+      else s.n_asked = before;
+    }
   }
   __syncthreads();
 }
@@ -506,9 +510,13 @@ __device__ __forceinline__ void copy_page(const PageUpdate& a, const PageScratch
   copy_rows<T, D>(K, V, idx, sumsq, g, (long long)q.page << a.in.shift, (long long)free_page(w, s, d.begin) << a.in.shift,
                   q.rows & (a.in.rows() - 1), h0, h1, thread, threads);
 }
-// Pages that are left, by a block of NT.
+// Pages that are left, by a block of NT: where there are enough for everyone, the sums say it; else what each one got.
 template <int NT>
 __device__ __forceinline__ void count_left(const PageUpdate& a, const PageScratch& w, const PageSums& s, long long* s_sums) {
+  if (s.n_asked <= s.n_free) {
+    if (threadIdx.x == 0) *a.n_free = s.n_free - (int)s.n_asked;
+    return;
+  }
   long long given = 0, all;
   for (int u = threadIdx.x; u < w.entries; u += NT) {
     const PageDeal d = deal_of(s, u, w.deal[u]);
@@ -578,6 +586,7 @@ page_update_small_kernel(const __grid_constant__ PageUpdate a, PageScratch w, T*
     sums.free_before[0] = 0;
     sums.asked_before[0] = 0;
     sums.n_free = n;
+    sums.n_asked = all;
   }
   __syncthreads();
   for (int u = warp; u < w.entries; u += kDealThreads / 32) {
