@@ -1,0 +1,327 @@
+// Attention over fp32 caches in pages, on the CUDA cores, fp32 throughout: there is no exact tensor-core form.
+//
+// An item is up to eight query rows, the (token, head-of-the-group) pairs of 8 / G tokens of one sequence that share a KV head,
+// and a block of 128 threads takes 64 cached rows of it at a time.  A thread asks for its pieces of K and V of a step all at
+// once (a table entry and then its row are two trips to memory); K goes through shared memory, because a score's thread wants a whole
+// row of it, V stays in the registers of the thread that multiplies it:
+//   S[row, query] = K Q^T   a row and four queries to a thread,    m, p = 2^(s - m) against a running maximum,
+//   O[query, dim] += P V    four dimensions of every 4th (64-wide heads: 8th) row to a thread, joined when the item ends.
+// Where there are few items their rows are cut into parts, as many as the SMs hold blocks, whose weighted values and
+// (maximum, sum) a second kernel joins; a logarithm there would cost bits.  Rows that a token does not see are neither counted
+// nor multiplied, whatever they hold.
+//
+// 8 heads of 128 in groups of 4, against the same rows by tiles of 32 query rows (token_attention_fp32.cu), which walk the cache in one
+// block each and whose table entries and rows came one after the other: one token behind 100 rows 11.4 us (45), 1000 rows 15.8
+// (338), 16 k rows 58.7 (6764; 131 MB, 20 at the copy rate), 16 tokens behind 2 k rows 129 (861), 300 tokens behind 500 rows 231
+// (329), 2 prompts of 600 427 (436).  Few rows are a chain of trips to memory and of barriers; many are bound by shared-memory
+// reads, five of 16 bytes per 16 FMAs in the scores.
+#include <algorithm>
+#include <climits>
+#include <type_traits>
+
+#include "tokens.cuh"
+
+namespace l2kv {
+
+constexpr int kFfRows = 8, kFfCols = 64, kFfThreads = 128;
+constexpr int kFfResident = 3 * 148;                     // blocks that the SMs hold at once
+template <int D> constexpr int kFfPitch = D + 4;         // floats between rows of K in shared memory (no bank twice in eight lanes)
+
+struct FfArgs {
+  TokenAttention a;
+  int G, TG;                                             // query heads per KV head, tokens per item
+  float* part;                                           // [item][part][kFfRows][D] weighted values
+  float2* stat;                                          // [item][part][kFfRows] maximum, sum of weights
+  int parts;
+};
+struct FfItem {
+  int l, h, tok0, rows;                                  // first token in the list, query rows; none: rows is 0
+  int first, end;                                        // rows its first token sees; rows that some token sees
+  int b, cur;
+};
+// Item `unit` of the call: heads inside layers inside items, 32 sequences at a time.
+__device__ __forceinline__ FfItem ff_item(const FfArgs& A, unsigned unit) {
+  const TokenAttention& a = A.a;
+  const int lane = threadIdx.x & 31;
+  FfItem it{};
+  it.h = (int)(unit % (unsigned)a.g.H);
+  it.l = (int)(unit / (unsigned)a.g.H % (unsigned)a.g.L);
+  int tile = (int)(unit / (unsigned)a.g.H / (unsigned)a.g.L);
+  for (int b0 = 0; b0 < a.g.B; b0 += 32) {
+    const int mine = b0 + lane < a.g.B ? (tokens_of(a.tok_off, b0 + lane, a.n_tokens).n + A.TG - 1) / A.TG : 0;
+    int incl = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, incl, off);
+      if (lane >= off) incl += o;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, tile < incl);
+    if (hit == 0) {
+      tile -= __shfl_sync(0xffffffffu, incl, 31);
+      continue;
+    }
+    const int who = __ffs(hit) - 1;
+    tile -= __shfl_sync(0xffffffffu, incl - mine, who);
+    it.b = b0 + who;
+    const TokRange r = tokens_of(a.tok_off, it.b, a.n_tokens);
+    const long long bl = (long long)it.b * a.g.L + it.l;
+    const int nq = min(A.TG, r.n - tile * A.TG);
+    it.cur = max(0, min(a.lens.at(bl, it.h, a.g.H), min(a.max_len, a.g.cap(bl))));
+    it.tok0 = r.first + tile * A.TG;
+    it.rows = nq * A.G;
+    it.first = it.cur - r.n + tile * A.TG + 1;
+    it.end = max(0, min(it.cur, it.first + nq - 1));
+    break;
+  }
+  return it;
+}
+// Rows of a part; `end` / that, rounded up, are the parts that an item has.
+__device__ __forceinline__ int ff_step(int end, int parts) { return max(kFfCols, ((end + parts - 1) / parts + kFfCols - 1) / kFfCols * kFfCols); }
+
+template <int D, bool PARTS>
+__global__ void __launch_bounds__(kFfThreads, 3)
+few_tokens_fp32_kernel(const __grid_constant__ FfArgs A, const float* __restrict__ K, const float* __restrict__ V) {
+  constexpr int LPR = D / 4, GROUPS = kFfThreads / LPR, F = kFfCols / GROUPS, PITCH = kFfPitch<D>;
+  static_assert(GROUPS * kFfRows * D <= kFfCols * PITCH, "the threads' values are joined where K was");
+  __shared__ __align__(16) float s_k[kFfCols * PITCH];
+  __shared__ __align__(16) float s_q[kFfRows * D];
+  __shared__ __align__(16) float s_p[kFfCols * kFfRows];
+  __shared__ __align__(16) float s_keep[kFfRows];
+  __shared__ __align__(16) float s_top[4][4], s_max[kFfRows], s_sum[4][4];
+  const TokenAttention& a = A.a;
+  const Geom& g = a.g;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int piece = tid % LPR, group = tid / LPR;        // of K and V: 16 bytes of every GROUPS-th row
+  const int row = tid & (kFfCols - 1), q0 = tid / kFfCols * 4;               // of the scores: a row and four queries
+  next_may_start();
+  wait_for_previous();
+  // A wait that gave up in an earlier call marks the workspace; nothing runs until it is cleared.
+  if (a.status && *reinterpret_cast<volatile int32_t*>(a.status + 2) != 0) return;
+  const unsigned parts = PARTS ? (unsigned)A.parts : 1u;
+  const FfItem it = ff_item(A, blockIdx.x / parts);
+  if (it.rows == 0) return;
+  int from = 0, to = it.end;
+  if constexpr (PARTS) {
+    const int step = ff_step(it.end, A.parts);
+    from = (int)min((long long)it.end, (long long)(blockIdx.x % parts) * step);
+    to = min(it.end, from + step);
+    if (from >= to) return;                              // (joined by the number of parts that there are)
+  }
+  for (int e = tid; e < kFfRows * LPR; e += kFfThreads) {
+    const int r = e / LPR, d = e % LPR * 4;
+    *reinterpret_cast<float4*>(s_q + r * D + d) =
+        r < it.rows ? *reinterpret_cast<const float4*>(a.q.row<float>(it.l, it.tok0 + r / A.G, it.h * A.G + r % A.G) + d) : make_float4(0, 0, 0, 0);
+  }
+  const int32_t* const table = a.pages.of(it.b, it.l);
+  const float* const Ku = K + it.h * g.sh + piece * 4;
+  const float* const Vu = V + it.h * g.sh + piece * 4;
+  int limit[4];
+  float m[4], sum[4], o[kFfRows][4] = {};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    limit[k] = q0 + k < it.rows ? min(it.cur, it.first + (q0 + k) / A.G) : 0;
+    m[k] = -INFINITY;
+    sum[k] = 0.f;
+  }
+  for (int t0 = from; t0 < to; t0 += kFfCols) {
+    int page[F];
+    float4 v[F];
+    {
+      float4 k[F];
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < F; ++i) {
+        const int t = t0 + group + i * GROUPS;
+        page[i] = t < to ? table[t >> a.pages.shift] : -1;
+      }
+#pragma unroll
+      for (int i = 0; i < F; ++i) {
+        const int t = t0 + group + i * GROUPS;
+        const bool in = a.pages.valid(page[i]);          // (rows of a page that is none, and those behind the end, are zeros)
+        bad = bad || (!in && t < to);
+        const long long at = (((long long)page[i] << a.pages.shift) | (t & (a.pages.rows() - 1))) * g.st;
+        k[i] = in ? *reinterpret_cast<const float4*>(Ku + at) : make_float4(0, 0, 0, 0);
+        v[i] = in ? *reinterpret_cast<const float4*>(Vu + at) : make_float4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < F; ++i) *reinterpret_cast<float4*>(s_k + (group + i * GROUPS) * PITCH + piece * 4) = k[i];
+      if (bad && a.status) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
+    }
+    __syncthreads();
+    float s[4] = {};
+#pragma unroll 8
+    for (int d = 0; d < D; d += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(s_k + row * PITCH + d);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float4 q = *reinterpret_cast<const float4*>(s_q + (q0 + k) * D + d);
+        s[k] = fmaf(q.x, x.x, fmaf(q.y, x.y, fmaf(q.z, x.z, fmaf(q.w, x.w, s[k]))));
+      }
+    }
+    float top[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      s[k] *= a.scale_log2e;
+      top[k] = t0 + row < limit[k] ? s[k] : -INFINITY;
+#pragma unroll
+      for (int off = 16; off; off >>= 1) top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], off));
+    }
+    if (lane == 0) *reinterpret_cast<float4*>(s_top[warp]) = make_float4(top[0], top[1], top[2], top[3]);
+    __syncthreads();
+    float p[4], keep[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float now = fmaxf(m[k], fmaxf(s_top[warp & ~1][k], s_top[warp | 1][k])), low = now == -INFINITY ? 0.f : now;
+      keep[k] = exp2f(m[k] - low);                       // (0 while nothing has been seen)
+      m[k] = now;
+      p[k] = t0 + row < limit[k] ? exp2f(s[k] - low) : 0.f;
+      sum[k] = fmaf(sum[k], keep[k], p[k]);
+    }
+    *reinterpret_cast<float4*>(s_p + row * kFfRows + q0) = make_float4(p[0], p[1], p[2], p[3]);
+    if (row == 0) *reinterpret_cast<float4*>(s_keep + q0) = make_float4(keep[0], keep[1], keep[2], keep[3]);
+    __syncthreads();
+    const bool all_seen = t0 + kFfCols <= it.first;
+#pragma unroll
+    for (int q = 0; q < kFfRows; ++q) {
+      const float f = s_keep[q];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[q][c] *= f;
+    }
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+      const float* const w = s_p + (group + i * GROUPS) * kFfRows;
+      const float4 wa = *reinterpret_cast<const float4*>(w), wb = *reinterpret_cast<const float4*>(w + 4);
+      const float ws[kFfRows] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
+#pragma unroll
+      for (int q = 0; q < kFfRows; ++q) {
+        if (!all_seen && ws[q] == 0.f) continue;         // (a value that the row does not see may be anything)
+        o[q][0] = fmaf(ws[q], v[i].x, o[q][0]);
+        o[q][1] = fmaf(ws[q], v[i].y, o[q][1]);
+        o[q][2] = fmaf(ws[q], v[i].z, o[q][2]);
+        o[q][3] = fmaf(ws[q], v[i].w, o[q][3]);
+      }
+    }
+  }
+  // ---- the threads' values are joined, in a fixed order -------------------------------------------------
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int off = 16; off; off >>= 1) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], off);
+  // (K of the last step was read before its tops were)
+  if (lane == 0) *reinterpret_cast<float4*>(s_sum[warp]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+  if (row == 0) *reinterpret_cast<float4*>(s_max + q0) = make_float4(m[0], m[1], m[2], m[3]);
+#pragma unroll
+  for (int q = 0; q < kFfRows; ++q)
+    *reinterpret_cast<float4*>(s_k + (group * kFfRows + q) * D + piece * 4) = make_float4(o[q][0], o[q][1], o[q][2], o[q][3]);
+  __syncthreads();
+  for (int e = tid; e < it.rows * LPR; e += kFfThreads) {
+    const int r = e / LPR, d = e % LPR * 4;
+    float4 x = make_float4(0, 0, 0, 0);
+#pragma unroll
+    for (int u = 0; u < GROUPS; ++u) {
+      const float4 y = *reinterpret_cast<const float4*>(s_k + (u * kFfRows + r) * D + d);
+      x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+    }
+    const float den = s_sum[r / 4 * 2][r % 4] + s_sum[r / 4 * 2 + 1][r % 4], top = s_max[r];
+    if constexpr (PARTS) {
+      const long long at = (long long)blockIdx.x * kFfRows + r;
+      *reinterpret_cast<float4*>(A.part + at * D + d) = x;
+      if (d == 0) A.stat[at] = make_float2(top, den);
+    } else {
+      const float inv = den == 0.f ? 0.f : 1.f / den;
+      const int i = it.tok0 + r / A.G, j = it.h * A.G + r % A.G;
+      *reinterpret_cast<float4*>(a.out.row<float>(it.l, i, j) + d) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+      if (a.lse && d == 0)
+        a.lse[((long long)it.l * a.n_tokens + i) * g.Hq + j] = den == 0.f ? -INFINITY : (top + log2f(den)) * 0.6931471805599453f;
+    }
+  }
+}
+
+// Joins the parts of an item, a warp per query row, in a fixed order: out = sum_p w_p O_p / sum_p w_p sum_p, w_p = 2^(m_p - max m).
+template <int D>
+__global__ void __launch_bounds__(32 * kFfRows)
+few_tokens_fp32_join_kernel(const __grid_constant__ FfArgs A) {
+  constexpr int N = D / 32, AHEAD = 8;
+  using Vec = std::conditional_t<N == 4, float4, float2>;
+  const TokenAttention& a = A.a;
+  const int lane = threadIdx.x & 31, r = threadIdx.x >> 5;
+  next_may_start();
+  wait_for_previous();
+  if (*reinterpret_cast<volatile int32_t*>(a.status + 2) != 0) return;
+  const FfItem it = ff_item(A, blockIdx.x);
+  if (r >= it.rows) return;
+  const int step = ff_step(it.end, A.parts), n = (it.end + step - 1) / step;
+  const long long at = (long long)blockIdx.x * A.parts * kFfRows + r;
+  float top = -INFINITY, den = 0.f, num[N] = {};
+  for (int p = lane; p < n; p += 32) top = fmaxf(top, A.stat[at + (long long)p * kFfRows].x);
+#pragma unroll
+  for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+  const float low = top == -INFINITY ? 0.f : top;
+  for (int p0 = 0; p0 < n; p0 += AHEAD) {
+    Vec x[AHEAD];
+    float2 st[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const long long of = at + (long long)min(p0 + k, n - 1) * kFfRows;
+      x[k] = reinterpret_cast<const Vec*>(A.part + of * D)[lane];
+      st[k] = A.stat[of];
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const float w = p0 + k < n ? exp2f(st[k].x - low) : 0.f;
+      if (w == 0.f) continue;                            // (nothing seen there)
+      den = fmaf(w, st[k].y, den);
+      num[0] = fmaf(w, x[k].x, num[0]);
+      num[1] = fmaf(w, x[k].y, num[1]);
+      if constexpr (N == 4) {
+        num[2] = fmaf(w, x[k].z, num[2]);
+        num[3] = fmaf(w, x[k].w, num[3]);
+      }
+    }
+  }
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  const int i = it.tok0 + r / A.G, j = it.h * A.G + r % A.G;
+  Vec out;
+  out.x = num[0] * inv;
+  out.y = num[1] * inv;
+  if constexpr (N == 4) {
+    out.z = num[2] * inv;
+    out.w = num[3] * inv;
+  }
+  reinterpret_cast<Vec*>(a.out.row<float>(it.l, i, j))[lane] = out;
+  if (a.lse && lane == 0)
+    a.lse[((long long)it.l * a.n_tokens + i) * a.g.Hq + j] = den == 0.f ? -INFINITY : (top + log2f(den)) * 0.6931471805599453f;
+}
+
+size_t few_tokens_fp32_scratch(const Geom& g, int max_len) {
+  return max_len > kFfCols ? (size_t)kFfResident * kFfRows * (g.D * sizeof(float) + sizeof(float2)) : 0;
+}
+
+template <int D>
+static int launch_ff(FfArgs& A, const float* K, const float* V, char* scratch, size_t scratch_bytes, cudaStream_t s) {
+  const TokenAttention& a = A.a;
+  const long long items = ((long long)a.n_tokens / A.TG + std::min(a.g.B, a.n_tokens)) * a.g.H * a.g.L;
+  if (items > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
+  const size_t need = few_tokens_fp32_scratch(a.g, a.max_len);
+  A.parts = 1;
+  // (kFfResident / items parts at most, so that the scratch holds them)
+  if (need > 0 && scratch && scratch_bytes >= need)
+    A.parts = (int)std::max(1ll, std::min<long long>(kFfResident / items, ((long long)a.max_len + kFfCols - 1) / kFfCols));
+  if (A.parts == 1) return launch_chained(few_tokens_fp32_kernel<D, false>, items, 1, kFfThreads, 0, s, A, K, V);
+  A.part = reinterpret_cast<float*>(scratch);
+  A.stat = reinterpret_cast<float2*>(A.part + (size_t)kFfResident * kFfRows * D);
+  const int rc = launch_chained(few_tokens_fp32_kernel<D, true>, items * A.parts, 1, kFfThreads, 0, s, A, K, V);
+  return rc != L2KV_OK ? rc : launch_chained(few_tokens_fp32_join_kernel<D>, items, 1, 32 * kFfRows, 0, s, A);
+}
+
+int launch_few_tokens_fp32(const TokenAttention& a, const void* K, const void* V, char* scratch, size_t scratch_bytes, cudaStream_t s) {
+  FfArgs A{};
+  A.a = a;
+  A.G = a.g.Hq / a.g.H;
+  A.TG = kFfRows / A.G;
+  const float* const k = static_cast<const float*>(K);
+  const float* const v = static_cast<const float*>(V);
+  return a.g.D == 128 ? launch_ff<128>(A, k, v, scratch, scratch_bytes, s) : launch_ff<64>(A, k, v, scratch, scratch_bytes, s);
+}
+
+}  // namespace l2kv

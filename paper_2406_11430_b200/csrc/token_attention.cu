@@ -1046,7 +1046,8 @@ static TaRoom ta_room(const Geom& g, int n_tokens, int max_len) {
 }
 
 size_t token_attention_scratch(const Geom& g, int dtype, int n_tokens, int max_len, bool pages) {
-  return dtype == L2KV_BF16 ? std::max(ta_room(g, n_tokens, max_len).bytes, pages ? few_tokens_scratch(g, max_len) : 0) : 0;
+  if (dtype != L2KV_BF16) return pages ? few_tokens_fp32_scratch(g, max_len) : 0;
+  return std::max(ta_room(g, n_tokens, max_len).bytes, pages ? few_tokens_scratch(g, max_len) : 0);
 }
 
 template <int D, bool TREE, bool PAGED = false>
@@ -1072,7 +1073,8 @@ static int launch_ta(const TaArgs& A, const void* K, const void* V, long long it
 
 int launch_token_attention(const TokenAttention& a, const void* K, const void* V, int dtype, char* scratch,
                            size_t scratch_bytes, cudaStream_t s) {
-  if (dtype != L2KV_BF16) return launch_token_attention_fp32(a, K, V, s);
+  if (dtype != L2KV_BF16)
+    return a.pages.table ? launch_few_tokens_fp32(a, K, V, scratch, scratch_bytes, s) : launch_token_attention_fp32(a, K, V, s);
   if (few_tokens(a, dtype)) return launch_few_tokens(a, K, V, scratch, scratch_bytes, s);
   const TaRoom room = ta_room(a.g, a.n_tokens, a.max_len);
   if (room.items > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;

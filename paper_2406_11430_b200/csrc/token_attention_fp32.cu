@@ -16,7 +16,7 @@ namespace l2kv {
 constexpr int kTfRows = 32, kTfCols = 32;
 template <int D> constexpr int kTfSmem = (kTfRows * D + kTfCols * (D + 4) + kTfCols * D + kTfRows * (kTfCols + 4)) * 4;
 
-template <int D, bool PAGED>
+template <int D>
 __global__ void __launch_bounds__(128)
 token_attention_fp32_kernel(const __grid_constant__ TokenAttention a, const float* __restrict__ K,
                             const float* __restrict__ V) {
@@ -57,7 +57,6 @@ token_attention_fp32_kernel(const __grid_constant__ TokenAttention a, const floa
   const int base = cur - range.n, first = tile * kTfRows, rows = min(kTfRows, range.n * G - first);
   int end = a.mask ? cur : max(0, min(cur, base + (first + rows - 1) / G + 1));
   if (end > 0 && !L2KV_BOUNDS(g.holds(bl, 0) && g.holds(bl, end - 1), a.status)) end = 0;
-  const int32_t* const table = PAGED ? a.pages.of(b, l) : nullptr;
   const int clear = a.mask ? base : base + first / G + 1;                    // rows below it are seen by all
 
   for (int e = tid; e < kTfRows * D / 4; e += 128) {
@@ -65,8 +64,8 @@ token_attention_fp32_kernel(const __grid_constant__ TokenAttention a, const floa
     *reinterpret_cast<float4*>(s_q + r * D + d) =
         r < rows ? *reinterpret_cast<const float4*>(a.q.row<float>(l, i, h * G + (first + r) % G) + d) : make_float4(0, 0, 0, 0);
   }
-  const float* const Ku = K + (PAGED ? h * g.sh : g.base(b, l, h));
-  const float* const Vu = V + (PAGED ? h * g.sh : g.base(b, l, h));
+  const float* const Ku = K + g.base(b, l, h);
+  const float* const Vu = V + g.base(b, l, h);
   int limit[2];
   const uint32_t* mask[2];
 #pragma unroll
@@ -80,15 +79,8 @@ token_attention_fp32_kernel(const __grid_constant__ TokenAttention a, const floa
     __syncthreads();                                     // the block before has been read
     for (int e = tid; e < kTfCols * D / 4; e += 128) {
       const int c = e / (D / 4), d = e % (D / 4) * 4;
-      bool in = t0 + c < end;
-      long long row = t0 + c;
-      if (PAGED && in) {                                 // (rows of a page that is none are zeros)
-        const int page = table[row >> a.pages.shift];
-        in = a.pages.valid(page);
-        if (!in && a.status) atomicExch(a.status, (int)L2KV_ERR_OUT_OF_RANGE);
-        row = ((long long)page << a.pages.shift) | (row & (a.pages.rows() - 1));
-      }
-      const long long at = row * g.st + d;
+      const long long at = (long long)(t0 + c) * g.st + d;
+      const bool in = t0 + c < end;
       *reinterpret_cast<float4*>(s_k + c * (D + 4) + d) = in ? *reinterpret_cast<const float4*>(Ku + at) : make_float4(0, 0, 0, 0);
       *reinterpret_cast<float4*>(s_v + c * D + d) = in ? *reinterpret_cast<const float4*>(Vu + at) : make_float4(0, 0, 0, 0);
     }
@@ -182,7 +174,7 @@ static int launch_tf(const TokenAttention& a, const void* K, const void* V, cuda
   const long long rows = (long long)a.n_tokens * (a.g.Hq / a.g.H);
   const long long blocks = (rows / kTfRows + std::min(a.g.B, a.n_tokens)) * a.g.H * a.g.L;
   if (blocks > INT_MAX) return L2KV_ERR_OUT_OF_RANGE;
-  auto kern = a.pages.table ? token_attention_fp32_kernel<D, true> : token_attention_fp32_kernel<D, false>;
+  auto kern = token_attention_fp32_kernel<D>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kTfSmem<D>) != cudaSuccess)
     return L2KV_ERR_CUDA;
   kern<<<(unsigned)blocks, 128, kTfSmem<D>, s>>>(a, static_cast<const float*>(K), static_cast<const float*>(V));

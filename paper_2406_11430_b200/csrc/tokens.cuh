@@ -127,5 +127,8 @@ bool few_tokens(const TokenAttention& a, int dtype);
 size_t few_tokens_scratch(const Geom& g, int max_len);
 int launch_few_tokens(const TokenAttention& a, const void* K, const void* V, char* scratch, size_t scratch_bytes, cudaStream_t s);
 int launch_token_attention_fp32(const TokenAttention& a, const void* K, const void* V, cudaStream_t s);
+// fp32 caches in pages, however many tokens.
+size_t few_tokens_fp32_scratch(const Geom& g, int max_len);
+int launch_few_tokens_fp32(const TokenAttention& a, const void* K, const void* V, char* scratch, size_t scratch_bytes, cudaStream_t s);
 
 }  // namespace l2kv
